@@ -307,6 +307,9 @@ int32_t ls_set_option(int32_t option, int32_t value);
 #define LS_TIMED_PREDICT 2 /* latent + scores + top-k of one predictor evaluation */
 #define LS_TIMED_FUSED 3   /* the fused per-layer step kernel */
 #define LS_TIMED_STACK 4   /* the whole-token kernel of ls_stack_decode */
+#define LS_TIMED_ATTEND 5  /* the kernels of one ls_paged_kv_attend */
+#define LS_TIMED_APPEND 6  /* ls_paged_kv_append */
+#define LS_TIMED_NORM 7    /* ls_block_norm */
 int32_t ls_timing_enable(int32_t on);
 int32_t ls_timing_read(int32_t kind, int64_t *launches, double *total_ms);
 
@@ -357,6 +360,83 @@ int32_t ls_hash_predict(ls_hash_predictor *pred, const float *d_feature, int32_t
 int32_t ls_controller_quantize(double remaining, double vmax, int32_t n_states);
 int32_t ls_controller_build(int32_t n_layers, int32_t n_states, int32_t n_plans, int32_t n_samples, int32_t horizon, const double *t_bar,
                             const int32_t *next_state, int32_t *lut, double *value);
+
+/*
+ * The attention half of a decoder layer (no counterpart in the paper, whose path is the FFN half): a paged key/value cache,
+ * the append to it, attention over it, and the norms around a block.  One layer's attention block at batch n is
+ *   ls_block_norm (h from the residual) -> projections by the caller -> ls_paged_kv_append -> ls_paged_kv_attend ->
+ *   output projection by the caller -> ls_block_norm (residual sum) -> ls_predict, ls_sparse_ffn_step.
+ *
+ * ls_paged_kv describes one layer's cache.  The pages are the CALLER's device memory, borrowed: they must outlive the handle.
+ *   Element (page, slot, head, i) of the keys is d_k[page * page_stride + slot * token_stride + head * head_stride + i], of
+ *   the values the same in d_v (strides in elements, the head dimension is contiguous), so that [page][slot][head][dim],
+ *   [page][head][slot][dim] and keys and values interleaved in one pool are all accepted.  Position p of sequence b is slot
+ *   p % page_size of page d_table[b * table_stride + p / page_size]; table_width entries of each row are valid.
+ *   dtype: LS_WDTYPE_* of pages, queries, new keys and values, and outputs.  head_dim: a multiple of 8, at most 256;
+ *   n_q_heads a multiple of n_kv_heads (query head h reads key head h / (n_q_heads / n_kv_heads)).
+ *   max_seqs, max_q_len size the workspace of ls_paged_kv_attend (0: the handle only appends).
+ *   d_rope: NULL, or float [rope_positions][rope_dim], row p = rope_dim / 2 cosines, then as many sines of position p
+ *   (borrowed); rope_dim even, at most head_dim; pairs are (i, i + rope_dim / 2), or (2 i, 2 i + 1) with rope_interleaved.
+ * One call at a time per handle (its workspace is reused by every call); calls enqueue kernels only, never synchronise or
+ * allocate, and may be captured in a CUDA graph.  The results do not depend on timing (sums have a fixed order).
+ *
+ * ls_paged_kv_append: for each of n_tokens tokens, turns query and key by the token's position and stores the key and the
+ *   value in the token's slot (position d_pos[t] of sequence d_seq[t]); the turned query goes to d_q_out.  d_q, d_k, d_v and
+ *   d_q_out are [n_tokens][heads][head_dim] with token strides (heads side by side), so slices of one projection's output
+ *   need no copy; d_q NULL: keys and values only; d_q_out may be d_q.  A token with a negative sequence or position is
+ *   padding: nothing is stored for it, its query is copied.  Two tokens of one call with the same slot: either one lands.
+ *
+ * ls_paged_kv_attend: causal attention of the last q_len tokens of each of n_seqs sequences; token i of sequence b stands at
+ *   position d_seq_len[b] - q_len + i and sees the positions up to its own, the last `window` of them (window = 0: all).
+ *   d_q, d_out [n_seqs * q_len][n_q_heads][head_dim] with token strides; d_lse (nullable) float [n_seqs * q_len][n_q_heads]:
+ *   natural log of the sum of e^score.  A token that sees nothing (an empty slot: d_seq_len 0) gets zeros and -inf.
+ *   Positions below prefix_len are the same for all sequences and are read from d_prefix_pages [ceil(prefix_len /
+ *   page_size)], once for the whole batch; entries of d_table for whole pages below it are not read.  prefix_len need not be
+ *   a multiple of page_size: the page it ends in is then the sequences' own from prefix_len on.  prefix_len = 0: no sharing.
+ *   Scores and softmax are fp32; weights are rounded to the 16-bit type for the product with the values.
+ *   Memory that no token of a sequence sees (slots behind its end or before its window) may hold anything.  A value that is
+ *   infinite or NaN at a position that some token of the batch sees may make NaN of a token that does not see it.
+ * Lengths beyond the table, and table entries outside the pool, are skipped (their keys count for nothing or as zeros, never
+ * read out of bounds) and recorded: ls_paged_kv_status reads and clears the handle's status word (it synchronises).
+ */
+typedef struct ls_paged_kv ls_paged_kv;
+typedef struct {
+  uint32_t struct_size;
+  int32_t device;
+  int32_t dtype, n_q_heads, n_kv_heads, head_dim, page_size, n_pages;
+  void *d_k, *d_v;
+  int64_t page_stride, token_stride, head_stride;
+  int32_t max_seqs, max_q_len;
+  const float *d_rope;
+  int32_t rope_positions, rope_dim, rope_interleaved;
+} ls_paged_kv_desc;
+int32_t ls_paged_kv_create(const ls_paged_kv_desc *desc, ls_paged_kv **out);
+int32_t ls_paged_kv_destroy(ls_paged_kv *kv);
+int32_t ls_paged_kv_append(ls_paged_kv *kv, const void *d_q, int64_t q_stride, void *d_q_out, int64_t q_out_stride, const void *d_k,
+                           int64_t k_stride, const void *d_v, int64_t v_stride, int32_t n_tokens, const int32_t *d_seq,
+                           const int32_t *d_pos, const int32_t *d_table, int32_t n_seqs, int32_t table_width, int64_t table_stride,
+                           void *stream);
+int32_t ls_paged_kv_attend(ls_paged_kv *kv, const void *d_q, int64_t q_stride, void *d_out, int64_t out_stride, float *d_lse,
+                           int32_t n_seqs, int32_t q_len, const int32_t *d_seq_len, const int32_t *d_table, int32_t table_width,
+                           int64_t table_stride, const int32_t *d_prefix_pages, int32_t prefix_len, int32_t window, float scale,
+                           void *stream);
+int32_t ls_paged_kv_status(ls_paged_kv *kv, int32_t *host_status);
+
+/*
+ * The norms before and after a block, fused with its gate, residual scale and residual sum, for n rows of d elements:
+ *   t = N(y) * w_post (N only with post_norm = LS_NORM_RMS);  x' = x + scale * gate * t;  h = N(x') * w_pre (pre_norm),
+ *   N(z) = z / sqrt(mean(z^2) + eps).
+ * x_dtype: type of d_x and d_x_out, LS_DTYPE_F32 or the block's type; dtype: type of d_y, d_h and d_gate (LS_WDTYPE_* or
+ * LS_DTYPE_F32).  Gains are float, NULL = none.  d_gate NULL = none; gate_stride 0 broadcasts one row [d] over all rows.
+ * d_y NULL: x' = x (the norm alone); d_x_out, d_h: NULL = not wanted, at least one of them is; d_x_out may be d_x, d_h may
+ * be d_y.  Row strides in elements.  Sums are fp32, every output is rounded once (h is made from the unrounded x').
+ * 1 <= d <= 16384.  Runs on the device that owns d_x; enqueues one kernel, never synchronises or allocates.
+ */
+#define LS_DTYPE_F32 2
+int32_t ls_block_norm(const void *d_x, int64_t x_stride, int32_t x_dtype, const void *d_y, int64_t y_stride, int32_t dtype, void *d_x_out,
+                      int64_t x_out_stride, void *d_h, int64_t h_stride, int32_t n, int32_t d, int32_t post_norm, const float *d_w_post,
+                      const void *d_gate, int64_t gate_stride, float scale, int32_t pre_norm, const float *d_w_pre, float eps,
+                      void *stream);
 
 /* Number of kernels launched by this library in the calling process since load (for launch accounting). */
 int64_t ls_kernel_launches(void);

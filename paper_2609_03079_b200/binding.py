@@ -18,13 +18,15 @@ LS_OK, LS_ERR_INVALID, LS_ERR_NOMEM, LS_ERR_CUDA, LS_ERR_STATE, LS_ERR_CAPACITY,
 LS_ACT_RELU, LS_ACT_SILU = 0, 1
 LS_WDTYPE_BF16, LS_WDTYPE_FP16 = 0, 1
 LS_NORM_RMS, LS_NORM_NONE = 0, 1
+LS_DTYPE_F32 = 2
 
 EXPORTS = [
     "ls_layer_create", "ls_layer_destroy", "ls_predict", "ls_sparse_ffn_step", "ls_cache_lookup", "ls_cache_reserve",
     "ls_cache_evict", "ls_cache_snapshot", "ls_cache_wait", "ls_cache_stats", "ls_layer_status", "ls_kernel_launches",
     "ls_last_error", "ls_version", "ls_timing_enable", "ls_timing_read", "ls_set_option", "ls_topk_select_static", "ls_stack_create",
     "ls_stack_destroy", "ls_stack_decode", "ls_controller_quantize", "ls_controller_build", "ls_hash_predictor_create",
-    "ls_hash_predictor_destroy", "ls_hash_predict",
+    "ls_hash_predictor_destroy", "ls_hash_predict", "ls_paged_kv_create", "ls_paged_kv_destroy", "ls_paged_kv_append",
+    "ls_paged_kv_attend", "ls_paged_kv_status", "ls_block_norm",
 ]
 
 
@@ -72,6 +74,14 @@ class ls_cache_stats_t(C.Structure):
                 ("h2d_copies", C.c_int64), ("resident", C.c_int64)]
 
 
+class ls_paged_kv_desc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("device", C.c_int32), ("dtype", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("d_k", C.c_void_p), ("d_v", C.c_void_p),
+                ("page_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64), ("max_seqs", C.c_int32),
+                ("max_q_len", C.c_int32), ("d_rope", C.c_void_p), ("rope_positions", C.c_int32), ("rope_dim", C.c_int32),
+                ("rope_interleaved", C.c_int32)]
+
+
 _lib = None
 
 
@@ -109,6 +119,13 @@ def lib() -> C.CDLL:
         L.ls_hash_predict.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.POINTER(ls_selection), C.c_void_p, C.c_void_p]
         L.ls_controller_quantize.argtypes = [C.c_double, C.c_double, C.c_int32]
         L.ls_controller_build.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        P, I, N = C.c_void_p, C.c_int32, C.c_int64
+        L.ls_paged_kv_create.argtypes = [C.POINTER(ls_paged_kv_desc), C.POINTER(P)]
+        L.ls_paged_kv_destroy.argtypes = [P]
+        L.ls_paged_kv_append.argtypes = [P, P, N, P, N, P, N, P, N, I, P, P, P, I, I, N, P]
+        L.ls_paged_kv_attend.argtypes = [P, P, N, P, N, P, I, I, P, P, I, N, P, I, I, C.c_float, P]
+        L.ls_paged_kv_status.argtypes = [P, C.POINTER(I)]
+        L.ls_block_norm.argtypes = [P, N, I, P, N, I, P, N, P, N, I, I, I, P, P, N, C.c_float, I, P, C.c_float, P]
         L.ls_timing_enable.argtypes = [C.c_int32]
         L.ls_timing_read.argtypes = [C.c_int32, C.POINTER(C.c_int64), C.POINTER(C.c_double)]
         L.ls_kernel_launches.restype = C.c_int64
@@ -309,6 +326,7 @@ def ls_version() -> int:
 
 
 LS_TIMED_GATEUP, LS_TIMED_DOWN, LS_TIMED_PREDICT, LS_TIMED_FUSED, LS_TIMED_STACK = 0, 1, 2, 3, 4
+LS_TIMED_ATTEND, LS_TIMED_APPEND, LS_TIMED_NORM = 5, 6, 7
 
 
 def ls_timing_enable(on: bool) -> None:
@@ -461,3 +479,142 @@ def ls_hash_predict(pred: HashPredictor, feature: torch.Tensor, k: int, out: Sel
     assert feature.dtype == torch.float32 and feature.is_cuda and feature.is_contiguous()
     _check(lib().ls_hash_predict(pred.handle, feature.data_ptr(), k, C.byref(out.c), _ptr(layer_idx), _stream(stream)))
     return out
+
+
+_DTYPE = {torch.bfloat16: LS_WDTYPE_BF16, torch.float16: LS_WDTYPE_FP16, torch.float32: LS_DTYPE_F32}
+
+
+class PagedKV:
+    """Owner of one ``ls_paged_kv*`` handle (keeps the borrowed pages and rotation table alive)."""
+
+    def __init__(self, handle: int, k_pages: torch.Tensor, v_pages: torch.Tensor, n_q_heads: int, max_seqs: int, max_q_len: int,
+                 rope: Optional[torch.Tensor]):
+        self.handle = handle
+        self.k_pages, self.v_pages, self.rope = k_pages, v_pages, rope
+        self.n_pages, self.page_size, self.n_kv_heads, self.head_dim = k_pages.shape
+        self.n_q_heads, self.max_seqs, self.max_q_len = n_q_heads, max_seqs, max_q_len
+        self.dtype, self.device = k_pages.dtype, k_pages.device.index
+
+    def close(self) -> None:
+        if self.handle:
+            lib().ls_paged_kv_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def ls_paged_kv_create(k_pages: torch.Tensor, v_pages: torch.Tensor, n_q_heads: int, max_seqs: int = 0, max_q_len: int = 0,
+                       rope: Optional[torch.Tensor] = None, rope_interleaved: bool = False) -> PagedKV:
+    """One layer's paged cache over the caller's pages, viewed as [n_pages, page_size, n_kv_heads, head_dim] with any strides
+    that keep head_dim contiguous (a pool stored head by head is passed as ``pool.transpose(1, 2)``).  ``rope``: float
+    [positions, rope_dim], cosines then sines, or None.  ``max_seqs`` = 0: for appends only."""
+    assert k_pages.dim() == 4 and k_pages.shape == v_pages.shape and k_pages.stride() == v_pages.stride() and k_pages.dtype == v_pages.dtype
+    assert k_pages.is_cuda and v_pages.device == k_pages.device and k_pages.stride(3) == 1 and k_pages.dtype in _DTYPE
+    d = ls_paged_kv_desc()
+    d.struct_size = C.sizeof(ls_paged_kv_desc)
+    d.device, d.dtype = k_pages.device.index, _DTYPE[k_pages.dtype]
+    d.n_pages, d.page_size, d.n_kv_heads, d.head_dim = k_pages.shape
+    d.n_q_heads = n_q_heads
+    d.d_k, d.d_v = k_pages.data_ptr(), v_pages.data_ptr()
+    d.page_stride, d.token_stride, d.head_stride = k_pages.stride()[:3]
+    d.max_seqs, d.max_q_len = max_seqs, max_q_len if max_seqs else 0
+    if rope is not None:
+        assert rope.dtype == torch.float32 and rope.dim() == 2 and rope.is_contiguous() and rope.device == k_pages.device
+        d.d_rope, d.rope_positions, d.rope_dim, d.rope_interleaved = rope.data_ptr(), rope.shape[0], rope.shape[1], int(rope_interleaved)
+    out = C.c_void_p()
+    _check(lib().ls_paged_kv_create(C.byref(d), C.byref(out)))
+    return PagedKV(out.value, k_pages, v_pages, n_q_heads, max_seqs, max_q_len, rope)
+
+
+def ls_paged_kv_destroy(kv: PagedKV) -> None:
+    kv.close()
+
+
+def ls_paged_kv_status(kv: PagedKV) -> int:
+    v = C.c_int32(0)
+    _check(lib().ls_paged_kv_status(kv.handle, C.byref(v)))
+    return v.value
+
+
+def _token_stride(kv: PagedKV, t: torch.Tensor, heads: int) -> int:
+    """Checks a [tokens, heads, head_dim] (or [sequences, tokens, heads, head_dim]) operand and returns its token stride."""
+    shape, st = t.shape, t.stride()
+    D = kv.head_dim
+    assert t.dtype == kv.dtype and t.is_cuda and shape[-1] == D and shape[-2] == heads
+    assert (st[-1] == 1 or D == 1) and (st[-2] == D or heads == 1)
+    if len(shape) == 4 and shape[1] > 1:
+        assert shape[0] == 1 or st[0] == shape[1] * st[1]
+        return st[1]
+    return st[0] if shape[0] > 1 else heads * D  # (a single token has no stride)
+
+
+def _table_args(table: torch.Tensor):
+    assert table.dtype == torch.int32 and table.dim() == 2 and table.is_cuda and (table.stride(1) == 1 or table.shape[1] <= 1)
+    return table.data_ptr(), table.shape[0], table.shape[1], table.stride(0)
+
+
+def ls_paged_kv_append(kv: PagedKV, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, q_out: Optional[torch.Tensor],
+                       seq: torch.Tensor, pos: torch.Tensor, table: torch.Tensor, stream=None) -> None:
+    """q, k, v, q_out: [tokens, heads, head_dim] (any token stride); seq, pos: int32 [tokens]; table: int32 [sequences, pages]."""
+    n = k.shape[0]
+    assert v.shape[0] == n and seq.numel() == n and pos.numel() == n and seq.dtype == pos.dtype == torch.int32
+    assert seq.is_cuda and pos.is_cuda and seq.is_contiguous() and pos.is_contiguous()
+    sq = so = 0
+    if q is not None:
+        assert q.shape[0] == n and q_out.shape[0] == n
+        sq, so = _token_stride(kv, q, kv.n_q_heads), _token_stride(kv, q_out, kv.n_q_heads)
+    tp, ns, tw, ts = _table_args(table)
+    _check(lib().ls_paged_kv_append(kv.handle, _ptr(q), sq, _ptr(q_out), so, k.data_ptr(), _token_stride(kv, k, kv.n_kv_heads), v.data_ptr(),
+                                    _token_stride(kv, v, kv.n_kv_heads), n, seq.data_ptr(), pos.data_ptr(), tp, ns, tw, ts, _stream(stream)))
+
+
+def ls_paged_kv_attend(kv: PagedKV, q: torch.Tensor, out: torch.Tensor, seq_len: torch.Tensor, table: torch.Tensor,
+                       prefix_pages: Optional[torch.Tensor] = None, prefix_len: int = 0, window: int = 0, scale: Optional[float] = None,
+                       lse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """q, out: [sequences, q_len, heads, head_dim], or [sequences, heads, head_dim] for one token each; seq_len: int32
+    [sequences]; table: int32 [sequences, pages]; lse: float, one per row of q.  ``scale`` defaults to head_dim ** -0.5."""
+    n, m = q.shape[0], (q.shape[1] if q.dim() == 4 else 1)
+    assert out.shape == q.shape and seq_len.dtype == torch.int32 and seq_len.is_cuda and seq_len.is_contiguous() and seq_len.numel() == n
+    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == n * m * kv.n_q_heads)
+    tp, ns, tw, ts = _table_args(table)
+    assert ns == n
+    if prefix_len:
+        assert prefix_pages.dtype == torch.int32 and prefix_pages.is_contiguous() and prefix_pages.numel() * kv.page_size >= prefix_len
+    _check(lib().ls_paged_kv_attend(kv.handle, q.data_ptr(), _token_stride(kv, q, kv.n_q_heads), out.data_ptr(),
+                                    _token_stride(kv, out, kv.n_q_heads), _ptr(lse), n, m, seq_len.data_ptr(), tp, tw, ts,
+                                    _ptr(prefix_pages) if prefix_len else None, prefix_len, window,
+                                    kv.head_dim ** -0.5 if scale is None else scale, _stream(stream)))
+
+
+def _rows(t: torch.Tensor, d: int) -> int:
+    """Checks a [rows, d] (or [d]) operand and returns its row stride."""
+    st = t.stride()
+    assert t.is_cuda and t.shape[-1] == d and t.dim() <= 2 and (st[-1] == 1 or d == 1)
+    return st[0] if len(st) == 2 and t.shape[0] > 1 else d
+
+
+def ls_block_norm(x: torch.Tensor, y: Optional[torch.Tensor], x_out: Optional[torch.Tensor], h: Optional[torch.Tensor],
+                  post_norm: bool = False, w_post: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, scale: float = 1.0,
+                  pre_norm: bool = True, w_pre: Optional[torch.Tensor] = None, eps: float = 1e-5, stream=None) -> None:
+    """x' = x + scale * gate * (N(y) * w_post) into ``x_out`` and N(x') * w_pre into ``h`` (either may be None; y None: x' = x).
+    x, x_out: float or the block's type; y, h, gate ([d] or [rows, d]): the block's type; gains: float [d]."""
+    d = x.shape[-1]
+    n = x.shape[0] if x.dim() == 2 else 1
+    kind = y if y is not None else h if h is not None else x
+    for t in (y, h, gate):
+        assert t is None or (t.dtype == kind.dtype and (t.shape == x.shape or t is gate))
+    assert x_out is None or (x_out.dtype == x.dtype and x_out.shape == x.shape)
+    for w in (w_post, w_pre):
+        assert w is None or (w.dtype == torch.float32 and w.is_cuda and w.is_contiguous() and w.numel() == d)
+    gs = 0
+    if gate is not None:
+        gs = _rows(gate, d) if gate.dim() == 2 else 0
+        assert gate.is_cuda and gate.stride(-1) == 1 and (gate.dim() == 1 or gate.shape == x.shape)
+    _check(lib().ls_block_norm(x.data_ptr(), _rows(x, d), _DTYPE[x.dtype], _ptr(y), 0 if y is None else _rows(y, d), _DTYPE[kind.dtype],
+                               _ptr(x_out), 0 if x_out is None else _rows(x_out, d), _ptr(h), 0 if h is None else _rows(h, d), n, d,
+                               LS_NORM_RMS if post_norm else LS_NORM_NONE, _ptr(w_post), _ptr(gate), gs, scale,
+                               LS_NORM_RMS if pre_norm else LS_NORM_NONE, _ptr(w_pre), eps, _stream(stream)))

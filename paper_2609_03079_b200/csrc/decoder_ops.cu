@@ -1,0 +1,257 @@
+// Host side of the attention half of a decoder layer: ls_paged_kv_*, ls_block_norm (argument checks, workspaces, launches).
+#include "../../include/leanstream.h"
+
+#include <algorithm>
+#include <new>
+
+#include "ls_append.cuh"
+#include "ls_attend.cuh"
+#include "ls_host.cuh"
+#include "ls_norm.cuh"
+
+using namespace ls_host;
+
+struct ls_paged_kv {
+  ls_paged_kv_desc d{};
+  int sm_count = 148;
+  float* part_o = nullptr;
+  float* part_lse = nullptr;
+  int* status = nullptr;
+};
+
+namespace {
+
+// Blocks that ls_attend_rows_kernel is split into when rows are few: eight blocks of four warps per SM.
+constexpr int kRowsBlocks = 148 * 8;
+constexpr int kRowsMaxGroup = 8;
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+void free_kv(ls_paged_kv* kv) {
+  cudaFree(kv->part_o); cudaFree(kv->part_lse); cudaFree(kv->status);
+  delete kv;
+}
+
+int32_t create_kv(ls_paged_kv* kv) {
+  const ls_paged_kv_desc& d = kv->d;
+  int sms = 0;
+  LS_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, d.device));
+  kv->sm_count = sms;
+  LS_TRY(dalloc(&kv->status, 1));
+  LS_CUDA(cudaMemset(kv->status, 0, sizeof(int)));
+  if (d.max_seqs > 0) {
+    const size_t rows = (size_t)kRowsBlocks * kRowsMaxGroup;
+    LS_TRY(dalloc(&kv->part_o, rows * d.head_dim));
+    LS_TRY(dalloc(&kv->part_lse, rows));
+  }
+  return LS_OK;
+}
+
+template <int WD, int NG>
+int32_t launch_rows(const ls::AttendArgs& a, int lpk, int vec, cudaStream_t st) {
+  const long long blocks = (long long)a.n_seqs * a.q_len * a.kv_heads * ((a.group + NG - 1) / NG) * a.splits;
+  ls::ls_attend_rows_kernel<WD, NG><<<(unsigned)blocks, ls::AR_THREADS, 4 * NG * (a.dim + 2) * sizeof(float), st>>>(a, lpk, vec);
+  LS_LAUNCHED();
+  return LS_OK;
+}
+
+template <int WD>
+int32_t attend_rows(ls::AttendArgs& a, bool q_vec, cudaStream_t st) {
+  const int ng = a.group == 1 ? 1 : a.group <= 4 ? 4 : 8;
+  const long long one = (long long)a.n_seqs * a.q_len * a.kv_heads * ((a.group + ng - 1) / ng);
+  a.splits = (int)std::max(1LL, std::min(64LL, kRowsBlocks / one));
+  if (one * a.splits > 0x7fffffffLL) return fail(LS_ERR_INVALID, "ls_paged_kv_attend: too many rows");
+  int lpk = 1;
+  while (lpk * 8 < a.dim) lpk *= 2;
+  const bool kv_vec = aligned16(a.k) && aligned16(a.v) && a.page_stride % 8 == 0 && a.token_stride % 8 == 0 && a.head_stride % 8 == 0;
+  const int vec = (kv_vec ? 1 : 0) | (q_vec ? 2 : 0);
+  if (ng == 1) LS_TRY((launch_rows<WD, 1>(a, lpk, vec, st)));
+  else if (ng == 4) LS_TRY((launch_rows<WD, 4>(a, lpk, vec, st)));
+  else LS_TRY((launch_rows<WD, 8>(a, lpk, vec, st)));
+  if (a.splits > 1) {
+    const long long rows = (long long)a.n_seqs * a.q_len * a.heads;
+    ls::ls_attend_rows_join_kernel<WD><<<(unsigned)((rows + 7) / 8), 256, 0, st>>>(a);
+    LS_LAUNCHED();
+  }
+  return LS_OK;
+}
+
+template <int XT, int BT>
+int32_t launch_norm(const ls::NormArgs& a, cudaStream_t st) {
+  const int threads = a.d >= 512 ? 512 : (a.d + 31) / 32 * 32;
+  const size_t smem = (size_t)a.d * sizeof(float);
+  if (smem > 48 * 1024 - 256)
+    LS_CUDA(cudaFuncSetAttribute(ls::ls_norm_rows_kernel<XT, BT>, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024));
+  ls::ls_norm_rows_kernel<XT, BT><<<(unsigned)a.n, threads, smem, st>>>(a);
+  LS_LAUNCHED();
+  return LS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t ls_paged_kv_create(const ls_paged_kv_desc* D, ls_paged_kv** out) {
+  if (out) *out = nullptr;
+  if (!D || !out) return fail(LS_ERR_INVALID, "ls_paged_kv_create: NULL argument");
+  if (D->struct_size != sizeof(ls_paged_kv_desc))
+    return fail(LS_ERR_INVALID, "ls_paged_kv_create: struct_size %u, expected %zu", D->struct_size, sizeof(ls_paged_kv_desc));
+  if (D->dtype != LS_WDTYPE_BF16 && D->dtype != LS_WDTYPE_FP16) return fail(LS_ERR_INVALID, "ls_paged_kv_create: unknown dtype");
+  if (D->n_kv_heads < 1 || D->n_q_heads < 1 || D->n_q_heads % D->n_kv_heads || D->n_q_heads > 65536)
+    return fail(LS_ERR_INVALID, "ls_paged_kv_create: n_q_heads must be a positive multiple of n_kv_heads");
+  if (D->head_dim < 8 || D->head_dim % 8 || D->head_dim > 256)
+    return fail(LS_ERR_INVALID, "ls_paged_kv_create: head_dim must be a multiple of 8 in [8, 256]");
+  if (D->page_size < 1 || D->n_pages < 1) return fail(LS_ERR_INVALID, "ls_paged_kv_create: page_size and n_pages must be positive");
+  if (!D->d_k || !D->d_v) return fail(LS_ERR_INVALID, "ls_paged_kv_create: missing pages");
+  if ((reinterpret_cast<uintptr_t>(D->d_k) | reinterpret_cast<uintptr_t>(D->d_v)) & 1)
+    return fail(LS_ERR_INVALID, "ls_paged_kv_create: misaligned pages");
+  if (D->page_stride < 0 || D->token_stride < 0 || D->head_stride < 0) return fail(LS_ERR_INVALID, "ls_paged_kv_create: negative stride");
+  if (D->max_seqs < 0 || D->max_q_len < 0 || (D->max_seqs > 0) != (D->max_q_len > 0))
+    return fail(LS_ERR_INVALID, "ls_paged_kv_create: max_seqs and max_q_len must both be positive, or both 0");
+  if (D->d_rope && (D->rope_dim < 2 || D->rope_dim % 2 || D->rope_dim > D->head_dim || D->rope_positions < 1))
+    return fail(LS_ERR_INVALID, "ls_paged_kv_create: rope_dim must be even in [2, head_dim] and rope_positions positive");
+  if (D->d_rope && (reinterpret_cast<uintptr_t>(D->d_rope) & 3)) return fail(LS_ERR_INVALID, "ls_paged_kv_create: misaligned rotation table");
+  int ndev = 0;
+  LS_CUDA(cudaGetDeviceCount(&ndev));
+  if (D->device < 0 || D->device >= ndev) return fail(LS_ERR_INVALID, "device %d out of range", D->device);
+  DeviceGuard guard(D->device);
+  ls_paged_kv* kv = new (std::nothrow) ls_paged_kv();
+  if (!kv) return fail(LS_ERR_NOMEM, "host allocation");
+  kv->d = *D;
+  if (!D->d_rope) kv->d.rope_dim = kv->d.rope_positions = 0;
+  const int32_t rc = create_kv(kv);
+  if (rc != LS_OK) {
+    const std::string keep = g_err;
+    free_kv(kv);
+    cudaGetLastError();
+    g_err = keep;
+    return rc;
+  }
+  *out = kv;
+  return LS_OK;
+}
+
+int32_t ls_paged_kv_destroy(ls_paged_kv* kv) {
+  if (!kv) return LS_OK;
+  DeviceGuard guard(kv->d.device);
+  cudaDeviceSynchronize();
+  free_kv(kv);
+  return LS_OK;
+}
+
+int32_t ls_paged_kv_status(ls_paged_kv* kv, int32_t* host_status) {
+  if (!kv || !host_status) return fail(LS_ERR_INVALID, "ls_paged_kv_status: NULL argument");
+  DeviceGuard guard(kv->d.device);
+  LS_CUDA(cudaDeviceSynchronize());
+  int v = 0;
+  LS_CUDA(cudaMemcpy(&v, kv->status, sizeof v, cudaMemcpyDeviceToHost));
+  LS_CUDA(cudaMemset(kv->status, 0, sizeof v));
+  *host_status = v;
+  return LS_OK;
+}
+
+int32_t ls_paged_kv_append(ls_paged_kv* kv, const void* d_q, int64_t q_stride, void* d_q_out, int64_t q_out_stride, const void* d_k,
+                           int64_t k_stride, const void* d_v, int64_t v_stride, int32_t n_tokens, const int32_t* d_seq,
+                           const int32_t* d_pos, const int32_t* d_table, int32_t n_seqs, int32_t table_width, int64_t table_stride,
+                           void* stream) {
+  if (!kv) return fail(LS_ERR_INVALID, "ls_paged_kv_append: NULL handle");
+  if (n_tokens < 0 || n_seqs < 0 || table_width < 0) return fail(LS_ERR_INVALID, "ls_paged_kv_append: negative size");
+  if (n_tokens == 0) return LS_OK;
+  if (!d_k || !d_v || !d_seq || !d_pos || (!d_table && n_seqs > 0 && table_width > 0))
+    return fail(LS_ERR_INVALID, "ls_paged_kv_append: k, v, seq, pos and table are required");
+  if ((d_q == nullptr) != (d_q_out == nullptr)) return fail(LS_ERR_INVALID, "ls_paged_kv_append: q and q_out go together");
+  const ls_paged_kv_desc& D = kv->d;
+  const int64_t qw = (int64_t)D.n_q_heads * D.head_dim, kw = (int64_t)D.n_kv_heads * D.head_dim;
+  if (k_stride < kw || v_stride < kw || (d_q && (q_stride < qw || q_out_stride < qw)))
+    return fail(LS_ERR_INVALID, "ls_paged_kv_append: a token stride is smaller than a token");
+  if (n_seqs > 1 && table_stride < table_width) return fail(LS_ERR_INVALID, "ls_paged_kv_append: table_stride is smaller than table_width");
+  DeviceGuard guard(D.device);
+  ls::AppendArgs a{};
+  a.q = static_cast<const uint16_t*>(d_q); a.q_out = static_cast<uint16_t*>(d_q_out);
+  a.k = static_cast<const uint16_t*>(d_k); a.v = static_cast<const uint16_t*>(d_v);
+  a.k_pages = static_cast<uint16_t*>(D.d_k); a.v_pages = static_cast<uint16_t*>(D.d_v);
+  a.seq = d_seq; a.pos = d_pos; a.table = d_table; a.rope = D.d_rope; a.status = kv->status;
+  a.q_stride = q_stride; a.q_out_stride = q_out_stride; a.k_stride = k_stride; a.v_stride = v_stride;
+  a.page_stride = D.page_stride; a.token_stride = D.token_stride; a.head_stride = D.head_stride; a.table_stride = table_stride;
+  a.n_tokens = n_tokens; a.n_seqs = n_seqs; a.heads = D.n_q_heads; a.kv_heads = D.n_kv_heads; a.dim = D.head_dim;
+  a.page = D.page_size; a.n_pages = D.n_pages; a.table_width = table_width;
+  a.rope_dim = D.rope_dim; a.rope_positions = D.rope_positions; a.interleaved = D.rope_interleaved;
+  const cudaStream_t st = (cudaStream_t)stream;
+  KernelTimer timer(LS_TIMED_APPEND, st);
+  const int items = ((d_q ? D.n_q_heads : 0) + 2 * D.n_kv_heads) * (D.head_dim / 2);
+  const dim3 grid((unsigned)n_tokens, (unsigned)std::min(64, (items + 255) / 256));
+  if (D.dtype == LS_WDTYPE_BF16) ls::ls_append_pairs_kernel<ls::WD_BF16><<<grid, 256, 0, st>>>(a);
+  else ls::ls_append_pairs_kernel<ls::WD_FP16><<<grid, 256, 0, st>>>(a);
+  LS_LAUNCHED();
+  return LS_OK;
+}
+
+int32_t ls_paged_kv_attend(ls_paged_kv* kv, const void* d_q, int64_t q_stride, void* d_out, int64_t out_stride, float* d_lse,
+                           int32_t n_seqs, int32_t q_len, const int32_t* d_seq_len, const int32_t* d_table, int32_t table_width,
+                           int64_t table_stride, const int32_t* d_prefix_pages, int32_t prefix_len, int32_t window, float scale,
+                           void* stream) {
+  if (!kv) return fail(LS_ERR_INVALID, "ls_paged_kv_attend: NULL handle");
+  if (n_seqs < 0 || q_len < 0 || table_width < 0 || prefix_len < 0 || window < 0)
+    return fail(LS_ERR_INVALID, "ls_paged_kv_attend: negative size");
+  const ls_paged_kv_desc& D = kv->d;
+  if (n_seqs > D.max_seqs || q_len > D.max_q_len)
+    return fail(LS_ERR_INVALID, "ls_paged_kv_attend: %d sequences of %d tokens, the handle was created for %d of %d", n_seqs, q_len, D.max_seqs,
+                D.max_q_len);
+  if (n_seqs == 0 || q_len == 0) return LS_OK;
+  if (!d_q || !d_out || !d_seq_len || (!d_table && table_width > 0)) return fail(LS_ERR_INVALID, "ls_paged_kv_attend: q, out, seq_len and table are required");
+  if (prefix_len > 0 && !d_prefix_pages) return fail(LS_ERR_INVALID, "ls_paged_kv_attend: prefix_len without prefix pages");
+  const int64_t qw = (int64_t)D.n_q_heads * D.head_dim;
+  if (q_stride < qw || out_stride < qw) return fail(LS_ERR_INVALID, "ls_paged_kv_attend: a token stride is smaller than a token");
+  if (n_seqs > 1 && table_stride < table_width) return fail(LS_ERR_INVALID, "ls_paged_kv_attend: table_stride is smaller than table_width");
+  if (!(scale > 0.f) || scale > 1e30f) return fail(LS_ERR_INVALID, "ls_paged_kv_attend: scale must be positive and finite");
+  DeviceGuard guard(D.device);
+  ls::AttendArgs a{};
+  a.q = d_q; a.out = d_out; a.lse = d_lse; a.k = D.d_k; a.v = D.d_v; a.seq_len = d_seq_len; a.table = d_table; a.prefix_pages = d_prefix_pages;
+  a.status = kv->status; a.part_o = kv->part_o; a.part_lse = kv->part_lse;
+  a.q_stride = q_stride; a.out_stride = out_stride; a.page_stride = D.page_stride; a.token_stride = D.token_stride;
+  a.head_stride = D.head_stride; a.table_stride = table_stride;
+  a.n_seqs = n_seqs; a.q_len = q_len; a.heads = D.n_q_heads; a.kv_heads = D.n_kv_heads; a.group = D.n_q_heads / D.n_kv_heads; a.dim = D.head_dim;
+  a.page = D.page_size; a.n_pages = D.n_pages; a.table_width = table_width; a.prefix = prefix_len; a.window = window;
+  a.scale_log2 = scale * ls::LOG2E;
+  const cudaStream_t st = (cudaStream_t)stream;
+  KernelTimer timer(LS_TIMED_ATTEND, st);
+  const bool q_vec = aligned16(d_q) && q_stride % 8 == 0;
+  return D.dtype == LS_WDTYPE_BF16 ? attend_rows<ls::WD_BF16>(a, q_vec, st) : attend_rows<ls::WD_FP16>(a, q_vec, st);
+}
+
+int32_t ls_block_norm(const void* d_x, int64_t x_stride, int32_t x_dtype, const void* d_y, int64_t y_stride, int32_t dtype, void* d_x_out,
+                      int64_t x_out_stride, void* d_h, int64_t h_stride, int32_t n, int32_t d, int32_t post_norm, const float* d_w_post,
+                      const void* d_gate, int64_t gate_stride, float scale, int32_t pre_norm, const float* d_w_pre, float eps,
+                      void* stream) {
+  if (n < 0 || d < 1 || d > 16384) return fail(LS_ERR_INVALID, "ls_block_norm: n must not be negative and d must be in [1, 16384]");
+  if (dtype != LS_WDTYPE_BF16 && dtype != LS_WDTYPE_FP16 && dtype != LS_DTYPE_F32) return fail(LS_ERR_INVALID, "ls_block_norm: unknown dtype");
+  if (x_dtype != LS_DTYPE_F32 && x_dtype != dtype) return fail(LS_ERR_INVALID, "ls_block_norm: the residual is float or of the block's type");
+  if ((post_norm != LS_NORM_RMS && post_norm != LS_NORM_NONE) || (pre_norm != LS_NORM_RMS && pre_norm != LS_NORM_NONE))
+    return fail(LS_ERR_INVALID, "ls_block_norm: unknown norm");
+  if (!(eps >= 0.f)) return fail(LS_ERR_INVALID, "ls_block_norm: eps must not be negative");
+  if (n == 0) return LS_OK;
+  if (!d_x || (!d_x_out && !d_h)) return fail(LS_ERR_INVALID, "ls_block_norm: x and one of x_out, h are required");
+  if (!d_y && (d_w_post || d_gate)) return fail(LS_ERR_INVALID, "ls_block_norm: a gain or gate of a block needs the block's output y");
+  if (n > 1 && (x_stride < d || (d_y && y_stride < d) || (d_x_out && x_out_stride < d) || (d_h && h_stride < d) ||
+                (d_gate && gate_stride != 0 && gate_stride < d)))
+    return fail(LS_ERR_INVALID, "ls_block_norm: a row stride is smaller than a row");
+  cudaPointerAttributes at{};
+  int dev = -1;
+  if (cudaPointerGetAttributes(&at, d_x) == cudaSuccess && at.type == cudaMemoryTypeDevice) dev = at.device;
+  else { cudaGetLastError(); LS_CUDA(cudaGetDevice(&dev)); }
+  DeviceGuard guard(dev);
+  ls::NormArgs a{};
+  a.x = d_x; a.y = d_y; a.x_out = d_x_out; a.h = d_h; a.w_post = d_w_post; a.w_pre = d_w_pre; a.gate = d_gate;
+  a.x_stride = x_stride; a.y_stride = y_stride; a.x_out_stride = x_out_stride; a.h_stride = h_stride; a.gate_stride = gate_stride;
+  a.n = n; a.d = d; a.post = post_norm == LS_NORM_RMS; a.pre = pre_norm == LS_NORM_RMS; a.scale = scale; a.eps = eps;
+  const cudaStream_t st = (cudaStream_t)stream;
+  KernelTimer timer(LS_TIMED_NORM, st);
+  if (x_dtype == LS_DTYPE_F32) {
+    if (dtype == LS_WDTYPE_BF16) return launch_norm<ls::DT_F32, ls::WD_BF16>(a, st);
+    if (dtype == LS_WDTYPE_FP16) return launch_norm<ls::DT_F32, ls::WD_FP16>(a, st);
+    return launch_norm<ls::DT_F32, ls::DT_F32>(a, st);
+  }
+  return dtype == LS_WDTYPE_BF16 ? launch_norm<ls::WD_BF16, ls::WD_BF16>(a, st) : launch_norm<ls::WD_FP16, ls::WD_FP16>(a, st);
+}
+
+}  // extern "C"

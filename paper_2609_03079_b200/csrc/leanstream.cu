@@ -14,80 +14,20 @@
 
 #include "ls_cache.cuh"
 #include "ls_hash.cuh"
+#include "ls_host.cuh"
 #include "ls_kernels.cuh"
 #include "ls_token.cuh"
 
 namespace {
 
-thread_local std::string g_err;
-std::atomic<int64_t> g_launches{0};
+using namespace ls_host;
+
 std::atomic<int> g_opt_fused{1};
 std::atomic<int> g_opt_miss_path{1};     // ls::MISS_PATH_GATHER
 std::atomic<int> g_opt_host_wait_ms{30000};
 
-int32_t fail(int32_t code, const char* fmt, ...) {
-  char buf[512];
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(buf, sizeof buf, fmt, ap);
-  va_end(ap);
-  g_err = buf;
-  return code;
-}
-
-#define LS_CUDA(call)                                                                         \
-  do {                                                                                        \
-    cudaError_t e_ = (call);                                                                  \
-    if (e_ != cudaSuccess) return fail(LS_ERR_CUDA, "%s: %s", #call, cudaGetErrorString(e_)); \
-  } while (0)
-
-#define LS_LAUNCHED()                                                                                   \
-  do {                                                                                                  \
-    g_launches.fetch_add(1, std::memory_order_relaxed);                                                 \
-    cudaError_t e_ = cudaPeekAtLastError();                                                             \
-    if (e_ != cudaSuccess) return fail(LS_ERR_CUDA, "kernel launch (%s:%d): %s", __FILE__, __LINE__,    \
-                                       cudaGetErrorString(e_));                                        \
-  } while (0)
-
-// Optional per-kernel timing with CUDA events on the launching stream (roofline accounting; off by default).
-struct TimedLaunch { int kind; cudaEvent_t a, b; };
-std::atomic<int> g_timing{0};
-std::mutex g_timing_mu;
-std::vector<TimedLaunch> g_timed;
-
-struct KernelTimer {
-  cudaStream_t st;
-  TimedLaunch t{};
-  bool on;
-  KernelTimer(int kind, cudaStream_t s) : st(s), on(g_timing.load(std::memory_order_relaxed) != 0) {
-    if (!on) return;
-    t.kind = kind;
-    if (cudaEventCreate(&t.a) != cudaSuccess || cudaEventCreate(&t.b) != cudaSuccess) { on = false; return; }
-    cudaEventRecord(t.a, st);
-  }
-  ~KernelTimer() {
-    if (!on) return;
-    cudaEventRecord(t.b, st);
-    std::lock_guard<std::mutex> lk(g_timing_mu);
-    g_timed.push_back(t);
-  }
-};
-
 // Dynamic shared memory the whole-token kernel is launched with (it also has about 1 KB of static shared memory).
 constexpr size_t kTokenSmemBudget = 222 * 1024;
-
-struct DeviceGuard {
-  int prev = -1;
-  explicit DeviceGuard(int dev) {
-    cudaGetDevice(&prev);
-    if (prev != dev) cudaSetDevice(dev);
-  }
-  ~DeviceGuard() {
-    int cur = -1;
-    cudaGetDevice(&cur);
-    if (prev >= 0 && cur != prev) cudaSetDevice(prev);
-  }
-};
 
 }  // namespace
 
@@ -165,22 +105,6 @@ struct ls_stack {
 };
 
 namespace {
-
-template <typename T>
-int32_t dalloc(T** p, size_t n) {
-  *p = nullptr;
-  if (n == 0) n = 1;
-  cudaError_t e = cudaMalloc(reinterpret_cast<void**>(p), n * sizeof(T));
-  if (e != cudaSuccess) return fail(e == cudaErrorMemoryAllocation ? LS_ERR_NOMEM : LS_ERR_CUDA, "cudaMalloc(%zu bytes): %s",
-                                    n * sizeof(T), cudaGetErrorString(e));
-  return LS_OK;
-}
-
-#define LS_TRY(expr)              \
-  do {                            \
-    int32_t rc_ = (expr);         \
-    if (rc_ != LS_OK) return rc_; \
-  } while (0)
 
 void free_layer(ls_layer* L) {
   if (!L) return;

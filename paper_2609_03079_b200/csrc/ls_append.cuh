@@ -1,0 +1,93 @@
+// Keys and values of new tokens go into their slots of a paged cache, queries and keys turned by their positions on the way.
+//
+// The first `rope_dim` components of a head are turned in pairs (x1, x2) -> (x1 c - x2 s, x2 c + x1 s), c and s from row
+// `position` of a table the caller keeps ([positions][rope_dim]: rope_dim / 2 cosines, then as many sines); a pair is
+// (i, i + rope_dim / 2), or (2 i, 2 i + 1) when interleaved.  The arithmetic is fp32, rounded once to the 16-bit type.
+#pragma once
+#include "ls_common.cuh"
+
+namespace ls {
+
+struct AppendArgs {
+  const uint16_t* q;   // [n_tokens][heads][dim] at token stride q_stride, or NULL
+  uint16_t* q_out;
+  const uint16_t* k;   // [n_tokens][kv_heads][dim]
+  const uint16_t* v;
+  uint16_t* k_pages;
+  uint16_t* v_pages;
+  const int32_t* seq;
+  const int32_t* pos;
+  const int32_t* table;
+  const float* rope;
+  int* status;
+  int64_t q_stride, q_out_stride, k_stride, v_stride, page_stride, token_stride, head_stride, table_stride;
+  int32_t n_tokens, n_seqs, heads, kv_heads, dim, page, n_pages, table_width, rope_dim, rope_positions, interleaved;
+};
+
+template <int WD>
+__device__ __forceinline__ float widen(uint16_t x) {
+  if (WD == WD_BF16) return __uint_as_float((uint32_t)x << 16);
+  return __half2float(__ushort_as_half(x));
+}
+template <int WD>
+__device__ __forceinline__ uint16_t narrow(float x) {
+  uint16_t r;
+  if (WD == WD_BF16) asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(r) : "f"(x));
+  else asm("cvt.rn.f16.f32 %0, %1;" : "=h"(r) : "f"(x));
+  return r;
+}
+
+// Where token t's keys and values go (element offset of head 0 in the pages), or -1: padding (a negative sequence or
+// position) is passed over silently, anything out of range is passed over and reported.
+__device__ __forceinline__ long long append_slot(const AppendArgs& A, int sq, int ps) {
+  if (sq < 0 || ps < 0) return -1;
+  const int pg = ps / A.page;
+  if (sq >= A.n_seqs || pg >= A.table_width || (A.rope_dim > 0 && ps >= A.rope_positions)) { set_status(A.status, ST_BAD_INDEX); return -1; }
+  const int id = A.table[(long long)sq * A.table_stride + pg];
+  if (id < 0 || id >= A.n_pages) { set_status(A.status, ST_BAD_INDEX); return -1; }
+  return id * A.page_stride + (long long)(ps - pg * A.page) * A.token_stride;
+}
+
+// One block row per token, one thread per pair of components: the route for any alignment and any even rope_dim.
+template <int WD>
+__global__ void __launch_bounds__(256) ls_append_pairs_kernel(const AppendArgs A) {
+  const long long t = blockIdx.x;
+  const int sq = A.seq[t], ps = A.pos[t];
+  const long long slot = append_slot(A, sq, ps);
+  const bool in_table = A.rope_dim == 0 || (ps >= 0 && ps < A.rope_positions);
+  const int half = A.dim / 2, r2 = A.rope_dim / 2, nq = A.q ? A.heads : 0;
+  const float* tab = A.rope + (long long)ps * A.rope_dim;
+  for (int j = blockIdx.y * blockDim.x + threadIdx.x; j < (nq + 2 * A.kv_heads) * half; j += gridDim.y * blockDim.x) {
+    const int hd = j / half, i = j - hd * half;
+    const uint16_t* src;
+    uint16_t* dst;
+    bool turn = i < r2;
+    if (hd < nq) {
+      src = A.q + t * A.q_stride + (long long)hd * A.dim;
+      dst = A.q_out + t * A.q_out_stride + (long long)hd * A.dim;
+      turn = turn && in_table;
+    } else {
+      if (slot < 0) continue;
+      const bool key = hd < nq + A.kv_heads;
+      const int h = hd - nq - (key ? 0 : A.kv_heads);
+      src = (key ? A.k + t * A.k_stride : A.v + t * A.v_stride) + (long long)h * A.dim;
+      dst = (key ? A.k_pages : A.v_pages) + slot + h * A.head_stride;
+      turn = turn && key;
+    }
+    // components of pair i: the turned ones first, the rest side by side
+    int c0, c1;
+    if (i < r2) { c0 = A.interleaved ? 2 * i : i; c1 = A.interleaved ? c0 + 1 : i + r2; }
+    else { c0 = 2 * i; c1 = c0 + 1; }
+    if (turn) {
+      const float x1 = widen<WD>(src[c0]), x2 = widen<WD>(src[c1]), c = tab[i], s = tab[r2 + i];
+      dst[c0] = narrow<WD>(x1 * c - x2 * s);
+      dst[c1] = narrow<WD>(x2 * c + x1 * s);
+    } else {
+      const uint16_t a = src[c0], b = src[c1];
+      dst[c0] = a;
+      dst[c1] = b;
+    }
+  }
+}
+
+}  // namespace ls
