@@ -12,7 +12,7 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libleanstream.so")
 SOURCES = ["leanstream.cu", "decoder_ops.cu"]
 HEADERS = ["ls_common.cuh", "ls_topk.cuh", "ls_kernels.cuh", "ls_cache.cuh", "ls_token.cuh", "ls_hash.cuh",
-           "ls_host.cuh", "ls_append.cuh", "ls_attend.cuh", "ls_norm.cuh"]
+           "ls_host.cuh", "ls_append.cuh", "ls_attend.cuh", "ls_attend_tile.cuh", "ls_tmem.cuh", "ls_norm.cuh"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

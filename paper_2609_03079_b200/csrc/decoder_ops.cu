@@ -6,6 +6,7 @@
 
 #include "ls_append.cuh"
 #include "ls_attend.cuh"
+#include "ls_attend_tile.cuh"
 #include "ls_host.cuh"
 #include "ls_norm.cuh"
 
@@ -14,9 +15,16 @@ using namespace ls_host;
 struct ls_paged_kv {
   ls_paged_kv_desc d{};
   int sm_count = 148;
-  float* part_o = nullptr;
+  float* part_o = nullptr;    // workspace of ls_attend_rows_kernel
   float* part_lse = nullptr;
   int* status = nullptr;
+  // the tile kernels, where the pages can be copied as boxes
+  bool tiles = false;
+  int box = 0;
+  CUtensorMap map_k{}, map_v{};
+  size_t pre_slots = 0, own_slots = 0, own_units = 0, pre_units = 0;  // in rows, rows, units, units
+  float* tile_ws = nullptr;
+  int32_t* tile_ids = nullptr;
 };
 
 namespace {
@@ -28,8 +36,137 @@ constexpr int kRowsMaxGroup = 8;
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 void free_kv(ls_paged_kv* kv) {
-  cudaFree(kv->part_o); cudaFree(kv->part_lse); cudaFree(kv->status);
+  cudaFree(kv->part_o); cudaFree(kv->part_lse); cudaFree(kv->status); cudaFree(kv->tile_ws); cudaFree(kv->tile_ids);
   delete kv;
+}
+
+// How the rows of n_seqs sequences of q_len tokens are cut into tiles, and what workspace the cut needs.
+struct TileCut {
+  int tq, ts, rt, pairs;
+  size_t pre_rows, own_rows, pre_units, own_units;
+  TileCut(int n_seqs, int q_len, int kv_heads, int group, int ctas) {
+    const long long tokens = (long long)n_seqs * q_len;
+    tq = 128 / group;
+    ts = std::min(tq, q_len);
+    rt = (q_len + ts - 1) / ts;
+    const long long tiles = (tokens + tq - 1) / tq;
+    pairs = tiles > 1 ? (int)((tiles + 1) / 2) : 0;
+    pre_units = (size_t)kv_heads * std::max(pairs, 1);
+    own_units = (size_t)n_seqs * kv_heads * rt;
+    pre_rows = pairs ? (pre_units + ctas) * 256 : (pre_units + 2 * ctas) * 128;
+    own_rows = (own_units + 2 * ctas) * ts * group;
+  }
+};
+
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+std::atomic<EncodeFn> g_encode{nullptr};
+
+int32_t encoder(EncodeFn* out) {
+  EncodeFn f = g_encode.load(std::memory_order_acquire);
+  if (!f) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    LS_CUDA(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q));
+    if (!p || q != cudaDriverEntryPointSuccess) return fail(LS_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
+    f = reinterpret_cast<EncodeFn>(p);
+    g_encode.store(f, std::memory_order_release);
+  }
+  *out = f;
+  return LS_OK;
+}
+
+// A map of 16-bit elements whose boxes are 64 elements (128 bytes, swizzled) wide; strides in bytes of dimensions 1...
+int32_t make_map(CUtensorMap* map, int dtype, void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+  EncodeFn enc = nullptr;
+  LS_TRY(encoder(&enc));
+  const cuuint32_t one[5] = {1, 1, 1, 1, 1};
+  const CUresult rc = enc(map, dtype == LS_WDTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank, base, dims, strides, box,
+                          one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (rc != CUDA_SUCCESS) return fail(LS_ERR_CUDA, "cuTensorMapEncodeTiled: error %d", (int)rc);
+  return LS_OK;
+}
+
+int32_t page_map(CUtensorMap* map, const ls_paged_kv_desc& d, void* base, int box) {
+  const cuuint64_t dims[4] = {(cuuint64_t)d.head_dim, (cuuint64_t)d.page_size, (cuuint64_t)d.n_kv_heads, (cuuint64_t)d.n_pages};
+  // (the stride of a dimension of one is never used; the pool's own may be anything)
+  const cuuint64_t strides[3] = {(cuuint64_t)d.token_stride * 2, (cuuint64_t)(d.n_kv_heads > 1 ? d.head_stride : d.head_dim) * 2,
+                                 (cuuint64_t)(d.n_pages > 1 ? d.page_stride : d.head_dim) * 2};
+  const cuuint32_t boxes[4] = {64, (cuuint32_t)box, 1, 1};
+  return make_map(map, d.dtype, base, 4, dims, strides, boxes);
+}
+
+// The tile kernels copy boxes of a page: head dimensions of whole 128-byte columns, pages of a multiple of eight tokens,
+// everything 16-byte aligned, a group that fits a tile.
+bool tiles_apply(const ls_paged_kv_desc& d) {
+  const int64_t limit = 1LL << 38;
+  auto good = [&](int64_t stride, int n) { return n == 1 || (stride >= 8 && stride % 8 == 0 && stride < limit); };
+  return (d.head_dim == 64 || d.head_dim == 128) && d.page_size % 8 == 0 && aligned16(d.d_k) && aligned16(d.d_v) && good(d.token_stride, d.page_size) &&
+         good(d.head_stride, d.n_kv_heads) && good(d.page_stride, d.n_pages) && d.n_q_heads / d.n_kv_heads <= 128;
+}
+
+template <int WD, int D>
+cudaError_t tile_attribute() {
+  return cudaFuncSetAttribute(ls::ls_attend_tile_kernel<WD, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, ls::TileShape<D>::SMEM);
+}
+
+int32_t create_tiles(ls_paged_kv* kv) {
+  const ls_paged_kv_desc& d = kv->d;
+  kv->box = 8;
+  while (kv->box < 128 && d.page_size % (kv->box * 2) == 0) kv->box *= 2;
+  LS_TRY(page_map(&kv->map_k, d, d.d_k, kv->box));
+  LS_TRY(page_map(&kv->map_v, d, d.d_v, kv->box));
+  if (d.head_dim == 64) LS_CUDA((d.dtype == LS_WDTYPE_BF16 ? tile_attribute<ls::WD_BF16, 64>() : tile_attribute<ls::WD_FP16, 64>()));
+  else LS_CUDA((d.dtype == LS_WDTYPE_BF16 ? tile_attribute<ls::WD_BF16, 128>() : tile_attribute<ls::WD_FP16, 128>()));
+  const TileCut c(d.max_seqs, d.max_q_len, d.n_kv_heads, d.n_q_heads / d.n_kv_heads, kv->sm_count);
+  // (fewer rows may need more pieces when they fit a single tile)
+  kv->pre_slots = std::max(c.pre_rows, (size_t)(d.n_kv_heads + 2 * kv->sm_count) * 128);
+  kv->own_slots = c.own_rows;
+  kv->pre_units = c.pre_units;
+  kv->own_units = c.own_units;
+  LS_TRY(dalloc(&kv->tile_ws, (kv->pre_slots + kv->own_slots) * (d.head_dim + 1)));
+  LS_TRY(dalloc(&kv->tile_ids, 2 * (kv->pre_units + kv->own_units) + 1));
+  kv->tiles = true;
+  return LS_OK;
+}
+
+template <int WD, int D>
+int32_t attend_tiles(ls_paged_kv* kv, const ls::AttendArgs& a, cudaStream_t st) {
+  ls::TileArgs t{};
+  t.a = a;
+  const TileCut c(a.n_seqs, a.q_len, a.kv_heads, a.group, kv->sm_count);
+  if (c.pre_rows > kv->pre_slots || c.own_rows > kv->own_slots || c.pre_units > kv->pre_units || c.own_units > kv->own_units)
+    return fail(LS_ERR_INTERNAL, "ls_paged_kv_attend: workspace");
+  t.tq = c.tq; t.ts = c.ts; t.rt = c.rt; t.pairs = c.pairs; t.box = kv->box;
+  t.pre_o = kv->tile_ws; t.own_o = t.pre_o + kv->pre_slots * D;
+  t.pre_lse = t.own_o + kv->own_slots * D; t.own_lse = t.pre_lse + kv->pre_slots;
+  t.pre_first = kv->tile_ids; t.pre_last = t.pre_first + kv->pre_units;
+  t.own_first = t.pre_last + kv->pre_units; t.own_last = t.own_first + kv->own_units;
+  t.plan = t.own_last + kv->own_units;
+  CUtensorMap q_all, q_own;
+  const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)a.heads, (cuuint64_t)a.n_seqs * a.q_len};
+  const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)a.q_stride * 2};
+  const cuuint32_t box_all[3] = {64, (cuuint32_t)a.group, (cuuint32_t)c.tq}, box_own[3] = {64, (cuuint32_t)a.group, (cuuint32_t)c.ts};
+  void* q = const_cast<void*>(a.q);
+  LS_TRY(make_map(&q_own, WD == ls::WD_BF16 ? LS_WDTYPE_BF16 : LS_WDTYPE_FP16, q, 3, dims, strides, box_own));
+  if (a.prefix > 0) LS_TRY(make_map(&q_all, WD == ls::WD_BF16 ? LS_WDTYPE_BF16 : LS_WDTYPE_FP16, q, 3, dims, strides, box_all));
+  else q_all = q_own;
+  ls::ls_attend_tile_kernel<WD, D><<<kv->sm_count, ls::AT_THREADS, ls::TileShape<D>::SMEM, st>>>(t, kv->map_k, kv->map_v, q_all, q_own);
+  LS_LAUNCHED();
+  const long long rows = (long long)a.n_seqs * a.q_len * a.heads;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)((rows + 7) / 8));
+  cfg.blockDim = dim3(256);
+  cfg.stream = st;
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  LS_CUDA((cudaLaunchKernelEx(&cfg, ls::ls_attend_tile_join_kernel<WD, D>, t)));
+  LS_LAUNCHED();
+  return LS_OK;
 }
 
 int32_t create_kv(ls_paged_kv* kv) {
@@ -43,6 +180,7 @@ int32_t create_kv(ls_paged_kv* kv) {
     const size_t rows = (size_t)kRowsBlocks * kRowsMaxGroup;
     LS_TRY(dalloc(&kv->part_o, rows * d.head_dim));
     LS_TRY(dalloc(&kv->part_lse, rows));
+    if (tiles_apply(d)) LS_TRY(create_tiles(kv));
   }
   return LS_OK;
 }
@@ -216,6 +354,10 @@ int32_t ls_paged_kv_attend(ls_paged_kv* kv, const void* d_q, int64_t q_stride, v
   const cudaStream_t st = (cudaStream_t)stream;
   KernelTimer timer(LS_TIMED_ATTEND, st);
   const bool q_vec = aligned16(d_q) && q_stride % 8 == 0;
+  if (kv->tiles && q_vec) {
+    if (D.head_dim == 64) return D.dtype == LS_WDTYPE_BF16 ? attend_tiles<ls::WD_BF16, 64>(kv, a, st) : attend_tiles<ls::WD_FP16, 64>(kv, a, st);
+    return D.dtype == LS_WDTYPE_BF16 ? attend_tiles<ls::WD_BF16, 128>(kv, a, st) : attend_tiles<ls::WD_FP16, 128>(kv, a, st);
+  }
   return D.dtype == LS_WDTYPE_BF16 ? attend_rows<ls::WD_BF16>(a, q_vec, st) : attend_rows<ls::WD_FP16>(a, q_vec, st);
 }
 

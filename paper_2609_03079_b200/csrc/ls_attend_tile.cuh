@@ -1,0 +1,617 @@
+// Attention over a paged cache on the 5th-generation tensor cores: tiles of 128 query rows by 128 keys.
+//
+// The rows of one key head fill a tile: (tokens, query heads of the group), 128 / group tokens at a time.  Work is cut into
+// units, each a set of rows and a range of keys:
+//   pair units    two row tiles of the whole batch against the shared prefix (rows of the batch exceed one tile),
+//   single units  the one row tile of the whole batch against the shared prefix (they do not),
+//   own units     the rows of one sequence against its own keys.
+// All (unit, key tile) pairs stand in one line, in a fixed order; every CTA takes an equal share of the line by cost and may
+// start and end inside a unit.  A piece (one unit on one worker) leaves its normalised output and its lse in a slot of the
+// workspace; a second kernel joins the pieces of every row in a fixed order.  Nothing about the lengths is needed on the host.
+//
+// A CTA has two lanes of 128 rows, each with its own score and output accumulators in tensor memory (2 x (128 + dim) columns),
+// and works on both in turn: while the tensor cores multiply for one lane, the four warps of the other do its softmax.  In a
+// pair the lanes share every key and value tile; elsewhere each lane has its own line of (unit, key tile).
+//   warp 8  copies keys, values and queries to shared memory (tensor maps, a box per page, ring of tiles);
+//   warp 9  issues S = Q K^T and O += P V (P is read from tensor memory, where it overwrites S);
+//   warps 0-3, 4-7  softmax of lanes 0 and 1, one thread per row.
+// A row's reference maximum follows its true maximum only when that has risen by more than 2^8: weights stay below 2^8, the
+// final division makes the reference irrelevant, and the accumulator in tensor memory is almost never rescaled.
+#pragma once
+#include "ls_attend.cuh"
+#include "ls_tmem.cuh"
+
+namespace ls {
+
+constexpr int AT_THREADS = 320;
+constexpr int AT_KEYS = 128;
+constexpr long long AT_SPIN_CLOCKS = 4000LL * 1000 * 1000;  // about two seconds
+constexpr int AT_COST_PAIR = 2, AT_COST_LANE = 1;           // of one key tile, in units of half a CTA
+
+template <int D>
+struct TileShape {
+  static constexpr int STAGES = D == 128 ? 5 : 8;
+  static constexpr int TILE = AT_KEYS * D * 2;   // bytes of a key, value or query tile
+  static constexpr int HALF = AT_KEYS * 128;     // bytes of 64 of its columns
+  static constexpr int SMEM = 1024 + (2 + STAGES) * TILE;
+};
+
+struct TileArgs {
+  AttendArgs a;
+  int32_t tq;        // tokens of a row tile (of the whole batch)
+  int32_t ts, rt;    // tokens of a row tile of one sequence, row tiles of a sequence
+  int32_t pairs;     // pairs of row tiles of the whole batch, 0: single
+  int32_t box;       // keys per copy: the largest power of two that divides the page, at most 128
+  float *pre_o, *pre_lse;  // slots of pair units ([2][128] rows) or single units ([128] rows)
+  float *own_o, *own_lse;  // slots of own units ([ts * group] rows)
+  int32_t *pre_first, *pre_last, *own_first, *own_last;  // per unit: the worker of its first and last piece
+  int32_t* plan;     // [1] key tiles of the prefix
+};
+
+// The keys of sequence b that are its own: [lo, hi) is what any of its tokens sees, tiles start at `origin`.
+struct OwnKeys { int lo, hi, origin, tiles; };
+__device__ __forceinline__ OwnKeys own_keys(const TileArgs& T, int len) {
+  OwnKeys k;
+  const int first = T.a.window > 0 ? max(len - T.a.q_len + 1 - T.a.window, 0) : 0;
+  k.lo = max(first, T.a.prefix);
+  k.hi = len;
+  k.origin = k.lo / T.box * T.box;
+  k.tiles = k.hi > k.lo ? (k.hi - k.origin + AT_KEYS - 1) / AT_KEYS : 0;
+  return k;
+}
+
+// What every CTA derives from the lengths: the line of work and its own share of it.
+struct Share {
+  int pre_lo, pre_origin, pre_tiles;  // prefix keys that any token sees: [pre_lo, prefix)
+  long long pair0, pair1;             // this CTA's (pair unit, tile) range
+  long long lane0[2], lane1[2];       // its lanes' ranges in the line of single and own units
+  int own_b[2], own_u[2], own_t[2];   // where a lane's range starts, if among the own units: sequence, unit within it, tile
+};
+
+// Walks one lane's (unit, tile) line; all roles of a CTA walk the same line.
+enum { AT_PAIR = 0, AT_SINGLE = 1, AT_OWN = 2 };
+struct Walk {
+  long long w, end;       // position in the current part of the line
+  bool pairs;             // still in the part of the pairs
+  int b, u, tile, tiles;  // next own unit (b = -1: still among the single ones), its next tile, its tiles (-1: to be looked up)
+  int left;               // tiles of the current piece not yet taken
+  // the tile just taken
+  int kind;
+  bool fresh, last;       // first, last tile of its piece
+  bool unit_first, unit_last;  // its piece holds the unit's first, last tile
+  int h, tok, ntok;       // key head, first token and number of tokens of the row tile
+  int k0, lo, hi, origin; // its first key; keys outside [lo, hi) are nobody's; first key of the unit's first tile
+  long long unit;         // number of the unit among its kind
+};
+
+__device__ __forceinline__ void walk_start(const Share& S, Walk& W) {
+  W.pairs = true;
+  W.w = S.pair0;
+  W.end = S.pair1;
+  W.left = 0;
+}
+
+// Takes the next tile of lane `lane`'s line; false at its end.
+__device__ __forceinline__ bool walk_next(const TileArgs& T, const Share& S, int lane, Walk& W) {
+  const AttendArgs& A = T.a;
+  if (W.left > 0) {
+    --W.left;
+    W.k0 += AT_KEYS;
+    W.fresh = false;
+    W.last = W.left == 0;
+    return true;
+  }
+  if (W.pairs && W.w == W.end) {
+    W.pairs = false;
+    W.w = S.lane0[lane]; W.end = S.lane1[lane];
+    W.b = S.own_b[lane]; W.u = S.own_u[lane]; W.tile = S.own_t[lane]; W.tiles = -1;
+  }
+  if (W.w >= W.end) return false;
+  int n, tile;
+  if (W.pairs || W.b < 0) {
+    W.unit = W.w / S.pre_tiles;
+    tile = (int)(W.w - W.unit * S.pre_tiles);
+    n = (int)min((long long)(S.pre_tiles - tile), W.end - W.w);
+    if (W.pairs) {
+      W.kind = AT_PAIR;
+      W.h = (int)(W.unit / T.pairs);
+      W.tok = ((int)(W.unit - (long long)W.h * T.pairs) * 2 + lane) * T.tq;
+    } else {
+      W.kind = AT_SINGLE;
+      W.h = (int)W.unit;
+      W.tok = 0;
+      if (W.w + n == (long long)A.kv_heads * S.pre_tiles) { W.b = 0; W.u = 0; W.tile = 0; }
+    }
+    W.ntok = min(T.tq, A.n_seqs * A.q_len - W.tok);
+    W.lo = S.pre_lo; W.hi = A.prefix; W.origin = S.pre_origin;
+    W.unit_first = tile == 0;
+    W.unit_last = tile + n == S.pre_tiles;
+  } else {
+    const int per = A.kv_heads * T.rt;
+    if (W.tiles < 0) {
+      for (;; ++W.b) {  // (sequences without keys of their own have no units; the line ends before the sequences do)
+        const OwnKeys k = own_keys(T, attend_len(A, W.b, false));
+        W.tiles = k.tiles; W.lo = k.lo; W.hi = k.hi; W.origin = k.origin;
+        if (k.tiles > 0) break;
+      }
+    }
+    W.kind = AT_OWN;
+    tile = W.tile;
+    n = (int)min((long long)(W.tiles - tile), W.end - W.w);
+    W.unit = (long long)W.b * per + W.u;
+    W.h = W.u / T.rt;
+    const int rt = W.u - W.h * T.rt;
+    W.tok = W.b * A.q_len + rt * T.ts;
+    W.ntok = min(T.ts, A.q_len - rt * T.ts);
+    W.unit_first = tile == 0;
+    W.unit_last = tile + n == W.tiles;
+    W.tile = 0;
+    if (W.unit_last && ++W.u == per) { W.u = 0; ++W.b; W.tiles = -1; }
+  }
+  W.w += n;
+  W.left = n - 1;
+  W.k0 = W.origin + tile * AT_KEYS;
+  W.fresh = true;
+  W.last = W.left == 0;
+  return true;
+}
+
+// Every thread of the CTA: the share of CTA c of n.
+__device__ __forceinline__ void make_share(const TileArgs& T, Share& S, long long* s_scan, int c, int n) {
+  const AttendArgs& A = T.a;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = AT_THREADS / 32;
+  const int per = (A.n_seqs + AT_THREADS - 1) / AT_THREADS;
+  const int b0 = min(tid * per, A.n_seqs), b1 = min(b0 + per, A.n_seqs);
+  long long sum = 0;
+  int lo = A.prefix;  // first prefix key that anybody sees
+  for (int b = b0; b < b1; ++b) {
+    const int len = attend_len(A, b, c == 0);
+    sum += own_keys(T, len).tiles;
+    if (len > 0) lo = min(lo, A.window > 0 ? max(len - A.q_len + 1 - A.window, 0) : 0);
+  }
+  long long incl = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += v;
+  }
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  if (lane == 31) { s_scan[warp] = incl; s_scan[nw + warp] = lo; }
+  __syncthreads();
+  long long before = incl - sum, total = 0;
+  for (int w = 0; w < nw; ++w) {
+    if (w < warp) before += s_scan[w];
+    total += s_scan[w];
+    lo = min(lo, (int)s_scan[nw + w]);
+  }
+  const int origin = lo / T.box * T.box;
+  const int pre_tiles = A.prefix > lo ? (A.prefix - origin + AT_KEYS - 1) / AT_KEYS : 0;
+  const long long n_pair = (long long)A.kv_heads * T.pairs * pre_tiles;
+  const long long n_single = T.pairs ? 0 : (long long)A.kv_heads * pre_tiles;
+  const long long mult = (long long)A.kv_heads * T.rt, n_lane = n_single + total * mult;
+  const long long cost = n_pair * AT_COST_PAIR + n_lane * AT_COST_LANE;
+  // Pieces of a unit have to be on consecutive workers: no worker between the first and the last may be empty, so that little
+  // work goes to fewer CTAs, each with a tile for both lanes.
+  const long long used = max(1LL, min((long long)n, cost / max(AT_COST_PAIR, 2 * AT_COST_LANE)));
+  const long long x0 = cost * min((long long)c, used) / used, x1 = cost * min(c + 1LL, used) / used;
+  auto pair_at = [&](long long x) { return min(n_pair, (x + AT_COST_PAIR - 1) / AT_COST_PAIR); };
+  auto lane_at = [&](long long x) {
+    x -= n_pair * AT_COST_PAIR;
+    return x <= 0 ? 0LL : min(n_lane, (x + AT_COST_LANE - 1) / AT_COST_LANE);
+  };
+  const long long g0 = lane_at(x0), g1 = lane_at(x1), mid = g0 + (g1 - g0) / 2;
+  if (tid == 0) {
+    S.pre_lo = lo; S.pre_origin = origin; S.pre_tiles = pre_tiles;
+    S.pair0 = pair_at(x0); S.pair1 = pair_at(x1);
+    S.lane0[0] = g0; S.lane1[0] = mid; S.lane0[1] = mid; S.lane1[1] = g1;
+    for (int l = 0; l < 2; ++l)
+      if ((l ? mid : g0) < n_single) { S.own_b[l] = -1; S.own_u[l] = 0; S.own_t[l] = 0; }
+  }
+  for (int l = 0; l < 2; ++l) {  // the thread whose sequences hold the start of a lane's range finds it
+    const long long w = (l ? mid : g0) - n_single;
+    long long acc = before * mult;
+    if (w < acc || w >= acc + sum * mult) continue;
+    for (int b = b0; b < b1; ++b) {
+      const int t = own_keys(T, attend_len(A, b, false)).tiles;
+      if (w < acc + t * mult) {
+        S.own_b[l] = b;
+        S.own_u[l] = (int)((w - acc) / t);
+        S.own_t[l] = (int)((w - acc) - (long long)S.own_u[l] * t);
+        break;
+      }
+      acc += t * mult;
+    }
+  }
+  __syncthreads();
+}
+
+template <int WD, int D>
+__global__ void __launch_bounds__(AT_THREADS, 1)
+    ls_attend_tile_kernel(const TileArgs T, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                          const __grid_constant__ CUtensorMap map_q_all, const __grid_constant__ CUtensorMap map_q_own) {
+  using TS = TileShape<D>;
+  constexpr int NST = TS::STAGES;
+  extern __shared__ unsigned char dyn[];
+  __shared__ Share S;
+  __shared__ long long s_scan[2 * AT_THREADS / 32];
+  __shared__ alignas(8) unsigned long long bars[2 * NST + 10];
+  __shared__ uint32_t s_tmem;
+  __shared__ volatile int s_dead;
+  const AttendArgs& A = T.a;
+  const int tid = threadIdx.x, lane_id = tid & 31, warp = tid >> 5;
+  const uint32_t q_base = (saddr(dyn) + 1023) & ~1023u, ring = q_base + 2 * TS::TILE;
+  const uint32_t bar0 = saddr(bars);
+  const uint32_t b_full = bar0, b_empty = bar0 + 8 * NST, b_qfull = b_empty + 8 * NST, b_qempty = b_qfull + 16, b_s = b_qempty + 16,
+                 b_p = b_s + 16, b_o = b_p + 16;
+
+  if (tid == 0) {
+    for (int i = 0; i < NST; ++i) { mb_init(b_full + 8 * i, 1); mb_init(b_empty + 8 * i, 1); }
+    for (int l = 0; l < 2; ++l) {
+      mb_init(b_qfull + 8 * l, 1); mb_init(b_qempty + 8 * l, 1); mb_init(b_s + 8 * l, 1); mb_init(b_p + 8 * l, 4); mb_init(b_o + 8 * l, 1);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    fence_async_shared();
+    s_dead = 0;
+  }
+  if (warp == 9) tm_alloc(saddr(&s_tmem), 512);
+  if (warp == 8 && lane_id < 4) tma_prefetch_map(lane_id == 0 ? &map_k : lane_id == 1 ? &map_v : lane_id == 2 ? &map_q_all : &map_q_own);
+  make_share(T, S, s_scan, blockIdx.x, gridDim.x);
+  tm_fence_before();
+  __syncthreads();
+  tm_fence_after();
+  const uint32_t tmem = s_tmem;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  // Bounded wait of a whole warp: false (for all of it) once any wait of the CTA has given up.
+  auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
+    bool got = mb_try(bar, parity);
+    if (!got) {
+      const long long t0 = clock64();
+      while (!(got = mb_try(bar, parity))) {
+        if (s_dead) break;
+        if (clock64() - t0 > AT_SPIN_CLOCKS) { s_dead = 1; set_status(A.status, ST_TIMEOUT); break; }
+      }
+    }
+    return __all_sync(0xffffffffu, got);
+  };
+
+  const long long n_pair = S.pair1 - S.pair0;
+  const long long cnt0 = n_pair + S.lane1[0] - S.lane0[0], cnt1 = n_pair + S.lane1[1] - S.lane0[1];
+  const long long rounds = max(cnt0, cnt1);
+
+  bool ok = true;
+  if (warp == 8) {
+    // ---- copies.  Order of the ring: for every round r and lane: values of round r - 1, keys of round r; a pair's once.
+    Walk W[2];
+    int vk0[2], vlo[2], vhi[2], vh[2], vpage[2];  // of the tile whose values are still to be fetched
+    uint32_t st = 0, st_par = 1, q_par[2] = {1, 1};
+    walk_start(S, W[0]);
+    walk_start(S, W[1]);
+    const int nbox = AT_KEYS / T.box;
+    const int my_box = lane_id & (nbox - 1), my_half = lane_id / nbox;
+    auto load_tile = [&](const CUtensorMap* map, int k0, int lo, int hi, int h, int page) -> bool {
+      const int key = k0 + my_box * T.box;
+      const bool on = my_half < D / 64 && key < hi && key + T.box > lo;
+      const int count = __popc(__ballot_sync(0xffffffffu, on));
+      if (!wait(b_empty + 8 * st, st_par)) return false;
+      if (lane_id == 0) mb_expect(b_full + 8 * st, count * T.box * 128);
+      __syncwarp();
+      if (on)
+        tma_load4(ring + st * TS::TILE + my_half * TS::HALF + my_box * T.box * 128, map, my_half * 64, key % A.page, h, page, b_full + 8 * st);
+      if (++st == NST) { st = 0; st_par ^= 1; }
+      return true;
+    };
+    auto page_of = [&](const Walk& w) {  // this lane's page of the tile just taken; one outside the pool reads as zeros
+      const int key = w.k0 + my_box * T.box;
+      if (key >= w.hi || key + T.box <= w.lo) return -1;
+      const int32_t* tab = w.kind == AT_OWN ? A.table + (long long)(w.tok / A.q_len) * A.table_stride : A.prefix_pages;
+      const int id = tab[key / A.page];
+      if (id >= 0 && id < A.n_pages) return id;
+      set_status(A.status, ST_BAD_INDEX);
+      return A.n_pages;
+    };
+    for (long long r = 0; ok && r <= rounds; ++r) {
+#pragma unroll
+      for (int l = 0; l < 2; ++l) {
+        const long long cnt = l ? cnt1 : cnt0;
+        if (ok && r > 0 && r <= cnt && !(r <= n_pair && l == 1)) ok = load_tile(&map_v, vk0[l], vlo[l], vhi[l], vh[l], vpage[l]);
+        if (!ok || r >= cnt) continue;
+        Walk& w = W[l];
+        walk_next(T, S, l, w);
+        if (w.fresh) {
+          ok = wait(b_qempty + 8 * l, q_par[l]);
+          if (!ok) continue;
+          q_par[l] ^= 1;
+          if (lane_id == 0) {
+            const bool own = w.kind == AT_OWN;
+            mb_expect(b_qfull + 8 * l, (own ? T.ts : T.tq) * A.group * D * 2);
+#pragma unroll
+            for (int f = 0; f < D / 64; ++f)
+              tma_load3(q_base + l * TS::TILE + f * TS::HALF, own ? &map_q_own : &map_q_all, f * 64, w.h * A.group, w.tok, b_qfull + 8 * l);
+          }
+          __syncwarp();
+        }
+        if (w.kind == AT_PAIR && l == 1) continue;
+        vk0[l] = w.k0; vlo[l] = w.lo; vhi[l] = w.hi; vh[l] = w.h; vpage[l] = page_of(w);
+        ok = load_tile(&map_k, w.k0, w.lo, w.hi, w.h, vpage[l]);
+      }
+    }
+  } else if (warp == 9) {
+    // ---- products, in the order of the ring: per round and lane O += P V of round r - 1, then S = Q K^T of round r (which
+    // overwrites P).  One thread issues; the warp clears value rows that are nobody's (whatever the page holds there, its
+    // weight of zero must not meet an infinity).
+    constexpr uint32_t ID_S = mma_idesc(WD == WD_BF16, 128, AT_KEYS, false), ID_O = mma_idesc(WD == WD_BF16, 128, D, true);
+    Walk W[2];
+    int vk0[2], vlo[2], vhi[2];
+    bool vfresh[2];
+    uint32_t st = 0, st_par = 0, q_par[2] = {0, 0}, p_par[2] = {0, 0}, kst = 0, vst = 0;
+    walk_start(S, W[0]);
+    walk_start(S, W[1]);
+    auto take = [&](uint32_t& slot) -> bool {
+      slot = st;
+      const bool got = wait(b_full + 8 * st, st_par);
+      if (++st == NST) { st = 0; st_par ^= 1; }
+      return got;
+    };
+    for (long long r = 0; ok && r <= rounds; ++r) {
+#pragma unroll
+      for (int l = 0; l < 2; ++l) {
+        const long long cnt = l ? cnt1 : cnt0;
+        if (ok && r > 0 && r <= cnt) {
+          const bool pair = r <= n_pair;
+          if (!(pair && l == 1)) {
+            ok = take(vst);
+            if (ok && (vk0[l] < vlo[l] || vk0[l] + AT_KEYS > vhi[l])) {
+              for (int c = lane_id; c < AT_KEYS; c += 32) {
+                if (vk0[l] + c >= vlo[l] && vk0[l] + c < vhi[l]) continue;
+                for (int f = 0; f < D / 64; ++f)
+                  for (int j = 0; j < 8; ++j)
+                    asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ring + vst * TS::TILE + f * TS::HALF + c * 128 + j * 16), "r"(0) : "memory");
+              }
+              fence_async_shared();
+              __syncwarp();
+            }
+          }
+          if (ok) ok = wait(b_p + 8 * l, p_par[l]);
+          p_par[l] ^= 1;
+          if (ok && lane_id == 0) {
+            tm_fence_after();
+            const uint32_t v = ring + vst * TS::TILE;
+#pragma unroll
+            for (int k = 0; k < AT_KEYS / 16; ++k)
+              tm_mma_ts(tmem + 256 + l * D, tmem + l * AT_KEYS + k * 8, smem_desc(v + k * 2048, TS::HALF), ID_O, !(vfresh[l] && k == 0));
+            tm_commit(b_o + 8 * l);
+            if (!(pair && l == 0)) tm_commit(b_empty + 8 * vst);
+          }
+          __syncwarp();
+        }
+        if (!ok || r >= cnt) continue;
+        Walk& w = W[l];
+        walk_next(T, S, l, w);
+        const bool pair = w.kind == AT_PAIR;
+        vk0[l] = w.k0; vlo[l] = w.lo; vhi[l] = w.hi; vfresh[l] = w.fresh;
+        if (!(pair && l == 1)) ok = take(kst);
+        if (ok && w.fresh) { ok = wait(b_qfull + 8 * l, q_par[l]); q_par[l] ^= 1; }
+        if (ok && lane_id == 0) {
+          tm_fence_after();
+          const uint32_t q = q_base + l * TS::TILE, k = ring + kst * TS::TILE;
+#pragma unroll
+          for (int c = 0; c < D / 16; ++c) {
+            const uint32_t off = (c / 4) * TS::HALF + (c % 4) * 32;
+            tm_mma_ss(tmem + l * AT_KEYS, smem_desc(q + off, 16), smem_desc(k + off, 16), ID_S, c > 0);
+          }
+          tm_commit(b_s + 8 * l);
+          if (!(pair && l == 0)) tm_commit(b_empty + 8 * kst);
+          if (w.last) tm_commit(b_qempty + 8 * l);
+        }
+        __syncwarp();
+      }
+    }
+  } else {
+    // ---- softmax: one thread per row
+    const int l = warp >> 2, row = (warp & 3) * 32 + lane_id;
+    const uint32_t t_s = tmem + ((warp & 3) << 21) + l * AT_KEYS, t_o = tmem + ((warp & 3) << 21) + 256 + l * D;
+    const int tr = row / A.group, worker = blockIdx.x * 2 + l;
+    Walk W;
+    walk_start(S, W);
+    int lo = 0, hi = 0;
+    bool live = false, warp_live = false;
+    float m = -INFINITY, sum = 0.f;
+    for (uint32_t n = 0; ok && walk_next(T, S, l, W); ++n) {
+      if (W.fresh) {
+        live = tr < W.ntok;
+        warp_live = __any_sync(0xffffffffu, live);
+        m = -INFINITY;
+        sum = 0.f;
+        if (live) {
+          const int t = W.tok + tr, b = t / A.q_len;
+          hi = max(attend_len(A, b, false) - A.q_len + (t - b * A.q_len) + 1, 0);
+          lo = A.window > 0 ? max(hi - A.window, 0) : 0;
+          if (W.kind == AT_OWN) lo = max(lo, A.prefix);
+          else hi = min(hi, A.prefix);
+        }
+      }
+      if (!wait(b_s + 8 * l, n & 1)) { ok = false; break; }
+      tm_fence_after();
+      if (warp_live) {
+        uint32_t s[AT_KEYS];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tm_ld32(t_s + 32 * c, s + 32 * c);
+        tm_wait_ld();
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tm_pin32(s + 32 * c);
+        if (!__all_sync(0xffffffffu, !live || (lo <= W.k0 && hi >= W.k0 + AT_KEYS))) {
+#pragma unroll
+          for (int c = 0; c < AT_KEYS; ++c) {
+            const int key = W.k0 + c;
+            if (key < lo || key >= hi) s[c] = 0xff800000u;
+          }
+        }
+        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int c = 0; c < AT_KEYS; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(s[c]));
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        const bool rise = live && top > m && (m == -INFINITY || (top - m) * A.scale_log2 > 8.f);
+        if (__any_sync(0xffffffffu, rise)) {
+          const float f = rise ? ex2((m - top) * A.scale_log2) : 1.f;
+          if (rise) { m = top; sum *= f; }
+          if (!W.fresh) {
+            if (!wait(b_o + 8 * l, (n - 1) & 1)) { ok = false; break; }
+            tm_fence_after();
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t o[32];
+              tm_ld32(t_o + 32 * c, o);
+              tm_wait_ld();
+              tm_pin32(o);
+#pragma unroll
+              for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+              tm_st32(t_o + 32 * c, o);
+            }
+          }
+        }
+        const float off = m == -INFINITY ? 0.f : -m * A.scale_log2;
+        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const float p0 = ex2(fmaf(__uint_as_float(s[32 * c + 2 * j]), A.scale_log2, off));
+            const float p1 = ex2(fmaf(__uint_as_float(s[32 * c + 2 * j + 1]), A.scale_log2, off));
+            acc[j & 1] += p0;
+            acc[2 + (j & 1)] += p1;
+            pk[j] = pack2<WD>(p0, p1);
+          }
+          tm_st16(t_s + 16 * c, pk);
+        }
+        sum += (acc[0] + acc[1]) + (acc[2] + acc[3]);
+        tm_wait_st();
+      }
+      tm_fence_before();
+      __syncwarp();
+      if (lane_id == 0) mb_arrive(b_p + 8 * l);
+      if (!W.last) continue;
+      // the piece is done: its output and lse go to the workspace
+      if (!wait(b_o + 8 * l, n & 1)) { ok = false; break; }
+      tm_fence_after();
+      long long slot;
+      float *po, *pl;
+      if (W.kind == AT_OWN) {
+        slot = (W.unit + worker) * ((long long)T.ts * A.group) + row;
+        po = T.own_o; pl = T.own_lse;
+        if (row == 0 && W.unit_first) T.own_first[W.unit] = worker;
+        if (row == 0 && W.unit_last) T.own_last[W.unit] = worker;
+      } else {
+        const int wk = W.kind == AT_PAIR ? blockIdx.x : worker;
+        slot = W.kind == AT_PAIR ? ((W.unit + wk) * 2 + l) * 128 + row : (W.unit + wk) * 128 + row;
+        po = T.pre_o; pl = T.pre_lse;
+        const bool mark = row == 0 && (l == 0 || W.kind == AT_SINGLE);
+        if (mark && W.unit_first) T.pre_first[W.unit] = wk;
+        if (mark && W.unit_last) T.pre_last[W.unit] = wk;
+      }
+      if (warp_live) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        if (live) pl[slot] = sum == 0.f ? -INFINITY : fmaf(m, A.scale_log2, log2f(sum));
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          tm_ld32(t_o + 32 * c, o);
+          tm_wait_ld();
+          tm_pin32(o);
+          if (live) {
+            float4* dst = reinterpret_cast<float4*>(po + slot * D + 32 * c);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              dst[j] = make_float4(__uint_as_float(o[4 * j]) * inv, __uint_as_float(o[4 * j + 1]) * inv, __uint_as_float(o[4 * j + 2]) * inv,
+                                   __uint_as_float(o[4 * j + 3]) * inv);
+          }
+        }
+      }
+    }
+  }
+  if (blockIdx.x == 0 && tid == 0) *T.plan = S.pre_tiles;
+  __syncthreads();
+  if (s_dead) {  // copies and products that are still in flight get time to land before the CTA's memory goes
+    const long long t0 = clock64();
+    while (clock64() - t0 < AT_SPIN_CLOCKS / 1000) {}
+    __syncthreads();
+  }
+  tm_fence_after();
+  if (warp == 9) tm_free(tmem, 512);
+}
+
+// ---- joins the pieces of every row in their order: one warp per row ---------------------------------------------------------
+template <int WD, int D>
+__global__ void __launch_bounds__(256) ls_attend_tile_join_kernel(const TileArgs T) {
+  const AttendArgs& A = T.a;
+  const long long rows = (long long)A.n_seqs * A.q_len * A.heads;
+  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (row >= rows) return;
+  const int t = (int)(row / A.heads), hd = (int)(row - (long long)t * A.heads), h = hd / A.group, g = hd - h * A.group;
+  const int b = t / A.q_len, i = t - b * A.q_len;
+  const bool own = own_keys(T, attend_len(A, b, false)).tiles > 0;
+  long long pre_unit, pre_row, pre_step;
+  if (T.pairs) {
+    const int tile = t / T.tq;
+    pre_unit = (long long)h * T.pairs + tile / 2;
+    pre_row = (tile & 1) * 128 + (t - tile * T.tq) * A.group + g;
+    pre_step = 256;
+  } else {
+    pre_unit = h;
+    pre_row = t * A.group + g;
+    pre_step = 128;
+  }
+  const int rt = i / T.ts;
+  const long long own_unit = ((long long)b * A.kv_heads + h) * T.rt + rt, own_step = (long long)T.ts * A.group;
+  const long long own_row = (i - rt * T.ts) * A.group + g;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  int n_pre = 0, n_own = 0;
+  long long pre_at = 0, own_at = 0;
+  if (*T.plan > 0) {
+    const int first = T.pre_first[pre_unit];
+    n_pre = T.pre_last[pre_unit] - first + 1;
+    pre_at = (pre_unit + first) * pre_step + pre_row;
+  }
+  if (own) {
+    const int first = T.own_first[own_unit];
+    n_own = T.own_last[own_unit] - first + 1;
+    own_at = (own_unit + first) * own_step + own_row;
+  }
+  const int n = n_pre + n_own;
+  auto lse_of = [&](int p) { return p < n_pre ? T.pre_lse[pre_at + p * pre_step] : T.own_lse[own_at + (p - n_pre) * own_step]; };
+  float top = -INFINITY;
+  for (int p = lane; p < n; p += 32) top = fmaxf(top, lse_of(p));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  constexpr int E = D / 32;
+  float acc[E] = {}, tot = 0.f;
+  for (int p0 = 0; p0 < n; p0 += 32) {
+    const float e = p0 + lane < n ? lse_of(p0 + lane) : -INFINITY;
+    const float wl = e == -INFINITY ? 0.f : ex2(e - top);
+    tot += warp_sum(wl);
+    for (int j = 0; j < min(32, n - p0); ++j) {
+      const float w = __shfl_sync(0xffffffffu, wl, j);
+      if (w == 0.f) continue;
+      const int p = p0 + j;
+      const float* src = (p < n_pre ? T.pre_o + (pre_at + p * pre_step) * D : T.own_o + (own_at + (p - n_pre) * own_step) * D) + lane * E;
+      float o[E];
+      if (E == 4) *reinterpret_cast<float4*>(o) = *reinterpret_cast<const float4*>(src);
+      else *reinterpret_cast<float2*>(o) = *reinterpret_cast<const float2*>(src);
+#pragma unroll
+      for (int c = 0; c < E; ++c) acc[c] = fmaf(w, o[c], acc[c]);
+    }
+  }
+  const float inv = tot == 0.f ? 0.f : 1.f / tot;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(A.out) + t * A.out_stride + (long long)hd * D + lane * E);
+#pragma unroll
+  for (int c = 0; c < E; c += 2) {
+    const uint32_t v = pack2<WD>(acc[c] * inv, acc[c + 1] * inv);
+    if ((A.out_stride & 1) == 0 && (reinterpret_cast<uintptr_t>(A.out) & 3) == 0) dst[c / 2] = v;
+    else { reinterpret_cast<uint16_t*>(dst)[c] = (uint16_t)v; reinterpret_cast<uint16_t*>(dst)[c + 1] = (uint16_t)(v >> 16); }
+  }
+  if (lane == 0 && A.lse) A.lse[row] = tot == 0.f ? -INFINITY : (top + log2f(tot)) * LN2;
+}
+
+}  // namespace ls
