@@ -13,17 +13,19 @@
 // and works on both in turn: while the tensor cores multiply for one lane, the four warps of the other do its softmax.  In a
 // pair the lanes share every key and value tile; elsewhere each lane has its own line of (unit, key tile).
 //   warp 8  copies keys, values and queries to shared memory (tensor maps, a box per page, ring of tiles);
-//   warp 9  issues S = Q K^T and O += P V (P is read from tensor memory, where it overwrites S);
+//   warps 9, 10  issue S = Q K^T and O += P V of lanes 0 and 1 (P is read from tensor memory, where it overwrites S);
 //   warps 0-3, 4-7  softmax of lanes 0 and 1, one thread per row.
 // A row's reference maximum follows its true maximum only when that has risen by more than 2^8: weights stay below 2^8, the
 // final division makes the reference irrelevant, and the accumulator in tensor memory is almost never rescaled.
 #pragma once
+#include <type_traits>
+
 #include "ls_attend.cuh"
 #include "ls_tmem.cuh"
 
 namespace ls {
 
-constexpr int AT_THREADS = 320;
+constexpr int AT_THREADS = 352;
 constexpr int AT_KEYS = 128;
 constexpr long long AT_SPIN_CLOCKS = 4000LL * 1000 * 1000;  // about two seconds
 constexpr int AT_COST_PAIR = 2, AT_COST_LANE = 1;           // of one key tile, in units of half a CTA
@@ -69,6 +71,8 @@ struct Share {
 };
 
 // Walks one lane's (unit, tile) line; all roles of a CTA walk the same line.
+using Lane0 = std::integral_constant<int, 0>;
+using Lane1 = std::integral_constant<int, 1>;
 enum { AT_PAIR = 0, AT_SINGLE = 1, AT_OWN = 2 };
 struct Walk {
   long long w, end;       // position in the current part of the line
@@ -234,20 +238,21 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
   extern __shared__ unsigned char dyn[];
   __shared__ Share S;
   __shared__ long long s_scan[2 * AT_THREADS / 32];
-  __shared__ alignas(8) unsigned long long bars[2 * NST + 10];
+  __shared__ alignas(8) unsigned long long bars[2 * NST + 22];
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_dead;
   const AttendArgs& A = T.a;
-  const int tid = threadIdx.x, lane_id = tid & 31, warp = tid >> 5;
+  const int tid = threadIdx.x, lane_id = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const uint32_t q_base = (saddr(dyn) + 1023) & ~1023u, ring = q_base + 2 * TS::TILE;
   const uint32_t bar0 = saddr(bars);
-  const uint32_t b_full = bar0, b_empty = bar0 + 8 * NST, b_qfull = b_empty + 8 * NST, b_qempty = b_qfull + 16, b_s = b_qempty + 16,
+  const uint32_t b_full = bar0, b_empty = bar0 + 8 * NST, b_qfull = b_empty + 8 * NST, b_qempty = b_qfull + 64, b_s = b_qempty + 64,
                  b_p = b_s + 16, b_o = b_p + 16;
 
   if (tid == 0) {
-    for (int i = 0; i < NST; ++i) { mb_init(b_full + 8 * i, 1); mb_init(b_empty + 8 * i, 1); }
+    for (int i = 0; i < NST; ++i) { mb_init(b_full + 8 * i, 1); mb_init(b_empty + 8 * i, 2); }
     for (int l = 0; l < 2; ++l) {
-      mb_init(b_qfull + 8 * l, 1); mb_init(b_qempty + 8 * l, 1); mb_init(b_s + 8 * l, 1); mb_init(b_p + 8 * l, 4); mb_init(b_o + 8 * l, 1);
+      for (int i = 0; i < 4; ++i) { mb_init(b_qfull + 32 * l + 8 * i, 1); mb_init(b_qempty + 32 * l + 8 * i, 1); }
+      mb_init(b_s + 8 * l, 1); mb_init(b_p + 8 * l, 4); mb_init(b_o + 8 * l, 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_shared();
@@ -280,132 +285,153 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
   const long long rounds = max(cnt0, cnt1);
 
   bool ok = true;
+  // Query tiles: a pair or a batch's rows take a lane's whole buffer; a sequence's rows take a slot of it, so that the copies
+  // run ahead by several pieces where these rows are few.  (A slot's product still reads 128 rows: what lies behind is ignored.)
+  const int q_rows = T.ts * A.group, q_slots = q_rows <= 32 ? 4 : q_rows <= 64 ? 2 : 1, q_step = 128 / q_slots * 128;
   if (warp == 8) {
     // ---- copies.  Order of the ring: for every round r and lane: values of round r - 1, keys of round r; a pair's once.
+    // The walk is one tile ahead of the copies, so that the page numbers are there when they are needed.
     Walk W[2];
-    int vk0[2], vlo[2], vhi[2], vh[2], vpage[2];  // of the tile whose values are still to be fetched
-    uint32_t st = 0, st_par = 1, q_par[2] = {1, 1};
-    walk_start(S, W[0]);
-    walk_start(S, W[1]);
+    int vk0[2], vlo[2], vhi[2], vh[2], vpage[2], page[2];  // v*: of the tile whose values are still to be fetched
+    uint32_t st = 0, st_par = 1, q_par[2] = {0xffffffffu, 0xffffffffu}, q_next[2] = {0, 0};
     const int nbox = AT_KEYS / T.box;
     const int my_box = lane_id & (nbox - 1), my_half = lane_id / nbox;
-    auto load_tile = [&](const CUtensorMap* map, int k0, int lo, int hi, int h, int page) -> bool {
+    auto load_tile = [&](const CUtensorMap* map, int k0, int lo, int hi, int h, int pg) {
       const int key = k0 + my_box * T.box;
       const bool on = my_half < D / 64 && key < hi && key + T.box > lo;
       const int count = __popc(__ballot_sync(0xffffffffu, on));
-      if (!wait(b_empty + 8 * st, st_par)) return false;
+      if (on && (uint32_t)pg >= (uint32_t)A.n_pages) { set_status(A.status, ST_BAD_INDEX); pg = A.n_pages; }  // (reads as zeros)
+      ok = wait(b_empty + 8 * st, st_par);
+      if (!ok) return;
       if (lane_id == 0) mb_expect(b_full + 8 * st, count * T.box * 128);
       __syncwarp();
       if (on)
-        tma_load4(ring + st * TS::TILE + my_half * TS::HALF + my_box * T.box * 128, map, my_half * 64, key % A.page, h, page, b_full + 8 * st);
+        tma_load4(ring + st * TS::TILE + my_half * TS::HALF + my_box * T.box * 128, map, my_half * 64, key % A.page, h, pg, b_full + 8 * st);
       if (++st == NST) { st = 0; st_par ^= 1; }
-      return true;
     };
-    auto page_of = [&](const Walk& w) {  // this lane's page of the tile just taken; one outside the pool reads as zeros
+    auto advance = [&](auto lc) {  // to the next tile, and this lane's page of it
+      constexpr int l = decltype(lc)::value;
+      Walk& w = W[l];
+      if (!walk_next(T, S, l, w)) return;
       const int key = w.k0 + my_box * T.box;
-      if (key >= w.hi || key + T.box <= w.lo) return -1;
+      if (key >= w.hi || key + T.box <= w.lo) return;
       const int32_t* tab = w.kind == AT_OWN ? A.table + (long long)(w.tok / A.q_len) * A.table_stride : A.prefix_pages;
-      const int id = tab[key / A.page];
-      if (id >= 0 && id < A.n_pages) return id;
-      set_status(A.status, ST_BAD_INDEX);
-      return A.n_pages;
+      page[l] = tab[key / A.page];
     };
-    for (long long r = 0; ok && r <= rounds; ++r) {
+    auto step = [&](auto lc, long long r, long long cnt) {
+      constexpr int l = decltype(lc)::value;
+      if (r > 0 && r <= cnt && !(r <= n_pair && l == 1)) load_tile(&map_v, vk0[l], vlo[l], vhi[l], vh[l], vpage[l]);
+      if (!ok || r >= cnt) return;
+      Walk& w = W[l];
+      if (w.fresh) {
+        const bool own = w.kind == AT_OWN;
+        const uint32_t slot = own ? q_next[l] : 0;
+        if (own && ++q_next[l] == q_slots) q_next[l] = 0;
+        ok = wait(b_qempty + 32 * l + 8 * slot, (q_par[l] >> slot) & 1);
+        if (!ok) return;
+        q_par[l] ^= 1u << slot;
+        if (lane_id == 0) {
+          const uint32_t full = b_qfull + 32 * l + 8 * slot;
+          mb_expect(full, (own ? T.ts : T.tq) * A.group * D * 2);
 #pragma unroll
-      for (int l = 0; l < 2; ++l) {
-        const long long cnt = l ? cnt1 : cnt0;
-        if (ok && r > 0 && r <= cnt && !(r <= n_pair && l == 1)) ok = load_tile(&map_v, vk0[l], vlo[l], vhi[l], vh[l], vpage[l]);
-        if (!ok || r >= cnt) continue;
-        Walk& w = W[l];
-        walk_next(T, S, l, w);
-        if (w.fresh) {
-          ok = wait(b_qempty + 8 * l, q_par[l]);
-          if (!ok) continue;
-          q_par[l] ^= 1;
-          if (lane_id == 0) {
-            const bool own = w.kind == AT_OWN;
-            mb_expect(b_qfull + 8 * l, (own ? T.ts : T.tq) * A.group * D * 2);
-#pragma unroll
-            for (int f = 0; f < D / 64; ++f)
-              tma_load3(q_base + l * TS::TILE + f * TS::HALF, own ? &map_q_own : &map_q_all, f * 64, w.h * A.group, w.tok, b_qfull + 8 * l);
-          }
-          __syncwarp();
-        }
-        if (w.kind == AT_PAIR && l == 1) continue;
-        vk0[l] = w.k0; vlo[l] = w.lo; vhi[l] = w.hi; vh[l] = w.h; vpage[l] = page_of(w);
-        ok = load_tile(&map_k, w.k0, w.lo, w.hi, w.h, vpage[l]);
-      }
-    }
-  } else if (warp == 9) {
-    // ---- products, in the order of the ring: per round and lane O += P V of round r - 1, then S = Q K^T of round r (which
-    // overwrites P).  One thread issues; the warp clears value rows that are nobody's (whatever the page holds there, its
-    // weight of zero must not meet an infinity).
-    constexpr uint32_t ID_S = mma_idesc(WD == WD_BF16, 128, AT_KEYS, false), ID_O = mma_idesc(WD == WD_BF16, 128, D, true);
-    Walk W[2];
-    int vk0[2], vlo[2], vhi[2];
-    bool vfresh[2];
-    uint32_t st = 0, st_par = 0, q_par[2] = {0, 0}, p_par[2] = {0, 0}, kst = 0, vst = 0;
-    walk_start(S, W[0]);
-    walk_start(S, W[1]);
-    auto take = [&](uint32_t& slot) -> bool {
-      slot = st;
-      const bool got = wait(b_full + 8 * st, st_par);
-      if (++st == NST) { st = 0; st_par ^= 1; }
-      return got;
-    };
-    for (long long r = 0; ok && r <= rounds; ++r) {
-#pragma unroll
-      for (int l = 0; l < 2; ++l) {
-        const long long cnt = l ? cnt1 : cnt0;
-        if (ok && r > 0 && r <= cnt) {
-          const bool pair = r <= n_pair;
-          if (!(pair && l == 1)) {
-            ok = take(vst);
-            if (ok && (vk0[l] < vlo[l] || vk0[l] + AT_KEYS > vhi[l])) {
-              for (int c = lane_id; c < AT_KEYS; c += 32) {
-                if (vk0[l] + c >= vlo[l] && vk0[l] + c < vhi[l]) continue;
-                for (int f = 0; f < D / 64; ++f)
-                  for (int j = 0; j < 8; ++j)
-                    asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ring + vst * TS::TILE + f * TS::HALF + c * 128 + j * 16), "r"(0) : "memory");
-              }
-              fence_async_shared();
-              __syncwarp();
-            }
-          }
-          if (ok) ok = wait(b_p + 8 * l, p_par[l]);
-          p_par[l] ^= 1;
-          if (ok && lane_id == 0) {
-            tm_fence_after();
-            const uint32_t v = ring + vst * TS::TILE;
-#pragma unroll
-            for (int k = 0; k < AT_KEYS / 16; ++k)
-              tm_mma_ts(tmem + 256 + l * D, tmem + l * AT_KEYS + k * 8, smem_desc(v + k * 2048, TS::HALF), ID_O, !(vfresh[l] && k == 0));
-            tm_commit(b_o + 8 * l);
-            if (!(pair && l == 0)) tm_commit(b_empty + 8 * vst);
-          }
-          __syncwarp();
-        }
-        if (!ok || r >= cnt) continue;
-        Walk& w = W[l];
-        walk_next(T, S, l, w);
-        const bool pair = w.kind == AT_PAIR;
-        vk0[l] = w.k0; vlo[l] = w.lo; vhi[l] = w.hi; vfresh[l] = w.fresh;
-        if (!(pair && l == 1)) ok = take(kst);
-        if (ok && w.fresh) { ok = wait(b_qfull + 8 * l, q_par[l]); q_par[l] ^= 1; }
-        if (ok && lane_id == 0) {
-          tm_fence_after();
-          const uint32_t q = q_base + l * TS::TILE, k = ring + kst * TS::TILE;
-#pragma unroll
-          for (int c = 0; c < D / 16; ++c) {
-            const uint32_t off = (c / 4) * TS::HALF + (c % 4) * 32;
-            tm_mma_ss(tmem + l * AT_KEYS, smem_desc(q + off, 16), smem_desc(k + off, 16), ID_S, c > 0);
-          }
-          tm_commit(b_s + 8 * l);
-          if (!(pair && l == 0)) tm_commit(b_empty + 8 * kst);
-          if (w.last) tm_commit(b_qempty + 8 * l);
+          for (int f = 0; f < D / 64; ++f)
+            tma_load3(q_base + l * TS::TILE + f * TS::HALF + slot * q_step, own ? &map_q_own : &map_q_all, f * 64, w.h * A.group, w.tok, full);
         }
         __syncwarp();
       }
+      if (!(w.kind == AT_PAIR && l == 1)) {
+        vk0[l] = w.k0; vlo[l] = w.lo; vhi[l] = w.hi; vh[l] = w.h; vpage[l] = page[l];
+        load_tile(&map_k, w.k0, w.lo, w.hi, w.h, page[l]);
+      }
+      if (ok) advance(lc);
+    };
+    walk_start(S, W[0]);
+    walk_start(S, W[1]);
+    page[0] = page[1] = 0;
+    advance(Lane0{});
+    advance(Lane1{});
+    for (long long r = 0; ok && r <= rounds; ++r) {
+      step(Lane0{}, r, cnt0);
+      if (ok) step(Lane1{}, r, cnt1);
+    }
+  } else if (warp >= 9) {
+    // ---- products of one lane: O += P V of round r - 1, then S = Q K^T of round r (which overwrites P).  One thread issues; the
+    // warp clears value rows that are nobody's (whatever the page holds there, its weight of zero must not meet an infinity;
+    // in a pair both lanes clear, the same).  A tile's two arrivals on `empty` come from the pair's two lanes, or twice from one.
+    constexpr uint32_t ID_S = mma_idesc(WD == WD_BF16, 128, AT_KEYS, false), ID_O = mma_idesc(WD == WD_BF16, 128, D, true);
+    const int l = warp - 9;
+    const long long cnt = l ? cnt1 : cnt0;
+    const uint32_t t_s = __shfl_sync(0xffffffffu, tmem + l * AT_KEYS, 0), t_o = __shfl_sync(0xffffffffu, tmem + 256 + l * D, 0);
+    const bool leader = elect_one();
+    Walk W;
+    walk_start(S, W);
+    bool more = walk_next(T, S, l, W);
+    int vk0 = 0, vlo = 0, vhi = AT_KEYS;
+    bool vfresh = true;
+    uint32_t st = 0, st_par = 0, q_par = 0, q_next = 0, q_slot = 0;
+    for (long long r = 0; r <= cnt; ++r) {
+      // places in the ring: values and keys of lane 0, then of lane 1 where they are not a pair's
+      const bool vpair = r <= n_pair, kpair = r < n_pair;
+      const uint32_t v0 = r > 0 && r <= cnt0, k0 = r < cnt0, v1 = r > 0 && r <= cnt1 && !vpair, k1 = r < cnt1 && !kpair;
+      auto place = [&](uint32_t ahead, uint32_t& slot, uint32_t& par) {
+        slot = st + ahead;
+        par = st_par;
+        if (slot >= NST) { slot -= NST; par ^= 1; }
+      };
+      uint32_t slot, par;
+      if (r > 0) {
+        place(l == 0 || vpair ? 0 : v0 + k0, slot, par);
+        if (!wait(b_full + 8 * slot, par)) break;
+        if (vk0 < vlo || vk0 + AT_KEYS > vhi) {
+          for (int c = lane_id; c < AT_KEYS; c += 32) {
+            if (vk0 + c >= vlo && vk0 + c < vhi) continue;
+            for (int f = 0; f < D / 64; ++f)
+              for (int j = 0; j < 8; ++j)
+                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ring + slot * TS::TILE + f * TS::HALF + c * 128 + j * 16), "r"(0) : "memory");
+          }
+          fence_async_shared();
+          __syncwarp();
+        }
+        if (!wait(b_p + 8 * l, (r - 1) & 1)) break;
+        tm_fence_after();
+        const uint64_t v = uniform64(smem_desc(ring + slot * TS::TILE, TS::HALF));
+        const uint32_t empty = b_empty + 8 * slot;
+        if (leader) {
+#pragma unroll
+          for (int k = 0; k < AT_KEYS / 16; ++k) tm_mma_ts(t_o, t_s + k * 8, v + k * (2048 >> 4), ID_O, !(vfresh && k == 0));
+          tm_commit(b_o + 8 * l);
+          tm_commit(empty);
+          if (!vpair) tm_commit(empty);
+        }
+        __syncwarp();
+      }
+      if (!more) break;
+      place(kpair ? v0 : l == 0 ? v0 : v0 + k0 + v1, slot, par);
+      if (!wait(b_full + 8 * slot, par)) break;
+      if (W.fresh) {
+        q_slot = W.kind == AT_OWN ? q_next : 0;
+        if (W.kind == AT_OWN && ++q_next == q_slots) q_next = 0;
+        if (!wait(b_qfull + 32 * l + 8 * q_slot, (q_par >> q_slot) & 1)) break;
+        q_par ^= 1u << q_slot;
+      }
+      tm_fence_after();
+      const uint64_t q = uniform64(smem_desc(q_base + l * TS::TILE + q_slot * q_step, 16)), k = uniform64(smem_desc(ring + slot * TS::TILE, 16));
+      if (leader) {
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+          const uint32_t off = ((c / 4) * TS::HALF + (c % 4) * 32) >> 4;
+          tm_mma_ss(t_s, q + off, k + off, ID_S, c > 0);
+        }
+        tm_commit(b_s + 8 * l);
+        tm_commit(b_empty + 8 * slot);
+        if (!kpair) tm_commit(b_empty + 8 * slot);
+        if (W.last) tm_commit(b_qempty + 32 * l + 8 * q_slot);
+      }
+      __syncwarp();
+      vk0 = W.k0; vlo = W.lo; vhi = W.hi; vfresh = W.fresh;
+      more = walk_next(T, S, l, W);
+      st += v0 + k0 + v1 + k1;
+      if (st >= NST) { st -= NST; st_par ^= 1; }
     }
   } else {
     // ---- softmax: one thread per row
@@ -425,7 +451,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         sum = 0.f;
         if (live) {
           const int t = W.tok + tr, b = t / A.q_len;
-          hi = max(attend_len(A, b, false) - A.q_len + (t - b * A.q_len) + 1, 0);
+          // (an own unit's last key is its sequence's last)
+          hi = max((W.kind == AT_OWN ? W.hi : attend_len(A, b, false)) - A.q_len + (t - b * A.q_len) + 1, 0);
           lo = A.window > 0 ? max(hi - A.window, 0) : 0;
           if (W.kind == AT_OWN) lo = max(lo, A.prefix);
           else hi = min(hi, A.prefix);
@@ -434,22 +461,26 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       if (!wait(b_s + 8 * l, n & 1)) { ok = false; break; }
       tm_fence_after();
       if (warp_live) {
-        uint32_t s[AT_KEYS];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tm_ld32(t_s + 32 * c, s + 32 * c);
-        tm_wait_ld();
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tm_pin32(s + 32 * c);
-        if (!__all_sync(0xffffffffu, !live || (lo <= W.k0 && hi >= W.k0 + AT_KEYS))) {
-#pragma unroll
-          for (int c = 0; c < AT_KEYS; ++c) {
-            const int key = W.k0 + c;
-            if (key < lo || key >= hi) s[c] = 0xff800000u;
-          }
-        }
+        // two passes over the scores in tensor memory (64 at a time in registers): the maximum, then the weights
+        const bool masked = !__all_sync(0xffffffffu, !live || (lo <= W.k0 && hi >= W.k0 + AT_KEYS));
+        const int mlo = live ? lo - W.k0 : 0, mhi = live ? hi - W.k0 : AT_KEYS;
         float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int c = 0; c < AT_KEYS; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(s[c]));
+        for (int c0 = 0; c0 < AT_KEYS; c0 += 64) {
+          uint32_t s[64];
+          tm_ld32(t_s + c0, s);
+          tm_ld32(t_s + c0 + 32, s + 32);
+          tm_wait_ld();
+          tm_pin32(s);
+          tm_pin32(s + 32);
+          if (masked) {
+#pragma unroll
+            for (int c = 0; c < 64; ++c)
+              if (c0 + c < mlo || c0 + c >= mhi) s[c] = 0xff800000u;
+          }
+#pragma unroll
+          for (int c = 0; c < 64; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(s[c]));
+        }
         const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
         const bool rise = live && top > m && (m == -INFINITY || (top - m) * A.scale_log2 > 8.f);
         if (__any_sync(0xffffffffu, rise)) {
@@ -473,17 +504,31 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         const float off = m == -INFINITY ? 0.f : -m * A.scale_log2;
         float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t pk[16];
+        for (int c0 = 0; c0 < AT_KEYS; c0 += 64) {
+          uint32_t s[64];
+          tm_ld32(t_s + c0, s);
+          tm_ld32(t_s + c0 + 32, s + 32);
+          tm_wait_ld();
+          tm_pin32(s);
+          tm_pin32(s + 32);
+          if (masked) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
-            const float p0 = ex2(fmaf(__uint_as_float(s[32 * c + 2 * j]), A.scale_log2, off));
-            const float p1 = ex2(fmaf(__uint_as_float(s[32 * c + 2 * j + 1]), A.scale_log2, off));
-            acc[j & 1] += p0;
-            acc[2 + (j & 1)] += p1;
-            pk[j] = pack2<WD>(p0, p1);
+            for (int c = 0; c < 64; ++c)
+              if (c0 + c < mlo || c0 + c >= mhi) s[c] = 0xff800000u;
           }
-          tm_st16(t_s + 16 * c, pk);
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+              const float p0 = ex2(fmaf(__uint_as_float(s[32 * c + 2 * j]), A.scale_log2, off));
+              const float p1 = ex2(fmaf(__uint_as_float(s[32 * c + 2 * j + 1]), A.scale_log2, off));
+              acc[j & 1] += p0;
+              acc[2 + (j & 1)] += p1;
+              pk[j] = pack2<WD>(p0, p1);
+            }
+            tm_st16(t_s + c0 / 2 + 16 * c, pk);  // (over scores that have been read)
+          }
         }
         sum += (acc[0] + acc[1]) + (acc[2] + acc[3]);
         tm_wait_st();

@@ -35,6 +35,17 @@ __device__ __forceinline__ void tma_load3(uint32_t dst, const CUtensorMap* map, 
 __device__ __forceinline__ void tma_prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+// One lane of a converged warp (always the same one).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+  return p != 0;
+}
+// The same value, known to be the same in the whole warp.
+__device__ __forceinline__ uint64_t uniform64(uint64_t x) {
+  return (uint64_t)__shfl_sync(0xffffffffu, (uint32_t)(x >> 32), 0) << 32 | __shfl_sync(0xffffffffu, (uint32_t)x, 0);
+}
+
 // ---- tensor memory ----------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void tm_alloc(uint32_t dst, uint32_t cols) {
   asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(cols) : "memory");
