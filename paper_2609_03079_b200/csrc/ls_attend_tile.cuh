@@ -57,81 +57,75 @@ __device__ __forceinline__ OwnKeys own_keys(const TileArgs& T, int len) {
   const int first = T.a.window > 0 ? max(len - T.a.q_len + 1 - T.a.window, 0) : 0;
   k.lo = max(first, T.a.prefix);
   k.hi = len;
-  k.origin = k.lo / T.box * T.box;
+  k.origin = k.lo & -T.box;
   k.tiles = k.hi > k.lo ? (k.hi - k.origin + AT_KEYS - 1) / AT_KEYS : 0;
   return k;
 }
 
-// What every CTA derives from the lengths: the line of work and its own share of it.
+// What every CTA derives from the lengths: its share of the line of work.  (The host has made sure that positions in the line
+// fit 31 bits.)
 struct Share {
   int pre_lo, pre_origin, pre_tiles;  // prefix keys that any token sees: [pre_lo, prefix)
-  long long pair0, pair1;             // this CTA's (pair unit, tile) range
-  long long lane0[2], lane1[2];       // its lanes' ranges in the line of single and own units
+  int pair0, pair1;                   // this CTA's (pair unit, tile) range
+  int lane0[2], lane1[2];             // its lanes' ranges in the line of single and own units
   int own_b[2], own_u[2], own_t[2];   // where a lane's range starts, if among the own units: sequence, unit within it, tile
+  int batch_pieces[2];                // pieces of each lane that are not of own units (they come first)
 };
 
-// Walks one lane's (unit, tile) line; all roles of a CTA walk the same line.
 using Lane0 = std::integral_constant<int, 0>;
 using Lane1 = std::integral_constant<int, 1>;
+
+// A piece: consecutive tiles of one unit on one lane.  The copying warp walks the line and leaves each piece here, with its
+// queries, for the warps that multiply and the ones that do the softmax.
 enum { AT_PAIR = 0, AT_SINGLE = 1, AT_OWN = 2 };
+struct Piece {
+  int kind, h, tok, ntok;    // key head, first token and number of tokens of the row tile
+  int k0, tiles, lo, hi;     // first key, number of tiles; keys outside [lo, hi) are nobody's
+  int unit, ends;            // number of the unit among its kind; bit 0: holds its first tile, bit 1: its last
+};
+
+// Walks one lane's line piece by piece.
 struct Walk {
-  long long w, end;       // position in the current part of the line
+  int w, end;             // position in the current part of the line
   bool pairs;             // still in the part of the pairs
   int b, u, tile, tiles;  // next own unit (b = -1: still among the single ones), its next tile, its tiles (-1: to be looked up)
-  int left;               // tiles of the current piece not yet taken
-  // the tile just taken
-  int kind;
-  bool fresh, last;       // first, last tile of its piece
-  bool unit_first, unit_last;  // its piece holds the unit's first, last tile
-  int h, tok, ntok;       // key head, first token and number of tokens of the row tile
-  int k0, lo, hi, origin; // its first key; keys outside [lo, hi) are nobody's; first key of the unit's first tile
-  long long unit;         // number of the unit among its kind
+  int lo, hi, origin;     // keys of the current sequence or of the prefix
 };
 
 __device__ __forceinline__ void walk_start(const Share& S, Walk& W) {
   W.pairs = true;
   W.w = S.pair0;
   W.end = S.pair1;
-  W.left = 0;
 }
 
-// Takes the next tile of lane `lane`'s line; false at its end.
-__device__ __forceinline__ bool walk_next(const TileArgs& T, const Share& S, int lane, Walk& W) {
+// Takes the next piece of lane `lane`'s line; false at its end.
+__device__ __forceinline__ bool walk_next(const TileArgs& T, const Share& S, int lane, Walk& W, Piece& P) {
   const AttendArgs& A = T.a;
-  if (W.left > 0) {
-    --W.left;
-    W.k0 += AT_KEYS;
-    W.fresh = false;
-    W.last = W.left == 0;
-    return true;
-  }
   if (W.pairs && W.w == W.end) {
     W.pairs = false;
     W.w = S.lane0[lane]; W.end = S.lane1[lane];
     W.b = S.own_b[lane]; W.u = S.own_u[lane]; W.tile = S.own_t[lane]; W.tiles = -1;
   }
   if (W.w >= W.end) return false;
-  int n, tile;
   if (W.pairs || W.b < 0) {
-    W.unit = W.w / S.pre_tiles;
-    tile = (int)(W.w - W.unit * S.pre_tiles);
-    n = (int)min((long long)(S.pre_tiles - tile), W.end - W.w);
+    P.unit = W.w / S.pre_tiles;
+    const int tile = W.w - P.unit * S.pre_tiles;
+    P.tiles = min(S.pre_tiles - tile, W.end - W.w);
+    P.ends = (tile == 0 ? 1 : 0) | (tile + P.tiles == S.pre_tiles ? 2 : 0);
+    P.k0 = S.pre_origin + tile * AT_KEYS;
+    P.lo = S.pre_lo; P.hi = A.prefix;
     if (W.pairs) {
-      W.kind = AT_PAIR;
-      W.h = (int)(W.unit / T.pairs);
-      W.tok = ((int)(W.unit - (long long)W.h * T.pairs) * 2 + lane) * T.tq;
+      P.kind = AT_PAIR;
+      P.h = P.unit / T.pairs;
+      P.tok = ((P.unit - P.h * T.pairs) * 2 + lane) * T.tq;
     } else {
-      W.kind = AT_SINGLE;
-      W.h = (int)W.unit;
-      W.tok = 0;
-      if (W.w + n == (long long)A.kv_heads * S.pre_tiles) { W.b = 0; W.u = 0; W.tile = 0; }
+      P.kind = AT_SINGLE;
+      P.h = P.unit;
+      P.tok = 0;
+      if ((P.ends & 2) && P.unit == A.kv_heads - 1) { W.b = 0; W.u = 0; W.tile = 0; }
     }
-    W.ntok = min(T.tq, A.n_seqs * A.q_len - W.tok);
-    W.lo = S.pre_lo; W.hi = A.prefix; W.origin = S.pre_origin;
-    W.unit_first = tile == 0;
-    W.unit_last = tile + n == S.pre_tiles;
+    P.ntok = min(T.tq, A.n_seqs * A.q_len - P.tok);
   } else {
-    const int per = A.kv_heads * T.rt;
     if (W.tiles < 0) {
       for (;; ++W.b) {  // (sequences without keys of their own have no units; the line ends before the sequences do)
         const OwnKeys k = own_keys(T, attend_len(A, W.b, false));
@@ -139,88 +133,88 @@ __device__ __forceinline__ bool walk_next(const TileArgs& T, const Share& S, int
         if (k.tiles > 0) break;
       }
     }
-    W.kind = AT_OWN;
-    tile = W.tile;
-    n = (int)min((long long)(W.tiles - tile), W.end - W.w);
-    W.unit = (long long)W.b * per + W.u;
-    W.h = W.u / T.rt;
-    const int rt = W.u - W.h * T.rt;
-    W.tok = W.b * A.q_len + rt * T.ts;
-    W.ntok = min(T.ts, A.q_len - rt * T.ts);
-    W.unit_first = tile == 0;
-    W.unit_last = tile + n == W.tiles;
+    const int per = A.kv_heads * T.rt;
+    P.kind = AT_OWN;
+    P.tiles = min(W.tiles - W.tile, W.end - W.w);
+    P.unit = W.b * per + W.u;
+    P.h = T.rt == 1 ? W.u : W.u / T.rt;
+    const int rt = W.u - P.h * T.rt;
+    P.tok = W.b * A.q_len + rt * T.ts;
+    P.ntok = min(T.ts, A.q_len - rt * T.ts);
+    P.ends = (W.tile == 0 ? 1 : 0) | (W.tile + P.tiles == W.tiles ? 2 : 0);
+    P.k0 = W.origin + W.tile * AT_KEYS;
+    P.lo = W.lo; P.hi = W.hi;
     W.tile = 0;
-    if (W.unit_last && ++W.u == per) { W.u = 0; ++W.b; W.tiles = -1; }
+    if ((P.ends & 2) && ++W.u == per) { W.u = 0; ++W.b; W.tiles = -1; }
   }
-  W.w += n;
-  W.left = n - 1;
-  W.k0 = W.origin + tile * AT_KEYS;
-  W.fresh = true;
-  W.last = W.left == 0;
+  W.w += P.tiles;
   return true;
 }
 
 // Every thread of the CTA: the share of CTA c of n.
-__device__ __forceinline__ void make_share(const TileArgs& T, Share& S, long long* s_scan, int c, int n) {
+__device__ __forceinline__ void make_share(const TileArgs& T, Share& S, int* s_scan, int c, int n) {
   const AttendArgs& A = T.a;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = AT_THREADS / 32;
   const int per = (A.n_seqs + AT_THREADS - 1) / AT_THREADS;
   const int b0 = min(tid * per, A.n_seqs), b1 = min(b0 + per, A.n_seqs);
-  long long sum = 0;
-  int lo = A.prefix;  // first prefix key that anybody sees
+  int sum = 0, lo = A.prefix;  // own tiles (of one head and row tile) of this thread's sequences; first prefix key that they see
+#pragma unroll 1
   for (int b = b0; b < b1; ++b) {
     const int len = attend_len(A, b, c == 0);
     sum += own_keys(T, len).tiles;
     if (len > 0) lo = min(lo, A.window > 0 ? max(len - A.q_len + 1 - A.window, 0) : 0);
   }
-  long long incl = sum;
+  int incl = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+    const int v = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += v;
   }
   lo = __reduce_min_sync(0xffffffffu, lo);
   if (lane == 31) { s_scan[warp] = incl; s_scan[nw + warp] = lo; }
   __syncthreads();
-  long long before = incl - sum, total = 0;
-  for (int w = 0; w < nw; ++w) {
-    if (w < warp) before += s_scan[w];
-    total += s_scan[w];
-    lo = min(lo, (int)s_scan[nw + w]);
-  }
-  const int origin = lo / T.box * T.box;
+  const int v = lane < nw ? s_scan[lane] : 0, vl = lane < nw ? s_scan[nw + lane] : A.prefix;
+  const int before = incl - sum + __reduce_add_sync(0xffffffffu, lane < warp ? v : 0), total = __reduce_add_sync(0xffffffffu, v);
+  lo = __reduce_min_sync(0xffffffffu, vl);
+  const int origin = lo & -T.box;
   const int pre_tiles = A.prefix > lo ? (A.prefix - origin + AT_KEYS - 1) / AT_KEYS : 0;
-  const long long n_pair = (long long)A.kv_heads * T.pairs * pre_tiles;
-  const long long n_single = T.pairs ? 0 : (long long)A.kv_heads * pre_tiles;
-  const long long mult = (long long)A.kv_heads * T.rt, n_lane = n_single + total * mult;
-  const long long cost = n_pair * AT_COST_PAIR + n_lane * AT_COST_LANE;
+  const int n_pair = A.kv_heads * T.pairs * pre_tiles, n_single = T.pairs ? 0 : A.kv_heads * pre_tiles;
+  const int mult = A.kv_heads * T.rt, n_lane = n_single + total * mult;
+  const int cost = n_pair * AT_COST_PAIR + n_lane * AT_COST_LANE;
   // Pieces of a unit have to be on consecutive workers: no worker between the first and the last may be empty, so that little
   // work goes to fewer CTAs, each with a tile for both lanes.
-  const long long used = max(1LL, min((long long)n, cost / max(AT_COST_PAIR, 2 * AT_COST_LANE)));
-  const long long x0 = cost * min((long long)c, used) / used, x1 = cost * min(c + 1LL, used) / used;
-  auto pair_at = [&](long long x) { return min(n_pair, (x + AT_COST_PAIR - 1) / AT_COST_PAIR); };
-  auto lane_at = [&](long long x) {
+  const int used = max(1, min(n, cost / max(AT_COST_PAIR, 2 * AT_COST_LANE)));
+  const int base = cost / used, rest = cost - base * used;  // CTA c takes the costs from c * base + c * rest / used on
+  auto start = [&](int i) { i = min(i, used); return i * base + (int)((unsigned)(i * rest) / (unsigned)used); };
+  const int x0 = start(c), x1 = start(c + 1);
+  auto pair_at = [&](int x) { return min(n_pair, (x + AT_COST_PAIR - 1) / AT_COST_PAIR); };
+  auto lane_at = [&](int x) {
     x -= n_pair * AT_COST_PAIR;
-    return x <= 0 ? 0LL : min(n_lane, (x + AT_COST_LANE - 1) / AT_COST_LANE);
+    return x <= 0 ? 0 : min(n_lane, (x + AT_COST_LANE - 1) / AT_COST_LANE);
   };
-  const long long g0 = lane_at(x0), g1 = lane_at(x1), mid = g0 + (g1 - g0) / 2;
+  const int g0 = lane_at(x0), g1 = lane_at(x1), mid = g0 + (g1 - g0) / 2;
   if (tid == 0) {
     S.pre_lo = lo; S.pre_origin = origin; S.pre_tiles = pre_tiles;
     S.pair0 = pair_at(x0); S.pair1 = pair_at(x1);
-    S.lane0[0] = g0; S.lane1[0] = mid; S.lane0[1] = mid; S.lane1[1] = g1;
-    for (int l = 0; l < 2; ++l)
-      if ((l ? mid : g0) < n_single) { S.own_b[l] = -1; S.own_u[l] = 0; S.own_t[l] = 0; }
+    const int pp = S.pair1 > S.pair0 ? (S.pair1 - 1) / pre_tiles - S.pair0 / pre_tiles + 1 : 0;
+    for (int l = 0; l < 2; ++l) {
+      const int from = l ? mid : g0, to = min(l ? g1 : mid, n_single);
+      S.lane0[l] = from; S.lane1[l] = l ? g1 : mid;
+      if (from < n_single) { S.own_b[l] = -1; S.own_u[l] = 0; S.own_t[l] = 0; }
+      S.batch_pieces[l] = pp + (to > from ? (to - 1) / pre_tiles - from / pre_tiles + 1 : 0);
+    }
   }
   for (int l = 0; l < 2; ++l) {  // the thread whose sequences hold the start of a lane's range finds it
-    const long long w = (l ? mid : g0) - n_single;
-    long long acc = before * mult;
+    const int w = (l ? mid : g0) - n_single;
+    int acc = before * mult;
     if (w < acc || w >= acc + sum * mult) continue;
+#pragma unroll 1
     for (int b = b0; b < b1; ++b) {
       const int t = own_keys(T, attend_len(A, b, false)).tiles;
       if (w < acc + t * mult) {
         S.own_b[l] = b;
-        S.own_u[l] = (int)((w - acc) / t);
-        S.own_t[l] = (int)((w - acc) - (long long)S.own_u[l] * t);
+        S.own_u[l] = (w - acc) / t;
+        S.own_t[l] = (w - acc) - S.own_u[l] * t;
         break;
       }
       acc += t * mult;
@@ -237,8 +231,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
   constexpr int NST = TS::STAGES;
   extern __shared__ unsigned char dyn[];
   __shared__ Share S;
-  __shared__ long long s_scan[2 * AT_THREADS / 32];
-  __shared__ alignas(8) unsigned long long bars[2 * NST + 22];
+  __shared__ int s_scan[2 * AT_THREADS / 32];
+  __shared__ Piece s_piece[2][4];
+  __shared__ alignas(8) unsigned long long bars[2 * NST + 24];
   __shared__ uint32_t s_tmem;
   __shared__ volatile int s_dead;
   const AttendArgs& A = T.a;
@@ -246,13 +241,13 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
   const uint32_t q_base = (saddr(dyn) + 1023) & ~1023u, ring = q_base + 2 * TS::TILE;
   const uint32_t bar0 = saddr(bars);
   const uint32_t b_full = bar0, b_empty = bar0 + 8 * NST, b_qfull = b_empty + 8 * NST, b_qempty = b_qfull + 64, b_s = b_qempty + 64,
-                 b_p = b_s + 16, b_o = b_p + 16;
+                 b_p = b_s + 16, b_o = b_p + 16, b_turn = b_o + 16;
 
   if (tid == 0) {
     for (int i = 0; i < NST; ++i) { mb_init(b_full + 8 * i, 1); mb_init(b_empty + 8 * i, 2); }
     for (int l = 0; l < 2; ++l) {
-      for (int i = 0; i < 4; ++i) { mb_init(b_qfull + 32 * l + 8 * i, 1); mb_init(b_qempty + 32 * l + 8 * i, 1); }
-      mb_init(b_s + 8 * l, 1); mb_init(b_p + 8 * l, 4); mb_init(b_o + 8 * l, 1);
+      for (int i = 0; i < 4; ++i) { mb_init(b_qfull + 32 * l + 8 * i, 1); mb_init(b_qempty + 32 * l + 8 * i, 5); }
+      mb_init(b_s + 8 * l, 1); mb_init(b_p + 8 * l, 4); mb_init(b_o + 8 * l, 1); mb_init(b_turn + 8 * l, 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_shared();
@@ -280,20 +275,36 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     return __all_sync(0xffffffffu, got);
   };
 
-  const long long n_pair = S.pair1 - S.pair0;
-  const long long cnt0 = n_pair + S.lane1[0] - S.lane0[0], cnt1 = n_pair + S.lane1[1] - S.lane0[1];
-  const long long rounds = max(cnt0, cnt1);
-
-  bool ok = true;
-  // Query tiles: a pair or a batch's rows take a lane's whole buffer; a sequence's rows take a slot of it, so that the copies
-  // run ahead by several pieces where these rows are few.  (A slot's product still reads 128 rows: what lies behind is ignored.)
+  // Tiles of the lanes; the first n_pair of both are pairs.
+  const int n_pair = S.pair1 - S.pair0;
+  const int cnt0 = n_pair + S.lane1[0] - S.lane0[0], cnt1 = n_pair + S.lane1[1] - S.lane0[1];
+  // Query tiles: rows of the whole batch take a lane's whole buffer; a sequence's rows take a slot of it, so that the copies run
+  // ahead by several pieces where these rows are few.  (A slot's product still reads 128 rows: what lies behind is ignored.)
+  // Piece i of a lane is in slot 0 if it is one of the first batch_pieces, else in slot (i - batch_pieces) % q_slots; the slot's
+  // barriers count the copy, and its release by the last product and by the four softmax warps.
   const int q_rows = T.ts * A.group, q_slots = q_rows <= 32 ? 4 : q_rows <= 64 ? 2 : 1, q_step = 128 / q_slots * 128;
+  struct Slots {
+    int batch, n;
+    uint32_t slot, par;
+    __device__ __forceinline__ Slots(int batch_pieces, int slots, uint32_t parity) : batch(batch_pieces), n(slots), slot(0), par(parity) {}
+    __device__ __forceinline__ uint32_t parity() const { return (par >> slot) & 1; }
+    __device__ __forceinline__ void next() {
+      par ^= 1u << slot;
+      if (batch > 0) { --batch; return; }  // (the first own piece is in slot 0 too)
+      if (++slot == (uint32_t)n) slot = 0;
+    }
+  };
+  bool ok = true;
   if (warp == 8) {
     // ---- copies.  Order of the ring: for every round r and lane: values of round r - 1, keys of round r; a pair's once.
     // The walk is one tile ahead of the copies, so that the page numbers are there when they are needed.
     Walk W[2];
-    int vk0[2], vlo[2], vhi[2], vh[2], vpage[2], page[2];  // v*: of the tile whose values are still to be fetched
-    uint32_t st = 0, st_par = 1, q_par[2] = {0xffffffffu, 0xffffffffu}, q_next[2] = {0, 0};
+    Piece P[2];
+    int left[2] = {0, 0}, page[2] = {0, 0};
+    bool fresh[2] = {false, false};
+    int vk0[2] = {0, 0}, vlo[2] = {0, 0}, vhi[2] = {0, 0}, vh[2] = {0, 0}, vpage[2] = {0, 0};  // tile whose values are to come
+    uint32_t st = 0, st_par = 1;
+    Slots Q[2] = {Slots(S.batch_pieces[0], q_slots, 15), Slots(S.batch_pieces[1], q_slots, 15)};
     const int nbox = AT_KEYS / T.box;
     const int my_box = lane_id & (nbox - 1), my_half = lane_id / nbox;
     auto load_tile = [&](const CUtensorMap* map, int k0, int lo, int hi, int h, int pg) {
@@ -311,253 +322,273 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     };
     auto advance = [&](auto lc) {  // to the next tile, and this lane's page of it
       constexpr int l = decltype(lc)::value;
-      Walk& w = W[l];
-      if (!walk_next(T, S, l, w)) return;
-      const int key = w.k0 + my_box * T.box;
-      if (key >= w.hi || key + T.box <= w.lo) return;
-      const int32_t* tab = w.kind == AT_OWN ? A.table + (long long)(w.tok / A.q_len) * A.table_stride : A.prefix_pages;
+      fresh[l] = false;
+      if (left[l] > 0) { --left[l]; P[l].k0 += AT_KEYS; }
+      else {
+        if (!walk_next(T, S, l, W[l], P[l])) return;
+        fresh[l] = true;
+        left[l] = P[l].tiles - 1;
+      }
+      const int key = P[l].k0 + my_box * T.box;
+      if (key >= P[l].hi || key + T.box <= P[l].lo) return;
+      const int32_t* tab = P[l].kind == AT_OWN ? A.table + (long long)(P[l].tok / A.q_len) * A.table_stride : A.prefix_pages;
       page[l] = tab[key / A.page];
     };
-    auto step = [&](auto lc, long long r, long long cnt) {
+    auto step = [&](auto lc, int r, int cnt) {
       constexpr int l = decltype(lc)::value;
       if (r > 0 && r <= cnt && !(r <= n_pair && l == 1)) load_tile(&map_v, vk0[l], vlo[l], vhi[l], vh[l], vpage[l]);
       if (!ok || r >= cnt) return;
-      Walk& w = W[l];
-      if (w.fresh) {
-        const bool own = w.kind == AT_OWN;
-        const uint32_t slot = own ? q_next[l] : 0;
-        if (own && ++q_next[l] == q_slots) q_next[l] = 0;
-        ok = wait(b_qempty + 32 * l + 8 * slot, (q_par[l] >> slot) & 1);
+      const bool own = P[l].kind == AT_OWN;
+      if (fresh[l]) {
+        const uint32_t slot = Q[l].slot;
+        ok = wait(b_qempty + 32 * l + 8 * slot, Q[l].parity());
         if (!ok) return;
-        q_par[l] ^= 1u << slot;
+        Q[l].next();
         if (lane_id == 0) {
+          s_piece[l][slot] = P[l];
           const uint32_t full = b_qfull + 32 * l + 8 * slot;
           mb_expect(full, (own ? T.ts : T.tq) * A.group * D * 2);
 #pragma unroll
           for (int f = 0; f < D / 64; ++f)
-            tma_load3(q_base + l * TS::TILE + f * TS::HALF + slot * q_step, own ? &map_q_own : &map_q_all, f * 64, w.h * A.group, w.tok, full);
+            tma_load3(q_base + l * TS::TILE + f * TS::HALF + slot * q_step, own ? &map_q_own : &map_q_all, f * 64, P[l].h * A.group, P[l].tok, full);
         }
         __syncwarp();
       }
-      if (!(w.kind == AT_PAIR && l == 1)) {
-        vk0[l] = w.k0; vlo[l] = w.lo; vhi[l] = w.hi; vh[l] = w.h; vpage[l] = page[l];
-        load_tile(&map_k, w.k0, w.lo, w.hi, w.h, page[l]);
+      if (!(r < n_pair && l == 1)) {
+        vk0[l] = P[l].k0; vlo[l] = P[l].lo; vhi[l] = P[l].hi; vh[l] = P[l].h; vpage[l] = page[l];
+        load_tile(&map_k, P[l].k0, P[l].lo, P[l].hi, P[l].h, page[l]);
       }
       if (ok) advance(lc);
     };
     walk_start(S, W[0]);
     walk_start(S, W[1]);
-    page[0] = page[1] = 0;
     advance(Lane0{});
     advance(Lane1{});
-    for (long long r = 0; ok && r <= rounds; ++r) {
+    const int rounds = max(cnt0, cnt1);
+    for (int r = 0; ok && r <= rounds; ++r) {
       step(Lane0{}, r, cnt0);
       if (ok) step(Lane1{}, r, cnt1);
     }
   } else if (warp >= 9) {
-    // ---- products of one lane: O += P V of round r - 1, then S = Q K^T of round r (which overwrites P).  One thread issues; the
+    // ---- products of one lane: O += P V of round r - 1, then S = Q K^T of round r (which overwrites P).  One thread issues.
+    // The lanes take strict turns: a lane's products run together, so that the other lane's softmax overlaps them (products of
+    // both lanes mixed would end at the same time and the two softmaxes would then share the same cycles).  The
     // warp clears value rows that are nobody's (whatever the page holds there, its weight of zero must not meet an infinity;
     // in a pair both lanes clear, the same).  A tile's two arrivals on `empty` come from the pair's two lanes, or twice from one.
     constexpr uint32_t ID_S = mma_idesc(WD == WD_BF16, 128, AT_KEYS, false), ID_O = mma_idesc(WD == WD_BF16, 128, D, true);
     const int l = warp - 9;
-    const long long cnt = l ? cnt1 : cnt0;
+    const int cnt = l ? cnt1 : cnt0;
     const uint32_t t_s = __shfl_sync(0xffffffffu, tmem + l * AT_KEYS, 0), t_o = __shfl_sync(0xffffffffu, tmem + 256 + l * D, 0);
     const bool leader = elect_one();
-    Walk W;
-    walk_start(S, W);
-    bool more = walk_next(T, S, l, W);
-    int vk0 = 0, vlo = 0, vhi = AT_KEYS;
+    Slots Q(S.batch_pieces[l], q_slots, 0);
+    int left = 0, k0 = 0, lo = 0, hi = 0;   // of the current piece: tiles to come, first key of the next; keys of anybody
     bool vfresh = true;
-    uint32_t st = 0, st_par = 0, q_par = 0, q_next = 0, q_slot = 0;
-    for (long long r = 0; r <= cnt; ++r) {
+    uint32_t q_slot = 0, st = 0, st_par = 0;
+    for (int r = 0; r <= cnt; ++r) {
       // places in the ring: values and keys of lane 0, then of lane 1 where they are not a pair's
       const bool vpair = r <= n_pair, kpair = r < n_pair;
-      const uint32_t v0 = r > 0 && r <= cnt0, k0 = r < cnt0, v1 = r > 0 && r <= cnt1 && !vpair, k1 = r < cnt1 && !kpair;
+      const uint32_t v0 = r > 0 && r <= cnt0, f0 = r < cnt0, v1 = r > 0 && r <= cnt1 && !vpair, f1 = r < cnt1 && !kpair;
       auto place = [&](uint32_t ahead, uint32_t& slot, uint32_t& par) {
         slot = st + ahead;
         par = st_par;
         if (slot >= NST) { slot -= NST; par ^= 1; }
       };
-      uint32_t slot, par;
+      uint32_t vslot = 0, kslot, par;
       if (r > 0) {
-        place(l == 0 || vpair ? 0 : v0 + k0, slot, par);
-        if (!wait(b_full + 8 * slot, par)) break;
-        if (vk0 < vlo || vk0 + AT_KEYS > vhi) {
+        place(l == 0 || vpair ? 0 : v0 + f0, vslot, par);
+        if (!wait(b_full + 8 * vslot, par)) break;
+        const int vk0 = k0 - AT_KEYS;
+        if (vk0 < lo || k0 > hi) {
           for (int c = lane_id; c < AT_KEYS; c += 32) {
-            if (vk0 + c >= vlo && vk0 + c < vhi) continue;
+            if (vk0 + c >= lo && vk0 + c < hi) continue;
             for (int f = 0; f < D / 64; ++f)
               for (int j = 0; j < 8; ++j)
-                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ring + slot * TS::TILE + f * TS::HALF + c * 128 + j * 16), "r"(0) : "memory");
+                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ring + vslot * TS::TILE + f * TS::HALF + c * 128 + j * 16), "r"(0) : "memory");
           }
           fence_async_shared();
           __syncwarp();
         }
         if (!wait(b_p + 8 * l, (r - 1) & 1)) break;
+      }
+      if (l == 1 ? r <= cnt0 : r > 0 && r - 1 <= cnt1)
+        if (!wait(b_turn + 8 * l, (l ? r : r - 1) & 1)) break;
+      if (r > 0) {
         tm_fence_after();
-        const uint64_t v = uniform64(smem_desc(ring + slot * TS::TILE, TS::HALF));
-        const uint32_t empty = b_empty + 8 * slot;
+        const uint64_t v = uniform64(smem_desc(ring + vslot * TS::TILE, TS::HALF));
         if (leader) {
 #pragma unroll
           for (int k = 0; k < AT_KEYS / 16; ++k) tm_mma_ts(t_o, t_s + k * 8, v + k * (2048 >> 4), ID_O, !(vfresh && k == 0));
           tm_commit(b_o + 8 * l);
-          tm_commit(empty);
-          if (!vpair) tm_commit(empty);
+          tm_commit(b_empty + 8 * vslot);
+          if (!vpair) tm_commit(b_empty + 8 * vslot);
         }
         __syncwarp();
       }
-      if (!more) break;
-      place(kpair ? v0 : l == 0 ? v0 : v0 + k0 + v1, slot, par);
-      if (!wait(b_full + 8 * slot, par)) break;
-      if (W.fresh) {
-        q_slot = W.kind == AT_OWN ? q_next : 0;
-        if (W.kind == AT_OWN && ++q_next == q_slots) q_next = 0;
-        if (!wait(b_qfull + 32 * l + 8 * q_slot, (q_par >> q_slot) & 1)) break;
-        q_par ^= 1u << q_slot;
-      }
-      tm_fence_after();
-      const uint64_t q = uniform64(smem_desc(q_base + l * TS::TILE + q_slot * q_step, 16)), k = uniform64(smem_desc(ring + slot * TS::TILE, 16));
-      if (leader) {
-#pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
-          const uint32_t off = ((c / 4) * TS::HALF + (c % 4) * 32) >> 4;
-          tm_mma_ss(t_s, q + off, k + off, ID_S, c > 0);
+      if (r < cnt) {
+        place(kpair ? v0 : l == 0 ? v0 : v0 + f0 + v1, kslot, par);
+        vfresh = left == 0;
+        if (left == 0) {
+          q_slot = Q.slot;
+          if (!wait(b_qfull + 32 * l + 8 * q_slot, Q.parity())) break;
+          Q.next();
+          const Piece& P = s_piece[l][q_slot];
+          left = P.tiles; k0 = P.k0; lo = P.lo; hi = P.hi;
         }
-        tm_commit(b_s + 8 * l);
-        tm_commit(b_empty + 8 * slot);
-        if (!kpair) tm_commit(b_empty + 8 * slot);
-        if (W.last) tm_commit(b_qempty + 32 * l + 8 * q_slot);
+        if (!wait(b_full + 8 * kslot, par)) break;
+        --left;
+        k0 += AT_KEYS;
+        tm_fence_after();
+        const uint64_t q = uniform64(smem_desc(q_base + l * TS::TILE + q_slot * q_step, 16)), k = uniform64(smem_desc(ring + kslot * TS::TILE, 16));
+        if (leader) {
+#pragma unroll
+          for (int c = 0; c < D / 16; ++c) {
+            const uint32_t off = ((c / 4) * TS::HALF + (c % 4) * 32) >> 4;
+            tm_mma_ss(t_s, q + off, k + off, ID_S, c > 0);
+          }
+          tm_commit(b_s + 8 * l);
+          tm_commit(b_empty + 8 * kslot);
+          if (!kpair) tm_commit(b_empty + 8 * kslot);
+          if (left == 0) tm_commit(b_qempty + 32 * l + 8 * q_slot);
+        }
+        __syncwarp();
       }
-      __syncwarp();
-      vk0 = W.k0; vlo = W.lo; vhi = W.hi; vfresh = W.fresh;
-      more = walk_next(T, S, l, W);
-      st += v0 + k0 + v1 + k1;
+      if (leader) mb_arrive(b_turn + 8 * (1 - l));
+      st += v0 + f0 + v1 + f1;
       if (st >= NST) { st -= NST; st_par ^= 1; }
     }
   } else {
     // ---- softmax: one thread per row
     const int l = warp >> 2, row = (warp & 3) * 32 + lane_id;
+    const int cnt = l ? cnt1 : cnt0;
     const uint32_t t_s = tmem + ((warp & 3) << 21) + l * AT_KEYS, t_o = tmem + ((warp & 3) << 21) + 256 + l * D;
-    const int tr = row / A.group, worker = blockIdx.x * 2 + l;
-    Walk W;
-    walk_start(S, W);
-    int lo = 0, hi = 0;
-    bool live = false, warp_live = false;
-    float m = -INFINITY, sum = 0.f;
-    for (uint32_t n = 0; ok && walk_next(T, S, l, W); ++n) {
-      if (W.fresh) {
-        live = tr < W.ntok;
-        warp_live = __any_sync(0xffffffffu, live);
-        m = -INFINITY;
-        sum = 0.f;
-        if (live) {
-          const int t = W.tok + tr, b = t / A.q_len;
-          // (an own unit's last key is its sequence's last)
-          hi = max((W.kind == AT_OWN ? W.hi : attend_len(A, b, false)) - A.q_len + (t - b * A.q_len) + 1, 0);
-          lo = A.window > 0 ? max(hi - A.window, 0) : 0;
-          if (W.kind == AT_OWN) lo = max(lo, A.prefix);
-          else hi = min(hi, A.prefix);
-        }
-      }
-      if (!wait(b_s + 8 * l, n & 1)) { ok = false; break; }
-      tm_fence_after();
-      if (warp_live) {
-        // two passes over the scores in tensor memory (64 at a time in registers): the maximum, then the weights
-        const bool masked = !__all_sync(0xffffffffu, !live || (lo <= W.k0 && hi >= W.k0 + AT_KEYS));
-        const int mlo = live ? lo - W.k0 : 0, mhi = live ? hi - W.k0 : AT_KEYS;
-        float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int c0 = 0; c0 < AT_KEYS; c0 += 64) {
-          uint32_t s[64];
-          tm_ld32(t_s + c0, s);
-          tm_ld32(t_s + c0 + 32, s + 32);
-          tm_wait_ld();
-          tm_pin32(s);
-          tm_pin32(s + 32);
-          if (masked) {
-#pragma unroll
-            for (int c = 0; c < 64; ++c)
-              if (c0 + c < mlo || c0 + c >= mhi) s[c] = 0xff800000u;
-          }
-#pragma unroll
-          for (int c = 0; c < 64; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(s[c]));
-        }
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-        const bool rise = live && top > m && (m == -INFINITY || (top - m) * A.scale_log2 > 8.f);
-        if (__any_sync(0xffffffffu, rise)) {
-          const float f = rise ? ex2((m - top) * A.scale_log2) : 1.f;
-          if (rise) { m = top; sum *= f; }
-          if (!W.fresh) {
-            if (!wait(b_o + 8 * l, (n - 1) & 1)) { ok = false; break; }
-            tm_fence_after();
-#pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
-              uint32_t o[32];
-              tm_ld32(t_o + 32 * c, o);
-              tm_wait_ld();
-              tm_pin32(o);
-#pragma unroll
-              for (int j = 0; j < 32; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
-              tm_st32(t_o + 32 * c, o);
-            }
-          }
-        }
-        const float off = m == -INFINITY ? 0.f : -m * A.scale_log2;
-        float acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int c0 = 0; c0 < AT_KEYS; c0 += 64) {
-          uint32_t s[64];
-          tm_ld32(t_s + c0, s);
-          tm_ld32(t_s + c0 + 32, s + 32);
-          tm_wait_ld();
-          tm_pin32(s);
-          tm_pin32(s + 32);
-          if (masked) {
-#pragma unroll
-            for (int c = 0; c < 64; ++c)
-              if (c0 + c < mlo || c0 + c >= mhi) s[c] = 0xff800000u;
-          }
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            uint32_t pk[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              const float p0 = ex2(fmaf(__uint_as_float(s[32 * c + 2 * j]), A.scale_log2, off));
-              const float p1 = ex2(fmaf(__uint_as_float(s[32 * c + 2 * j + 1]), A.scale_log2, off));
-              acc[j & 1] += p0;
-              acc[2 + (j & 1)] += p1;
-              pk[j] = pack2<WD>(p0, p1);
-            }
-            tm_st16(t_s + c0 / 2 + 16 * c, pk);  // (over scores that have been read)
-          }
-        }
-        sum += (acc[0] + acc[1]) + (acc[2] + acc[3]);
-        tm_wait_st();
-      }
-      tm_fence_before();
+    Slots Q(S.batch_pieces[l], q_slots, 0);
+    const float scale = A.scale_log2;
+    for (int n = 0; ok && n < cnt;) {
+      const uint32_t slot = Q.slot;
+      if (!wait(b_qfull + 32 * l + 8 * slot, Q.parity())) break;
+      Q.next();
+      const Piece P = s_piece[l][slot];
       __syncwarp();
-      if (lane_id == 0) mb_arrive(b_p + 8 * l);
-      if (!W.last) continue;
+      if (lane_id == 0) mb_arrive(b_qempty + 32 * l + 8 * slot);
+      const int tr = row / A.group;
+      const bool live = tr < P.ntok, warp_live = __any_sync(0xffffffffu, live);
+      int lo = P.k0, hi = 0x7fffffff;  // keys this row sees
+      if (live) {
+        const int t = P.tok + tr, b = t / A.q_len;
+        // (an own unit's last key is its sequence's last)
+        hi = max((P.kind == AT_OWN ? P.hi : attend_len(A, b, false)) - A.q_len + (t - b * A.q_len) + 1, 0);
+        lo = A.window > 0 ? max(hi - A.window, 0) : 0;
+        if (P.kind == AT_OWN) lo = max(lo, A.prefix);
+        else hi = min(hi, A.prefix);
+      }
+      lo -= P.k0; hi -= P.k0;  // from here on relative to the tile
+      float m = -INFINITY, sum = 0.f;
+      for (int j = 0; j < P.tiles; ++j, ++n, lo -= AT_KEYS, hi -= AT_KEYS) {
+        ok = wait(b_s + 8 * l, n & 1);
+        if (!ok) break;
+        tm_fence_after();
+        if (warp_live) {
+          // two passes over the scores in tensor memory (64 at a time in registers): the maximum, then the weights
+          const bool masked = !__all_sync(0xffffffffu, lo <= 0 && hi >= AT_KEYS);
+          float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+          for (int c0 = 0; c0 < AT_KEYS; c0 += 64) {
+            uint32_t s[64];
+            tm_ld32(t_s + c0, s);
+            tm_ld32(t_s + c0 + 32, s + 32);
+            tm_wait_ld();
+            tm_pin32(s);
+            tm_pin32(s + 32);
+            if (masked) {
+#pragma unroll
+              for (int c = 0; c < 64; ++c)
+                if (c0 + c < lo || c0 + c >= hi) s[c] = 0xff800000u;
+            }
+#pragma unroll
+            for (int c = 0; c < 64; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(s[c]));
+          }
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+          const bool rise = live && top > m && (m == -INFINITY || (top - m) * scale > 8.f);
+          if (__any_sync(0xffffffffu, rise)) {
+            const float f = rise ? ex2((m - top) * scale) : 1.f;
+            if (rise) { m = top; sum *= f; }
+            if (j > 0) {
+              ok = wait(b_o + 8 * l, (n - 1) & 1);
+              if (!ok) break;
+              tm_fence_after();
+#pragma unroll
+              for (int c = 0; c < D / 32; ++c) {
+                uint32_t o[32];
+                tm_ld32(t_o + 32 * c, o);
+                tm_wait_ld();
+                tm_pin32(o);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                tm_st32(t_o + 32 * c, o);
+              }
+            }
+          }
+          const float off = m == -INFINITY ? 0.f : -m * scale;
+          float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int c0 = 0; c0 < AT_KEYS; c0 += 64) {
+            uint32_t s[64];
+            tm_ld32(t_s + c0, s);
+            tm_ld32(t_s + c0 + 32, s + 32);
+            tm_wait_ld();
+            tm_pin32(s);
+            tm_pin32(s + 32);
+            if (masked) {
+#pragma unroll
+              for (int c = 0; c < 64; ++c)
+                if (c0 + c < lo || c0 + c >= hi) s[c] = 0xff800000u;
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+              uint32_t pk[16];
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const float p0 = ex2(fmaf(__uint_as_float(s[32 * c + 2 * e]), scale, off));
+                const float p1 = ex2(fmaf(__uint_as_float(s[32 * c + 2 * e + 1]), scale, off));
+                acc[e & 1] += p0;
+                acc[2 + (e & 1)] += p1;
+                pk[e] = pack2<WD>(p0, p1);
+              }
+              tm_st16(t_s + c0 / 2 + 16 * c, pk);  // (over scores that have been read)
+            }
+          }
+          sum += (acc[0] + acc[1]) + (acc[2] + acc[3]);
+          tm_wait_st();
+        }
+        tm_fence_before();
+        __syncwarp();
+        if (lane_id == 0) mb_arrive(b_p + 8 * l);
+      }
+      if (!ok) break;
       // the piece is done: its output and lse go to the workspace
-      if (!wait(b_o + 8 * l, n & 1)) { ok = false; break; }
+      ok = wait(b_o + 8 * l, (n - 1) & 1);
+      if (!ok) break;
       tm_fence_after();
-      long long slot;
+      const int worker = blockIdx.x * 2 + l;
+      long long slot_row;
       float *po, *pl;
-      if (W.kind == AT_OWN) {
-        slot = (W.unit + worker) * ((long long)T.ts * A.group) + row;
+      if (P.kind == AT_OWN) {
+        slot_row = (long long)(P.unit + worker) * (T.ts * A.group) + row;
         po = T.own_o; pl = T.own_lse;
-        if (row == 0 && W.unit_first) T.own_first[W.unit] = worker;
-        if (row == 0 && W.unit_last) T.own_last[W.unit] = worker;
+        if (row == 0 && (P.ends & 1)) T.own_first[P.unit] = worker;
+        if (row == 0 && (P.ends & 2)) T.own_last[P.unit] = worker;
       } else {
-        const int wk = W.kind == AT_PAIR ? blockIdx.x : worker;
-        slot = W.kind == AT_PAIR ? ((W.unit + wk) * 2 + l) * 128 + row : (W.unit + wk) * 128 + row;
+        const bool pair = P.kind == AT_PAIR;
+        const int wk = pair ? blockIdx.x : worker;
+        slot_row = (pair ? (P.unit + wk) * 2LL + l : (long long)(P.unit + wk)) * 128 + row;
         po = T.pre_o; pl = T.pre_lse;
-        const bool mark = row == 0 && (l == 0 || W.kind == AT_SINGLE);
-        if (mark && W.unit_first) T.pre_first[W.unit] = wk;
-        if (mark && W.unit_last) T.pre_last[W.unit] = wk;
+        const bool mark = row == 0 && !(pair && l == 1);
+        if (mark && (P.ends & 1)) T.pre_first[P.unit] = wk;
+        if (mark && (P.ends & 2)) T.pre_last[P.unit] = wk;
       }
       if (warp_live) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        if (live) pl[slot] = sum == 0.f ? -INFINITY : fmaf(m, A.scale_log2, log2f(sum));
+        if (live) pl[slot_row] = sum == 0.f ? -INFINITY : fmaf(m, scale, log2f(sum));
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
           uint32_t o[32];
@@ -565,13 +596,14 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
           tm_wait_ld();
           tm_pin32(o);
           if (live) {
-            float4* dst = reinterpret_cast<float4*>(po + slot * D + 32 * c);
+            float4* dst = reinterpret_cast<float4*>(po + slot_row * D + 32 * c);
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-              dst[j] = make_float4(__uint_as_float(o[4 * j]) * inv, __uint_as_float(o[4 * j + 1]) * inv, __uint_as_float(o[4 * j + 2]) * inv,
-                                   __uint_as_float(o[4 * j + 3]) * inv);
+            for (int e = 0; e < 8; ++e)
+              dst[e] = make_float4(__uint_as_float(o[4 * e]) * inv, __uint_as_float(o[4 * e + 1]) * inv, __uint_as_float(o[4 * e + 2]) * inv,
+                                   __uint_as_float(o[4 * e + 3]) * inv);
           }
         }
+        tm_fence_before();
       }
     }
   }
