@@ -491,7 +491,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
           // two passes over the scores in tensor memory (64 at a time in registers): the maximum, then the weights
           const bool masked = !__all_sync(0xffffffffu, lo <= 0 && hi >= AT_KEYS);
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
+#pragma unroll 1
           for (int c0 = 0; c0 < AT_KEYS; c0 += 64) {
             uint32_t s[64];
             tm_ld32(t_s + c0, s);
@@ -505,7 +505,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
                 if (c0 + c < lo || c0 + c >= hi) s[c] = 0xff800000u;
             }
 #pragma unroll
-            for (int c = 0; c < 64; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(s[c]));
+            for (int c = 0; c < 64; c += 2)
+              mx[(c / 2) & 3] = max3(mx[(c / 2) & 3], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
           }
           const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
           const bool rise = live && top > m && (m == -INFINITY || (top - m) * scale > 8.f);
@@ -529,8 +530,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
             }
           }
           const float off = m == -INFINITY ? 0.f : -m * scale;
-          float acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
+          uint64_t acc[2] = {0, 0};
+          const uint64_t scale2 = both(scale), off2 = both(off);
+#pragma unroll 1
           for (int c0 = 0; c0 < AT_KEYS; c0 += 64) {
             uint32_t s[64];
             tm_ld32(t_s + c0, s);
@@ -544,20 +546,16 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
                 if (c0 + c < lo || c0 + c >= hi) s[c] = 0xff800000u;
             }
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-              uint32_t pk[16];
-#pragma unroll
-              for (int e = 0; e < 16; ++e) {
-                const float p0 = ex2(fmaf(__uint_as_float(s[32 * c + 2 * e]), scale, off));
-                const float p1 = ex2(fmaf(__uint_as_float(s[32 * c + 2 * e + 1]), scale, off));
-                acc[e & 1] += p0;
-                acc[2 + (e & 1)] += p1;
-                pk[e] = pack2<WD>(p0, p1);
-              }
-              tm_st16(t_s + c0 / 2 + 16 * c, pk);  // (over scores that have been read)
+            for (int c = 0; c < 64; c += 2) {
+              const uint64_t x = fma2(pair32(s[c], s[c + 1]), scale2, off2);
+              const float p0 = ex2(__uint_as_float((uint32_t)x)), p1 = ex2(__uint_as_float((uint32_t)(x >> 32)));
+              acc[(c / 2) & 1] = add2(acc[(c / 2) & 1], pair32(__float_as_uint(p0), __float_as_uint(p1)));
+              s[c / 2] = pack2<WD>(p0, p1);
             }
+            tm_st32(t_s + c0 / 2, s);  // (over scores that have been read)
           }
-          sum += (acc[0] + acc[1]) + (acc[2] + acc[3]);
+          const uint64_t acc_all = add2(acc[0], acc[1]);
+          sum += __uint_as_float((uint32_t)acc_all) + __uint_as_float((uint32_t)(acc_all >> 32));
           tm_wait_st();
         }
         tm_fence_before();
