@@ -30,6 +30,15 @@ constexpr int AT_KEYS = 128;
 constexpr long long AT_SPIN_CLOCKS = 4000LL * 1000 * 1000;  // about two seconds
 constexpr int AT_COST_PAIR = 2, AT_COST_LANE = 1;           // of one key tile, in units of half a CTA
 
+constexpr int AT_POLY = 4;  // of 16 pairs of weights, how many are computed by ex2_poly2
+
+// The bits [lo, hi) of a word, as far as they lie in it.
+__device__ __forceinline__ uint32_t range_bits(int lo, int hi) {
+  const int a = min(max(lo, 0), 32), b = min(max(hi, 0), 32);
+  const uint32_t below_b = b == 32 ? ~0u : (1u << b) - 1, below_a = a == 32 ? ~0u : (1u << a) - 1;
+  return below_b & ~below_a;
+}
+
 template <int D>
 struct TileShape {
   static constexpr int STAGES = D == 128 ? 5 : 8;
@@ -499,15 +508,19 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
             tm_wait_ld();
             tm_pin32(s);
             tm_pin32(s + 32);
-            if (masked) {
+            if (masked) {  // (the second pass finds them masked)
+              const uint32_t on0 = range_bits(lo - c0, hi - c0), on1 = range_bits(lo - c0 - 32, hi - c0 - 32);
 #pragma unroll
               for (int c = 0; c < 64; ++c)
-                if (c0 + c < lo || c0 + c >= hi) s[c] = 0xff800000u;
+                if (!((c < 32 ? on0 : on1) & 1u << (c & 31))) s[c] = 0xff800000u;
+              tm_st32(t_s + c0, s);
+              tm_st32(t_s + c0 + 32, s + 32);
             }
 #pragma unroll
             for (int c = 0; c < 64; c += 2)
               mx[(c / 2) & 3] = max3(mx[(c / 2) & 3], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
           }
+          if (masked) tm_wait_st();
           const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
           const bool rise = live && top > m && (m == -INFINITY || (top - m) * scale > 8.f);
           if (__any_sync(0xffffffffu, rise)) {
@@ -540,22 +553,17 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
             tm_wait_ld();
             tm_pin32(s);
             tm_pin32(s + 32);
-            if (masked) {
-#pragma unroll
-              for (int c = 0; c < 64; ++c)
-                if (c0 + c < lo || c0 + c >= hi) s[c] = 0xff800000u;
-            }
 #pragma unroll
             for (int c = 0; c < 64; c += 2) {
               const uint64_t x = fma2(pair32(s[c], s[c + 1]), scale2, off2);
-              const float p0 = ex2(__uint_as_float((uint32_t)x)), p1 = ex2(__uint_as_float((uint32_t)(x >> 32)));
-              acc[(c / 2) & 1] = add2(acc[(c / 2) & 1], pair32(__float_as_uint(p0), __float_as_uint(p1)));
-              s[c / 2] = pack2<WD>(p0, p1);
+              const uint64_t p = (c / 2) % 16 < AT_POLY ? ex2_poly2(x) : pair32(__float_as_uint(ex2(lo32(x))), __float_as_uint(ex2(hi32(x))));
+              acc[(c / 2) & 1] = add2(acc[(c / 2) & 1], p);
+              s[c / 2] = pack2<WD>(lo32(p), hi32(p));
             }
             tm_st32(t_s + c0 / 2, s);  // (over scores that have been read)
           }
           const uint64_t acc_all = add2(acc[0], acc[1]);
-          sum += __uint_as_float((uint32_t)acc_all) + __uint_as_float((uint32_t)(acc_all >> 32));
+          sum += lo32(acc_all) + hi32(acc_all);
           tm_wait_st();
         }
         tm_fence_before();
