@@ -78,6 +78,7 @@ struct Share {
   int pair0, pair1;                   // this CTA's (pair unit, tile) range
   int lane0[2], lane1[2];             // its lanes' ranges in the line of single and own units
   int own_b[2], own_u[2], own_t[2];   // where a lane's range starts, if among the own units: sequence, unit within it, tile
+  OwnKeys own_k[2];                   // ... and that sequence's keys
   int batch_pieces[2];                // pieces of each lane that are not of own units (they come first)
 };
 
@@ -113,7 +114,9 @@ __device__ __forceinline__ bool walk_next(const TileArgs& T, const Share& S, int
   if (W.pairs && W.w == W.end) {
     W.pairs = false;
     W.w = S.lane0[lane]; W.end = S.lane1[lane];
-    W.b = S.own_b[lane]; W.u = S.own_u[lane]; W.tile = S.own_t[lane]; W.tiles = -1;
+    W.b = S.own_b[lane]; W.u = S.own_u[lane]; W.tile = S.own_t[lane];
+    const OwnKeys k = S.own_k[lane];
+    W.tiles = W.b < 0 ? -1 : k.tiles; W.lo = k.lo; W.hi = k.hi; W.origin = k.origin;
   }
   if (W.w >= W.end) return false;
   if (W.pairs || W.b < 0) {
@@ -219,9 +222,11 @@ __device__ __forceinline__ void make_share(const TileArgs& T, Share& S, int* s_s
     if (w < acc || w >= acc + sum * mult) continue;
 #pragma unroll 1
     for (int b = b0; b < b1; ++b) {
-      const int t = own_keys(T, attend_len(A, b, false)).tiles;
+      const OwnKeys k = own_keys(T, attend_len(A, b, false));
+      const int t = k.tiles;
       if (w < acc + t * mult) {
         S.own_b[l] = b;
+        S.own_k[l] = k;
         S.own_u[l] = (w - acc) / t;
         S.own_t[l] = (w - acc) - S.own_u[l] * t;
         break;
@@ -497,28 +502,36 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         if (!ok) break;
         tm_fence_after();
         if (warp_live) {
-          // two passes over the scores in tensor memory (64 at a time in registers): the maximum, then the weights
+          // Two passes over the scores: the maximum (all four quarters of the columns), then the weights.  The quarters 0 and 1 stay in
+          // registers between the passes; 2 and 3 are read again (masked ones are written back first).  The weights of a
+          // quarter go over scores that are in registers or done with.
           const bool masked = !__all_sync(0xffffffffu, lo <= 0 && hi >= AT_KEYS);
+          uint32_t s0[32], s1[32];
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 1
-          for (int c0 = 0; c0 < AT_KEYS; c0 += 64) {
-            uint32_t s[64];
-            tm_ld32(t_s + c0, s);
-            tm_ld32(t_s + c0 + 32, s + 32);
-            tm_wait_ld();
-            tm_pin32(s);
-            tm_pin32(s + 32);
-            if (masked) {  // (the second pass finds them masked)
-              const uint32_t on0 = range_bits(lo - c0, hi - c0), on1 = range_bits(lo - c0 - 32, hi - c0 - 32);
 #pragma unroll
-              for (int c = 0; c < 64; ++c)
-                if (!((c < 32 ? on0 : on1) & 1u << (c & 31))) s[c] = 0xff800000u;
-              tm_st32(t_s + c0, s);
-              tm_st32(t_s + c0 + 32, s + 32);
+          for (int half = 1; half >= 0; --half) {
+            tm_ld32(t_s + 64 * half, s0);
+            tm_ld32(t_s + 64 * half + 32, s1);
+            tm_wait_ld();
+            tm_pin32(s0);
+            tm_pin32(s1);
+            if (masked) {
+              const uint32_t on0 = range_bits(lo - 64 * half, hi - 64 * half), on1 = range_bits(lo - 64 * half - 32, hi - 64 * half - 32);
+#pragma unroll
+              for (int c = 0; c < 32; ++c) {
+                if (!(on0 & 1u << c)) s0[c] = 0xff800000u;
+                if (!(on1 & 1u << c)) s1[c] = 0xff800000u;
+              }
+              if (half) {
+                tm_st32(t_s + 64, s0);
+                tm_st32(t_s + 96, s1);
+              }
             }
 #pragma unroll
-            for (int c = 0; c < 64; c += 2)
-              mx[(c / 2) & 3] = max3(mx[(c / 2) & 3], __uint_as_float(s[c]), __uint_as_float(s[c + 1]));
+            for (int c = 0; c < 32; c += 2) {
+              mx[(c / 2) & 1] = max3(mx[(c / 2) & 1], __uint_as_float(s0[c]), __uint_as_float(s0[c + 1]));
+              mx[2 + ((c / 2) & 1)] = max3(mx[2 + ((c / 2) & 1)], __uint_as_float(s1[c]), __uint_as_float(s1[c + 1]));
+            }
           }
           if (masked) tm_wait_st();
           const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
@@ -545,23 +558,26 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
           const float off = m == -INFINITY ? 0.f : -m * scale;
           uint64_t acc[2] = {0, 0};
           const uint64_t scale2 = both(scale), off2 = both(off);
-#pragma unroll 1
-          for (int c0 = 0; c0 < AT_KEYS; c0 += 64) {
-            uint32_t s[64];
-            tm_ld32(t_s + c0, s);
-            tm_ld32(t_s + c0 + 32, s + 32);
-            tm_wait_ld();
-            tm_pin32(s);
-            tm_pin32(s + 32);
+          auto quarter = [&](uint32_t* s, int i) {
 #pragma unroll
-            for (int c = 0; c < 64; c += 2) {
+            for (int c = 0; c < 32; c += 2) {
               const uint64_t x = fma2(pair32(s[c], s[c + 1]), scale2, off2);
-              const uint64_t p = (c / 2) % 16 < AT_POLY ? ex2_poly2(x) : pair32(__float_as_uint(ex2(lo32(x))), __float_as_uint(ex2(hi32(x))));
+              const uint64_t p = (c / 2) % 16 * AT_POLY % 16 < AT_POLY ? ex2_poly2(x) : pair32(__float_as_uint(ex2(lo32(x))), __float_as_uint(ex2(hi32(x))));
               acc[(c / 2) & 1] = add2(acc[(c / 2) & 1], p);
               s[c / 2] = pack2<WD>(lo32(p), hi32(p));
             }
-            tm_st32(t_s + c0 / 2, s);  // (over scores that have been read)
-          }
+            tm_st16(t_s + 16 * i, s);
+          };
+          quarter(s0, 0);
+          tm_ld32(t_s + 64, s0);
+          quarter(s1, 1);
+          tm_wait_ld();
+          tm_pin32(s0);
+          tm_ld32(t_s + 96, s1);
+          quarter(s0, 2);
+          tm_wait_ld();
+          tm_pin32(s1);
+          quarter(s1, 3);
           const uint64_t acc_all = add2(acc[0], acc[1]);
           sum += lo32(acc_all) + hi32(acc_all);
           tm_wait_st();
