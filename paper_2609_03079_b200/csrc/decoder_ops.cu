@@ -32,6 +32,8 @@ namespace {
 // Blocks that ls_attend_rows_kernel is split into when rows are few: eight blocks of four warps per SM.
 constexpr int kRowsBlocks = 148 * 8;
 constexpr int kRowsMaxGroup = 8;
+// Up to this many output rows the pieces of each are joined by eight warps (all blocks are resident at once), else by one.
+constexpr long long kJoinFewRows = 148 * 8;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
@@ -156,7 +158,8 @@ int32_t attend_tiles(ls_paged_kv* kv, const ls::AttendArgs& a, cudaStream_t st) 
   LS_LAUNCHED();
   const long long rows = (long long)a.n_seqs * a.q_len * a.heads;
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)((rows + 7) / 8));
+  const bool few = rows <= kJoinFewRows;
+  cfg.gridDim = dim3((unsigned)(few ? rows : (rows + 7) / 8));
   cfg.blockDim = dim3(256);
   cfg.stream = st;
   cudaLaunchAttribute at{};
@@ -164,7 +167,8 @@ int32_t attend_tiles(ls_paged_kv* kv, const ls::AttendArgs& a, cudaStream_t st) 
   at.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
-  LS_CUDA((cudaLaunchKernelEx(&cfg, ls::ls_attend_tile_join_kernel<WD, D>, t)));
+  if (few) LS_CUDA((cudaLaunchKernelEx(&cfg, ls::ls_attend_tile_join_kernel<WD, D, 8>, t)));
+  else LS_CUDA((cudaLaunchKernelEx(&cfg, ls::ls_attend_tile_join_kernel<WD, D, 1>, t)));
   LS_LAUNCHED();
   return LS_OK;
 }

@@ -89,6 +89,14 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 }
 
 template <int WD>
+__device__ __forceinline__ uint16_t narrow16(float x) {
+  uint16_t r;
+  if (WD == WD_BF16) asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(r) : "f"(x));
+  else asm("cvt.rn.f16.f32 %0, %1;" : "=h"(r) : "f"(x));
+  return r;
+}
+
+template <int WD>
 __device__ __forceinline__ void load8(const uint16_t* p, bool vec, float (&f)[8]) {
   uint4 v;
   if (vec) v = ldg128(p);

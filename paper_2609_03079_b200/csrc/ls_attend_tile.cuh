@@ -44,7 +44,10 @@ struct TileShape {
   static constexpr int STAGES = D == 128 ? 5 : 8;
   static constexpr int TILE = AT_KEYS * D * 2;   // bytes of a key, value or query tile
   static constexpr int HALF = AT_KEYS * 128;     // bytes of 64 of its columns
-  static constexpr int SMEM = 1024 + (2 + STAGES) * TILE;
+  // weights of a narrow piece: [2 x 64 keys][32 rows] of 128 bytes, in the last rows of the lane's query buffer
+  static constexpr int NARROW_SLOTS = D == 128 ? 3 : 2, P_AT = NARROW_SLOTS * 32 * 128, P_HALF = D == 128 ? HALF : 32 * 128;
+  static constexpr int CTL = (2 + STAGES) * TILE;  // offset of the control block
+  static constexpr int SMEM = CTL + 3072;
 };
 
 struct TileArgs {
@@ -92,7 +95,10 @@ struct Piece {
   int kind, h, tok, ntok;    // key head, first token and number of tokens of the row tile
   int k0, tiles, lo, hi;     // first key, number of tiles; keys outside [lo, hi) are nobody's
   int unit, ends;            // number of the unit among its kind; bit 0: holds its first tile, bit 1: its last
+  int narrow;                // rows of a narrow piece, padded (16 or 32), 0: a wide one
 };
+
+__device__ __forceinline__ int narrow_rows(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 0; }
 
 // Walks one lane's line piece by piece.
 struct Walk {
@@ -128,10 +134,12 @@ __device__ __forceinline__ bool walk_next(const TileArgs& T, const Share& S, int
     P.lo = S.pre_lo; P.hi = A.prefix;
     if (W.pairs) {
       P.kind = AT_PAIR;
+      P.narrow = 0;
       P.h = P.unit / T.pairs;
       P.tok = ((P.unit - P.h * T.pairs) * 2 + lane) * T.tq;
     } else {
       P.kind = AT_SINGLE;
+      P.narrow = narrow_rows(A.n_seqs * A.q_len * A.group);
       P.h = P.unit;
       P.tok = 0;
       if ((P.ends & 2) && P.unit == A.kv_heads - 1) { W.b = 0; W.u = 0; W.tile = 0; }
@@ -147,6 +155,7 @@ __device__ __forceinline__ bool walk_next(const TileArgs& T, const Share& S, int
     }
     const int per = A.kv_heads * T.rt;
     P.kind = AT_OWN;
+    P.narrow = narrow_rows(T.ts * A.group);
     P.tiles = min(W.tiles - W.tile, W.end - W.w);
     P.unit = W.b * per + W.u;
     P.h = T.rt == 1 ? W.u : W.u / T.rt;
@@ -234,8 +243,20 @@ __device__ __forceinline__ void make_share(const TileArgs& T, Share& S, int* s_s
       acc += t * mult;
     }
   }
-  __syncthreads();
 }
+
+// Control block of a CTA, behind the tiles in shared memory.
+template <int NST>
+struct TileCtl {
+  unsigned long long full[NST], empty[NST], qfull[2][4], qempty[2][4], s[2][2], p[2], o[2], turn[2];
+  Share share;
+  int scan[2 * AT_THREADS / 32];
+  Piece piece[2][4];
+  float red[2][4][32];        // narrow pieces: maxima or sums of each warp's keys
+  int lo[2][32], hi[2][32];   // ... keys of each row, relative to the piece's first
+  uint32_t tmem;
+  volatile int dead;
+};
 
 template <int WD, int D>
 __global__ void __launch_bounds__(AT_THREADS, 1)
@@ -243,37 +264,36 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
                           const __grid_constant__ CUtensorMap map_q_all, const __grid_constant__ CUtensorMap map_q_own) {
   using TS = TileShape<D>;
   constexpr int NST = TS::STAGES;
-  extern __shared__ unsigned char dyn[];
-  __shared__ Share S;
-  __shared__ int s_scan[2 * AT_THREADS / 32];
-  __shared__ Piece s_piece[2][4];
-  __shared__ alignas(8) unsigned long long bars[2 * NST + 24];
-  __shared__ uint32_t s_tmem;
-  __shared__ volatile int s_dead;
+  extern __shared__ __align__(1024) unsigned char dyn[];
+  static_assert(sizeof(TileCtl<NST>) <= TS::SMEM - TS::CTL, "control block");
+  TileCtl<NST>& C = *reinterpret_cast<TileCtl<NST>*>(dyn + TS::CTL);
+  Share& S = C.share;
   const AttendArgs& A = T.a;
   const int tid = threadIdx.x, lane_id = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
-  const uint32_t q_base = (saddr(dyn) + 1023) & ~1023u, ring = q_base + 2 * TS::TILE;
-  const uint32_t bar0 = saddr(bars);
-  const uint32_t b_full = bar0, b_empty = bar0 + 8 * NST, b_qfull = b_empty + 8 * NST, b_qempty = b_qfull + 64, b_s = b_qempty + 64,
-                 b_p = b_s + 16, b_o = b_p + 16, b_turn = b_o + 16;
+  const uint32_t q_base = saddr(dyn), ring = q_base + 2 * TS::TILE;
+  const uint32_t b_full = saddr(C.full), b_empty = saddr(C.empty), b_qfull = saddr(C.qfull), b_qempty = saddr(C.qempty), b_s = saddr(C.s),
+                 b_p = saddr(C.p), b_o = saddr(C.o), b_turn = saddr(C.turn);
+  if (q_base & 1023) {  // (swizzled tiles need it; the first byte of a block's shared memory has it)
+    if (tid == 0) set_status(A.status, ST_INTERNAL);
+    return;
+  }
 
-  if (tid == 0) {
-    for (int i = 0; i < NST; ++i) { mb_init(b_full + 8 * i, 1); mb_init(b_empty + 8 * i, 2); }
-    for (int l = 0; l < 2; ++l) {
-      for (int i = 0; i < 4; ++i) { mb_init(b_qfull + 32 * l + 8 * i, 1); mb_init(b_qempty + 32 * l + 8 * i, 5); }
-      mb_init(b_s + 8 * l, 1); mb_init(b_p + 8 * l, 4); mb_init(b_o + 8 * l, 1); mb_init(b_turn + 8 * l, 1);
-    }
+  if (warp == 0) {
+    if (lane_id < NST) { mb_init(b_full + 8 * lane_id, 1); mb_init(b_empty + 8 * lane_id, 2); }
+    if (lane_id < 8) { mb_init(b_qfull + 8 * lane_id, 1); mb_init(b_qempty + 8 * lane_id, 5); }
+    if (lane_id < 4) mb_init(b_s + 8 * lane_id, 1);
+    if (lane_id < 2) { mb_init(b_p + 8 * lane_id, 4); mb_init(b_o + 8 * lane_id, 1); mb_init(b_turn + 8 * lane_id, 1); }
+    if (lane_id == 0) C.dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_shared();
-    s_dead = 0;
   }
-  if (warp == 9) tm_alloc(saddr(&s_tmem), 512);
+  if (warp == 9) tm_alloc(saddr(&C.tmem), 512);
   if (warp == 8 && lane_id < 4) tma_prefetch_map(lane_id == 0 ? &map_k : lane_id == 1 ? &map_v : lane_id == 2 ? &map_q_all : &map_q_own);
-  make_share(T, S, s_scan, blockIdx.x, gridDim.x);
+  make_share(T, S, C.scan, blockIdx.x, gridDim.x);
   tm_fence_before();
   __syncthreads();
   tm_fence_after();
-  const uint32_t tmem = s_tmem;
+  const uint32_t tmem = C.tmem;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   // Bounded wait of a whole warp: false (for all of it) once any wait of the CTA has given up.
@@ -282,8 +302,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     if (!got) {
       const long long t0 = clock64();
       while (!(got = mb_try(bar, parity))) {
-        if (s_dead) break;
-        if (clock64() - t0 > AT_SPIN_CLOCKS) { s_dead = 1; set_status(A.status, ST_TIMEOUT); break; }
+        if (C.dead) break;
+        if (clock64() - t0 > AT_SPIN_CLOCKS) { C.dead = 1; set_status(A.status, ST_TIMEOUT); break; }
       }
     }
     return __all_sync(0xffffffffu, got);
@@ -293,10 +313,11 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
   const int n_pair = S.pair1 - S.pair0;
   const int cnt0 = n_pair + S.lane1[0] - S.lane0[0], cnt1 = n_pair + S.lane1[1] - S.lane0[1];
   // Query tiles: rows of the whole batch take a lane's whole buffer; a sequence's rows take a slot of it, so that the copies run
-  // ahead by several pieces where these rows are few.  (A slot's product still reads 128 rows: what lies behind is ignored.)
+  // ahead by several pieces where these rows are few.  (A slot's product may read 128 rows: what lies behind is ignored.)
   // Piece i of a lane is in slot 0 if it is one of the first batch_pieces, else in slot (i - batch_pieces) % q_slots; the slot's
-  // barriers count the copy, and its release by the last product and by the four softmax warps.
-  const int q_rows = T.ts * A.group, q_slots = q_rows <= 32 ? 4 : q_rows <= 64 ? 2 : 1, q_step = 128 / q_slots * 128;
+  // barriers count the copy, and its release by the last product and by the four softmax warps.  A narrow piece's rows are at
+  // most 32; its weights are behind the slots.
+  const int q_rows = T.ts * A.group, q_slots = q_rows <= 32 ? TS::NARROW_SLOTS : q_rows <= 64 ? 2 : 1, q_step = q_rows <= 32 ? 32 * 128 : 64 * 128;
   struct Slots {
     int batch, n;
     uint32_t slot, par;
@@ -311,16 +332,20 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
   bool ok = true;
   if (warp == 8) {
     // ---- copies.  Order of the ring: for every round r and lane: values of round r - 1, keys of round r; a pair's once.
-    // The walk is one tile ahead of the copies, so that the page numbers are there when they are needed.
+    // Page numbers come 32 boxes at a time, one to each thread, a batch ahead: the next batch of the piece, or the first of the
+    // next piece (so the walk is a piece ahead).
     Walk W[2];
-    Piece P[2];
-    int left[2] = {0, 0}, page[2] = {0, 0};
-    bool fresh[2] = {false, false};
+    Piece P[2], N[2];
+    bool more[2], fresh[2] = {false, false};
+    int left[2] = {0, 0}, batch[2], pages[2], pages_next[2];                               // batch: key of its first box
     int vk0[2] = {0, 0}, vlo[2] = {0, 0}, vhi[2] = {0, 0}, vh[2] = {0, 0}, vpage[2] = {0, 0};  // tile whose values are to come
     uint32_t st = 0, st_par = 1;
     Slots Q[2] = {Slots(S.batch_pieces[0], q_slots, 15), Slots(S.batch_pieces[1], q_slots, 15)};
-    const int nbox = AT_KEYS / T.box;
+    const int nbox = AT_KEYS / T.box, box_shift = 31 - __clz(T.box);
     const int my_box = lane_id & (nbox - 1), my_half = lane_id / nbox;
+    const bool page_pow2 = (A.page & (A.page - 1)) == 0;
+    const int page_shift = 31 - __clz(A.page);
+    auto page_index = [&](int key) { return page_pow2 ? key >> page_shift : key / A.page; };
     auto load_tile = [&](const CUtensorMap* map, int k0, int lo, int hi, int h, int pg) {
       const int key = k0 + my_box * T.box;
       const bool on = my_half < D / 64 && key < hi && key + T.box > lo;
@@ -331,22 +356,31 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       if (lane_id == 0) mb_expect(b_full + 8 * st, count * T.box * 128);
       __syncwarp();
       if (on)
-        tma_load4(ring + st * TS::TILE + my_half * TS::HALF + my_box * T.box * 128, map, my_half * 64, key % A.page, h, pg, b_full + 8 * st);
+        tma_load4(ring + st * TS::TILE + my_half * TS::HALF + my_box * T.box * 128, map, my_half * 64, key - page_index(key) * A.page, h, pg, b_full + 8 * st);
       if (++st == NST) { st = 0; st_par ^= 1; }
     };
-    auto advance = [&](auto lc) {  // to the next tile, and this lane's page of it
+    auto fetch_pages = [&](const Piece& p, int key) {  // (no branch around the load: nothing waits for it here)
+      key += lane_id * T.box;
+      const bool on = key < p.hi && key + T.box > p.lo;
+      const int32_t* tab = p.kind == AT_OWN ? A.table + (long long)(A.q_len == 1 ? p.tok : p.tok / A.q_len) * A.table_stride : A.prefix_pages;
+      return *(on ? tab + page_index(key) : A.seq_len);
+    };
+    auto advance = [&](auto lc) {  // to the next tile
       constexpr int l = decltype(lc)::value;
-      fresh[l] = false;
-      if (left[l] > 0) { --left[l]; P[l].k0 += AT_KEYS; }
+      fresh[l] = left[l] == 0;
+      if (!fresh[l]) { --left[l]; P[l].k0 += AT_KEYS; }
       else {
-        if (!walk_next(T, S, l, W[l], P[l])) return;
-        fresh[l] = true;
+        if (!more[l]) return;
+        P[l] = N[l];
         left[l] = P[l].tiles - 1;
+        more[l] = walk_next(T, S, l, W[l], N[l]);
       }
-      const int key = P[l].k0 + my_box * T.box;
-      if (key >= P[l].hi || key + T.box <= P[l].lo) return;
-      const int32_t* tab = P[l].kind == AT_OWN ? A.table + (long long)(P[l].tok / A.q_len) * A.table_stride : A.prefix_pages;
-      page[l] = tab[key / A.page];
+      if (!fresh[l] && P[l].k0 < batch[l] + 32 * T.box) return;
+      pages[l] = pages_next[l];
+      batch[l] = P[l].k0;
+      const int next = batch[l] + 32 * T.box;
+      if (next < P[l].k0 + (left[l] + 1) * AT_KEYS) pages_next[l] = fetch_pages(P[l], next);
+      else if (more[l]) pages_next[l] = fetch_pages(N[l], N[l].k0);
     };
     auto step = [&](auto lc, int r, int cnt) {
       constexpr int l = decltype(lc)::value;
@@ -359,7 +393,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         if (!ok) return;
         Q[l].next();
         if (lane_id == 0) {
-          s_piece[l][slot] = P[l];
+          C.piece[l][slot] = P[l];
           const uint32_t full = b_qfull + 32 * l + 8 * slot;
           mb_expect(full, (own ? T.ts : T.tq) * A.group * D * 2);
 #pragma unroll
@@ -369,13 +403,21 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         __syncwarp();
       }
       if (!(r < n_pair && l == 1)) {
-        vk0[l] = P[l].k0; vlo[l] = P[l].lo; vhi[l] = P[l].hi; vh[l] = P[l].h; vpage[l] = page[l];
-        load_tile(&map_k, P[l].k0, P[l].lo, P[l].hi, P[l].h, page[l]);
+        const int page = __shfl_sync(0xffffffffu, pages[l], ((P[l].k0 - batch[l]) >> box_shift) + my_box);
+        vk0[l] = P[l].k0; vlo[l] = P[l].lo; vhi[l] = P[l].hi; vh[l] = P[l].h; vpage[l] = page;
+        load_tile(&map_k, P[l].k0, P[l].lo, P[l].hi, P[l].h, page);
       }
       if (ok) advance(lc);
     };
-    walk_start(S, W[0]);
-    walk_start(S, W[1]);
+    auto begin = [&](auto lc) {
+      constexpr int l = decltype(lc)::value;
+      walk_start(S, W[l]);
+      more[l] = walk_next(T, S, l, W[l], N[l]);
+      batch[l] = 0;
+      pages[l] = pages_next[l] = more[l] ? fetch_pages(N[l], N[l].k0) : 0;
+    };
+    begin(Lane0{});
+    begin(Lane1{});
     advance(Lane0{});
     advance(Lane1{});
     const int rounds = max(cnt0, cnt1);
@@ -384,18 +426,21 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       if (ok) step(Lane1{}, r, cnt1);
     }
   } else if (warp >= 9) {
-    // ---- products of one lane: O += P V of round r - 1, then S = Q K^T of round r (which overwrites P).  One thread issues.
-    // The lanes take strict turns: a lane's products run together, so that the other lane's softmax overlaps them (products of
-    // both lanes mixed would end at the same time and the two softmaxes would then share the same cycles).  The
-    // warp clears value rows that are nobody's (whatever the page holds there, its weight of zero must not meet an infinity;
+    // ---- products of one lane, issued by one thread.  Wide tiles: O += P V of round r - 1, then S = Q K^T of round r, which
+    // overwrites P; the lanes take strict turns on pairs, so that one lane's products run together while the other lane is in
+    // its softmax (products of both lanes mixed would end at the same time, and the two softmaxes share the same cycles).
+    // Narrow tiles: S^T = K Q^T of round r first (two buffers of scores), then O^T += V^T P^T of round r - 1.
+    // The warp clears value rows that are nobody's (whatever the page holds there, its weight of zero must not meet an infinity;
     // in a pair both lanes clear, the same).  A tile's two arrivals on `empty` come from the pair's two lanes, or twice from one.
-    constexpr uint32_t ID_S = mma_idesc(WD == WD_BF16, 128, AT_KEYS, false), ID_O = mma_idesc(WD == WD_BF16, 128, D, true);
+    constexpr int TYPE = WD == WD_BF16;
+    constexpr uint32_t ID_S = mma_idesc(TYPE, 128, AT_KEYS, false, false), ID_O = mma_idesc(TYPE, 128, D, false, true);
     const int l = warp - 9;
     const int cnt = l ? cnt1 : cnt0;
     const uint32_t t_s = __shfl_sync(0xffffffffu, tmem + l * AT_KEYS, 0), t_o = __shfl_sync(0xffffffffu, tmem + 256 + l * D, 0);
     const bool leader = elect_one();
     Slots Q(S.batch_pieces[l], q_slots, 0);
     int left = 0, k0 = 0, lo = 0, hi = 0;   // of the current piece: tiles to come, first key of the next; keys of anybody
+    int narrow = 0, vk0 = 0, vlo = 0, vhi = 0, vnarrow = 0;  // v*: of the tile whose values are still to be multiplied
     bool vfresh = true;
     uint32_t q_slot = 0, st = 0, st_par = 0;
     for (int r = 0; r <= cnt; ++r) {
@@ -407,99 +452,264 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         par = st_par;
         if (slot >= NST) { slot -= NST; par ^= 1; }
       };
-      uint32_t vslot = 0, kslot, par;
-      if (r > 0) {
-        place(l == 0 || vpair ? 0 : v0 + f0, vslot, par);
-        if (!wait(b_full + 8 * vslot, par)) break;
-        const int vk0 = k0 - AT_KEYS;
-        if (vk0 < lo || k0 > hi) {
+      bool kfresh = false;
+      auto scores = [&]() -> bool {
+        uint32_t slot, par;
+        place(kpair ? v0 : l == 0 ? v0 : v0 + f0 + v1, slot, par);
+        kfresh = left == 0;
+        if (kfresh) {
+          q_slot = Q.slot;
+          if (!wait(b_qfull + 32 * l + 8 * q_slot, Q.parity())) return false;
+          Q.next();
+          const Piece& P = C.piece[l][q_slot];
+          left = P.tiles; k0 = P.k0; lo = P.lo; hi = P.hi; narrow = P.narrow;
+        }
+        if (!wait(b_full + 8 * slot, par)) return false;
+        --left;
+        tm_fence_after();
+        const uint64_t q = uniform64(smem_desc(q_base + l * TS::TILE + q_slot * q_step, 16)), k = uniform64(smem_desc(ring + slot * TS::TILE, 16));
+        if (leader) {
+          if (narrow) {
+            const uint32_t id = mma_idesc(TYPE, 128, narrow, false, false);
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) {
+              const uint32_t off = ((c / 4) * TS::HALF + (c % 4) * 32) >> 4;
+              tm_mma_ss(t_s + (r & 1) * 32, k + off, q + off, id, c > 0);
+            }
+          } else {
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) {
+              const uint32_t off = ((c / 4) * TS::HALF + (c % 4) * 32) >> 4;
+              tm_mma_ss(t_s, q + off, k + off, ID_S, c > 0);
+            }
+          }
+          tm_commit(b_s + 16 * l + 8 * (r & 1));
+          tm_commit(b_empty + 8 * slot);
+          if (!kpair) tm_commit(b_empty + 8 * slot);
+          if (left == 0) tm_commit(b_qempty + 32 * l + 8 * q_slot);
+        }
+        __syncwarp();
+        return true;
+      };
+      auto outputs = [&]() -> bool {
+        uint32_t slot, par;
+        place(l == 0 || vpair ? 0 : v0 + f0, slot, par);
+        if (!wait(b_full + 8 * slot, par)) return false;
+        if (vk0 < vlo || vk0 + AT_KEYS > vhi) {
           for (int c = lane_id; c < AT_KEYS; c += 32) {
-            if (vk0 + c >= lo && vk0 + c < hi) continue;
+            if (vk0 + c >= vlo && vk0 + c < vhi) continue;
             for (int f = 0; f < D / 64; ++f)
               for (int j = 0; j < 8; ++j)
-                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ring + vslot * TS::TILE + f * TS::HALF + c * 128 + j * 16), "r"(0) : "memory");
+                asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(ring + slot * TS::TILE + f * TS::HALF + c * 128 + j * 16), "r"(0) : "memory");
           }
           fence_async_shared();
           __syncwarp();
         }
-        if (!wait(b_p + 8 * l, (r - 1) & 1)) break;
-      }
-      if (l == 1 ? r <= cnt0 : r > 0 && r - 1 <= cnt1)
-        if (!wait(b_turn + 8 * l, (l ? r : r - 1) & 1)) break;
-      if (r > 0) {
+        if (!wait(b_p + 8 * l, (r - 1) & 1)) return false;
+        if (r <= n_pair && (l || r > 0) && !wait(b_turn + 8 * l, (l ? r : r - 1) & 1)) return false;
         tm_fence_after();
-        const uint64_t v = uniform64(smem_desc(ring + vslot * TS::TILE, TS::HALF));
+        const uint64_t v = uniform64(smem_desc(ring + slot * TS::TILE, TS::HALF));
+        const uint64_t p = uniform64(smem_desc(q_base + l * TS::TILE + TS::P_AT, 16));
         if (leader) {
+          if (vnarrow) {
+            // (64 columns of values fill a 128-row product twice: both blocks of 64 are the same one)
+            const uint64_t va = D == 128 ? v : v & ~((uint64_t)0x3fff << 16);
+            const uint32_t id = mma_idesc(TYPE, 128, vnarrow, true, false);
 #pragma unroll
-          for (int k = 0; k < AT_KEYS / 16; ++k) tm_mma_ts(t_o, t_s + k * 8, v + k * (2048 >> 4), ID_O, !(vfresh && k == 0));
-          tm_commit(b_o + 8 * l);
-          tm_commit(b_empty + 8 * vslot);
-          if (!vpair) tm_commit(b_empty + 8 * vslot);
-        }
-        __syncwarp();
-      }
-      if (r < cnt) {
-        place(kpair ? v0 : l == 0 ? v0 : v0 + f0 + v1, kslot, par);
-        vfresh = left == 0;
-        if (left == 0) {
-          q_slot = Q.slot;
-          if (!wait(b_qfull + 32 * l + 8 * q_slot, Q.parity())) break;
-          Q.next();
-          const Piece& P = s_piece[l][q_slot];
-          left = P.tiles; k0 = P.k0; lo = P.lo; hi = P.hi;
-        }
-        if (!wait(b_full + 8 * kslot, par)) break;
-        --left;
-        k0 += AT_KEYS;
-        tm_fence_after();
-        const uint64_t q = uniform64(smem_desc(q_base + l * TS::TILE + q_slot * q_step, 16)), k = uniform64(smem_desc(ring + kslot * TS::TILE, 16));
-        if (leader) {
+            for (int k = 0; k < AT_KEYS / 16; ++k)
+              tm_mma_ss(t_o, va + k * (2048 >> 4), p + (((k / 4) * TS::P_HALF + (k % 4) * 32) >> 4), id, !(vfresh && k == 0));
+          } else {
 #pragma unroll
-          for (int c = 0; c < D / 16; ++c) {
-            const uint32_t off = ((c / 4) * TS::HALF + (c % 4) * 32) >> 4;
-            tm_mma_ss(t_s, q + off, k + off, ID_S, c > 0);
+            for (int k = 0; k < AT_KEYS / 16; ++k) tm_mma_ts(t_o, t_s + k * 8, v + k * (2048 >> 4), ID_O, !(vfresh && k == 0));
           }
-          tm_commit(b_s + 8 * l);
-          tm_commit(b_empty + 8 * kslot);
-          if (!kpair) tm_commit(b_empty + 8 * kslot);
-          if (left == 0) tm_commit(b_qempty + 32 * l + 8 * q_slot);
+          tm_commit(b_o + 8 * l);
+          tm_commit(b_empty + 8 * slot);
+          if (!vpair) tm_commit(b_empty + 8 * slot);
         }
         __syncwarp();
-      }
-      if (leader) mb_arrive(b_turn + 8 * (1 - l));
+        return true;
+      };
+      // (the first piece of a lane, and one behind a wide piece, has its products in the wide order)
+      const bool scores_first = r > 0 && vnarrow && r < cnt;
+      bool good = true;
+      if (scores_first) good = scores();
+      if (good && r > 0) good = outputs();
+      if (r == 0 && l == 1 && n_pair > 0 && good) good = wait(b_turn + 8, 0);
+      if (good && r < cnt && !scores_first) good = scores();
+      if (!good) break;
+      vk0 = k0; vlo = lo; vhi = hi; vnarrow = narrow; vfresh = kfresh;
+      k0 += AT_KEYS;
+      if (r <= n_pair && leader) mb_arrive(b_turn + 8 * (1 - l));
       st += v0 + f0 + v1 + f1;
       if (st >= NST) { st -= NST; st_par ^= 1; }
     }
   } else {
-    // ---- softmax: one thread per row
-    const int l = warp >> 2, row = (warp & 3) * 32 + lane_id;
+    // ---- softmax.  A wait that gives up does not change the way of a warp through a piece (its four warps meet at barriers);
+    // they all leave before the next one.
+    const int l = warp >> 2, quad = warp & 3, row = quad * 32 + lane_id;
     const int cnt = l ? cnt1 : cnt0;
-    const uint32_t t_s = tmem + ((warp & 3) << 21) + l * AT_KEYS, t_o = tmem + ((warp & 3) << 21) + 256 + l * D;
+    const uint32_t t_s = tmem + (quad << 21) + l * AT_KEYS, t_o = tmem + (quad << 21) + 256 + l * D;
     Slots Q(S.batch_pieces[l], q_slots, 0);
     const float scale = A.scale_log2;
-    for (int n = 0; ok && n < cnt;) {
-      const uint32_t slot = Q.slot;
-      if (!wait(b_qfull + 32 * l + 8 * slot, Q.parity())) break;
-      Q.next();
-      const Piece P = s_piece[l][slot];
+    const int worker = blockIdx.x * 2 + l;
+    int n = 0;
+    auto arrive_p = [&]() {
+      tm_fence_before();
       __syncwarp();
-      if (lane_id == 0) mb_arrive(b_qempty + 32 * l + 8 * slot);
-      const int tr = row / A.group;
-      const bool live = tr < P.ntok, warp_live = __any_sync(0xffffffffu, live);
-      int lo = P.k0, hi = 0x7fffffff;  // keys this row sees
-      if (live) {
-        const int t = P.tok + tr, b = t / A.q_len;
-        // (an own unit's last key is its sequence's last)
-        hi = max((P.kind == AT_OWN ? P.hi : attend_len(A, b, false)) - A.q_len + (t - b * A.q_len) + 1, 0);
-        lo = A.window > 0 ? max(hi - A.window, 0) : 0;
-        if (P.kind == AT_OWN) lo = max(lo, A.prefix);
-        else hi = min(hi, A.prefix);
+      if (lane_id == 0) mb_arrive(b_p + 8 * l);
+    };
+    // Keys [lo, hi) that row x of a piece sees, relative to the piece's first.
+    auto row_keys = [&](const Piece& P, int x, int& lo, int& hi) {
+      const int tr = x / A.group, t = P.tok + tr, b = t / A.q_len;
+      // (an own unit's last key is its sequence's last)
+      hi = max((P.kind == AT_OWN ? P.hi : attend_len(A, b, false)) - A.q_len + (t - b * A.q_len) + 1, 0);
+      lo = A.window > 0 ? max(hi - A.window, 0) : 0;
+      if (P.kind == AT_OWN) lo = max(lo, A.prefix);
+      else hi = min(hi, A.prefix);
+      lo -= P.k0; hi -= P.k0;
+    };
+    // Where row 0 of a piece goes in the workspace; one thread notes which workers hold a unit.
+    auto place_piece = [&](const Piece& P, float*& po, float*& pl) -> long long {
+      if (P.kind == AT_OWN) {
+        po = T.own_o; pl = T.own_lse;
+        if (row == 0 && (P.ends & 1)) T.own_first[P.unit] = worker;
+        if (row == 0 && (P.ends & 2)) T.own_last[P.unit] = worker;
+        return (long long)(P.unit + worker) * (T.ts * A.group);
       }
-      lo -= P.k0; hi -= P.k0;  // from here on relative to the tile
+      const bool pair = P.kind == AT_PAIR;
+      const int wk = pair ? blockIdx.x : worker;
+      po = T.pre_o; pl = T.pre_lse;
+      const bool mark = row == 0 && !(pair && l == 1);
+      if (mark && (P.ends & 1)) T.pre_first[P.unit] = wk;
+      if (mark && (P.ends & 2)) T.pre_last[P.unit] = wk;
+      return (pair ? (P.unit + wk) * 2LL + l : (long long)(P.unit + wk)) * 128;
+    };
+
+    // Narrow pieces: at most 32 rows.  The product is turned round, S^T = K Q^T: a thread has one key and the scores of all
+    // rows, so that the few exponentials are spread over all 128 threads.  Weights go to shared memory as P^T's other operand.
+    // The reference of a row is kept as its negative in the exponent, `off`; 3e38 stands for a row that has seen nothing, so that
+    // its first score exceeds the reference too.  The rows' sums stay apart, by key, until the end of the piece.
+    auto narrow_piece = [&](const Piece& P, auto nr) {
+      constexpr int NR = decltype(nr)::value;
+      const int rows = P.ntok * A.group;
+      const uint32_t p_base = q_base + l * TS::TILE + TS::P_AT + (quad >> 1) * TS::P_HALF;  // this thread's half of the keys
+      const uint32_t p_chunk = (uint32_t)(row & 63) >> 3, p_byte = (row & 7) * 2;
+      int my_lo = -0x7fffffff, my_hi = 0x7fffffff;
+      if (lane_id < rows) { my_lo = C.lo[l][lane_id]; my_hi = C.hi[l][lane_id]; }
+      int all_lo = __reduce_max_sync(0xffffffffu, my_lo), all_hi = __reduce_min_sync(0xffffffffu, my_hi);  // what every row sees
+      float off[NR], sum[NR];
+#pragma unroll
+      for (int x = 0; x < NR; ++x) { off[x] = 3e38f; sum[x] = 0.f; }
+      for (int j = 0; j < P.tiles; ++j, ++n, all_lo -= AT_KEYS, all_hi -= AT_KEYS) {
+        wait(b_s + 16 * l + 8 * (n & 1), (n >> 1) & 1);
+        if (n > 0) wait(b_o + 8 * l, (n - 1) & 1);  // (its weights are done with)
+        tm_fence_after();
+        uint32_t s[NR];
+        if (NR == 16) tm_ld16(t_s + (n & 1) * 32, s);
+        else tm_ld32(t_s + (n & 1) * 32, s);
+        tm_wait_ld();
+        if (NR == 16) tm_pin16(s);
+        else tm_pin32(s);
+        if (all_lo > 0 || all_hi < AT_KEYS) {
+          const int key = j * AT_KEYS + row;
+#pragma unroll
+          for (int x = 0; x < NR; ++x)
+            if (x < rows && (key < C.lo[l][x] || key >= C.hi[l][x])) s[x] = 0xff800000u;
+        }
+        bool rise = false;
+#pragma unroll
+        for (int x = 0; x < NR; ++x)
+          if (x < rows) rise |= fmaf(__uint_as_float(s[x]), scale, off[x]) > 8.f;
+        if (group_any(1 + l, 128, rise)) {
+#pragma unroll
+          for (int x = 0; x < NR; ++x)
+            if (x < rows) {
+              const float v = warp_max(__uint_as_float(s[x]));
+              if (lane_id == x) C.red[l][quad][x] = v;
+            }
+          group_sync(1 + l, 128);
+#pragma unroll
+          for (int x = 0; x < NR; ++x)
+            if (x < rows) {
+              const float top = fmaxf(fmaxf(C.red[l][0][x], C.red[l][1][x]), fmaxf(C.red[l][2][x], C.red[l][3][x])) * scale;
+              if (top + off[x] > 8.f) {
+                const float f = ex2(-top - off[x]);
+                sum[x] *= f;
+                off[x] = -top;
+                if (j > 0) {
+                  uint32_t o;
+                  tm_ld1(t_o + x, &o);
+                  tm_wait_ld();
+                  tm_pin1(&o);
+                  o = __float_as_uint(__uint_as_float(o) * f);
+                  tm_st1(t_o + x, &o);
+                }
+              }
+            }
+          tm_wait_st();
+        }
+#pragma unroll
+        for (int x = 0; x < NR; ++x)
+          if (x < rows) {
+            const float p = ex2(fmaf(__uint_as_float(s[x]), scale, off[x]));
+            sum[x] += p;
+            asm volatile("st.shared.b16 [%0], %1;" ::"r"(p_base + x * 128 + ((p_chunk ^ (x & 7)) << 4) + p_byte), "h"(narrow16<WD>(p)) : "memory");
+          }
+        fence_async_shared();
+        arrive_p();
+      }
+      wait(b_o + 8 * l, (n - 1) & 1);
+      tm_fence_after();
+      float my_sum = 0.f, my_off = 0.f;
+#pragma unroll
+      for (int x = 0; x < NR; ++x)
+        if (x < rows) {
+          const float v = warp_sum(sum[x]);
+          if (lane_id == x) { C.red[l][quad][x] = v; my_off = off[x]; }
+        }
+      group_sync(1 + l, 128);
+      if (lane_id < rows) my_sum = (C.red[l][0][lane_id] + C.red[l][1][lane_id]) + (C.red[l][2][lane_id] + C.red[l][3][lane_id]);
+      const float inv = my_sum == 0.f ? 0.f : 1.f / my_sum;
+      float *po, *pl;
+      const long long at = place_piece(P, po, pl);
+      if (quad == 0 && lane_id < rows) pl[at + lane_id] = my_sum == 0.f ? -INFINITY : log2f(my_sum) - my_off;
+      uint32_t o[NR];
+      if (NR == 16) tm_ld16(t_o, o);
+      else tm_ld32(t_o, o);
+      tm_wait_ld();
+      if (NR == 16) tm_pin16(o);
+      else tm_pin32(o);
+#pragma unroll
+      for (int x = 0; x < NR; ++x)
+        if (x < rows) {
+          const float f = __shfl_sync(0xffffffffu, inv, x);
+          if (row < D) po[(at + x) * D + row] = __uint_as_float(o[x]) * f;
+        }
+      tm_fence_before();
+    };
+
+    while (n < cnt) {
+      const uint32_t slot = Q.slot;
+      bool good = wait(b_qfull + 32 * l + 8 * slot, Q.parity()) && !C.dead;
+      Q.next();
+      const Piece P = C.piece[l][slot];
+      if (good && P.narrow && row < P.ntok * A.group) {
+        int a, b;
+        row_keys(P, row, a, b);
+        C.lo[l][row] = a;
+        C.hi[l][row] = b;
+      }
+      if (group_any(1 + l, 128, !good)) break;
+      if (lane_id == 0) mb_arrive(b_qempty + 32 * l + 8 * slot);
+      if (P.narrow == 16) { narrow_piece(P, std::integral_constant<int, 16>{}); continue; }
+      if (P.narrow == 32) { narrow_piece(P, std::integral_constant<int, 32>{}); continue; }
+      // Wide pieces: one thread per row.
+      const bool live = row / A.group < P.ntok, warp_live = __any_sync(0xffffffffu, live);
+      int lo = 0, hi = 0x7fffffff;  // keys this row sees, relative to the tile
+      if (live) row_keys(P, row, lo, hi);
       float m = -INFINITY, sum = 0.f;
       for (int j = 0; j < P.tiles; ++j, ++n, lo -= AT_KEYS, hi -= AT_KEYS) {
-        ok = wait(b_s + 8 * l, n & 1);
-        if (!ok) break;
+        wait(b_s + 16 * l + 8 * (n & 1), (n >> 1) & 1);
         tm_fence_after();
         if (warp_live) {
           // Two passes over the scores: the maximum (all four quarters of the columns), then the weights.  The quarters 0 and 1 stay in
@@ -540,8 +750,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
             const float f = rise ? ex2((m - top) * scale) : 1.f;
             if (rise) { m = top; sum *= f; }
             if (j > 0) {
-              ok = wait(b_o + 8 * l, (n - 1) & 1);
-              if (!ok) break;
+              wait(b_o + 8 * l, (n - 1) & 1);
               tm_fence_after();
 #pragma unroll
               for (int c = 0; c < D / 32; ++c) {
@@ -582,35 +791,16 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
           sum += lo32(acc_all) + hi32(acc_all);
           tm_wait_st();
         }
-        tm_fence_before();
-        __syncwarp();
-        if (lane_id == 0) mb_arrive(b_p + 8 * l);
+        arrive_p();
       }
-      if (!ok) break;
       // the piece is done: its output and lse go to the workspace
-      ok = wait(b_o + 8 * l, (n - 1) & 1);
-      if (!ok) break;
+      wait(b_o + 8 * l, (n - 1) & 1);
       tm_fence_after();
-      const int worker = blockIdx.x * 2 + l;
-      long long slot_row;
       float *po, *pl;
-      if (P.kind == AT_OWN) {
-        slot_row = (long long)(P.unit + worker) * (T.ts * A.group) + row;
-        po = T.own_o; pl = T.own_lse;
-        if (row == 0 && (P.ends & 1)) T.own_first[P.unit] = worker;
-        if (row == 0 && (P.ends & 2)) T.own_last[P.unit] = worker;
-      } else {
-        const bool pair = P.kind == AT_PAIR;
-        const int wk = pair ? blockIdx.x : worker;
-        slot_row = (pair ? (P.unit + wk) * 2LL + l : (long long)(P.unit + wk)) * 128 + row;
-        po = T.pre_o; pl = T.pre_lse;
-        const bool mark = row == 0 && !(pair && l == 1);
-        if (mark && (P.ends & 1)) T.pre_first[P.unit] = wk;
-        if (mark && (P.ends & 2)) T.pre_last[P.unit] = wk;
-      }
+      const long long at = place_piece(P, po, pl) + row;
       if (warp_live) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        if (live) pl[slot_row] = sum == 0.f ? -INFINITY : fmaf(m, scale, log2f(sum));
+        if (live) pl[at] = sum == 0.f ? -INFINITY : fmaf(m, scale, log2f(sum));
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
           uint32_t o[32];
@@ -618,7 +808,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
           tm_wait_ld();
           tm_pin32(o);
           if (live) {
-            float4* dst = reinterpret_cast<float4*>(po + slot_row * D + 32 * c);
+            float4* dst = reinterpret_cast<float4*>(po + at * D + 32 * c);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
               dst[e] = make_float4(__uint_as_float(o[4 * e]) * inv, __uint_as_float(o[4 * e + 1]) * inv, __uint_as_float(o[4 * e + 2]) * inv,
@@ -631,7 +821,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
   }
   if (blockIdx.x == 0 && tid == 0) *T.plan = S.pre_tiles;
   __syncthreads();
-  if (s_dead) {  // copies and products that are still in flight get time to land before the CTA's memory goes
+  if (C.dead) {  // copies and products that are still in flight get time to land before the CTA's memory goes
     const long long t0 = clock64();
     while (clock64() - t0 < AT_SPIN_CLOCKS / 1000) {}
     __syncthreads();
@@ -640,14 +830,16 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
   if (warp == 9) tm_free(tmem, 512);
 }
 
-// ---- joins the pieces of every row in their order: one warp per row ---------------------------------------------------------
-template <int WD, int D>
+// ---- joins the pieces of every row in their order: WARPS warps per row take turns at its pieces ------------------------------
+// (one warp where rows are many and have a few pieces each; eight where rows are few and may be cut into a hundred)
+template <int WD, int D, int WARPS>
 __global__ void __launch_bounds__(256) ls_attend_tile_join_kernel(const TileArgs T) {
   const AttendArgs& A = T.a;
   const long long rows = (long long)A.n_seqs * A.q_len * A.heads;
-  const long long row = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (row >= rows) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % WARPS;
+  const long long row = (long long)blockIdx.x * (8 / WARPS) + warp / WARPS;
+  __shared__ float s_acc[WARPS > 1 ? 8 : 1][D + 1];
+  if (row >= rows) return;  // (a block of its own row when WARPS is 8: all of it returns)
   const int t = (int)(row / A.heads), hd = (int)(row - (long long)t * A.heads), h = hd / A.group, g = hd - h * A.group;
   const int b = t / A.q_len, i = t - b * A.q_len;
   const bool own = own_keys(T, attend_len(A, b, false)).tiles > 0;
@@ -690,27 +882,41 @@ __global__ void __launch_bounds__(256) ls_attend_tile_join_kernel(const TileArgs
     const float e = p0 + lane < n ? lse_of(p0 + lane) : -INFINITY;
     const float wl = e == -INFINITY ? 0.f : ex2(e - top);
     tot += warp_sum(wl);
-    for (int j = 0; j < min(32, n - p0); ++j) {
+    const int m = min(32, n - p0);
+#pragma unroll 4
+    for (int j = part; j < m; j += WARPS) {
       const float w = __shfl_sync(0xffffffffu, wl, j);
-      if (w == 0.f) continue;
       const int p = p0 + j;
       const float* src = (p < n_pre ? T.pre_o + (pre_at + p * pre_step) * D : T.own_o + (own_at + (p - n_pre) * own_step) * D) + lane * E;
       float o[E];
       if (E == 4) *reinterpret_cast<float4*>(o) = *reinterpret_cast<const float4*>(src);
       else *reinterpret_cast<float2*>(o) = *reinterpret_cast<const float2*>(src);
 #pragma unroll
-      for (int c = 0; c < E; ++c) acc[c] = fmaf(w, o[c], acc[c]);
+      for (int c = 0; c < E; ++c) acc[c] = w == 0.f ? acc[c] : fmaf(w, o[c], acc[c]);  // (a piece that saw nothing has no output)
     }
   }
   const float inv = tot == 0.f ? 0.f : 1.f / tot;
-  uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(A.out) + t * A.out_stride + (long long)hd * D + lane * E);
+  uint16_t* dst = static_cast<uint16_t*>(A.out) + t * A.out_stride + (long long)hd * D;
+  if (lane == 0 && part == 0 && A.lse) A.lse[row] = tot == 0.f ? -INFINITY : (top + log2f(tot)) * LN2;
+  if (WARPS > 1) {
+#pragma unroll
+    for (int c = 0; c < E; ++c) s_acc[warp][lane * E + c] = acc[c];
+    __syncthreads();
+    const int c = threadIdx.x;
+    if (c < D) {
+      float o = 0.f;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) o += s_acc[w][c];
+      dst[c] = narrow16<WD>(o * inv);
+    }
+    return;
+  }
 #pragma unroll
   for (int c = 0; c < E; c += 2) {
     const uint32_t v = pack2<WD>(acc[c] * inv, acc[c + 1] * inv);
-    if ((A.out_stride & 1) == 0 && (reinterpret_cast<uintptr_t>(A.out) & 3) == 0) dst[c / 2] = v;
-    else { reinterpret_cast<uint16_t*>(dst)[c] = (uint16_t)v; reinterpret_cast<uint16_t*>(dst)[c + 1] = (uint16_t)(v >> 16); }
+    if ((A.out_stride & 1) == 0 && (reinterpret_cast<uintptr_t>(A.out) & 3) == 0) reinterpret_cast<uint32_t*>(dst + lane * E)[c / 2] = v;
+    else { dst[lane * E + c] = (uint16_t)v; dst[lane * E + c + 1] = (uint16_t)(v >> 16); }
   }
-  if (lane == 0 && A.lse) A.lse[row] = tot == 0.f ? -INFINITY : (top + log2f(tot)) * LN2;
 }
 
 }  // namespace ls
