@@ -146,6 +146,7 @@ int32_t attend_tiles(ls_paged_kv* kv, const ls::AttendArgs& a, cudaStream_t st) 
   t.pre_first = kv->tile_ids; t.pre_last = t.pre_first + kv->pre_units;
   t.own_first = t.pre_last + kv->pre_units; t.own_last = t.own_first + kv->own_units;
   t.plan = t.own_last + kv->own_units;
+  t.workers = 2 * kv->sm_count;
   CUtensorMap q_all, q_own;
   const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)a.heads, (cuuint64_t)a.n_seqs * a.q_len};
   const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)a.q_stride * 2};

@@ -60,6 +60,7 @@ struct TileArgs {
   float *own_o, *own_lse;  // slots of own units ([ts * group] rows)
   int32_t *pre_first, *pre_last, *own_first, *own_last;  // per unit: the worker of its first and last piece
   int32_t* plan;     // [1] key tiles of the prefix
+  int32_t workers;   // two per CTA
 };
 
 // The keys of sequence b that are its own: [lo, hi) is what any of its tokens sees, tiles start at `origin`.
@@ -248,7 +249,7 @@ __device__ __forceinline__ void make_share(const TileArgs& T, Share& S, int* s_s
 // Control block of a CTA, behind the tiles in shared memory.
 template <int NST>
 struct TileCtl {
-  unsigned long long full[NST], empty[NST], qfull[2][4], qempty[2][4], s[2][2], p[2], o[2], turn[2];
+  unsigned long long full[2][NST], empty[NST], qfull[2][4], qempty[2][4], s[2][2], p[2], o[2], turn[2], done[2];
   Share share;
   int scan[2 * AT_THREADS / 32];
   Piece piece[2][4];
@@ -272,17 +273,18 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
   const int tid = threadIdx.x, lane_id = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const uint32_t q_base = saddr(dyn), ring = q_base + 2 * TS::TILE;
   const uint32_t b_full = saddr(C.full), b_empty = saddr(C.empty), b_qfull = saddr(C.qfull), b_qempty = saddr(C.qempty), b_s = saddr(C.s),
-                 b_p = saddr(C.p), b_o = saddr(C.o), b_turn = saddr(C.turn);
+                 b_p = saddr(C.p), b_o = saddr(C.o), b_turn = saddr(C.turn), b_done = saddr(C.done);
   if (q_base & 1023) {  // (swizzled tiles need it; the first byte of a block's shared memory has it)
     if (tid == 0) set_status(A.status, ST_INTERNAL);
     return;
   }
 
   if (warp == 0) {
-    if (lane_id < NST) { mb_init(b_full + 8 * lane_id, 1); mb_init(b_empty + 8 * lane_id, 2); }
+    if (lane_id < 2 * NST) mb_init(b_full + 8 * lane_id, 1);
+    if (lane_id < NST) mb_init(b_empty + 8 * lane_id, 2);
     if (lane_id < 8) { mb_init(b_qfull + 8 * lane_id, 1); mb_init(b_qempty + 8 * lane_id, 5); }
     if (lane_id < 4) mb_init(b_s + 8 * lane_id, 1);
-    if (lane_id < 2) { mb_init(b_p + 8 * lane_id, 4); mb_init(b_o + 8 * lane_id, 1); mb_init(b_turn + 8 * lane_id, 1); }
+    if (lane_id < 2) { mb_init(b_p + 8 * lane_id, 4); mb_init(b_o + 8 * lane_id, 1); mb_init(b_turn + 8 * lane_id, 1); mb_init(b_done + 8 * lane_id, 1); }
     if (lane_id == 0) C.dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_shared();
@@ -332,6 +334,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
   bool ok = true;
   if (warp == 8) {
     // ---- copies.  Order of the ring: for every round r and lane: values of round r - 1, keys of round r; a pair's once.
+    // A lane's tiles have barriers of their own (a place of the ring is filled now for one lane, now for the other; a lane that
+    // watched both kinds of fills could be two behind and take an old one for its own); a pair's are those of lane 0.
     // Page numbers come 32 boxes at a time, one to each thread, a batch ahead: the next batch of the piece, or the first of the
     // next piece (so the walk is a piece ahead).
     Walk W[2];
@@ -346,17 +350,17 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     const bool page_pow2 = (A.page & (A.page - 1)) == 0;
     const int page_shift = 31 - __clz(A.page);
     auto page_index = [&](int key) { return page_pow2 ? key >> page_shift : key / A.page; };
-    auto load_tile = [&](const CUtensorMap* map, int k0, int lo, int hi, int h, int pg) {
+    auto load_tile = [&](const CUtensorMap* map, uint32_t full, int k0, int lo, int hi, int h, int pg) {
       const int key = k0 + my_box * T.box;
       const bool on = my_half < D / 64 && key < hi && key + T.box > lo;
       const int count = __popc(__ballot_sync(0xffffffffu, on));
       if (on && (uint32_t)pg >= (uint32_t)A.n_pages) { set_status(A.status, ST_BAD_INDEX); pg = A.n_pages; }  // (reads as zeros)
       ok = wait(b_empty + 8 * st, st_par);
       if (!ok) return;
-      if (lane_id == 0) mb_expect(b_full + 8 * st, count * T.box * 128);
+      if (lane_id == 0) mb_expect(full + 8 * st, count * T.box * 128);
       __syncwarp();
       if (on)
-        tma_load4(ring + st * TS::TILE + my_half * TS::HALF + my_box * T.box * 128, map, my_half * 64, key - page_index(key) * A.page, h, pg, b_full + 8 * st);
+        tma_load4(ring + st * TS::TILE + my_half * TS::HALF + my_box * T.box * 128, map, my_half * 64, key - page_index(key) * A.page, h, pg, full + 8 * st);
       if (++st == NST) { st = 0; st_par ^= 1; }
     };
     auto fetch_pages = [&](const Piece& p, int key) {  // (no branch around the load: nothing waits for it here)
@@ -384,7 +388,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     };
     auto step = [&](auto lc, int r, int cnt) {
       constexpr int l = decltype(lc)::value;
-      if (r > 0 && r <= cnt && !(r <= n_pair && l == 1)) load_tile(&map_v, vk0[l], vlo[l], vhi[l], vh[l], vpage[l]);
+      if (r > 0 && r <= cnt && !(r <= n_pair && l == 1)) load_tile(&map_v, b_full + (r > n_pair ? 8 * NST * l : 0), vk0[l], vlo[l], vhi[l], vh[l], vpage[l]);
       if (!ok || r >= cnt) return;
       const bool own = P[l].kind == AT_OWN;
       if (fresh[l]) {
@@ -405,7 +409,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       if (!(r < n_pair && l == 1)) {
         const int page = __shfl_sync(0xffffffffu, pages[l], ((P[l].k0 - batch[l]) >> box_shift) + my_box);
         vk0[l] = P[l].k0; vlo[l] = P[l].lo; vhi[l] = P[l].hi; vh[l] = P[l].h; vpage[l] = page;
-        load_tile(&map_k, P[l].k0, P[l].lo, P[l].hi, P[l].h, page);
+        load_tile(&map_k, b_full + (r >= n_pair ? 8 * NST * l : 0), P[l].k0, P[l].lo, P[l].hi, P[l].h, page);
       }
       if (ok) advance(lc);
     };
@@ -431,7 +435,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     // its softmax (products of both lanes mixed would end at the same time, and the two softmaxes share the same cycles).
     // Narrow tiles: S^T = K Q^T of round r first (two buffers of scores), then O^T += V^T P^T of round r - 1.
     // The warp clears value rows that are nobody's (whatever the page holds there, its weight of zero must not meet an infinity;
-    // in a pair both lanes clear, the same).  A tile's two arrivals on `empty` come from the pair's two lanes, or twice from one.
+    // in a pair both lanes clear, the same).  A tile's two arrivals on `empty` are the commits of the pair's two lanes, or the
+    // commit of the one lane that reads it and an arrival of its own in place of the other.
     constexpr int TYPE = WD == WD_BF16;
     constexpr uint32_t ID_S = mma_idesc(TYPE, 128, AT_KEYS, false, false), ID_O = mma_idesc(TYPE, 128, D, false, true);
     const int l = warp - 9;
@@ -442,20 +447,24 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     int left = 0, k0 = 0, lo = 0, hi = 0;   // of the current piece: tiles to come, first key of the next; keys of anybody
     int narrow = 0, vk0 = 0, vlo = 0, vhi = 0, vnarrow = 0;  // v*: of the tile whose values are still to be multiplied
     bool vfresh = true;
-    uint32_t q_slot = 0, st = 0, st_par = 0;
+    uint32_t q_slot = 0, st = 0, par0 = 0, par1 = 0;  // par*: parity of each place's next fill, by set of barriers
     for (int r = 0; r <= cnt; ++r) {
       // places in the ring: values and keys of lane 0, then of lane 1 where they are not a pair's
       const bool vpair = r <= n_pair, kpair = r < n_pair;
       const uint32_t v0 = r > 0 && r <= cnt0, f0 = r < cnt0, v1 = r > 0 && r <= cnt1 && !vpair, f1 = r < cnt1 && !kpair;
-      auto place = [&](uint32_t ahead, uint32_t& slot, uint32_t& par) {
-        slot = st + ahead;
-        par = st_par;
-        if (slot >= NST) { slot -= NST; par ^= 1; }
+      auto filled = [&](uint32_t slot, bool pair) -> bool {
+        const bool set0 = pair || l == 0;
+        const uint32_t par = set0 ? par0 : par1;
+        if (set0) par0 ^= 1u << slot;
+        else par1 ^= 1u << slot;
+        if (!wait(b_full + 8 * (set0 ? slot : NST + slot), (par >> slot) & 1)) return false;
+        if (!pair && leader) mb_arrive(b_empty + 8 * slot);
+        return true;
       };
       bool kfresh = false;
       auto scores = [&]() -> bool {
-        uint32_t slot, par;
-        place(kpair ? v0 : l == 0 ? v0 : v0 + f0 + v1, slot, par);
+        uint32_t slot = st + (kpair || l == 0 ? v0 : v0 + f0 + v1);
+        if (slot >= NST) slot -= NST;
         kfresh = left == 0;
         if (kfresh) {
           q_slot = Q.slot;
@@ -464,7 +473,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
           const Piece& P = C.piece[l][q_slot];
           left = P.tiles; k0 = P.k0; lo = P.lo; hi = P.hi; narrow = P.narrow;
         }
-        if (!wait(b_full + 8 * slot, par)) return false;
+        if (!filled(slot, kpair)) return false;
         --left;
         tm_fence_after();
         const uint64_t q = uniform64(smem_desc(q_base + l * TS::TILE + q_slot * q_step, 16)), k = uniform64(smem_desc(ring + slot * TS::TILE, 16));
@@ -485,16 +494,15 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
           }
           tm_commit(b_s + 16 * l + 8 * (r & 1));
           tm_commit(b_empty + 8 * slot);
-          if (!kpair) tm_commit(b_empty + 8 * slot);
           if (left == 0) tm_commit(b_qempty + 32 * l + 8 * q_slot);
         }
         __syncwarp();
         return true;
       };
       auto outputs = [&]() -> bool {
-        uint32_t slot, par;
-        place(l == 0 || vpair ? 0 : v0 + f0, slot, par);
-        if (!wait(b_full + 8 * slot, par)) return false;
+        uint32_t slot = st + (l == 0 || vpair ? 0 : v0 + f0);
+        if (slot >= NST) slot -= NST;
+        if (!filled(slot, vpair)) return false;
         if (vk0 < vlo || vk0 + AT_KEYS > vhi) {
           for (int c = lane_id; c < AT_KEYS; c += 32) {
             if (vk0 + c >= vlo && vk0 + c < vhi) continue;
@@ -524,7 +532,6 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
           }
           tm_commit(b_o + 8 * l);
           tm_commit(b_empty + 8 * slot);
-          if (!vpair) tm_commit(b_empty + 8 * slot);
         }
         __syncwarp();
         return true;
@@ -541,8 +548,11 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       k0 += AT_KEYS;
       if (r <= n_pair && leader) mb_arrive(b_turn + 8 * (1 - l));
       st += v0 + f0 + v1 + f1;
-      if (st >= NST) { st -= NST; st_par ^= 1; }
+      if (st >= NST) st -= NST;
     }
+    // every arrival that the tensor cores owe this block has come when the last one has
+    if (leader) tm_commit(b_done + 8 * l);
+    wait(b_done + 8 * l, 0);
   } else {
     // ---- softmax.  A wait that gives up does not change the way of a warp through a piece (its four warps meet at barriers);
     // they all leave before the next one.
@@ -860,14 +870,20 @@ __global__ void __launch_bounds__(256) ls_attend_tile_join_kernel(const TileArgs
   asm volatile("griddepcontrol.wait;" ::: "memory");
   int n_pre = 0, n_own = 0;
   long long pre_at = 0, own_at = 0;
+  // (a kernel that gave up on a wait leaves workers unnoted: its rows are reported and come out as zeros)
+  auto pieces = [&](int first, int last) {
+    if (first >= 0 && first <= last && last < T.workers) return last - first + 1;
+    set_status(A.status, ST_INTERNAL);
+    return 0;
+  };
   if (*T.plan > 0) {
     const int first = T.pre_first[pre_unit];
-    n_pre = T.pre_last[pre_unit] - first + 1;
+    n_pre = pieces(first, T.pre_last[pre_unit]);
     pre_at = (pre_unit + first) * pre_step + pre_row;
   }
   if (own) {
     const int first = T.own_first[own_unit];
-    n_own = T.own_last[own_unit] - first + 1;
+    n_own = pieces(first, T.own_last[own_unit]);
     own_at = (own_unit + first) * own_step + own_row;
   }
   const int n = n_pre + n_own;
