@@ -35,15 +35,17 @@ def attend(q, k_pages, v_pages, seq_len, table, prefix_pages, prefix_len, window
             ids = np.where(shared, np.asarray(prefix_pages)[np.minimum(pos // ps, max(len(prefix_pages) - 1, 0))] if len(prefix_pages) else 0,
                            row[pos // ps])
             k, v = k_pages[ids, pos % ps], v_pages[ids, pos % ps]  # [keys, hk, D]
-            for h in range(H):
-                qh, kh, vh = q[b, i, h], k[:, h // G], v[:, h // G]
-                s = kh @ qh * scale
-                top = s.max()
+            for j in range(hk):
+                h = slice(j * G, (j + 1) * G)
+                qh, kh, vh = q[b, i, h], k[:, j], v[:, j]
+                s = qh @ kh.T * scale
+                top = s.max(1, keepdims=True)
                 e = np.exp(s - top)
-                w = e / e.sum()
+                total = e.sum(1, keepdims=True)
+                w = e / total
                 out[b, i, h], absout[b, i, h], absv[b, i, h] = w @ vh, w @ np.abs(vh), np.abs(vh).sum(0)
-                lse[b, i, h] = top + np.log(e.sum())
-                absqk[b, i, h] = (np.abs(kh) @ np.abs(qh)).max()
+                lse[b, i, h] = (top + np.log(total))[:, 0]
+                absqk[b, i, h] = (np.abs(qh) @ np.abs(kh).T).max(1)
     return out, lse, absout, absv, absqk
 
 

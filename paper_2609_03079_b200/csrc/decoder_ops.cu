@@ -44,11 +44,12 @@ void free_kv(ls_paged_kv* kv) {
 
 // How the rows of n_seqs sequences of q_len tokens are cut into tiles, and what workspace the cut needs.
 struct TileCut {
-  int tq, ts, rt, pairs;
+  int tq, tb, ts, rt, pairs;
   size_t pre_rows, own_rows, pre_units, own_units;
   TileCut(int n_seqs, int q_len, int kv_heads, int group, int ctas) {
     const long long tokens = (long long)n_seqs * q_len;
     tq = 128 / group;
+    tb = (int)std::min<long long>(tq, tokens);
     ts = std::min(tq, q_len);
     rt = (q_len + ts - 1) / ts;
     const long long tiles = (tokens + tq - 1) / tq;
@@ -140,7 +141,7 @@ int32_t attend_tiles(ls_paged_kv* kv, const ls::AttendArgs& a, cudaStream_t st) 
   const TileCut c(a.n_seqs, a.q_len, a.kv_heads, a.group, kv->sm_count);
   if (c.pre_rows > kv->pre_slots || c.own_rows > kv->own_slots || c.pre_units > kv->pre_units || c.own_units > kv->own_units)
     return fail(LS_ERR_INTERNAL, "ls_paged_kv_attend: workspace");
-  t.tq = c.tq; t.ts = c.ts; t.rt = c.rt; t.pairs = c.pairs; t.box = kv->box;
+  t.tq = c.tq; t.tb = c.tb; t.ts = c.ts; t.rt = c.rt; t.pairs = c.pairs; t.box = kv->box;
   t.pre_o = kv->tile_ws; t.own_o = t.pre_o + kv->pre_slots * D;
   t.pre_lse = t.own_o + kv->own_slots * D; t.own_lse = t.pre_lse + kv->pre_slots;
   t.pre_first = kv->tile_ids; t.pre_last = t.pre_first + kv->pre_units;
@@ -150,7 +151,7 @@ int32_t attend_tiles(ls_paged_kv* kv, const ls::AttendArgs& a, cudaStream_t st) 
   CUtensorMap q_all, q_own;
   const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)a.heads, (cuuint64_t)a.n_seqs * a.q_len};
   const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)a.q_stride * 2};
-  const cuuint32_t box_all[3] = {64, (cuuint32_t)a.group, (cuuint32_t)c.tq}, box_own[3] = {64, (cuuint32_t)a.group, (cuuint32_t)c.ts};
+  const cuuint32_t box_all[3] = {64, (cuuint32_t)a.group, (cuuint32_t)c.tb}, box_own[3] = {64, (cuuint32_t)a.group, (cuuint32_t)c.ts};
   void* q = const_cast<void*>(a.q);
   LS_TRY(make_map(&q_own, WD == ls::WD_BF16 ? LS_WDTYPE_BF16 : LS_WDTYPE_FP16, q, 3, dims, strides, box_own));
   if (a.prefix > 0) LS_TRY(make_map(&q_all, WD == ls::WD_BF16 ? LS_WDTYPE_BF16 : LS_WDTYPE_FP16, q, 3, dims, strides, box_all));

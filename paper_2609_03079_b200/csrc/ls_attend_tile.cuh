@@ -52,7 +52,7 @@ struct TileShape {
 
 struct TileArgs {
   AttendArgs a;
-  int32_t tq;        // tokens of a row tile (of the whole batch)
+  int32_t tq, tb;    // tokens of a row tile of the whole batch; tokens a copy of it brings (fewer if the batch is smaller)
   int32_t ts, rt;    // tokens of a row tile of one sequence, row tiles of a sequence
   int32_t pairs;     // pairs of row tiles of the whole batch, 0: single
   int32_t box;       // keys per copy: the largest power of two that divides the page, at most 128
@@ -96,10 +96,10 @@ struct Piece {
   int kind, h, tok, ntok;    // key head, first token and number of tokens of the row tile
   int k0, tiles, lo, hi;     // first key, number of tiles; keys outside [lo, hi) are nobody's
   int unit, ends;            // number of the unit among its kind; bit 0: holds its first tile, bit 1: its last
-  int narrow;                // rows of a narrow piece, padded (16 or 32), 0: a wide one
+  int narrow;                // at most AT_NARROW rows
 };
 
-__device__ __forceinline__ int narrow_rows(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : 0; }
+constexpr int AT_NARROW = 16;
 
 // Walks one lane's line piece by piece.
 struct Walk {
@@ -140,7 +140,7 @@ __device__ __forceinline__ bool walk_next(const TileArgs& T, const Share& S, int
       P.tok = ((P.unit - P.h * T.pairs) * 2 + lane) * T.tq;
     } else {
       P.kind = AT_SINGLE;
-      P.narrow = narrow_rows(A.n_seqs * A.q_len * A.group);
+      P.narrow = A.n_seqs * A.q_len * A.group <= AT_NARROW;
       P.h = P.unit;
       P.tok = 0;
       if ((P.ends & 2) && P.unit == A.kv_heads - 1) { W.b = 0; W.u = 0; W.tile = 0; }
@@ -156,7 +156,7 @@ __device__ __forceinline__ bool walk_next(const TileArgs& T, const Share& S, int
     }
     const int per = A.kv_heads * T.rt;
     P.kind = AT_OWN;
-    P.narrow = narrow_rows(T.ts * A.group);
+    P.narrow = T.ts * A.group <= AT_NARROW;
     P.tiles = min(W.tiles - W.tile, W.end - W.w);
     P.unit = W.b * per + W.u;
     P.h = T.rt == 1 ? W.u : W.u / T.rt;
@@ -253,8 +253,8 @@ struct TileCtl {
   Share share;
   int scan[2 * AT_THREADS / 32];
   Piece piece[2][4];
-  float red[2][4][32];        // narrow pieces: maxima or sums of each warp's keys
-  int lo[2][32], hi[2][32];   // ... keys of each row, relative to the piece's first
+  float red[2][4][AT_NARROW]; // narrow pieces: maxima or sums of each warp's keys
+  int lo[2][AT_NARROW], hi[2][AT_NARROW];  // ... keys of each row, relative to the piece's first
   uint32_t tmem;
   volatile int dead;
 };
@@ -317,8 +317,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
   // Query tiles: rows of the whole batch take a lane's whole buffer; a sequence's rows take a slot of it, so that the copies run
   // ahead by several pieces where these rows are few.  (A slot's product may read 128 rows: what lies behind is ignored.)
   // Piece i of a lane is in slot 0 if it is one of the first batch_pieces, else in slot (i - batch_pieces) % q_slots; the slot's
-  // barriers count the copy, and its release by the last product and by the four softmax warps.  A narrow piece's rows are at
-  // most 32; its weights are behind the slots.
+  // barriers count the copy, and its release by the last product and by the four softmax warps.  The weights of
+  // narrow pieces are behind the slots.
   const int q_rows = T.ts * A.group, q_slots = q_rows <= 32 ? TS::NARROW_SLOTS : q_rows <= 64 ? 2 : 1, q_step = q_rows <= 32 ? 32 * 128 : 64 * 128;
   struct Slots {
     int batch, n;
@@ -399,7 +399,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         if (lane_id == 0) {
           C.piece[l][slot] = P[l];
           const uint32_t full = b_qfull + 32 * l + 8 * slot;
-          mb_expect(full, (own ? T.ts : T.tq) * A.group * D * 2);
+          mb_expect(full, (own ? T.ts : T.tb) * A.group * D * 2);
 #pragma unroll
           for (int f = 0; f < D / 64; ++f)
             tma_load3(q_base + l * TS::TILE + f * TS::HALF + slot * q_step, own ? &map_q_own : &map_q_all, f * 64, P[l].h * A.group, P[l].tok, full);
@@ -439,10 +439,11 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     // commit of the one lane that reads it and an arrival of its own in place of the other.
     constexpr int TYPE = WD == WD_BF16;
     constexpr uint32_t ID_S = mma_idesc(TYPE, 128, AT_KEYS, false, false), ID_O = mma_idesc(TYPE, 128, D, false, true);
+    constexpr uint32_t ID_ST = mma_idesc(TYPE, 128, AT_NARROW, false, false), ID_OT = mma_idesc(TYPE, 128, AT_NARROW, true, false);
     const int l = warp - 9;
     const int cnt = l ? cnt1 : cnt0;
     const uint32_t t_s = __shfl_sync(0xffffffffu, tmem + l * AT_KEYS, 0), t_o = __shfl_sync(0xffffffffu, tmem + 256 + l * D, 0);
-    const bool leader = elect_one();
+    const uint64_t p_desc = uniform64(smem_desc(q_base + l * TS::TILE + TS::P_AT, 16));
     Slots Q(S.batch_pieces[l], q_slots, 0);
     int left = 0, k0 = 0, lo = 0, hi = 0;   // of the current piece: tiles to come, first key of the next; keys of anybody
     int narrow = 0, vk0 = 0, vlo = 0, vhi = 0, vnarrow = 0;  // v*: of the tile whose values are still to be multiplied
@@ -458,7 +459,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         if (set0) par0 ^= 1u << slot;
         else par1 ^= 1u << slot;
         if (!wait(b_full + 8 * (set0 ? slot : NST + slot), (par >> slot) & 1)) return false;
-        if (!pair && leader) mb_arrive(b_empty + 8 * slot);
+        if (!pair && elect_one()) mb_arrive(b_empty + 8 * slot);
         return true;
       };
       bool kfresh = false;
@@ -477,20 +478,13 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         --left;
         tm_fence_after();
         const uint64_t q = uniform64(smem_desc(q_base + l * TS::TILE + q_slot * q_step, 16)), k = uniform64(smem_desc(ring + slot * TS::TILE, 16));
-        if (leader) {
-          if (narrow) {
-            const uint32_t id = mma_idesc(TYPE, 128, narrow, false, false);
+        const uint64_t a = narrow ? k : q, b = narrow ? q : k;
+        const uint32_t id = narrow ? ID_ST : ID_S, d = narrow ? t_s + (r & 1) * 32 : t_s;
+        if (elect_one()) {
 #pragma unroll
-            for (int c = 0; c < D / 16; ++c) {
-              const uint32_t off = ((c / 4) * TS::HALF + (c % 4) * 32) >> 4;
-              tm_mma_ss(t_s + (r & 1) * 32, k + off, q + off, id, c > 0);
-            }
-          } else {
-#pragma unroll
-            for (int c = 0; c < D / 16; ++c) {
-              const uint32_t off = ((c / 4) * TS::HALF + (c % 4) * 32) >> 4;
-              tm_mma_ss(t_s, q + off, k + off, ID_S, c > 0);
-            }
+          for (int c = 0; c < D / 16; ++c) {
+            const uint32_t off = ((c / 4) * TS::HALF + (c % 4) * 32) >> 4;
+            tm_mma_ss(d, a + off, b + off, id, c > 0);
           }
           tm_commit(b_s + 16 * l + 8 * (r & 1));
           tm_commit(b_empty + 8 * slot);
@@ -517,15 +511,13 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         if (r <= n_pair && (l || r > 0) && !wait(b_turn + 8 * l, (l ? r : r - 1) & 1)) return false;
         tm_fence_after();
         const uint64_t v = uniform64(smem_desc(ring + slot * TS::TILE, TS::HALF));
-        const uint64_t p = uniform64(smem_desc(q_base + l * TS::TILE + TS::P_AT, 16));
-        if (leader) {
+        if (elect_one()) {
           if (vnarrow) {
             // (64 columns of values fill a 128-row product twice: both blocks of 64 are the same one)
             const uint64_t va = D == 128 ? v : v & ~((uint64_t)0x3fff << 16);
-            const uint32_t id = mma_idesc(TYPE, 128, vnarrow, true, false);
 #pragma unroll
             for (int k = 0; k < AT_KEYS / 16; ++k)
-              tm_mma_ss(t_o, va + k * (2048 >> 4), p + (((k / 4) * TS::P_HALF + (k % 4) * 32) >> 4), id, !(vfresh && k == 0));
+              tm_mma_ss(t_o, va + k * (2048 >> 4), p_desc + (((k / 4) * TS::P_HALF + (k % 4) * 32) >> 4), ID_OT, !(vfresh && k == 0));
           } else {
 #pragma unroll
             for (int k = 0; k < AT_KEYS / 16; ++k) tm_mma_ts(t_o, t_s + k * 8, v + k * (2048 >> 4), ID_O, !(vfresh && k == 0));
@@ -546,12 +538,12 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       if (!good) break;
       vk0 = k0; vlo = lo; vhi = hi; vnarrow = narrow; vfresh = kfresh;
       k0 += AT_KEYS;
-      if (r <= n_pair && leader) mb_arrive(b_turn + 8 * (1 - l));
+      if (r <= n_pair && elect_one()) mb_arrive(b_turn + 8 * (1 - l));
       st += v0 + f0 + v1 + f1;
       if (st >= NST) st -= NST;
     }
     // every arrival that the tensor cores owe this block has come when the last one has
-    if (leader) tm_commit(b_done + 8 * l);
+    if (elect_one()) tm_commit(b_done + 8 * l);
     wait(b_done + 8 * l, 0);
   } else {
     // ---- softmax.  A wait that gives up does not change the way of a warp through a piece (its four warps meet at barriers);
@@ -595,12 +587,12 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       return (pair ? (P.unit + wk) * 2LL + l : (long long)(P.unit + wk)) * 128;
     };
 
-    // Narrow pieces: at most 32 rows.  The product is turned round, S^T = K Q^T: a thread has one key and the scores of all
+    // Narrow pieces: at most 16 rows.  The product is turned round, S^T = K Q^T: a thread has one key and the scores of all
     // rows, so that the few exponentials are spread over all 128 threads.  Weights go to shared memory as P^T's other operand.
     // The reference of a row is kept as its negative in the exponent, `off`; 3e38 stands for a row that has seen nothing, so that
     // its first score exceeds the reference too.  The rows' sums stay apart, by key, until the end of the piece.
-    auto narrow_piece = [&](const Piece& P, auto nr) {
-      constexpr int NR = decltype(nr)::value;
+    auto narrow_piece = [&](const Piece& P) {
+      constexpr int NR = AT_NARROW;
       const int rows = P.ntok * A.group;
       const uint32_t p_base = q_base + l * TS::TILE + TS::P_AT + (quad >> 1) * TS::P_HALF;  // this thread's half of the keys
       const uint32_t p_chunk = (uint32_t)(row & 63) >> 3, p_byte = (row & 7) * 2;
@@ -615,11 +607,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         if (n > 0) wait(b_o + 8 * l, (n - 1) & 1);  // (its weights are done with)
         tm_fence_after();
         uint32_t s[NR];
-        if (NR == 16) tm_ld16(t_s + (n & 1) * 32, s);
-        else tm_ld32(t_s + (n & 1) * 32, s);
+        tm_ld16(t_s + (n & 1) * 32, s);
         tm_wait_ld();
-        if (NR == 16) tm_pin16(s);
-        else tm_pin32(s);
+        tm_pin16(s);
         if (all_lo > 0 || all_hi < AT_KEYS) {
           const int key = j * AT_KEYS + row;
 #pragma unroll
@@ -684,11 +674,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       const long long at = place_piece(P, po, pl);
       if (quad == 0 && lane_id < rows) pl[at + lane_id] = my_sum == 0.f ? -INFINITY : log2f(my_sum) - my_off;
       uint32_t o[NR];
-      if (NR == 16) tm_ld16(t_o, o);
-      else tm_ld32(t_o, o);
+      tm_ld16(t_o, o);
       tm_wait_ld();
-      if (NR == 16) tm_pin16(o);
-      else tm_pin32(o);
+      tm_pin16(o);
 #pragma unroll
       for (int x = 0; x < NR; ++x)
         if (x < rows) {
@@ -711,8 +699,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       }
       if (group_any(1 + l, 128, !good)) break;
       if (lane_id == 0) mb_arrive(b_qempty + 32 * l + 8 * slot);
-      if (P.narrow == 16) { narrow_piece(P, std::integral_constant<int, 16>{}); continue; }
-      if (P.narrow == 32) { narrow_piece(P, std::integral_constant<int, 32>{}); continue; }
+      if (P.narrow) { narrow_piece(P); continue; }
       // Wide pieces: one thread per row.
       const bool live = row / A.group < P.ntok, warp_live = __any_sync(0xffffffffu, live);
       int lo = 0, hi = 0x7fffffff;  // keys this row sees, relative to the tile
