@@ -81,7 +81,7 @@ struct Share {
   int pre_lo, pre_origin, pre_tiles;  // prefix keys that any token sees: [pre_lo, prefix)
   int pair0, pair1;                   // this CTA's (pair unit, tile) range
   int lane0[2], lane1[2];             // its lanes' ranges in the line of single and own units
-  int own_b[2], own_u[2], own_t[2];   // where a lane's range starts, if among the own units: sequence, unit within it, tile
+  int own_h[2], own_b[2], own_r[2], own_t[2];  // where a lane's range starts, if among the own units: head, sequence, row tile, tile
   OwnKeys own_k[2];                   // ... and that sequence's keys
   int batch_pieces[2];                // pieces of each lane that are not of own units (they come first)
 };
@@ -105,7 +105,8 @@ constexpr int AT_NARROW = 16;
 struct Walk {
   int w, end;             // position in the current part of the line
   bool pairs;             // still in the part of the pairs
-  int b, u, tile, tiles;  // next own unit (b = -1: still among the single ones), its next tile, its tiles (-1: to be looked up)
+  int h, b, r;            // next own unit (b = -1: still among the single ones): key head, sequence, row tile
+  int tile, tiles;        // its next tile, its tiles (-1: to be looked up)
   int lo, hi, origin;     // keys of the current sequence or of the prefix
 };
 
@@ -121,7 +122,7 @@ __device__ __forceinline__ bool walk_next(const TileArgs& T, const Share& S, int
   if (W.pairs && W.w == W.end) {
     W.pairs = false;
     W.w = S.lane0[lane]; W.end = S.lane1[lane];
-    W.b = S.own_b[lane]; W.u = S.own_u[lane]; W.tile = S.own_t[lane];
+    W.h = S.own_h[lane]; W.b = S.own_b[lane]; W.r = S.own_r[lane]; W.tile = S.own_t[lane];
     const OwnKeys k = S.own_k[lane];
     W.tiles = W.b < 0 ? -1 : k.tiles; W.lo = k.lo; W.hi = k.hi; W.origin = k.origin;
   }
@@ -143,31 +144,34 @@ __device__ __forceinline__ bool walk_next(const TileArgs& T, const Share& S, int
       P.narrow = A.n_seqs * A.q_len * A.group <= AT_NARROW;
       P.h = P.unit;
       P.tok = 0;
-      if ((P.ends & 2) && P.unit == A.kv_heads - 1) { W.b = 0; W.u = 0; W.tile = 0; }
+      if ((P.ends & 2) && P.unit == A.kv_heads - 1) { W.h = 0; W.b = 0; W.r = 0; W.tile = 0; }
     }
     P.ntok = min(T.tq, A.n_seqs * A.q_len - P.tok);
   } else {
     if (W.tiles < 0) {
-      for (;; ++W.b) {  // (sequences without keys of their own have no units; the line ends before the sequences do)
+      for (;;) {  // (sequences without keys of their own have no units; the line ends before the last head's sequences do)
         const OwnKeys k = own_keys(T, attend_len(A, W.b, false));
         W.tiles = k.tiles; W.lo = k.lo; W.hi = k.hi; W.origin = k.origin;
         if (k.tiles > 0) break;
+        if (++W.b == A.n_seqs) { W.b = 0; ++W.h; }
       }
     }
-    const int per = A.kv_heads * T.rt;
     P.kind = AT_OWN;
     P.narrow = T.ts * A.group <= AT_NARROW;
     P.tiles = min(W.tiles - W.tile, W.end - W.w);
-    P.unit = W.b * per + W.u;
-    P.h = T.rt == 1 ? W.u : W.u / T.rt;
-    const int rt = W.u - P.h * T.rt;
-    P.tok = W.b * A.q_len + rt * T.ts;
-    P.ntok = min(T.ts, A.q_len - rt * T.ts);
+    P.unit = (W.h * A.n_seqs + W.b) * T.rt + W.r;
+    P.h = W.h;
+    P.tok = W.b * A.q_len + W.r * T.ts;
+    P.ntok = min(T.ts, A.q_len - W.r * T.ts);
     P.ends = (W.tile == 0 ? 1 : 0) | (W.tile + P.tiles == W.tiles ? 2 : 0);
     P.k0 = W.origin + W.tile * AT_KEYS;
     P.lo = W.lo; P.hi = W.hi;
     W.tile = 0;
-    if ((P.ends & 2) && ++W.u == per) { W.u = 0; ++W.b; W.tiles = -1; }
+    if ((P.ends & 2) && ++W.r == T.rt) {
+      W.r = 0;
+      W.tiles = -1;
+      if (++W.b == A.n_seqs) { W.b = 0; ++W.h; }
+    }
   }
   W.w += P.tiles;
   return true;
@@ -222,26 +226,31 @@ __device__ __forceinline__ void make_share(const TileArgs& T, Share& S, int* s_s
     for (int l = 0; l < 2; ++l) {
       const int from = l ? mid : g0, to = min(l ? g1 : mid, n_single);
       S.lane0[l] = from; S.lane1[l] = l ? g1 : mid;
-      if (from < n_single) { S.own_b[l] = -1; S.own_u[l] = 0; S.own_t[l] = 0; }
+      if (from < n_single) S.own_b[l] = -1;
       S.batch_pieces[l] = pp + (to > from ? (to - 1) / pre_tiles - from / pre_tiles + 1 : 0);
     }
   }
-  for (int l = 0; l < 2; ++l) {  // the thread whose sequences hold the start of a lane's range finds it
+  // Own units stand head by head, so that workers at the same place of their heads read neighbouring rows of the same tokens.
+  const int line = total * T.rt;  // of one head
+  for (int l = 0; l < 2; ++l) {   // the thread whose sequences hold the start of a lane's range finds it
     const int w = (l ? mid : g0) - n_single;
-    int acc = before * mult;
-    if (w < acc || w >= acc + sum * mult) continue;
+    if (w < 0 || line == 0) continue;
+    const int h = w / line, at = w - h * line;
+    int acc = before * T.rt;
+    if (at < acc || at >= acc + sum * T.rt) continue;
 #pragma unroll 1
     for (int b = b0; b < b1; ++b) {
       const OwnKeys k = own_keys(T, attend_len(A, b, false));
       const int t = k.tiles;
-      if (w < acc + t * mult) {
+      if (at < acc + t * T.rt) {
+        S.own_h[l] = h;
         S.own_b[l] = b;
         S.own_k[l] = k;
-        S.own_u[l] = (w - acc) / t;
-        S.own_t[l] = (w - acc) - S.own_u[l] * t;
+        S.own_r[l] = (at - acc) / t;
+        S.own_t[l] = (at - acc) - S.own_r[l] * t;
         break;
       }
-      acc += t * mult;
+      acc += t * T.rt;
     }
   }
 }
@@ -709,10 +718,21 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         wait(b_s + 16 * l + 8 * (n & 1), (n >> 1) & 1);
         tm_fence_after();
         if (warp_live) {
+          const bool masked = !__all_sync(0xffffffffu, lo <= 0 && hi >= AT_KEYS);
+          const uint64_t scale2 = both(scale);
+          uint64_t acc[2] = {0, 0};
+          auto weights = [&](uint32_t* s, uint64_t off2) {  // 32 scores to 16 pairs of weights
+#pragma unroll
+            for (int c = 0; c < 32; c += 2) {
+              const uint64_t x = fma2(pair32(s[c], s[c + 1]), scale2, off2);
+              const uint64_t p = (c / 2) % 16 * AT_POLY % 16 < AT_POLY ? ex2_poly2(x) : pair32(__float_as_uint(ex2(lo32(x))), __float_as_uint(ex2(hi32(x))));
+              acc[(c / 2) & 1] = add2(acc[(c / 2) & 1], p);
+              s[c / 2] = pack2<WD>(lo32(p), hi32(p));
+            }
+          };
           // Two passes over the scores: the maximum (all four quarters of the columns), then the weights.  The quarters 0 and 1 stay in
           // registers between the passes; 2 and 3 are read again (masked ones are written back first).  The weights of a
           // quarter go over scores that are in registers or done with.
-          const bool masked = !__all_sync(0xffffffffu, lo <= 0 && hi >= AT_KEYS);
           uint32_t s0[32], s1[32];
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -762,28 +782,21 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
             }
           }
           const float off = m == -INFINITY ? 0.f : -m * scale;
-          uint64_t acc[2] = {0, 0};
-          const uint64_t scale2 = both(scale), off2 = both(off);
-          auto quarter = [&](uint32_t* s, int i) {
-#pragma unroll
-            for (int c = 0; c < 32; c += 2) {
-              const uint64_t x = fma2(pair32(s[c], s[c + 1]), scale2, off2);
-              const uint64_t p = (c / 2) % 16 * AT_POLY % 16 < AT_POLY ? ex2_poly2(x) : pair32(__float_as_uint(ex2(lo32(x))), __float_as_uint(ex2(hi32(x))));
-              acc[(c / 2) & 1] = add2(acc[(c / 2) & 1], p);
-              s[c / 2] = pack2<WD>(lo32(p), hi32(p));
-            }
-            tm_st16(t_s + 16 * i, s);
-          };
-          quarter(s0, 0);
+          const uint64_t off2 = both(off);
+          weights(s0, off2);
+          tm_st16(t_s, s0);
           tm_ld32(t_s + 64, s0);
-          quarter(s1, 1);
+          weights(s1, off2);
+          tm_st16(t_s + 16, s1);
           tm_wait_ld();
           tm_pin32(s0);
           tm_ld32(t_s + 96, s1);
-          quarter(s0, 2);
+          weights(s0, off2);
+          tm_st16(t_s + 32, s0);
           tm_wait_ld();
           tm_pin32(s1);
-          quarter(s1, 3);
+          weights(s1, off2);
+          tm_st16(t_s + 48, s1);
           const uint64_t acc_all = add2(acc[0], acc[1]);
           sum += lo32(acc_all) + hi32(acc_all);
           tm_wait_st();
@@ -852,7 +865,7 @@ __global__ void __launch_bounds__(256) ls_attend_tile_join_kernel(const TileArgs
     pre_step = 128;
   }
   const int rt = i / T.ts;
-  const long long own_unit = ((long long)b * A.kv_heads + h) * T.rt + rt, own_step = (long long)T.ts * A.group;
+  const long long own_unit = ((long long)h * A.n_seqs + b) * T.rt + rt, own_step = (long long)T.ts * A.group;
   const long long own_row = (i - rt * T.ts) * A.group + g;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   int n_pre = 0, n_own = 0;
