@@ -451,7 +451,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     constexpr uint32_t ID_ST = mma_idesc(TYPE, 128, AT_NARROW, false, false), ID_OT = mma_idesc(TYPE, 128, AT_NARROW, true, false);
     const int l = warp - 9;
     const int cnt = l ? cnt1 : cnt0;
-    const uint32_t t_s = __shfl_sync(0xffffffffu, tmem + l * AT_KEYS, 0), t_o = __shfl_sync(0xffffffffu, tmem + 256 + l * D, 0);
+    const uint32_t t_s = uniform32(tmem + l * AT_KEYS), t_o = uniform32(tmem + 256 + l * D);
     const uint64_t p_desc = uniform64(smem_desc(q_base + l * TS::TILE + TS::P_AT, 16));
     Slots Q(S.batch_pieces[l], q_slots, 0);
     int left = 0, k0 = 0, lo = 0, hi = 0;   // of the current piece: tiles to come, first key of the next; keys of anybody
@@ -486,9 +486,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         if (!filled(slot, kpair)) return false;
         --left;
         tm_fence_after();
-        const uint64_t q = uniform64(smem_desc(q_base + l * TS::TILE + q_slot * q_step, 16)), k = uniform64(smem_desc(ring + slot * TS::TILE, 16));
-        const uint64_t a = narrow ? k : q, b = narrow ? q : k;
-        const uint32_t id = narrow ? ID_ST : ID_S, d = narrow ? t_s + (r & 1) * 32 : t_s;
+        const uint32_t q = q_base + l * TS::TILE + q_slot * q_step, k = ring + slot * TS::TILE;
+        const uint64_t a = uniform64(smem_desc(narrow ? k : q, 16)), b = uniform64(smem_desc(narrow ? q : k, 16));
+        const uint32_t id = uniform32(narrow ? ID_ST : ID_S), d = uniform32(narrow ? t_s + (r & 1) * 32 : t_s);
         if (elect_one()) {
 #pragma unroll
           for (int c = 0; c < D / 16; ++c) {
@@ -537,8 +537,16 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         __syncwarp();
         return true;
       };
-      // (the first piece of a lane, and one behind a wide piece, has its products in the wide order)
-      const bool scores_first = r > 0 && vnarrow && r < cnt;
+      // Scores first only if their operands are there (the outputs' weights come soon, keys may come late), and never behind a
+      // wide tile, whose weights they would overwrite.
+      bool scores_first = r > 0 && vnarrow && r < cnt;
+      if (scores_first) {
+        uint32_t slot = st + (l == 0 ? v0 : v0 + f0 + v1);
+        if (slot >= NST) slot -= NST;
+        scores_first = mb_try(b_full + 8 * (l ? NST + slot : slot), ((l ? par1 : par0) >> slot) & 1);
+        if (left == 0) scores_first = scores_first && mb_try(b_qfull + 32 * l + 8 * Q.slot, Q.parity());
+        scores_first = __all_sync(0xffffffffu, scores_first);
+      }
       bool good = true;
       if (scores_first) good = scores();
       if (good && r > 0) good = outputs();
@@ -571,7 +579,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     };
     // Keys [lo, hi) that row x of a piece sees, relative to the piece's first.
     auto row_keys = [&](const Piece& P, int x, int& lo, int& hi) {
-      const int tr = x / A.group, t = P.tok + tr, b = t / A.q_len;
+      const int t = P.tok + (P.ntok == 1 ? 0 : x / A.group), b = A.q_len == 1 ? t : t / A.q_len;
       // (an own unit's last key is its sequence's last)
       hi = max((P.kind == AT_OWN ? P.hi : attend_len(A, b, false)) - A.q_len + (t - b * A.q_len) + 1, 0);
       lo = A.window > 0 ? max(hi - A.window, 0) : 0;
@@ -627,8 +635,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         }
         bool rise = false;
 #pragma unroll
-        for (int x = 0; x < NR; ++x)
-          if (x < rows) rise |= fmaf(__uint_as_float(s[x]), scale, off[x]) > 8.f;
+        for (int x = 0; x < NR; ++x) rise |= x < rows && fmaf(__uint_as_float(s[x]), scale, off[x]) > 8.f;
         if (group_any(1 + l, 128, rise)) {
 #pragma unroll
           for (int x = 0; x < NR; ++x)
@@ -657,40 +664,59 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
             }
           tm_wait_st();
         }
+        // (four rows at a time, whether there are as many or not: what a row that is not there leaves behind is not used)
 #pragma unroll
-        for (int x = 0; x < NR; ++x)
-          if (x < rows) {
-            const float p = ex2(fmaf(__uint_as_float(s[x]), scale, off[x]));
-            sum[x] += p;
-            asm volatile("st.shared.b16 [%0], %1;" ::"r"(p_base + x * 128 + ((p_chunk ^ (x & 7)) << 4) + p_byte), "h"(narrow16<WD>(p)) : "memory");
+        for (int g = 0; g < NR; g += 4)
+          if (g < rows) {
+            uint16_t w[4];
+#pragma unroll
+            for (int x = g; x < g + 4; ++x) {
+              const float p = ex2(fmaf(__uint_as_float(s[x]), scale, off[x]));
+              sum[x] += p;
+              w[x - g] = narrow16<WD>(p);
+            }
+#pragma unroll
+            for (int x = g; x < g + 4; ++x)
+              asm volatile("st.shared.b16 [%0], %1;" ::"r"(p_base + x * 128 + ((p_chunk ^ (x & 7)) << 4) + p_byte), "h"(w[x - g]) : "memory");
           }
         fence_async_shared();
         arrive_p();
       }
-      wait(b_o + 8 * l, (n - 1) & 1);
-      tm_fence_after();
       float my_sum = 0.f, my_off = 0.f;
 #pragma unroll
-      for (int x = 0; x < NR; ++x)
-        if (x < rows) {
-          const float v = warp_sum(sum[x]);
-          if (lane_id == x) { C.red[l][quad][x] = v; my_off = off[x]; }
+      for (int g = 0; g < NR; g += 4)
+        if (g < rows) {
+          float v[4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) v[x] = sum[g + x];
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) v[x] += __shfl_xor_sync(0xffffffffu, v[x], o);
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (lane_id == g + x) { C.red[l][quad][g + x] = v[x]; my_off = off[g + x]; }
         }
+      uint32_t o[NR];
+      wait(b_o + 8 * l, (n - 1) & 1);
+      tm_fence_after();
+      tm_ld16(t_o, o);
       group_sync(1 + l, 128);
       if (lane_id < rows) my_sum = (C.red[l][0][lane_id] + C.red[l][1][lane_id]) + (C.red[l][2][lane_id] + C.red[l][3][lane_id]);
       const float inv = my_sum == 0.f ? 0.f : 1.f / my_sum;
       float *po, *pl;
       const long long at = place_piece(P, po, pl);
       if (quad == 0 && lane_id < rows) pl[at + lane_id] = my_sum == 0.f ? -INFINITY : log2f(my_sum) - my_off;
-      uint32_t o[NR];
-      tm_ld16(t_o, o);
       tm_wait_ld();
       tm_pin16(o);
 #pragma unroll
-      for (int x = 0; x < NR; ++x)
-        if (x < rows) {
-          const float f = __shfl_sync(0xffffffffu, inv, x);
-          if (row < D) po[(at + x) * D + row] = __uint_as_float(o[x]) * f;
+      for (int g = 0; g < NR; g += 4)
+        if (g < rows) {
+#pragma unroll
+          for (int x = g; x < g + 4; ++x) {
+            const float f = __shfl_sync(0xffffffffu, inv, x);
+            if (row < D && x < rows) po[(at + x) * D + row] = __uint_as_float(o[x]) * f;
+          }
         }
       tm_fence_before();
     };

@@ -54,10 +54,10 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(p));
   return p != 0;
 }
-// The same value, known to be the same in the whole warp.
-__device__ __forceinline__ uint64_t uniform64(uint64_t x) {
-  return (uint64_t)__shfl_sync(0xffffffffu, (uint32_t)(x >> 32), 0) << 32 | __shfl_sync(0xffffffffu, (uint32_t)x, 0);
-}
+// The same value, in uniform registers (where a warp-wide reduction leaves it): operands of the tensor instructions come from
+// there, and one that the compiler does not know to be uniform is moved over before every single instruction.
+__device__ __forceinline__ uint32_t uniform32(uint32_t x) { return __reduce_or_sync(0xffffffffu, x); }
+__device__ __forceinline__ uint64_t uniform64(uint64_t x) { return (uint64_t)uniform32((uint32_t)(x >> 32)) << 32 | uniform32((uint32_t)x); }
 
 // ---- tensor memory ----------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void tm_alloc(uint32_t dst, uint32_t cols) {
