@@ -543,8 +543,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       if (scores_first) {
         uint32_t slot = st + (l == 0 ? v0 : v0 + f0 + v1);
         if (slot >= NST) slot -= NST;
-        scores_first = mb_try(b_full + 8 * (l ? NST + slot : slot), ((l ? par1 : par0) >> slot) & 1);
-        if (left == 0) scores_first = scores_first && mb_try(b_qfull + 32 * l + 8 * Q.slot, Q.parity());
+        scores_first = mb_test(b_full + 8 * (l ? NST + slot : slot), ((l ? par1 : par0) >> slot) & 1);
+        if (left == 0) scores_first = scores_first && mb_test(b_qfull + 32 * l + 8 * Q.slot, Q.parity());
         scores_first = __all_sync(0xffffffffu, scores_first);
       }
       bool good = true;
@@ -616,7 +616,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       int my_lo = -0x7fffffff, my_hi = 0x7fffffff;
       if (lane_id < rows) { my_lo = C.lo[l][lane_id]; my_hi = C.hi[l][lane_id]; }
       int all_lo = __reduce_max_sync(0xffffffffu, my_lo), all_hi = __reduce_min_sync(0xffffffffu, my_hi);  // what every row sees
-      float off[NR], sum[NR];
+      float off[NR], sum[NR], my_off = 3e38f;  // my_off: of row `lane`
 #pragma unroll
       for (int x = 0; x < NR; ++x) { off[x] = 3e38f; sum[x] = 0.f; }
       for (int j = 0; j < P.tiles; ++j, ++n, all_lo -= AT_KEYS, all_hi -= AT_KEYS) {
@@ -637,32 +637,38 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
 #pragma unroll
         for (int x = 0; x < NR; ++x) rise |= x < rows && fmaf(__uint_as_float(s[x]), scale, off[x]) > 8.f;
         if (group_any(1 + l, 128, rise)) {
+          // the rows' true maxima: of each warp's keys, then of all (lane x of every warp keeps row x)
+          float top = -INFINITY;
 #pragma unroll
-          for (int x = 0; x < NR; ++x)
-            if (x < rows) {
-              const float v = warp_max(__uint_as_float(s[x]));
-              if (lane_id == x) C.red[l][quad][x] = v;
-            }
+          for (int x = 0; x < NR; ++x) {
+            const float v = warp_max(__uint_as_float(s[x]));
+            if (lane_id == x) top = v;
+          }
+          if (lane_id < NR) C.red[l][quad][lane_id] = top;
           group_sync(1 + l, 128);
+          if (lane_id < rows) {
+            top = fmaxf(fmaxf(C.red[l][0][lane_id], C.red[l][1][lane_id]), fmaxf(C.red[l][2][lane_id], C.red[l][3][lane_id])) * scale;
+            rise = top + my_off > 8.f;
+          } else rise = false;
+          const float f = rise ? ex2(-top - my_off) : 1.f;
+          if (rise) my_off = -top;
+          uint32_t o[NR];
+          if (j > 0) {
+            tm_ld16(t_o, o);
+            tm_wait_ld();
+            tm_pin16(o);
+          }
 #pragma unroll
-          for (int x = 0; x < NR; ++x)
-            if (x < rows) {
-              const float top = fmaxf(fmaxf(C.red[l][0][x], C.red[l][1][x]), fmaxf(C.red[l][2][x], C.red[l][3][x])) * scale;
-              if (top + off[x] > 8.f) {
-                const float f = ex2(-top - off[x]);
-                sum[x] *= f;
-                off[x] = -top;
-                if (j > 0) {
-                  uint32_t o;
-                  tm_ld1(t_o + x, &o);
-                  tm_wait_ld();
-                  tm_pin1(&o);
-                  o = __float_as_uint(__uint_as_float(o) * f);
-                  tm_st1(t_o + x, &o);
-                }
-              }
-            }
-          tm_wait_st();
+          for (int x = 0; x < NR; ++x) {
+            const float fx = __shfl_sync(0xffffffffu, f, x);
+            off[x] = __shfl_sync(0xffffffffu, my_off, x);
+            sum[x] *= fx;
+            o[x] = __float_as_uint(__uint_as_float(o[x]) * fx);
+          }
+          if (j > 0) {
+            tm_st16(t_o, o);
+            tm_wait_st();
+          }
         }
         // (four rows at a time, whether there are as many or not: what a row that is not there leaves behind is not used)
 #pragma unroll
@@ -682,7 +688,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         fence_async_shared();
         arrive_p();
       }
-      float my_sum = 0.f, my_off = 0.f;
+      float my_sum = 0.f;
 #pragma unroll
       for (int g = 0; g < NR; g += 4)
         if (g < rows) {
@@ -695,7 +701,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
             for (int x = 0; x < 4; ++x) v[x] += __shfl_xor_sync(0xffffffffu, v[x], o);
 #pragma unroll
           for (int x = 0; x < 4; ++x)
-            if (lane_id == g + x) { C.red[l][quad][g + x] = v[x]; my_off = off[g + x]; }
+            if (lane_id == g + x) C.red[l][quad][g + x] = v[x];
         }
       uint32_t o[NR];
       wait(b_o + 8 * l, (n - 1) & 1);

@@ -23,6 +23,14 @@ __device__ __forceinline__ bool mb_try(uint32_t bar, uint32_t parity) {
   return ok != 0;
 }
 
+// The same without waiting (try_wait may hold the thread for a while).
+__device__ __forceinline__ bool mb_test(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
+
 // One box of a tensor map to shared memory (128-byte swizzled), counted off on `bar`; no multicast.
 __device__ __forceinline__ void tma_load4(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
