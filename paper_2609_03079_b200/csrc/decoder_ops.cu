@@ -156,19 +156,24 @@ int32_t attend_tiles(ls_paged_kv* kv, const ls::AttendArgs& a, cudaStream_t st) 
   LS_TRY(make_map(&q_own, WD == ls::WD_BF16 ? LS_WDTYPE_BF16 : LS_WDTYPE_FP16, q, 3, dims, strides, box_own));
   if (a.prefix > 0) LS_TRY(make_map(&q_all, WD == ls::WD_BF16 ? LS_WDTYPE_BF16 : LS_WDTYPE_FP16, q, 3, dims, strides, box_all));
   else q_all = q_own;
-  ls::ls_attend_tile_kernel<WD, D><<<kv->sm_count, ls::AT_THREADS, ls::TileShape<D>::SMEM, st>>>(t, kv->map_k, kv->map_v, q_all, q_own);
-  LS_LAUNCHED();
-  const long long rows = (long long)a.n_seqs * a.q_len * a.heads;
-  cudaLaunchConfig_t cfg{};
-  const bool few = rows <= kJoinFewRows;
-  cfg.gridDim = dim3((unsigned)(few ? rows : (rows + 7) / 8));
-  cfg.blockDim = dim3(256);
-  cfg.stream = st;
+  // Both launches may start while the kernel in front of them ends; each waits for it before it reads memory.
   cudaLaunchAttribute at{};
   at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.stream = st;
   cfg.attrs = &at;
   cfg.numAttrs = 1;
+  cfg.gridDim = dim3(kv->sm_count);
+  cfg.blockDim = dim3(ls::AT_THREADS);
+  cfg.dynamicSmemBytes = ls::TileShape<D>::SMEM;
+  LS_CUDA((cudaLaunchKernelEx(&cfg, ls::ls_attend_tile_kernel<WD, D>, t, kv->map_k, kv->map_v, q_all, q_own)));
+  LS_LAUNCHED();
+  const long long rows = (long long)a.n_seqs * a.q_len * a.heads;
+  const bool few = rows <= kJoinFewRows;
+  cfg.gridDim = dim3((unsigned)(few ? rows : (rows + 7) / 8));
+  cfg.blockDim = dim3(256);
+  cfg.dynamicSmemBytes = 0;
   if (few) LS_CUDA((cudaLaunchKernelEx(&cfg, ls::ls_attend_tile_join_kernel<WD, D, 8>, t)));
   else LS_CUDA((cudaLaunchKernelEx(&cfg, ls::ls_attend_tile_join_kernel<WD, D, 1>, t)));
   LS_LAUNCHED();

@@ -28,7 +28,7 @@ namespace ls {
 constexpr int AT_THREADS = 352;
 constexpr int AT_KEYS = 128;
 constexpr long long AT_SPIN_CLOCKS = 4000LL * 1000 * 1000;  // about two seconds
-constexpr int AT_COST_PAIR = 2, AT_COST_LANE = 1;           // of one key tile, in units of half a CTA
+constexpr int AT_COST_PAIR = 2, AT_COST_LANE = 1;           // of one key tile, in time of half a CTA
 
 constexpr int AT_POLY = 4;  // of 16 pairs of weights, how many are computed by ex2_poly2
 
@@ -300,6 +300,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
   }
   if (warp == 9) tm_alloc(saddr(&C.tmem), 512);
   if (warp == 8 && lane_id < 4) tma_prefetch_map(lane_id == 0 ? &map_k : lane_id == 1 ? &map_v : lane_id == 2 ? &map_q_all : &map_q_own);
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // (all before this overlaps the end of the kernel in front)
   make_share(T, S, C.scan, blockIdx.x, gridDim.x);
   tm_fence_before();
   __syncthreads();
@@ -352,6 +353,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     bool more[2], fresh[2] = {false, false};
     int left[2] = {0, 0}, batch[2], pages[2], pages_next[2];                               // batch: key of its first box
     int vk0[2] = {0, 0}, vlo[2] = {0, 0}, vhi[2] = {0, 0}, vh[2] = {0, 0}, vpage[2] = {0, 0};  // tile whose values are to come
+    bool vown[2] = {false, false};
     uint32_t st = 0, st_par = 1;
     Slots Q[2] = {Slots(S.batch_pieces[0], q_slots, 15), Slots(S.batch_pieces[1], q_slots, 15)};
     const int nbox = AT_KEYS / T.box, box_shift = 31 - __clz(T.box);
@@ -359,7 +361,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     const bool page_pow2 = (A.page & (A.page - 1)) == 0;
     const int page_shift = 31 - __clz(A.page);
     auto page_index = [&](int key) { return page_pow2 ? key >> page_shift : key / A.page; };
-    auto load_tile = [&](const CUtensorMap* map, uint32_t full, int k0, int lo, int hi, int h, int pg) {
+    // (the prefix is read again by other rows, a sequence's own keys are not)
+    const uint64_t l2_keep = l2_evict_last(), l2_once = l2_evict_first();
+    auto load_tile = [&](const CUtensorMap* map, uint32_t full, bool own, int k0, int lo, int hi, int h, int pg) {
       const int key = k0 + my_box * T.box;
       const bool on = my_half < D / 64 && key < hi && key + T.box > lo;
       const int count = __popc(__ballot_sync(0xffffffffu, on));
@@ -369,7 +373,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       if (lane_id == 0) mb_expect(full + 8 * st, count * T.box * 128);
       __syncwarp();
       if (on)
-        tma_load4(ring + st * TS::TILE + my_half * TS::HALF + my_box * T.box * 128, map, my_half * 64, key - page_index(key) * A.page, h, pg, full + 8 * st);
+        tma_load4(ring + st * TS::TILE + my_half * TS::HALF + my_box * T.box * 128, map, my_half * 64, key - page_index(key) * A.page, h, pg, full + 8 * st,
+                  own ? l2_once : l2_keep);
       if (++st == NST) { st = 0; st_par ^= 1; }
     };
     auto fetch_pages = [&](const Piece& p, int key) {  // (no branch around the load: nothing waits for it here)
@@ -397,7 +402,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     };
     auto step = [&](auto lc, int r, int cnt) {
       constexpr int l = decltype(lc)::value;
-      if (r > 0 && r <= cnt && !(r <= n_pair && l == 1)) load_tile(&map_v, b_full + (r > n_pair ? 8 * NST * l : 0), vk0[l], vlo[l], vhi[l], vh[l], vpage[l]);
+      if (r > 0 && r <= cnt && !(r <= n_pair && l == 1)) load_tile(&map_v, b_full + (r > n_pair ? 8 * NST * l : 0), vown[l], vk0[l], vlo[l], vhi[l], vh[l], vpage[l]);
       if (!ok || r >= cnt) return;
       const bool own = P[l].kind == AT_OWN;
       if (fresh[l]) {
@@ -417,8 +422,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       }
       if (!(r < n_pair && l == 1)) {
         const int page = __shfl_sync(0xffffffffu, pages[l], ((P[l].k0 - batch[l]) >> box_shift) + my_box);
-        vk0[l] = P[l].k0; vlo[l] = P[l].lo; vhi[l] = P[l].hi; vh[l] = P[l].h; vpage[l] = page;
-        load_tile(&map_k, b_full + (r >= n_pair ? 8 * NST * l : 0), P[l].k0, P[l].lo, P[l].hi, P[l].h, page);
+        vown[l] = own; vk0[l] = P[l].k0; vlo[l] = P[l].lo; vhi[l] = P[l].hi; vh[l] = P[l].h; vpage[l] = page;
+        load_tile(&map_k, b_full + (r >= n_pair ? 8 * NST * l : 0), own, P[l].k0, P[l].lo, P[l].hi, P[l].h, page);
       }
       if (ok) advance(lc);
     };
@@ -900,6 +905,8 @@ __global__ void __launch_bounds__(256) ls_attend_tile_join_kernel(const TileArgs
   const long long own_unit = ((long long)h * A.n_seqs + b) * T.rt + rt, own_step = (long long)T.ts * A.group;
   const long long own_row = (i - rt * T.ts) * A.group + g;
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  // (with many rows the next kernel's blocks, waiting here early, were measured to cost more than their start takes)
+  if (WARPS > 1) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   int n_pre = 0, n_own = 0;
   long long pre_at = 0, own_at = 0;
   // (a kernel that gave up on a wait leaves workers unnoted: its rows are reported and come out as zeros)
