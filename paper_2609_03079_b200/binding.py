@@ -6,6 +6,7 @@ fails to load, the first call raises.  PyTorch supplies device memory (tensors) 
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
 import os
 from typing import Optional
 
@@ -136,6 +137,23 @@ def lib() -> C.CDLL:
                 getattr(L, name).restype = C.c_int32
         _lib = L
     return _lib
+
+
+_fast = None
+
+
+def _marshal():
+    """The marshalling module of the per-token calls, bound to the library (built in-tree on first use where g++ is available)."""
+    global _fast
+    if _fast is None:
+        path = _build.build_marshal()
+        spec = importlib.util.spec_from_file_location("ls_marshal", path)
+        m = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(m)
+        L = lib()
+        m.bind(*(C.cast(f, C.c_void_p).value for f in (L.ls_paged_kv_append, L.ls_paged_kv_attend, L.ls_block_norm)))
+        _fast = m
+    return _fast
 
 
 def last_error() -> str:
@@ -489,16 +507,17 @@ class PagedKV:
 
     def __init__(self, handle: int, k_pages: torch.Tensor, v_pages: torch.Tensor, n_q_heads: int, max_seqs: int, max_q_len: int,
                  rope: Optional[torch.Tensor]):
-        self.handle = handle
+        self.handle, self.plan = handle, None
         self.k_pages, self.v_pages, self.rope = k_pages, v_pages, rope
         self.n_pages, self.page_size, self.n_kv_heads, self.head_dim = k_pages.shape
         self.n_q_heads, self.max_seqs, self.max_q_len = n_q_heads, max_seqs, max_q_len
         self.dtype, self.device = k_pages.dtype, k_pages.device.index
+        self.plan = _marshal().plan(handle, k_pages, n_q_heads)
 
     def close(self) -> None:
         if self.handle:
             lib().ls_paged_kv_destroy(self.handle)
-            self.handle = None
+            self.handle = self.plan = None
 
     def __del__(self):
         try:
@@ -540,36 +559,16 @@ def ls_paged_kv_status(kv: PagedKV) -> int:
     return v.value
 
 
-def _token_stride(kv: PagedKV, t: torch.Tensor, heads: int) -> int:
-    """Checks a [tokens, heads, head_dim] (or [sequences, tokens, heads, head_dim]) operand and returns its token stride."""
-    shape, st = t.shape, t.stride()
-    D = kv.head_dim
-    assert t.dtype == kv.dtype and t.is_cuda and shape[-1] == D and shape[-2] == heads
-    assert (st[-1] == 1 or D == 1) and (st[-2] == D or heads == 1)
-    if len(shape) == 4 and shape[1] > 1:
-        assert shape[0] == 1 or st[0] == shape[1] * st[1]
-        return st[1]
-    return st[0] if shape[0] > 1 else heads * D  # (a single token has no stride)
-
-
-def _table_args(table: torch.Tensor):
-    assert table.dtype == torch.int32 and table.dim() == 2 and table.is_cuda and (table.stride(1) == 1 or table.shape[1] <= 1)
-    return table.data_ptr(), table.shape[0], table.shape[1], table.stride(0)
+def _raw(stream) -> Optional[int]:
+    return None if stream is None else stream.cuda_stream
 
 
 def ls_paged_kv_append(kv: PagedKV, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, q_out: Optional[torch.Tensor],
                        seq: torch.Tensor, pos: torch.Tensor, table: torch.Tensor, stream=None) -> None:
     """q, k, v, q_out: [tokens, heads, head_dim] (any token stride); seq, pos: int32 [tokens]; table: int32 [sequences, pages]."""
-    n = k.shape[0]
-    assert v.shape[0] == n and seq.numel() == n and pos.numel() == n and seq.dtype == pos.dtype == torch.int32
-    assert seq.is_cuda and pos.is_cuda and seq.is_contiguous() and pos.is_contiguous()
-    sq = so = 0
-    if q is not None:
-        assert q.shape[0] == n and q_out.shape[0] == n
-        sq, so = _token_stride(kv, q, kv.n_q_heads), _token_stride(kv, q_out, kv.n_q_heads)
-    tp, ns, tw, ts = _table_args(table)
-    _check(lib().ls_paged_kv_append(kv.handle, _ptr(q), sq, _ptr(q_out), so, k.data_ptr(), _token_stride(kv, k, kv.n_kv_heads), v.data_ptr(),
-                                    _token_stride(kv, v, kv.n_kv_heads), n, seq.data_ptr(), pos.data_ptr(), tp, ns, tw, ts, _stream(stream)))
+    rc = _fast.append(kv.plan, q, k, v, q_out, seq, pos, table, _raw(stream))
+    if rc:
+        _check(rc)
 
 
 def ls_paged_kv_attend(kv: PagedKV, q: torch.Tensor, out: torch.Tensor, seq_len: torch.Tensor, table: torch.Tensor,
@@ -577,24 +576,9 @@ def ls_paged_kv_attend(kv: PagedKV, q: torch.Tensor, out: torch.Tensor, seq_len:
                        lse: Optional[torch.Tensor] = None, stream=None) -> None:
     """q, out: [sequences, q_len, heads, head_dim], or [sequences, heads, head_dim] for one token each; seq_len: int32
     [sequences]; table: int32 [sequences, pages]; lse: float, one per row of q.  ``scale`` defaults to head_dim ** -0.5."""
-    n, m = q.shape[0], (q.shape[1] if q.dim() == 4 else 1)
-    assert out.shape == q.shape and seq_len.dtype == torch.int32 and seq_len.is_cuda and seq_len.is_contiguous() and seq_len.numel() == n
-    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == n * m * kv.n_q_heads)
-    tp, ns, tw, ts = _table_args(table)
-    assert ns == n
-    if prefix_len:
-        assert prefix_pages.dtype == torch.int32 and prefix_pages.is_contiguous() and prefix_pages.numel() * kv.page_size >= prefix_len
-    _check(lib().ls_paged_kv_attend(kv.handle, q.data_ptr(), _token_stride(kv, q, kv.n_q_heads), out.data_ptr(),
-                                    _token_stride(kv, out, kv.n_q_heads), _ptr(lse), n, m, seq_len.data_ptr(), tp, tw, ts,
-                                    _ptr(prefix_pages) if prefix_len else None, prefix_len, window,
-                                    kv.head_dim ** -0.5 if scale is None else scale, _stream(stream)))
-
-
-def _rows(t: torch.Tensor, d: int) -> int:
-    """Checks a [rows, d] (or [d]) operand and returns its row stride."""
-    st = t.stride()
-    assert t.is_cuda and t.shape[-1] == d and t.dim() <= 2 and (st[-1] == 1 or d == 1)
-    return st[0] if len(st) == 2 and t.shape[0] > 1 else d
+    rc = _fast.attend(kv.plan, q, out, seq_len, table, prefix_pages, prefix_len, window, kv.head_dim ** -0.5 if scale is None else scale, lse, _raw(stream))
+    if rc:
+        _check(rc)
 
 
 def ls_block_norm(x: torch.Tensor, y: Optional[torch.Tensor], x_out: Optional[torch.Tensor], h: Optional[torch.Tensor],
@@ -602,19 +586,6 @@ def ls_block_norm(x: torch.Tensor, y: Optional[torch.Tensor], x_out: Optional[to
                   pre_norm: bool = True, w_pre: Optional[torch.Tensor] = None, eps: float = 1e-5, stream=None) -> None:
     """x' = x + scale * gate * (N(y) * w_post) into ``x_out`` and N(x') * w_pre into ``h`` (either may be None; y None: x' = x).
     x, x_out: float or the block's type; y, h, gate ([d] or [rows, d]): the block's type; gains: float [d]."""
-    d = x.shape[-1]
-    n = x.shape[0] if x.dim() == 2 else 1
-    kind = y if y is not None else h if h is not None else x
-    for t in (y, h, gate):
-        assert t is None or (t.dtype == kind.dtype and (t.shape == x.shape or t is gate))
-    assert x_out is None or (x_out.dtype == x.dtype and x_out.shape == x.shape)
-    for w in (w_post, w_pre):
-        assert w is None or (w.dtype == torch.float32 and w.is_cuda and w.is_contiguous() and w.numel() == d)
-    gs = 0
-    if gate is not None:
-        gs = _rows(gate, d) if gate.dim() == 2 else 0
-        assert gate.is_cuda and gate.stride(-1) == 1 and (gate.dim() == 1 or gate.shape == x.shape)
-    _check(lib().ls_block_norm(x.data_ptr(), _rows(x, d), _DTYPE[x.dtype], _ptr(y), 0 if y is None else _rows(y, d), _DTYPE[kind.dtype],
-                               _ptr(x_out), 0 if x_out is None else _rows(x_out, d), _ptr(h), 0 if h is None else _rows(h, d), n, d,
-                               LS_NORM_RMS if post_norm else LS_NORM_NONE, _ptr(w_post), _ptr(gate), gs, scale,
-                               LS_NORM_RMS if pre_norm else LS_NORM_NONE, _ptr(w_pre), eps, _stream(stream)))
+    rc = (_fast or _marshal()).norm(x, y, x_out, h, post_norm, w_post, gate, scale, pre_norm, w_pre, eps, _raw(stream))
+    if rc:
+        _check(rc)

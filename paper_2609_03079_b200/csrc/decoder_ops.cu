@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <new>
+#include <utility>
 
 #include "ls_append.cuh"
 #include "ls_attend.cuh"
@@ -32,6 +33,7 @@ namespace {
 // Blocks that ls_attend_rows_kernel is split into when rows are few: eight blocks of four warps per SM.
 constexpr int kRowsBlocks = 148 * 8;
 constexpr int kRowsMaxGroup = 8;
+constexpr int kNormManyRows = 148 * 4;
 // Up to this many output rows the pieces of each are joined by eight warps (all blocks are resident at once), else by one.
 constexpr long long kJoinFewRows = 148 * 8;
 
@@ -134,6 +136,24 @@ int32_t create_tiles(ls_paged_kv* kv) {
   return LS_OK;
 }
 
+// Launches that may start while the kernel in front of them ends; the kernels wait for it before they touch memory.
+template <class... P, class... Q>
+int32_t launch_early(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, Q&&... args) {
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  LS_CUDA(cudaLaunchKernelEx(&cfg, kernel, std::forward<Q>(args)...));
+  LS_LAUNCHED();
+  return LS_OK;
+}
+
 template <int WD, int D>
 int32_t attend_tiles(ls_paged_kv* kv, const ls::AttendArgs& a, cudaStream_t st) {
   ls::TileArgs t{};
@@ -156,28 +176,11 @@ int32_t attend_tiles(ls_paged_kv* kv, const ls::AttendArgs& a, cudaStream_t st) 
   LS_TRY(make_map(&q_own, WD == ls::WD_BF16 ? LS_WDTYPE_BF16 : LS_WDTYPE_FP16, q, 3, dims, strides, box_own));
   if (a.prefix > 0) LS_TRY(make_map(&q_all, WD == ls::WD_BF16 ? LS_WDTYPE_BF16 : LS_WDTYPE_FP16, q, 3, dims, strides, box_all));
   else q_all = q_own;
-  // Both launches may start while the kernel in front of them ends; each waits for it before it reads memory.
-  cudaLaunchAttribute at{};
-  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at.val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.stream = st;
-  cfg.attrs = &at;
-  cfg.numAttrs = 1;
-  cfg.gridDim = dim3(kv->sm_count);
-  cfg.blockDim = dim3(ls::AT_THREADS);
-  cfg.dynamicSmemBytes = ls::TileShape<D>::SMEM;
-  LS_CUDA((cudaLaunchKernelEx(&cfg, ls::ls_attend_tile_kernel<WD, D>, t, kv->map_k, kv->map_v, q_all, q_own)));
-  LS_LAUNCHED();
+  LS_TRY(launch_early(ls::ls_attend_tile_kernel<WD, D>, dim3((unsigned)kv->sm_count), ls::AT_THREADS, ls::TileShape<D>::SMEM, st, t, kv->map_k, kv->map_v,
+                      q_all, q_own));
   const long long rows = (long long)a.n_seqs * a.q_len * a.heads;
-  const bool few = rows <= kJoinFewRows;
-  cfg.gridDim = dim3((unsigned)(few ? rows : (rows + 7) / 8));
-  cfg.blockDim = dim3(256);
-  cfg.dynamicSmemBytes = 0;
-  if (few) LS_CUDA((cudaLaunchKernelEx(&cfg, ls::ls_attend_tile_join_kernel<WD, D, 8>, t)));
-  else LS_CUDA((cudaLaunchKernelEx(&cfg, ls::ls_attend_tile_join_kernel<WD, D, 1>, t)));
-  LS_LAUNCHED();
-  return LS_OK;
+  if (rows <= kJoinFewRows) return launch_early(ls::ls_attend_tile_join_kernel<WD, D, 8>, dim3((unsigned)rows), 256, 0, st, t);
+  return launch_early(ls::ls_attend_tile_join_kernel<WD, D, 1>, dim3((unsigned)((rows + 7) / 8)), 256, 0, st, t);
 }
 
 int32_t create_kv(ls_paged_kv* kv) {
@@ -225,15 +228,35 @@ int32_t attend_rows(ls::AttendArgs& a, bool q_vec, cudaStream_t st) {
   return LS_OK;
 }
 
+template <int XT, int BT, int V, int K>
+int32_t norm_blocks(const ls::NormArgs& a, cudaStream_t st) {
+  const int chunks = a.d / V, threads = ((chunks + K - 1) / K + 31) / 32 * 32;
+  return launch_early(ls::ls_norm_kernel<XT, BT, V, K, false>, dim3((unsigned)a.n), threads, 0, st, a);
+}
+template <int XT, int BT, int V, int K>
+int32_t norm_warps(const ls::NormArgs& a, cudaStream_t st) {
+  return launch_early(ls::ls_norm_kernel<XT, BT, V, K, true>, dim3((unsigned)((a.n + 7) / 8)), 256, 0, st, a);
+}
+
 template <int XT, int BT>
 int32_t launch_norm(const ls::NormArgs& a, cudaStream_t st) {
-  const int threads = a.d >= 512 ? 512 : (a.d + 31) / 32 * 32;
-  const size_t smem = (size_t)a.d * sizeof(float);
-  if (smem > 48 * 1024 - 256)
-    LS_CUDA(cudaFuncSetAttribute(ls::ls_norm_rows_kernel<XT, BT>, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024));
-  ls::ls_norm_rows_kernel<XT, BT><<<(unsigned)a.n, threads, smem, st>>>(a);
-  LS_LAUNCHED();
-  return LS_OK;
+  auto fits = [](const void* p, int64_t stride, bool rows) { return !p || (aligned16(p) && (!rows || stride % 8 == 0)); };
+  const bool rows = a.n > 1;
+  const bool vec = a.d % 8 == 0 && fits(a.x, a.x_stride, rows) && fits(a.y, a.y_stride, rows) && fits(a.x_out, a.x_out_stride, rows) &&
+                   fits(a.h, a.h_stride, rows) && fits(a.gate, a.gate_stride, rows) && fits(a.w_post, 0, false) && fits(a.w_pre, 0, false);
+  // Few rows are spread over as many threads as they have chunks; many rows take more per thread, so that fewer threads wait for
+  // a row's sums, and short ones a warp each.
+  if (vec) {
+    const int chunks = a.d / 8;
+    if (a.n >= kNormManyRows && chunks <= 32) return norm_warps<XT, BT, 8, 1>(a, st);
+    if (a.n >= kNormManyRows && chunks <= 64) return norm_warps<XT, BT, 8, 2>(a, st);
+    if (chunks <= 256 || (a.n < kNormManyRows && chunks <= 1024)) return norm_blocks<XT, BT, 8, 1>(a, st);
+    return norm_blocks<XT, BT, 8, 2>(a, st);
+  }
+  if (a.d <= 1024) return norm_blocks<XT, BT, 1, 1>(a, st);
+  if (a.d <= 4096) return norm_blocks<XT, BT, 1, 4>(a, st);
+  if (a.d <= 8192) return norm_blocks<XT, BT, 1, 8>(a, st);
+  return norm_blocks<XT, BT, 1, 16>(a, st);
 }
 
 }  // namespace
@@ -327,12 +350,15 @@ int32_t ls_paged_kv_append(ls_paged_kv* kv, const void* d_q, int64_t q_stride, v
   a.rope_dim = D.rope_dim; a.rope_positions = D.rope_positions; a.interleaved = D.rope_interleaved;
   const cudaStream_t st = (cudaStream_t)stream;
   KernelTimer timer(LS_TIMED_APPEND, st);
+  const bool bf = D.dtype == LS_WDTYPE_BF16;
+  const bool vec = D.head_dim % 16 == 0 && D.rope_dim % 16 == 0 && aligned16(d_k) && aligned16(d_v) && aligned16(D.d_k) && aligned16(D.d_v) &&
+                   aligned16(d_q) && aligned16(d_q_out) && aligned16(D.d_rope) &&
+                   (n_tokens == 1 || (k_stride | v_stride | (d_q ? q_stride | q_out_stride : 0)) % 8 == 0) &&
+                   (D.page_stride | D.token_stride | D.head_stride) % 8 == 0;
+  if (vec) return launch_early(bf ? ls::ls_append_kernel<ls::WD_BF16> : ls::ls_append_kernel<ls::WD_FP16>, dim3((unsigned)n_tokens), 256, 0, st, a);
   const int items = ((d_q ? D.n_q_heads : 0) + 2 * D.n_kv_heads) * (D.head_dim / 2);
   const dim3 grid((unsigned)n_tokens, (unsigned)std::min(64, (items + 255) / 256));
-  if (D.dtype == LS_WDTYPE_BF16) ls::ls_append_pairs_kernel<ls::WD_BF16><<<grid, 256, 0, st>>>(a);
-  else ls::ls_append_pairs_kernel<ls::WD_FP16><<<grid, 256, 0, st>>>(a);
-  LS_LAUNCHED();
-  return LS_OK;
+  return launch_early(bf ? ls::ls_append_pairs_kernel<ls::WD_BF16> : ls::ls_append_pairs_kernel<ls::WD_FP16>, grid, 256, 0, st, a);
 }
 
 int32_t ls_paged_kv_attend(ls_paged_kv* kv, const void* d_q, int64_t q_stride, void* d_out, int64_t out_stride, float* d_lse,
@@ -390,10 +416,14 @@ int32_t ls_block_norm(const void* d_x, int64_t x_stride, int32_t x_dtype, const 
   if (n > 1 && (x_stride < d || (d_y && y_stride < d) || (d_x_out && x_out_stride < d) || (d_h && h_stride < d) ||
                 (d_gate && gate_stride != 0 && gate_stride < d)))
     return fail(LS_ERR_INVALID, "ls_block_norm: a row stride is smaller than a row");
-  cudaPointerAttributes at{};
   int dev = -1;
-  if (cudaPointerGetAttributes(&at, d_x) == cudaSuccess && at.type == cudaMemoryTypeDevice) dev = at.device;
-  else { cudaGetLastError(); LS_CUDA(cudaGetDevice(&dev)); }
+  LS_CUDA(cudaGetDevice(&dev));
+  static const int n_dev = [] { int k = 0; return cudaGetDeviceCount(&k) == cudaSuccess ? k : 0; }();
+  if (n_dev > 1) {
+    cudaPointerAttributes at{};
+    if (cudaPointerGetAttributes(&at, d_x) == cudaSuccess && at.type == cudaMemoryTypeDevice) dev = at.device;
+    else cudaGetLastError();
+  }
   DeviceGuard guard(dev);
   ls::NormArgs a{};
   a.x = d_x; a.y = d_y; a.x_out = d_x_out; a.h = d_h; a.w_post = d_w_post; a.w_pre = d_w_pre; a.gate = d_gate;

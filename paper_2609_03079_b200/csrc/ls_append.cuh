@@ -4,6 +4,7 @@
 // `position` of a table the caller keeps ([positions][rope_dim]: rope_dim / 2 cosines, then as many sines); a pair is
 // (i, i + rope_dim / 2), or (2 i, 2 i + 1) when interleaved.  The arithmetic is fp32, rounded once to the 16-bit type.
 #pragma once
+#include "ls_attend.cuh"
 #include "ls_common.cuh"
 
 namespace ls {
@@ -48,9 +49,78 @@ __device__ __forceinline__ long long append_slot(const AppendArgs& A, int sq, in
   return id * A.page_stride + (long long)(ps - pg * A.page) * A.token_stride;
 }
 
-// One block row per token, one thread per pair of components: the route for any alignment and any even rope_dim.
+// One block per token; 16-byte loads and stores.  A thread has the same two chunks of eight components in every head that it
+// visits (chunks whose components are each other's partners, or two neighbours where nothing is turned), so that it reads its
+// cosines and sines once per token.  For head and rotation sizes of a multiple of 16 and 16-byte aligned operands.
+template <int WD>
+__global__ void __launch_bounds__(256) ls_append_kernel(const AppendArgs A) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const long long t = blockIdx.x;
+  const int sq = A.seq[t], ps = A.pos[t];
+  const int per = A.dim / 16, nq = A.q ? A.heads : 0, heads = nq + 2 * A.kv_heads;
+  const int i = threadIdx.x % per, step = blockDim.x / per;
+  const bool turned = 16 * i < A.rope_dim;
+  const int c0 = turned && !A.interleaved ? 8 * i : 16 * i, c1 = turned && !A.interleaved ? c0 + A.rope_dim / 2 : c0 + 8;
+  float c[8], s[8];
+  const bool in_table = ps >= 0 && ps < A.rope_positions;
+  if (turned && in_table) {
+    const float4* tab = reinterpret_cast<const float4*>(A.rope + (long long)ps * A.rope_dim + 8 * i);
+    const float4* tas = reinterpret_cast<const float4*>(A.rope + (long long)ps * A.rope_dim + A.rope_dim / 2 + 8 * i);
+    const float4 a = __ldg(tab), b = __ldg(tab + 1), e = __ldg(tas), f = __ldg(tas + 1);
+    c[0] = a.x; c[1] = a.y; c[2] = a.z; c[3] = a.w; c[4] = b.x; c[5] = b.y; c[6] = b.z; c[7] = b.w;
+    s[0] = e.x; s[1] = e.y; s[2] = e.z; s[3] = e.w; s[4] = f.x; s[5] = f.y; s[6] = f.z; s[7] = f.w;
+  }
+  const long long slot = append_slot(A, sq, ps);
+  auto source = [&](int hd) {
+    return (hd < nq ? A.q + t * A.q_stride + (long long)hd * A.dim
+            : hd < nq + A.kv_heads ? A.k + t * A.k_stride + (long long)(hd - nq) * A.dim
+                                   : A.v + t * A.v_stride + (long long)(hd - nq - A.kv_heads) * A.dim);
+  };
+  auto finish = [&](int hd, uint4 ra, uint4 rb) {
+    uint16_t* dst;
+    if (hd < nq) dst = A.q_out + t * A.q_out_stride + (long long)hd * A.dim;
+    else if (slot < 0) return;
+    else dst = hd < nq + A.kv_heads ? A.k_pages + slot + (hd - nq) * A.head_stride : A.v_pages + slot + (hd - nq - A.kv_heads) * A.head_stride;
+    if (turned && in_table && hd < nq + A.kv_heads) {
+      float a[8], b[8], x[8], y[8];
+      unpack8<WD>(ra, a);
+      unpack8<WD>(rb, b);
+      if (A.interleaved) {  // pairs side by side: four in each chunk
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[2 * e] = a[2 * e] * c[e] - a[2 * e + 1] * s[e];
+          x[2 * e + 1] = a[2 * e + 1] * c[e] + a[2 * e] * s[e];
+          y[2 * e] = b[2 * e] * c[4 + e] - b[2 * e + 1] * s[4 + e];
+          y[2 * e + 1] = b[2 * e + 1] * c[4 + e] + b[2 * e] * s[4 + e];
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) { x[e] = a[e] * c[e] - b[e] * s[e]; y[e] = b[e] * c[e] + a[e] * s[e]; }
+      }
+      ra = make_uint4(pack2<WD>(x[0], x[1]), pack2<WD>(x[2], x[3]), pack2<WD>(x[4], x[5]), pack2<WD>(x[6], x[7]));
+      rb = make_uint4(pack2<WD>(y[0], y[1]), pack2<WD>(y[2], y[3]), pack2<WD>(y[4], y[5]), pack2<WD>(y[6], y[7]));
+    }
+    *reinterpret_cast<uint4*>(dst + c0) = ra;
+    *reinterpret_cast<uint4*>(dst + c1) = rb;
+  };
+  if (threadIdx.x >= step * per) return;
+  // two heads at a time, all four loads before the first store
+  for (int hd = threadIdx.x / per; hd < heads; hd += 2 * step) {
+    const bool two = hd + step < heads;
+    const uint16_t *p = source(hd), *q = source(two ? hd + step : hd);
+    const uint4 a0 = ld_stream128(p + c0), b0 = ld_stream128(p + c1);
+    uint4 a1 = a0, b1 = b0;
+    if (two) { a1 = ld_stream128(q + c0); b1 = ld_stream128(q + c1); }
+    finish(hd, a0, b0);
+    if (two) finish(hd + step, a1, b1);
+  }
+}
+
+// One thread per pair of components: the route for any alignment and any even rope_dim.
 template <int WD>
 __global__ void __launch_bounds__(256) ls_append_pairs_kernel(const AppendArgs A) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const long long t = blockIdx.x;
   const int sq = A.seq[t], ps = A.pos[t];
   const long long slot = append_slot(A, sq, ps);
