@@ -57,11 +57,26 @@ __global__ void __launch_bounds__(256) ls_append_kernel(const AppendArgs A) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const long long t = blockIdx.x;
-  const int sq = A.seq[t], ps = A.pos[t];
   const int per = A.dim / 16, nq = A.q ? A.heads : 0, heads = nq + 2 * A.kv_heads;
   const int i = threadIdx.x % per, step = blockDim.x / per;
   const bool turned = 16 * i < A.rope_dim;
   const int c0 = turned && !A.interleaved ? 8 * i : 16 * i, c1 = turned && !A.interleaved ? c0 + A.rope_dim / 2 : c0 + 8;
+  if (threadIdx.x >= step * per) return;
+  auto source = [&](int hd) {
+    return (hd < nq ? A.q + t * A.q_stride + (long long)hd * A.dim
+            : hd < nq + A.kv_heads ? A.k + t * A.k_stride + (long long)(hd - nq) * A.dim
+                                   : A.v + t * A.v_stride + (long long)(hd - nq - A.kv_heads) * A.dim);
+  };
+  // Two heads at a time; the first two are under way before the token's place and angles are looked up.
+  uint4 a0, b0, a1, b1;
+  auto fetch = [&](int hd) {
+    const uint16_t *p = source(min(hd, heads - 1)), *q = source(min(hd + step, heads - 1));
+    a0 = ld_stream128(p + c0); b0 = ld_stream128(p + c1);
+    a1 = ld_stream128(q + c0); b1 = ld_stream128(q + c1);
+  };
+  int hd = threadIdx.x / per;
+  fetch(hd);
+  const int sq = A.seq[t], ps = A.pos[t];
   float c[8], s[8];
   const bool in_table = ps >= 0 && ps < A.rope_positions;
   if (turned && in_table) {
@@ -72,11 +87,6 @@ __global__ void __launch_bounds__(256) ls_append_kernel(const AppendArgs A) {
     s[0] = e.x; s[1] = e.y; s[2] = e.z; s[3] = e.w; s[4] = f.x; s[5] = f.y; s[6] = f.z; s[7] = f.w;
   }
   const long long slot = append_slot(A, sq, ps);
-  auto source = [&](int hd) {
-    return (hd < nq ? A.q + t * A.q_stride + (long long)hd * A.dim
-            : hd < nq + A.kv_heads ? A.k + t * A.k_stride + (long long)(hd - nq) * A.dim
-                                   : A.v + t * A.v_stride + (long long)(hd - nq - A.kv_heads) * A.dim);
-  };
   auto finish = [&](int hd, uint4 ra, uint4 rb) {
     uint16_t* dst;
     if (hd < nq) dst = A.q_out + t * A.q_out_stride + (long long)hd * A.dim;
@@ -104,16 +114,12 @@ __global__ void __launch_bounds__(256) ls_append_kernel(const AppendArgs A) {
     *reinterpret_cast<uint4*>(dst + c0) = ra;
     *reinterpret_cast<uint4*>(dst + c1) = rb;
   };
-  if (threadIdx.x >= step * per) return;
-  // two heads at a time, all four loads before the first store
-  for (int hd = threadIdx.x / per; hd < heads; hd += 2 * step) {
-    const bool two = hd + step < heads;
-    const uint16_t *p = source(hd), *q = source(two ? hd + step : hd);
-    const uint4 a0 = ld_stream128(p + c0), b0 = ld_stream128(p + c1);
-    uint4 a1 = a0, b1 = b0;
-    if (two) { a1 = ld_stream128(q + c0); b1 = ld_stream128(q + c1); }
-    finish(hd, a0, b0);
-    if (two) finish(hd + step, a1, b1);
+  for (;;) {
+    if (hd < heads) finish(hd, a0, b0);
+    if (hd + step < heads) finish(hd + step, a1, b1);
+    hd += 2 * step;
+    if (hd >= heads) break;
+    fetch(hd);
   }
 }
 

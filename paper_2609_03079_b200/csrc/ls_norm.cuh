@@ -2,6 +2,8 @@
 //   t = N(y) w_post (or y);  x' = x + scale * gate * t;  h = N(x') w_pre (or x'),  N(z) = z / sqrt(mean z^2 + eps).
 // Sums of squares, x' and h are fp32; x' and h are rounded once, when they are stored (h is made from the unrounded x').
 #pragma once
+#include <type_traits>
+
 #include "ls_append.cuh"
 #include "ls_attend.cuh"
 #include "ls_common.cuh"
@@ -34,15 +36,40 @@ __device__ __forceinline__ void st1(void* p, long long i, float v) {
   else static_cast<uint16_t*>(p)[i] = narrow<DT == DT_F32 ? 0 : DT>(v);
 }
 
-// V elements from element i on (one 16- or two 32-byte loads where V is 8; the caller has checked the alignment).
+// V elements as they lie in memory (one 16-byte load, or two of them, where V is 8; the caller has checked the alignment).
 template <int DT, int V>
-__device__ __forceinline__ void ldv(const void* p, long long i, float (&f)[V]) {
-  if constexpr (V == 1) f[0] = ld1<DT>(p, i);
-  else if constexpr (DT == DT_F32) {
-    const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i), b = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i + 4);
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-  } else unpack8<DT>(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + i), f);
-}
+struct Chunk {
+  using Word = std::conditional_t<DT == DT_F32, float, uint16_t>;
+  static constexpr int N = V == 1 ? 1 : DT == DT_F32 ? 2 : 1;
+  std::conditional_t<V == 1, Word, uint4> r[N];
+  __device__ __forceinline__ void load(const void* p, long long i) {
+    const Word* q = static_cast<const Word*>(p) + i;
+    if constexpr (V == 1) r[0] = *q;
+    else {
+#pragma unroll
+      for (int k = 0; k < N; ++k) r[k] = reinterpret_cast<const uint4*>(q)[k];
+    }
+  }
+  __device__ __forceinline__ void clear() {
+    if constexpr (V == 1) r[0] = Word(0);
+    else {
+#pragma unroll
+      for (int k = 0; k < N; ++k) r[k] = make_uint4(0u, 0u, 0u, 0u);
+    }
+  }
+  __device__ __forceinline__ void get(float (&f)[V]) const {
+    if constexpr (V == 1) {
+      if constexpr (DT == DT_F32) f[0] = r[0];
+      else f[0] = widen<DT>(r[0]);
+    } else if constexpr (DT == DT_F32) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        f[4 * k] = __uint_as_float(r[k].x); f[4 * k + 1] = __uint_as_float(r[k].y);
+        f[4 * k + 2] = __uint_as_float(r[k].z); f[4 * k + 3] = __uint_as_float(r[k].w);
+      }
+    } else unpack8<DT>(r[0], f);
+  }
+};
 template <int DT, int V>
 __device__ __forceinline__ void stv(void* p, long long i, const float (&f)[V]) {
   if constexpr (V == 1) st1<DT>(p, i, f[0]);
@@ -66,10 +93,13 @@ __device__ __forceinline__ float row_sum(float v, float* s) {
   return warp_sum(lane < nw ? s[lane] : 0.f);
 }
 
-// A row is held in registers, K chunks of V elements per thread, so that everything is read once and all loads are under way
-// before the first sum; a row belongs to a block, or (WARP) to one of its warps.
+// A row is held in registers, K chunks of V elements per thread, as it lies in memory until it is used, so that everything is
+// read once, all loads are under way before the first sum, and two blocks of 512 threads fit an SM (64 registers a thread).  A
+// row belongs to a block, or (WARP) to one of its warps.  Gains are asked for ahead of the sum before their use where that
+// takes few registers (one chunk a thread: few rows, where latency counts), else when they are used (they are in L1 then).
 template <int XT, int BT, int V, int K, bool WARP>
 __global__ void __launch_bounds__(WARP ? 256 : 1024) ls_norm_kernel(const NormArgs A) {
+  constexpr bool AHEAD = V * K <= 8;
   __shared__ float s_sum[2][32];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -77,68 +107,78 @@ __global__ void __launch_bounds__(WARP ? 256 : 1024) ls_norm_kernel(const NormAr
   const int tid = WARP ? threadIdx.x & 31 : threadIdx.x, nt = WARP ? 32 : blockDim.x;
   if (WARP && t >= A.n) return;
   const int chunks = A.d / V;
-  float x[K][V], y[K][V], g[K][V];
+  const bool has_y = A.y != nullptr, has_g = A.gate != nullptr;
+  Chunk<XT, V> xr[K];
+  Chunk<BT, V> yr[K], gr[K];
+  Chunk<DT_F32, V> w1[AHEAD ? K : 1], w2[AHEAD ? K : 1];
 #pragma unroll
   for (int i = 0; i < K; ++i) {
-    const int c = tid + i * nt;
-#pragma unroll
-    for (int e = 0; e < V; ++e) { x[i][e] = 0.f; y[i][e] = 0.f; g[i][e] = 1.f; }
-    if (c >= chunks) continue;
-    ldv<XT, V>(A.x, t * A.x_stride + (long long)c * V, x[i]);
-    if (A.y) ldv<BT, V>(A.y, t * A.y_stride + (long long)c * V, y[i]);
-    if (A.gate) ldv<BT, V>(A.gate, t * A.gate_stride + (long long)c * V, g[i]);
+    const int c = (tid + i * nt) * V;
+    xr[i].clear(); yr[i].clear(); gr[i].clear();
+    if (tid + i * nt >= chunks) continue;
+    xr[i].load(A.x, t * A.x_stride + c);
+    if (has_y) yr[i].load(A.y, t * A.y_stride + c);
+    if (has_g) gr[i].load(A.gate, t * A.gate_stride + c);
+    if (AHEAD && A.w_post) w1[i].load(A.w_post, c);
+    if (AHEAD && A.w_pre) w2[i].load(A.w_pre, c);
   }
-  if (A.y) {
-    float f = A.scale;
-    if (A.post) {
-      float q = 0.f;
-#pragma unroll
-      for (int i = 0; i < K; ++i)
-#pragma unroll
-        for (int e = 0; e < V; ++e) q = fmaf(y[i][e], y[i][e], q);
-      f *= 1.f / sqrtf(row_sum<WARP>(q, s_sum[0]) / A.d + A.eps);
-    }
-#pragma unroll
-    for (int i = 0; i < K; ++i) {
-      const int c = tid + i * nt;
-      float w[V];
-#pragma unroll
-      for (int e = 0; e < V; ++e) w[e] = f;
-      if (A.w_post && c < chunks) {
-        ldv<DT_F32, V>(A.w_post, (long long)c * V, w);
-#pragma unroll
-        for (int e = 0; e < V; ++e) w[e] *= f;
-      }
-#pragma unroll
-      for (int e = 0; e < V; ++e) x[i][e] += y[i][e] * w[e] * g[i][e];
-    }
-  }
-  if (A.x_out) {
-#pragma unroll
-    for (int i = 0; i < K; ++i)
-      if (tid + i * nt < chunks) stv<XT, V>(A.x_out, t * A.x_out_stride + (long long)(tid + i * nt) * V, x[i]);
-  }
-  if (!A.h) return;
-  float r = 1.f;
-  if (A.pre) {
+  float f = A.scale;
+  if (has_y && A.post) {
     float q = 0.f;
 #pragma unroll
-    for (int i = 0; i < K; ++i)
+    for (int i = 0; i < K; ++i) {
+      float y[V];
+      yr[i].get(y);
 #pragma unroll
-      for (int e = 0; e < V; ++e) q = fmaf(x[i][e], x[i][e], q);
-    r = 1.f / sqrtf(row_sum<WARP>(q, s_sum[1]) / A.d + A.eps);
+      for (int e = 0; e < V; ++e) q = fmaf(y[e], y[e], q);
+    }
+    f *= 1.f / sqrtf(row_sum<WARP>(q, s_sum[0]) / A.d + A.eps);
   }
+  float x[K][V], q = 0.f;
 #pragma unroll
   for (int i = 0; i < K; ++i) {
-    const int c = tid + i * nt;
-    if (c >= chunks) continue;
-    float w[V];
+    const int c = (tid + i * nt) * V;
+    const bool on = tid + i * nt < chunks;
+    xr[i].get(x[i]);
+    if (has_y) {
+      float y[V], m[V];
+      yr[i].get(y);
 #pragma unroll
-    for (int e = 0; e < V; ++e) w[e] = 1.f;
-    if (A.w_pre) ldv<DT_F32, V>(A.w_pre, (long long)c * V, w);
+      for (int e = 0; e < V; ++e) y[e] *= f;
+      if (A.w_post && on) {
+        if (!AHEAD) w1[0].load(A.w_post, c);
+        w1[AHEAD ? i : 0].get(m);
 #pragma unroll
-    for (int e = 0; e < V; ++e) x[i][e] *= r * w[e];
-    stv<BT, V>(A.h, t * A.h_stride + (long long)c * V, x[i]);
+        for (int e = 0; e < V; ++e) y[e] *= m[e];
+      }
+      if (has_g) {
+        gr[i].get(m);
+#pragma unroll
+        for (int e = 0; e < V; ++e) y[e] *= m[e];
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) x[i][e] += y[e];
+    }
+    if (A.x_out && on) stv<XT, V>(A.x_out, t * A.x_out_stride + c, x[i]);
+#pragma unroll
+    for (int e = 0; e < V; ++e) q = fmaf(x[i][e], x[i][e], q);
+  }
+  if (!A.h) return;
+  const float r = A.pre ? 1.f / sqrtf(row_sum<WARP>(q, s_sum[1]) / A.d + A.eps) : 1.f;
+#pragma unroll
+  for (int i = 0; i < K; ++i) {
+    const int c = (tid + i * nt) * V;
+    if (tid + i * nt >= chunks) continue;
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[i][e] *= r;
+    if (A.w_pre) {
+      float m[V];
+      if (!AHEAD) w2[0].load(A.w_pre, c);
+      w2[AHEAD ? i : 0].get(m);
+#pragma unroll
+      for (int e = 0; e < V; ++e) x[i][e] *= m[e];
+    }
+    stv<BT, V>(A.h, t * A.h_stride + c, x[i]);
   }
 }
 

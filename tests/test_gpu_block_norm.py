@@ -82,6 +82,12 @@ def test_row_counts(n, d):
     case(n=n, d=d, gate="token")
 
 
+@pytest.mark.parametrize("d", [40, 255, 264, 500, 1001, 4097, 5121, 16383])
+def test_many_rows(d):
+    case(n=700, d=d, gate="token")
+    case(n=601, d=d, xt="fp16", bt="fp16", pad=5, gate="channel")
+
+
 @pytest.mark.parametrize("pad,off", [(8, 0), (3, 0), (0, 1), (8, 8), (5, 3)])
 @pytest.mark.parametrize("xt,bt", [("f32", "bf16"), ("fp16", "fp16")])
 def test_strides_and_alignment(pad, off, xt, bt):
