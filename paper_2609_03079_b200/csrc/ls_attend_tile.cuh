@@ -12,7 +12,7 @@
 // A CTA has two lanes of 128 rows, each with its own score and output accumulators in tensor memory (2 x (128 + dim) columns),
 // and works on both in turn: while the tensor cores multiply for one lane, the four warps of the other do its softmax.  In a
 // pair the lanes share every key and value tile; elsewhere each lane has its own line of (unit, key tile).
-//   warp 8  copies keys, values and queries to shared memory (tensor maps, a box per page, ring of tiles);
+//   warps 8, 11  copy keys (and queries) and values to shared memory (tensor maps, a box per page, a ring of tiles each);
 //   warps 9, 10  issue S = Q K^T and O += P V of lanes 0 and 1 (P is read from tensor memory, where it overwrites S);
 //   warps 0-3, 4-7  softmax of lanes 0 and 1, one thread per row.
 // A row's reference maximum follows its true maximum only when that has risen by more than 2^8: weights stay below 2^8, the
@@ -25,7 +25,7 @@
 
 namespace ls {
 
-constexpr int AT_THREADS = 352;
+constexpr int AT_THREADS = 384;
 constexpr int AT_KEYS = 128;
 constexpr long long AT_SPIN_CLOCKS = 4000LL * 1000 * 1000;  // about two seconds
 constexpr int AT_COST_PAIR = 2, AT_COST_LANE = 1;           // of one key tile, in time of half a CTA
@@ -41,7 +41,7 @@ __device__ __forceinline__ uint32_t range_bits(int lo, int hi) {
 
 template <int D>
 struct TileShape {
-  static constexpr int STAGES = D == 128 ? 5 : 8;
+  static constexpr int KST = D == 128 ? 2 : 4, VST = D == 128 ? 3 : 4, STAGES = KST + VST;  // places for keys and for values
   static constexpr int TILE = AT_KEYS * D * 2;   // bytes of a key, value or query tile
   static constexpr int HALF = AT_KEYS * 128;     // bytes of 64 of its columns
   // weights of a narrow piece: [2 x 64 keys][32 rows] of 128 bytes, in the last rows of the lane's query buffer
@@ -342,18 +342,21 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     }
   };
   bool ok = true;
-  if (warp == 8) {
-    // ---- copies.  Order of the ring: for every round r and lane: values of round r - 1, keys of round r; a pair's once.
+  if (warp == 8 || warp == 11) {
+    // ---- copies: warp 8 keys, in rounds of a tile for each lane (a pair's once), and the queries of each piece; warp 11 values.
+    // (Lanes of a warp issue a copy each, but are served one after the other: with pages of 16 tokens a tile takes sixteen, which
+    // one warp could not issue as fast as memory brings them.)
     // A lane's tiles have barriers of their own (a place of the ring is filled now for one lane, now for the other; a lane that
     // watched both kinds of fills could be two behind and take an old one for its own); a pair's are those of lane 0.
     // Page numbers come 32 boxes at a time, one to each thread, a batch ahead: the next batch of the piece, or the first of the
     // next piece (so the walk is a piece ahead).
+    const bool keys = warp == 8;
+    const CUtensorMap* map = keys ? &map_k : &map_v;
+    const uint32_t places = keys ? TS::KST : TS::VST, base = keys ? 0 : TS::KST;
     Walk W[2];
     Piece P[2], N[2];
     bool more[2], fresh[2] = {false, false};
-    int left[2] = {0, 0}, batch[2], pages[2], pages_next[2];                               // batch: key of its first box
-    int vk0[2] = {0, 0}, vlo[2] = {0, 0}, vhi[2] = {0, 0}, vh[2] = {0, 0}, vpage[2] = {0, 0};  // tile whose values are to come
-    bool vown[2] = {false, false};
+    int left[2] = {0, 0}, batch[2], pages[2], pages_next[2];  // batch: key of its first box
     uint32_t st = 0, st_par = 1;
     Slots Q[2] = {Slots(S.batch_pieces[0], q_slots, 15), Slots(S.batch_pieces[1], q_slots, 15)};
     const int nbox = AT_KEYS / T.box, box_shift = 31 - __clz(T.box);
@@ -363,20 +366,6 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     auto page_index = [&](int key) { return page_pow2 ? key >> page_shift : key / A.page; };
     // (the prefix is read again by other rows, a sequence's own keys are not)
     const uint64_t l2_keep = l2_evict_last(), l2_once = l2_evict_first();
-    auto load_tile = [&](const CUtensorMap* map, uint32_t full, bool own, int k0, int lo, int hi, int h, int pg) {
-      const int key = k0 + my_box * T.box;
-      const bool on = my_half < D / 64 && key < hi && key + T.box > lo;
-      const int count = __popc(__ballot_sync(0xffffffffu, on));
-      if (on && (uint32_t)pg >= (uint32_t)A.n_pages) { set_status(A.status, ST_BAD_INDEX); pg = A.n_pages; }  // (reads as zeros)
-      ok = wait(b_empty + 8 * st, st_par);
-      if (!ok) return;
-      if (lane_id == 0) mb_expect(full + 8 * st, count * T.box * 128);
-      __syncwarp();
-      if (on)
-        tma_load4(ring + st * TS::TILE + my_half * TS::HALF + my_box * T.box * 128, map, my_half * 64, key - page_index(key) * A.page, h, pg, full + 8 * st,
-                  own ? l2_once : l2_keep);
-      if (++st == NST) { st = 0; st_par ^= 1; }
-    };
     auto fetch_pages = [&](const Piece& p, int key) {  // (no branch around the load: nothing waits for it here)
       key += lane_id * T.box;
       const bool on = key < p.hi && key + T.box > p.lo;
@@ -402,10 +391,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     };
     auto step = [&](auto lc, int r, int cnt) {
       constexpr int l = decltype(lc)::value;
-      if (r > 0 && r <= cnt && !(r <= n_pair && l == 1)) load_tile(&map_v, b_full + (r > n_pair ? 8 * NST * l : 0), vown[l], vk0[l], vlo[l], vhi[l], vh[l], vpage[l]);
-      if (!ok || r >= cnt) return;
+      if (r >= cnt) return;
       const bool own = P[l].kind == AT_OWN;
-      if (fresh[l]) {
+      if (keys && fresh[l]) {
         const uint32_t slot = Q[l].slot;
         ok = wait(b_qempty + 32 * l + 8 * slot, Q[l].parity());
         if (!ok) return;
@@ -421,11 +409,22 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         __syncwarp();
       }
       if (!(r < n_pair && l == 1)) {
-        const int page = __shfl_sync(0xffffffffu, pages[l], ((P[l].k0 - batch[l]) >> box_shift) + my_box);
-        vown[l] = own; vk0[l] = P[l].k0; vlo[l] = P[l].lo; vhi[l] = P[l].hi; vh[l] = P[l].h; vpage[l] = page;
-        load_tile(&map_k, b_full + (r >= n_pair ? 8 * NST * l : 0), own, P[l].k0, P[l].lo, P[l].hi, P[l].h, page);
+        int page = __shfl_sync(0xffffffffu, pages[l], ((P[l].k0 - batch[l]) >> box_shift) + my_box);
+        const int key = P[l].k0 + my_box * T.box;
+        const bool on = my_half < D / 64 && key < P[l].hi && key + T.box > P[l].lo;
+        const int count = __popc(__ballot_sync(0xffffffffu, on));
+        if (on && (uint32_t)page >= (uint32_t)A.n_pages) { set_status(A.status, ST_BAD_INDEX); page = A.n_pages; }  // (reads as zeros)
+        const uint32_t place = base + st, full = b_full + 8 * (place + (r >= n_pair ? NST * l : 0));
+        ok = wait(b_empty + 8 * place, st_par);
+        if (!ok) return;
+        if (lane_id == 0) mb_expect(full, count * T.box * 128);
+        __syncwarp();
+        if (on)
+          tma_load4(ring + place * TS::TILE + my_half * TS::HALF + my_box * T.box * 128, map, my_half * 64, key - page_index(key) * A.page, P[l].h, page, full,
+                    own ? l2_once : l2_keep);
+        if (++st == places) { st = 0; st_par ^= 1; }
       }
-      if (ok) advance(lc);
+      advance(lc);
     };
     auto begin = [&](auto lc) {
       constexpr int l = decltype(lc)::value;
@@ -439,7 +438,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     advance(Lane0{});
     advance(Lane1{});
     const int rounds = max(cnt0, cnt1);
-    for (int r = 0; ok && r <= rounds; ++r) {
+    for (int r = 0; ok && r < rounds; ++r) {
       step(Lane0{}, r, cnt0);
       if (ok) step(Lane1{}, r, cnt1);
     }
@@ -462,11 +461,12 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     int left = 0, k0 = 0, lo = 0, hi = 0;   // of the current piece: tiles to come, first key of the next; keys of anybody
     int narrow = 0, vk0 = 0, vlo = 0, vhi = 0, vnarrow = 0;  // v*: of the tile whose values are still to be multiplied
     bool vfresh = true;
-    uint32_t q_slot = 0, st = 0, par0 = 0, par1 = 0;  // par*: parity of each place's next fill, by set of barriers
+    uint32_t q_slot = 0, kst = 0, vst = 0, par0 = 0, par1 = 0;  // par*: parity of each place's next fill, by set of barriers
     for (int r = 0; r <= cnt; ++r) {
-      // places in the ring: values and keys of lane 0, then of lane 1 where they are not a pair's
+      // places in the rings: lane 0's tile, then lane 1's, a pair's once
       const bool vpair = r <= n_pair, kpair = r < n_pair;
-      const uint32_t v0 = r > 0 && r <= cnt0, f0 = r < cnt0, v1 = r > 0 && r <= cnt1 && !vpair, f1 = r < cnt1 && !kpair;
+      const uint32_t kplace = kst + (l == 1 && !kpair && r < cnt0), vplace = vst + (l == 1 && !vpair && r <= cnt0);
+      const uint32_t kslot = kplace >= TS::KST ? kplace - TS::KST : kplace, vslot = TS::KST + (vplace >= TS::VST ? vplace - TS::VST : vplace);
       auto filled = [&](uint32_t slot, bool pair) -> bool {
         const bool set0 = pair || l == 0;
         const uint32_t par = set0 ? par0 : par1;
@@ -478,8 +478,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       };
       bool kfresh = false;
       auto scores = [&]() -> bool {
-        uint32_t slot = st + (kpair || l == 0 ? v0 : v0 + f0 + v1);
-        if (slot >= NST) slot -= NST;
+        const uint32_t slot = kslot;
         kfresh = left == 0;
         if (kfresh) {
           q_slot = Q.slot;
@@ -508,8 +507,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         return true;
       };
       auto outputs = [&]() -> bool {
-        uint32_t slot = st + (l == 0 || vpair ? 0 : v0 + f0);
-        if (slot >= NST) slot -= NST;
+        const uint32_t slot = vslot;
         if (!filled(slot, vpair)) return false;
         if (vk0 < vlo || vk0 + AT_KEYS > vhi) {
           for (int c = lane_id; c < AT_KEYS; c += 32) {
@@ -546,9 +544,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       // wide tile, whose weights they would overwrite.
       bool scores_first = r > 0 && vnarrow && r < cnt;
       if (scores_first) {
-        uint32_t slot = st + (l == 0 ? v0 : v0 + f0 + v1);
-        if (slot >= NST) slot -= NST;
-        scores_first = mb_test(b_full + 8 * (l ? NST + slot : slot), ((l ? par1 : par0) >> slot) & 1);
+        scores_first = mb_test(b_full + 8 * (l ? NST + kslot : kslot), ((l ? par1 : par0) >> kslot) & 1);
         if (left == 0) scores_first = scores_first && mb_test(b_qfull + 32 * l + 8 * Q.slot, Q.parity());
         scores_first = __all_sync(0xffffffffu, scores_first);
       }
@@ -561,8 +557,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       vk0 = k0; vlo = lo; vhi = hi; vnarrow = narrow; vfresh = kfresh;
       k0 += AT_KEYS;
       if (r <= n_pair && elect_one()) mb_arrive(b_turn + 8 * (1 - l));
-      st += v0 + f0 + v1 + f1;
-      if (st >= NST) st -= NST;
+      kst += (r < cnt0) + (r < cnt1 && !kpair);
+      if (kst >= TS::KST) kst -= TS::KST;
+      if (r > 0) vst += (r <= cnt0) + (r <= cnt1 && !vpair);
+      if (vst >= TS::VST) vst -= TS::VST;
     }
     // every arrival that the tensor cores owe this block has come when the last one has
     if (elect_one()) tm_commit(b_done + 8 * l);
