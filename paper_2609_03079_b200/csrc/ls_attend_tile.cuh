@@ -18,8 +18,6 @@
 // A row's reference maximum follows its true maximum only when that has risen by more than 2^8: weights stay below 2^8, the
 // final division makes the reference irrelevant, and the accumulator in tensor memory is almost never rescaled.
 #pragma once
-#include <type_traits>
-
 #include "ls_attend.cuh"
 #include "ls_tmem.cuh"
 
@@ -85,9 +83,6 @@ struct Share {
   OwnKeys own_k[2];                   // ... and that sequence's keys
   int batch_pieces[2];                // pieces of each lane that are not of own units (they come first)
 };
-
-using Lane0 = std::integral_constant<int, 0>;
-using Lane1 = std::integral_constant<int, 1>;
 
 // A piece: consecutive tiles of one unit on one lane.  The copying warp walks the line and leaves each piece here, with its
 // queries, for the warps that multiply and the ones that do the softmax.
@@ -255,6 +250,26 @@ __device__ __forceinline__ void make_share(const TileArgs& T, Share& S, int* s_s
   }
 }
 
+// (Out of line, like everything that is not on the way of every tile: a CTA's warps run six different programs, and what does not
+// stay in the instruction cache is fetched through a memory system that the copies keep saturated.)
+__device__ __forceinline__ bool tile_wait(uint32_t bar, uint32_t parity, volatile int* dead, int* status) {
+  const long long t0 = clock64();
+  bool got;
+  while (!(got = mb_try(bar, parity))) {
+    if (*dead) break;
+    if (clock64() - t0 > AT_SPIN_CLOCKS) { *dead = 1; set_status(status, ST_TIMEOUT); break; }
+  }
+  return __all_sync(0xffffffffu, got);
+}
+
+// What a copying warp knows of a lane.
+struct Feed {
+  Walk w;
+  Piece p, next;     // the piece of the current tile, and the one behind it
+  int left, batch;   // tiles behind the current one; key of the first box whose page number is at hand
+  int more, fresh;   // `next` is one; the current tile is the first of its piece
+};
+
 // Control block of a CTA, behind the tiles in shared memory.
 template <int NST>
 struct TileCtl {
@@ -264,13 +279,14 @@ struct TileCtl {
   Piece piece[2][4];
   float red[2][4][AT_NARROW]; // narrow pieces: maxima or sums of each warp's keys
   int lo[2][AT_NARROW], hi[2][AT_NARROW];  // ... keys of each row, relative to the piece's first
+  Feed feed[2][2];            // of the warps that copy keys and values, for each lane
   uint32_t tmem;
   volatile int dead;
 };
 
 template <int WD, int D>
 __global__ void __launch_bounds__(AT_THREADS, 1)
-    ls_attend_tile_kernel(const TileArgs T, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+    ls_attend_tile_kernel(const __grid_constant__ TileArgs T, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                           const __grid_constant__ CUtensorMap map_q_all, const __grid_constant__ CUtensorMap map_q_own) {
   using TS = TileShape<D>;
   constexpr int NST = TS::STAGES;
@@ -310,15 +326,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
 
   // Bounded wait of a whole warp: false (for all of it) once any wait of the CTA has given up.
   auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
-    bool got = mb_try(bar, parity);
-    if (!got) {
-      const long long t0 = clock64();
-      while (!(got = mb_try(bar, parity))) {
-        if (C.dead) break;
-        if (clock64() - t0 > AT_SPIN_CLOCKS) { C.dead = 1; set_status(A.status, ST_TIMEOUT); break; }
-      }
-    }
-    return __all_sync(0xffffffffu, got);
+    if (__all_sync(0xffffffffu, mb_try(bar, parity))) return true;
+    return tile_wait(bar, parity, &C.dead, A.status);
   };
 
   // Tiles of the lanes; the first n_pair of both are pairs.
@@ -353,12 +362,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     const bool keys = warp == 8;
     const CUtensorMap* map = keys ? &map_k : &map_v;
     const uint32_t places = keys ? TS::KST : TS::VST, base = keys ? 0 : TS::KST;
-    Walk W[2];
-    Piece P[2], N[2];
-    bool more[2], fresh[2] = {false, false};
-    int left[2] = {0, 0}, batch[2], pages[2], pages_next[2];  // batch: key of its first box
+    Feed* const feeds = C.feed[keys ? 0 : 1];
+    int pages0 = 0, pages1 = 0, next0 = 0, next1 = 0;  // page numbers of the two lanes: this batch, the next one
     uint32_t st = 0, st_par = 1;
-    Slots Q[2] = {Slots(S.batch_pieces[0], q_slots, 15), Slots(S.batch_pieces[1], q_slots, 15)};
+    Slots Q0(S.batch_pieces[0], q_slots, 15), Q1(S.batch_pieces[1], q_slots, 15);
     const int nbox = AT_KEYS / T.box, box_shift = 31 - __clz(T.box);
     const int my_box = lane_id & (nbox - 1), my_half = lane_id / nbox;
     const bool page_pow2 = (A.page & (A.page - 1)) == 0;
@@ -372,75 +379,80 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       const int32_t* tab = p.kind == AT_OWN ? A.table + (long long)(A.q_len == 1 ? p.tok : p.tok / A.q_len) * A.table_stride : A.prefix_pages;
       return *(on ? tab + page_index(key) : A.seq_len);
     };
-    auto advance = [&](auto lc) {  // to the next tile
-      constexpr int l = decltype(lc)::value;
-      fresh[l] = left[l] == 0;
-      if (!fresh[l]) { --left[l]; P[l].k0 += AT_KEYS; }
-      else {
-        if (!more[l]) return;
-        P[l] = N[l];
-        left[l] = P[l].tiles - 1;
-        more[l] = walk_next(T, S, l, W[l], N[l]);
+    auto advance = [&](int l) {  // to the next tile (the first call only brings up the first piece)
+      Feed& F = feeds[l];
+      const bool fresh = F.left == 0;
+      if (fresh && !F.more) return;
+      __syncwarp();
+      if (lane_id == 0) {
+        F.fresh = fresh;
+        if (!fresh) { --F.left; F.p.k0 += AT_KEYS; }
+        else {
+          F.p = F.next;
+          F.left = max(F.p.tiles - 1, 0);
+          F.more = walk_next(T, S, l, F.w, F.next);
+        }
       }
-      if (!fresh[l] && P[l].k0 < batch[l] + 32 * T.box) return;
-      pages[l] = pages_next[l];
-      batch[l] = P[l].k0;
-      const int next = batch[l] + 32 * T.box;
-      if (next < P[l].k0 + (left[l] + 1) * AT_KEYS) pages_next[l] = fetch_pages(P[l], next);
-      else if (more[l]) pages_next[l] = fetch_pages(N[l], N[l].k0);
+      __syncwarp();
+      if (!fresh && F.p.k0 < F.batch + 32 * T.box) return;
+      const int k0 = F.p.k0, next = k0 + 32 * T.box;
+      const bool same = F.p.tiles > 0 && next < k0 + (F.left + 1) * AT_KEYS;
+      const int got = same || F.more ? fetch_pages(same ? F.p : F.next, same ? next : F.next.k0) : 0;
+      if (l) { pages1 = next1; next1 = got; }
+      else { pages0 = next0; next0 = got; }
+      __syncwarp();
+      if (lane_id == 0) F.batch = k0;
+      __syncwarp();
     };
-    auto step = [&](auto lc, int r, int cnt) {
-      constexpr int l = decltype(lc)::value;
-      if (r >= cnt) return;
-      const bool own = P[l].kind == AT_OWN;
-      if (keys && fresh[l]) {
-        const uint32_t slot = Q[l].slot;
-        ok = wait(b_qempty + 32 * l + 8 * slot, Q[l].parity());
-        if (!ok) return;
-        Q[l].next();
+    if (lane_id < 2) {
+      Feed& F = feeds[lane_id];
+      walk_start(S, F.w);
+      F.p.tiles = F.next.tiles = F.next.k0 = F.left = F.batch = 0;
+      F.more = 1;
+    }
+    __syncwarp();
+#pragma unroll 1
+    for (int x = 0; x < 4; ++x) advance(x & 1);
+    const int last = 2 * max(cnt0, cnt1);
+#pragma unroll 1
+    for (int x = 0; ok && x < last; ++x) {
+      const int l = x & 1, r = x >> 1;
+      if (r >= (l ? cnt1 : cnt0)) continue;
+      const Feed& F = feeds[l];
+      const bool own = F.p.kind == AT_OWN;
+      if (keys && F.fresh) {
+        const uint32_t slot = l ? Q1.slot : Q0.slot;
+        ok = wait(b_qempty + 32 * l + 8 * slot, l ? Q1.parity() : Q0.parity());
+        if (!ok) break;
+        if (l) Q1.next();
+        else Q0.next();
         if (lane_id == 0) {
-          C.piece[l][slot] = P[l];
+          C.piece[l][slot] = F.p;
           const uint32_t full = b_qfull + 32 * l + 8 * slot;
           mb_expect(full, (own ? T.ts : T.tb) * A.group * D * 2);
 #pragma unroll
           for (int f = 0; f < D / 64; ++f)
-            tma_load3(q_base + l * TS::TILE + f * TS::HALF + slot * q_step, own ? &map_q_own : &map_q_all, f * 64, P[l].h * A.group, P[l].tok, full);
+            tma_load3(q_base + l * TS::TILE + f * TS::HALF + slot * q_step, own ? &map_q_own : &map_q_all, f * 64, F.p.h * A.group, F.p.tok, full);
         }
         __syncwarp();
       }
       if (!(r < n_pair && l == 1)) {
-        int page = __shfl_sync(0xffffffffu, pages[l], ((P[l].k0 - batch[l]) >> box_shift) + my_box);
-        const int key = P[l].k0 + my_box * T.box;
-        const bool on = my_half < D / 64 && key < P[l].hi && key + T.box > P[l].lo;
+        int page = __shfl_sync(0xffffffffu, l ? pages1 : pages0, ((F.p.k0 - F.batch) >> box_shift) + my_box);
+        const int key = F.p.k0 + my_box * T.box;
+        const bool on = my_half < D / 64 && key < F.p.hi && key + T.box > F.p.lo;
         const int count = __popc(__ballot_sync(0xffffffffu, on));
         if (on && (uint32_t)page >= (uint32_t)A.n_pages) { set_status(A.status, ST_BAD_INDEX); page = A.n_pages; }  // (reads as zeros)
         const uint32_t place = base + st, full = b_full + 8 * (place + (r >= n_pair ? NST * l : 0));
         ok = wait(b_empty + 8 * place, st_par);
-        if (!ok) return;
+        if (!ok) break;
         if (lane_id == 0) mb_expect(full, count * T.box * 128);
         __syncwarp();
         if (on)
-          tma_load4(ring + place * TS::TILE + my_half * TS::HALF + my_box * T.box * 128, map, my_half * 64, key - page_index(key) * A.page, P[l].h, page, full,
+          tma_load4(ring + place * TS::TILE + my_half * TS::HALF + my_box * T.box * 128, map, my_half * 64, key - page_index(key) * A.page, F.p.h, page, full,
                     own ? l2_once : l2_keep);
         if (++st == places) { st = 0; st_par ^= 1; }
       }
-      advance(lc);
-    };
-    auto begin = [&](auto lc) {
-      constexpr int l = decltype(lc)::value;
-      walk_start(S, W[l]);
-      more[l] = walk_next(T, S, l, W[l], N[l]);
-      batch[l] = 0;
-      pages[l] = pages_next[l] = more[l] ? fetch_pages(N[l], N[l].k0) : 0;
-    };
-    begin(Lane0{});
-    begin(Lane1{});
-    advance(Lane0{});
-    advance(Lane1{});
-    const int rounds = max(cnt0, cnt1);
-    for (int r = 0; ok && r < rounds; ++r) {
-      step(Lane0{}, r, cnt0);
-      if (ok) step(Lane1{}, r, cnt1);
+      advance(l);
     }
   } else if (warp >= 9) {
     // ---- products of one lane, issued by one thread.  Wide tiles: O += P V of round r - 1, then S = Q K^T of round r, which
@@ -549,10 +561,12 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         scores_first = __all_sync(0xffffffffu, scores_first);
       }
       bool good = true;
-      if (scores_first) good = scores();
-      if (good && r > 0) good = outputs();
-      if (r == 0 && l == 1 && n_pair > 0 && good) good = wait(b_turn + 8, 0);
-      if (good && r < cnt && !scores_first) good = scores();
+      if (r == 0 && l == 1 && n_pair > 0) good = wait(b_turn + 8, 0);
+#pragma unroll 1
+      for (int x = 0; x < 2 && good; ++x) {
+        if ((x == 0) == scores_first) { if (r < cnt) good = scores(); }
+        else if (r > 0) good = outputs();
+      }
       if (!good) break;
       vk0 = k0; vlo = lo; vhi = hi; vnarrow = narrow; vfresh = kfresh;
       k0 += AT_KEYS;
