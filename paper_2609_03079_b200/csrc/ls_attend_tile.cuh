@@ -784,7 +784,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
           // quarter go over scores that are in registers or done with.
           uint32_t s0[32], s1[32];
           float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
+#pragma unroll 1
           for (int half = 1; half >= 0; --half) {
             tm_ld32(t_s + 64 * half, s0);
             tm_ld32(t_s + 64 * half + 32, s1);
@@ -818,7 +818,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
             if (j > 0) {
               wait(b_o + 8 * l, (n - 1) & 1);
               tm_fence_after();
-#pragma unroll
+#pragma unroll 1
               for (int c = 0; c < D / 32; ++c) {
                 uint32_t o[32];
                 tm_ld32(t_o + 32 * c, o);
@@ -832,20 +832,19 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
           }
           const float off = m == -INFINITY ? 0.f : -m * scale;
           const uint64_t off2 = both(off);
-          weights(s0, off2);
-          tm_st16(t_s, s0);
-          tm_ld32(t_s + 64, s0);
-          weights(s1, off2);
-          tm_st16(t_s + 16, s1);
-          tm_wait_ld();
-          tm_pin32(s0);
-          tm_ld32(t_s + 96, s1);
-          weights(s0, off2);
-          tm_st16(t_s + 32, s0);
-          tm_wait_ld();
-          tm_pin32(s1);
-          weights(s1, off2);
-          tm_st16(t_s + 48, s1);
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            weights(s0, off2);
+            tm_st16(t_s + 32 * half, s0);
+            if (half == 0) tm_ld32(t_s + 64, s0);
+            weights(s1, off2);
+            tm_st16(t_s + 32 * half + 16, s1);
+            if (half == 1) break;
+            tm_ld32(t_s + 96, s1);
+            tm_wait_ld();
+            tm_pin32(s0);
+            tm_pin32(s1);
+          }
           const uint64_t acc_all = add2(acc[0], acc[1]);
           sum += lo32(acc_all) + hi32(acc_all);
           tm_wait_st();
@@ -860,7 +859,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       if (warp_live) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         if (live) pl[at] = sum == 0.f ? -INFINITY : fmaf(m, scale, log2f(sum));
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < D / 32; ++c) {
           uint32_t o[32];
           tm_ld32(t_o + 32 * c, o);
