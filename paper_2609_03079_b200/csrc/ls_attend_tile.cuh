@@ -61,6 +61,13 @@ struct TileArgs {
   int32_t workers;   // two per CTA
 };
 
+// a / b for a >= 0, b > 0 and a quotient below 2^22 (then the estimate is off by one at most).
+__device__ __forceinline__ int quotient(int a, int b) {
+  int q = (int)((float)a * __frcp_rn((float)b));
+  const int r = a - q * b;
+  return r < 0 ? q - 1 : r >= b ? q + 1 : q;
+}
+
 // The keys of sequence b that are its own: [lo, hi) is what any of its tokens sees, tiles start at `origin`.
 struct OwnKeys { int lo, hi, origin, tiles; };
 __device__ __forceinline__ OwnKeys own_keys(const TileArgs& T, int len) {
@@ -123,7 +130,7 @@ __device__ __forceinline__ bool walk_next(const TileArgs& T, const Share& S, int
   }
   if (W.w >= W.end) return false;
   if (W.pairs || W.b < 0) {
-    P.unit = W.w / S.pre_tiles;
+    P.unit = quotient(W.w, S.pre_tiles);
     const int tile = W.w - P.unit * S.pre_tiles;
     P.tiles = min(S.pre_tiles - tile, W.end - W.w);
     P.ends = (tile == 0 ? 1 : 0) | (tile + P.tiles == S.pre_tiles ? 2 : 0);
@@ -132,7 +139,7 @@ __device__ __forceinline__ bool walk_next(const TileArgs& T, const Share& S, int
     if (W.pairs) {
       P.kind = AT_PAIR;
       P.narrow = 0;
-      P.h = P.unit / T.pairs;
+      P.h = quotient(P.unit, T.pairs);
       P.tok = ((P.unit - P.h * T.pairs) * 2 + lane) * T.tq;
     } else {
       P.kind = AT_SINGLE;
@@ -205,8 +212,8 @@ __device__ __forceinline__ void make_share(const TileArgs& T, Share& S, int* s_s
   // Pieces of a unit have to be on consecutive workers: no worker between the first and the last may be empty, so that little
   // work goes to fewer CTAs, each with a tile for both lanes.
   const int used = max(1, min(n, cost / max(AT_COST_PAIR, 2 * AT_COST_LANE)));
-  const int base = cost / used, rest = cost - base * used;  // CTA c takes the costs from c * base + c * rest / used on
-  auto start = [&](int i) { i = min(i, used); return i * base + (int)((unsigned)(i * rest) / (unsigned)used); };
+  const int base = quotient(cost, used), rest = cost - base * used;  // CTA c takes the costs from c * base + c * rest / used on
+  auto start = [&](int i) { i = min(i, used); return i * base + quotient(i * rest, used); };
   const int x0 = start(c), x1 = start(c + 1);
   auto pair_at = [&](int x) { return min(n_pair, (x + AT_COST_PAIR - 1) / AT_COST_PAIR); };
   auto lane_at = [&](int x) {
@@ -217,12 +224,12 @@ __device__ __forceinline__ void make_share(const TileArgs& T, Share& S, int* s_s
   if (tid == 0) {
     S.pre_lo = lo; S.pre_origin = origin; S.pre_tiles = pre_tiles;
     S.pair0 = pair_at(x0); S.pair1 = pair_at(x1);
-    const int pp = S.pair1 > S.pair0 ? (S.pair1 - 1) / pre_tiles - S.pair0 / pre_tiles + 1 : 0;
+    const int pp = S.pair1 > S.pair0 ? quotient(S.pair1 - 1, pre_tiles) - quotient(S.pair0, pre_tiles) + 1 : 0;
     for (int l = 0; l < 2; ++l) {
       const int from = l ? mid : g0, to = min(l ? g1 : mid, n_single);
       S.lane0[l] = from; S.lane1[l] = l ? g1 : mid;
       if (from < n_single) S.own_b[l] = -1;
-      S.batch_pieces[l] = pp + (to > from ? (to - 1) / pre_tiles - from / pre_tiles + 1 : 0);
+      S.batch_pieces[l] = pp + (to > from ? quotient(to - 1, pre_tiles) - quotient(from, pre_tiles) + 1 : 0);
     }
   }
   // Own units stand head by head, so that workers at the same place of their heads read neighbouring rows of the same tokens.
@@ -230,7 +237,7 @@ __device__ __forceinline__ void make_share(const TileArgs& T, Share& S, int* s_s
   for (int l = 0; l < 2; ++l) {   // the thread whose sequences hold the start of a lane's range finds it
     const int w = (l ? mid : g0) - n_single;
     if (w < 0 || line == 0) continue;
-    const int h = w / line, at = w - h * line;
+    const int h = quotient(w, line), at = w - h * line;
     int acc = before * T.rt;
     if (at < acc || at >= acc + sum * T.rt) continue;
 #pragma unroll 1
@@ -241,7 +248,7 @@ __device__ __forceinline__ void make_share(const TileArgs& T, Share& S, int* s_s
         S.own_h[l] = h;
         S.own_b[l] = b;
         S.own_k[l] = k;
-        S.own_r[l] = (at - acc) / t;
+        S.own_r[l] = quotient(at - acc, t);
         S.own_t[l] = (at - acc) - S.own_r[l] * t;
         break;
       }
@@ -268,6 +275,7 @@ struct Feed {
   Piece p, next;     // the piece of the current tile, and the one behind it
   int left, batch;   // tiles behind the current one; key of the first box whose page number is at hand
   int more, fresh;   // `next` is one; the current tile is the first of its piece
+  int turn, same, key;  // the next batch of page numbers becomes the current one; the one to fetch: of this piece?, its first key
 };
 
 // Control block of a CTA, behind the tiles in shared memory.
@@ -379,30 +387,39 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       const int32_t* tab = p.kind == AT_OWN ? A.table + (long long)(A.q_len == 1 ? p.tok : p.tok / A.q_len) * A.table_stride : A.prefix_pages;
       return *(on ? tab + page_index(key) : A.seq_len);
     };
-    auto advance = [&](int l) {  // to the next tile (the first call only brings up the first piece)
-      Feed& F = feeds[l];
-      const bool fresh = F.left == 0;
-      if (fresh && !F.more) return;
+    // Both lanes go on to their next tile, a thread for each (the first call only brings up the first pieces).
+    auto advance = [&]() {
       __syncwarp();
-      if (lane_id == 0) {
-        F.fresh = fresh;
-        if (!fresh) { --F.left; F.p.k0 += AT_KEYS; }
-        else {
+      if (lane_id < 2) {
+        Feed& F = feeds[lane_id];
+        F.fresh = F.left == 0;
+        F.turn = 0;
+        if (!F.fresh) {
+          --F.left;
+          F.p.k0 += AT_KEYS;
+          F.turn = F.p.k0 >= F.batch + 32 * T.box;
+        } else if (F.more) {
           F.p = F.next;
           F.left = max(F.p.tiles - 1, 0);
-          F.more = walk_next(T, S, l, F.w, F.next);
+          F.more = walk_next(T, S, lane_id, F.w, F.next);
+          F.turn = 1;
+        }
+        if (F.turn) {
+          F.batch = F.p.k0;
+          F.key = F.batch + 32 * T.box;
+          F.same = F.p.tiles > 0 && F.key < F.p.k0 + (F.left + 1) * AT_KEYS;
+          if (!F.same) F.key = F.next.k0;
         }
       }
       __syncwarp();
-      if (!fresh && F.p.k0 < F.batch + 32 * T.box) return;
-      const int k0 = F.p.k0, next = k0 + 32 * T.box;
-      const bool same = F.p.tiles > 0 && next < k0 + (F.left + 1) * AT_KEYS;
-      const int got = same || F.more ? fetch_pages(same ? F.p : F.next, same ? next : F.next.k0) : 0;
-      if (l) { pages1 = next1; next1 = got; }
-      else { pages0 = next0; next0 = got; }
-      __syncwarp();
-      if (lane_id == 0) F.batch = k0;
-      __syncwarp();
+      if (feeds[0].turn) {
+        pages0 = next0;
+        next0 = feeds[0].same || feeds[0].more ? fetch_pages(feeds[0].same ? feeds[0].p : feeds[0].next, feeds[0].key) : 0;
+      }
+      if (feeds[1].turn) {
+        pages1 = next1;
+        next1 = feeds[1].same || feeds[1].more ? fetch_pages(feeds[1].same ? feeds[1].p : feeds[1].next, feeds[1].key) : 0;
+      }
     };
     if (lane_id < 2) {
       Feed& F = feeds[lane_id];
@@ -410,14 +427,11 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       F.p.tiles = F.next.tiles = F.next.k0 = F.left = F.batch = 0;
       F.more = 1;
     }
-    __syncwarp();
 #pragma unroll 1
-    for (int x = 0; x < 4; ++x) advance(x & 1);
-    const int last = 2 * max(cnt0, cnt1);
-#pragma unroll 1
-    for (int x = 0; ok && x < last; ++x) {
+    for (int x = -2; x < 2 * max(cnt0, cnt1); ++x) {
       const int l = x & 1, r = x >> 1;
-      if (r >= (l ? cnt1 : cnt0)) continue;
+      if (l == 0) advance();
+      if (x < 0 || r >= (l ? cnt1 : cnt0)) continue;
       const Feed& F = feeds[l];
       const bool own = F.p.kind == AT_OWN;
       if (keys && F.fresh) {
@@ -452,7 +466,6 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
                     own ? l2_once : l2_keep);
         if (++st == places) { st = 0; st_par ^= 1; }
       }
-      advance(l);
     }
   } else if (warp >= 9) {
     // ---- products of one lane, issued by one thread.  Wide tiles: O += P V of round r - 1, then S = Q K^T of round r, which
@@ -596,7 +609,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     };
     // Keys [lo, hi) that row x of a piece sees, relative to the piece's first.
     auto row_keys = [&](const Piece& P, int x, int& lo, int& hi) {
-      const int t = P.tok + (P.ntok == 1 ? 0 : x / A.group), b = A.q_len == 1 ? t : t / A.q_len;
+      const int t = P.tok + (P.ntok == 1 ? 0 : quotient(x, A.group)), b = A.q_len == 1 ? t : quotient(t, A.q_len);
       // (an own unit's last key is its sequence's last)
       hi = max((P.kind == AT_OWN ? P.hi : attend_len(A, b, false)) - A.q_len + (t - b * A.q_len) + 1, 0);
       lo = A.window > 0 ? max(hi - A.window, 0) : 0;
@@ -759,7 +772,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       if (lane_id == 0) mb_arrive(b_qempty + 32 * l + 8 * slot);
       if (P.narrow) { narrow_piece(P); continue; }
       // Wide pieces: one thread per row.
-      const bool live = row / A.group < P.ntok, warp_live = __any_sync(0xffffffffu, live);
+      const bool live = row < P.ntok * A.group, warp_live = __any_sync(0xffffffffu, live);
       int lo = 0, hi = 0x7fffffff;  // keys this row sees, relative to the tile
       if (live) row_keys(P, row, lo, hi);
       float m = -INFINITY, sum = 0.f;
