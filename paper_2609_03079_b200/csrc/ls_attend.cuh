@@ -48,32 +48,8 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 __device__ __forceinline__ float lo32(uint64_t x) { return __uint_as_float((uint32_t)x); }
 __device__ __forceinline__ float hi32(uint64_t x) { return __uint_as_float((uint32_t)(x >> 32)); }
-// 2^x of two values on the multiply-add units (the special function unit does 4 exponentials a cycle and quarter of an SM, a
-// quarter of what a softmax of 128 x 128 scores needs next to its matrix products).  x = n + f, n the nearest integer, f in
-// [-1/2, 1/2]: 2^f by a polynomial of degree 5 whose largest relative error on that range was minimised (Remez exchange, 7.5e-8;
-// 2.3e-7 with fp32 evaluation), 2^n by the exponent field.  Below 2^-126 the result is 0; NaN stays NaN; x < 127.
-__device__ __forceinline__ uint64_t ex2_poly2(uint64_t x) {
-  float a, b;
-  asm("max.NaN.f32 %0, %1, 0fC2FE0000;" : "=f"(a) : "f"(lo32(x)));  // -127
-  asm("max.NaN.f32 %0, %1, 0fC2FE0000;" : "=f"(b) : "f"(hi32(x)));
-  x = pair32(__float_as_uint(a), __float_as_uint(b));
-  const uint64_t t = add2(x, both(12582912.f));                   // 1.5 * 2^23: the low bits hold n
-  const uint64_t f = fma2(add2(t, both(-12582912.f)), both(-1.f), x);
-  uint64_t p = fma2(both(1.3276472454890609e-3f), f, both(9.675540961325169e-3f));
-  p = fma2(p, f, both(5.550713092088699e-2f));
-  p = fma2(p, f, both(2.4022120237350464e-1f));
-  p = fma2(p, f, both(6.931469440460205e-1f));
-  p = fma2(p, f, both(1.0000001192092896f));
-  const uint32_t e0 = ((uint32_t)t << 23) + 0x3f800000u, e1 = ((uint32_t)(t >> 32) << 23) + 0x3f800000u;
-  return mul2(p, pair32(e0, e1));
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));

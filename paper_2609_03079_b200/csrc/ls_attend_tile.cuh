@@ -28,8 +28,6 @@ constexpr int AT_KEYS = 128;
 constexpr long long AT_SPIN_CLOCKS = 4000LL * 1000 * 1000;  // about two seconds
 constexpr int AT_COST_PAIR = 2, AT_COST_LANE = 1;           // of one key tile, in time of half a CTA
 
-constexpr int AT_POLY = 4;  // of 16 pairs of weights, how many are computed by ex2_poly2
-
 // The bits [lo, hi) of a word, as far as they lie in it.
 __device__ __forceinline__ uint32_t range_bits(int lo, int hi) {
   const int a = min(max(lo, 0), 32), b = min(max(hi, 0), 32);
@@ -787,9 +785,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
 #pragma unroll
             for (int c = 0; c < 32; c += 2) {
               const uint64_t x = fma2(pair32(s[c], s[c + 1]), scale2, off2);
-              const uint64_t p = (c / 2) % 16 * AT_POLY % 16 < AT_POLY ? ex2_poly2(x) : pair32(__float_as_uint(ex2(lo32(x))), __float_as_uint(ex2(hi32(x))));
-              acc[(c / 2) & 1] = add2(acc[(c / 2) & 1], p);
-              s[c / 2] = pack2<WD>(lo32(p), hi32(p));
+              const float p0 = ex2(lo32(x)), p1 = ex2(hi32(x));
+              acc[(c / 2) & 1] = add2(acc[(c / 2) & 1], pair32(__float_as_uint(p0), __float_as_uint(p1)));
+              s[c / 2] = pack2<WD>(p0, p1);
             }
           };
           // Two passes over the scores: the maximum (all four quarters of the columns), then the weights.  The quarters 0 and 1 stay in
