@@ -253,7 +253,7 @@ int32_t launch_norm(const ls::NormArgs& a, cudaStream_t st) {
     if (chunks <= 256 || (a.n < kNormManyRows && chunks <= 1024)) return norm_blocks<XT, BT, 8, 1>(a, st);
     return norm_blocks<XT, BT, 8, 2>(a, st);
   }
-  if (a.n >= kNormManyRows) {
+  if (a.n >= kNormManyRows / 2) {
     if (a.d <= 256) return norm_warps<XT, BT, 1, 8>(a, st);
     if (a.d <= 4096) return norm_blocks<XT, BT, 1, 8>(a, st);
     return norm_blocks<XT, BT, 1, 16>(a, st);

@@ -385,51 +385,58 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       const int32_t* tab = p.kind == AT_OWN ? A.table + (long long)(A.q_len == 1 ? p.tok : p.tok / A.q_len) * A.table_stride : A.prefix_pages;
       return *(on ? tab + page_index(key) : A.seq_len);
     };
-    // Both lanes go on to their next tile, a thread for each (the first call only brings up the first pieces).
+    // Both lanes go on to their next tile, a thread for each ...
     auto advance = [&]() {
       __syncwarp();
       if (lane_id < 2) {
         Feed& F = feeds[lane_id];
-        F.fresh = F.left == 0;
-        F.turn = 0;
-        if (!F.fresh) {
+        F.fresh = F.left == 0 && F.more;
+        if (F.left > 0) {
           --F.left;
           F.p.k0 += AT_KEYS;
           F.turn = F.p.k0 >= F.batch + 32 * T.box;
         } else if (F.more) {
           F.p = F.next;
-          F.left = max(F.p.tiles - 1, 0);
-          F.more = walk_next(T, S, lane_id, F.w, F.next);
+          F.left = F.p.tiles - 1;
           F.turn = 1;
         }
-        if (F.turn) {
-          F.batch = F.p.k0;
-          F.key = F.batch + 32 * T.box;
-          F.same = F.p.tiles > 0 && F.key < F.p.k0 + (F.left + 1) * AT_KEYS;
-          if (!F.same) F.key = F.next.k0;
-        }
+        if (F.turn) F.batch = F.p.k0;
       }
       __syncwarp();
-      if (feeds[0].turn) {
-        pages0 = next0;
-        next0 = feeds[0].same || feeds[0].more ? fetch_pages(feeds[0].same ? feeds[0].p : feeds[0].next, feeds[0].key) : 0;
+      if (feeds[0].turn) pages0 = next0;
+      if (feeds[1].turn) pages1 = next1;
+    };
+    // ... and, with that tile's copies under way, look ahead: for the piece behind a new one, and the next batch of page numbers.
+    auto look = [&]() {
+      __syncwarp();
+      if (lane_id < 2) {
+        Feed& F = feeds[lane_id];
+        if (F.fresh) F.more = walk_next(T, S, lane_id, F.w, F.next);
+        F.fresh = 0;
+        F.key = F.batch + 32 * T.box;
+        F.same = F.left > 0 && F.key < F.p.k0 + (F.left + 1) * AT_KEYS;
+        if (!F.same) F.key = F.next.k0;
       }
-      if (feeds[1].turn) {
-        pages1 = next1;
-        next1 = feeds[1].same || feeds[1].more ? fetch_pages(feeds[1].same ? feeds[1].p : feeds[1].next, feeds[1].key) : 0;
-      }
+      __syncwarp();
+      if (feeds[0].turn) next0 = feeds[0].same || feeds[0].more ? fetch_pages(feeds[0].same ? feeds[0].p : feeds[0].next, feeds[0].key) : 0;
+      if (feeds[1].turn) next1 = feeds[1].same || feeds[1].more ? fetch_pages(feeds[1].same ? feeds[1].p : feeds[1].next, feeds[1].key) : 0;
+      __syncwarp();
+      if (lane_id < 2) feeds[lane_id].turn = 0;
     };
     if (lane_id < 2) {
       Feed& F = feeds[lane_id];
       walk_start(S, F.w);
-      F.p.tiles = F.next.tiles = F.next.k0 = F.left = F.batch = 0;
-      F.more = 1;
+      F.p.k0 = F.next.k0 = F.left = F.batch = 0;
+      F.more = F.fresh = F.turn = 1;
     }
 #pragma unroll 1
-    for (int x = -2; x < 2 * max(cnt0, cnt1); ++x) {
+    for (int x = -1; x < 2 * max(cnt0, cnt1); ++x) {
       const int l = x & 1, r = x >> 1;
-      if (l == 0) advance();
-      if (x < 0 || r >= (l ? cnt1 : cnt0)) continue;
+      if (x >= 0 && l == 0) advance();
+      if (x < 0 || r >= (l ? cnt1 : cnt0)) {
+        if (l) look();
+        continue;
+      }
       const Feed& F = feeds[l];
       const bool own = F.p.kind == AT_OWN;
       if (keys && F.fresh) {
@@ -464,6 +471,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
                     own ? l2_once : l2_keep);
         if (++st == places) { st = 0; st_par ^= 1; }
       }
+      if (l) look();
     }
   } else if (warp >= 9) {
     // ---- products of one lane, issued by one thread.  Wide tiles: O += P V of round r - 1, then S = Q K^T of round r, which
@@ -937,39 +945,54 @@ __global__ void __launch_bounds__(256) ls_attend_tile_join_kernel(const TileArgs
     set_status(A.status, ST_INTERNAL);
     return 0;
   };
-  if (*T.plan > 0) {
-    const int first = T.pre_first[pre_unit];
-    n_pre = pieces(first, T.pre_last[pre_unit]);
-    pre_at = (pre_unit + first) * pre_step + pre_row;
+  const int with_pre = *T.plan, pre0 = T.pre_first[pre_unit], pre1 = T.pre_last[pre_unit], own0 = T.own_first[own_unit], own1 = T.own_last[own_unit];
+  if (with_pre > 0) {
+    n_pre = pieces(pre0, pre1);
+    pre_at = (pre_unit + pre0) * pre_step + pre_row;
   }
   if (own) {
-    const int first = T.own_first[own_unit];
-    n_own = pieces(first, T.own_last[own_unit]);
-    own_at = (own_unit + first) * own_step + own_row;
+    n_own = pieces(own0, own1);
+    own_at = (own_unit + own0) * own_step + own_row;
   }
   const int n = n_pre + n_own;
   auto lse_of = [&](int p) { return p < n_pre ? T.pre_lse[pre_at + p * pre_step] : T.own_lse[own_at + (p - n_pre) * own_step]; };
-  float top = -INFINITY;
+  constexpr int E = D / 32;
+  auto load = [&](int p, float (&o)[E]) {
+    const float* src = (p < n_pre ? T.pre_o + (pre_at + p * pre_step) * D : T.own_o + (own_at + (p - n_pre) * own_step) * D) + lane * E;
+    if (E == 4) *reinterpret_cast<float4*>(o) = *reinterpret_cast<const float4*>(src);
+    else *reinterpret_cast<float2*>(o) = *reinterpret_cast<const float2*>(src);
+  };
+  // the outputs of this warp's first pieces are asked for together with the weights
+  constexpr int AHEAD = 4;
+  float o[AHEAD][E], acc[E] = {}, tot = 0.f, top = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < AHEAD; ++k)
+    if (part + k * WARPS < n) load(part + k * WARPS, o[k]);
   for (int p = lane; p < n; p += 32) top = fmaxf(top, lse_of(p));
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  constexpr int E = D / 32;
-  float acc[E] = {}, tot = 0.f;
+  for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
   for (int p0 = 0; p0 < n; p0 += 32) {
     const float e = p0 + lane < n ? lse_of(p0 + lane) : -INFINITY;
     const float wl = e == -INFINITY ? 0.f : ex2(e - top);
     tot += warp_sum(wl);
-    const int m = min(32, n - p0);
-#pragma unroll 4
-    for (int j = part; j < m; j += WARPS) {
-      const float w = __shfl_sync(0xffffffffu, wl, j);
-      const int p = p0 + j;
-      const float* src = (p < n_pre ? T.pre_o + (pre_at + p * pre_step) * D : T.own_o + (own_at + (p - n_pre) * own_step) * D) + lane * E;
-      float o[E];
-      if (E == 4) *reinterpret_cast<float4*>(o) = *reinterpret_cast<const float4*>(src);
-      else *reinterpret_cast<float2*>(o) = *reinterpret_cast<const float2*>(src);
+    // (a piece that saw nothing has no output: its place may hold anything)
+    if (p0 == 0) {
 #pragma unroll
-      for (int c = 0; c < E; ++c) acc[c] = w == 0.f ? acc[c] : fmaf(w, o[c], acc[c]);  // (a piece that saw nothing has no output)
+      for (int k = 0; k < AHEAD; ++k) {
+        const int j = part + k * WARPS;
+        const float w = __shfl_sync(0xffffffffu, wl, j & 31);
+        if (j < min(32, n) && w != 0.f) {
+#pragma unroll
+          for (int c = 0; c < E; ++c) acc[c] = fmaf(w, o[k][c], acc[c]);
+        }
+      }
+    }
+    for (int j = part + (p0 == 0 ? AHEAD * WARPS : 0); j < min(32, n - p0); j += WARPS) {
+      const float w = __shfl_sync(0xffffffffu, wl, j);
+      if (w == 0.f) continue;
+      load(p0 + j, o[0]);
+#pragma unroll
+      for (int c = 0; c < E; ++c) acc[c] = fmaf(w, o[0][c], acc[c]);
     }
   }
   const float inv = tot == 0.f ? 0.f : 1.f / tot;
