@@ -396,9 +396,9 @@ int32_t ls_paged_kv_attend(ls_paged_kv* kv, const void* d_q, int64_t q_stride, v
   const cudaStream_t st = (cudaStream_t)stream;
   KernelTimer timer(LS_TIMED_ATTEND, st);
   const bool q_vec = aligned16(d_q) && q_stride % 8 == 0;
-  // The tile kernel counts (unit, tile) pairs in 31 bits; what could exceed that goes the other way.
+  // The tile kernel counts the cost of (unit, tile) pairs, at most five each, in 31 bits; what could exceed that goes the other way.
   const double tiles = (double)D.n_kv_heads * (((double)n_seqs * q_len + 1) * (prefix_len / 128.0 + 2) + (double)n_seqs * q_len * ((double)table_width * D.page_size / 128 + 2));
-  if (kv->tiles && q_vec && tiles < 5e8) {
+  if (kv->tiles && q_vec && tiles < 4e8) {
     if (D.head_dim == 64) return D.dtype == LS_WDTYPE_BF16 ? attend_tiles<ls::WD_BF16, 64>(kv, a, st) : attend_tiles<ls::WD_FP16, 64>(kv, a, st);
     return D.dtype == LS_WDTYPE_BF16 ? attend_tiles<ls::WD_BF16, 128>(kv, a, st) : attend_tiles<ls::WD_FP16, 128>(kv, a, st);
   }

@@ -26,7 +26,10 @@ namespace ls {
 constexpr int AT_THREADS = 384;
 constexpr int AT_KEYS = 128;
 constexpr long long AT_SPIN_CLOCKS = 4000LL * 1000 * 1000;  // about two seconds
-constexpr int AT_COST_PAIR = 2, AT_COST_LANE = 1;           // of one key tile, in time of half a CTA
+// What a key tile costs, in quarters of a CTA's time for a lane's tile and the next one on the other lane: measured 4.9 thousand
+// cycles for a pair's tile (8 with a window, where rows see parts of it) and 3 for a lane's, and best at 2 : 1 (5 : 2 with a
+// window); 128 sequences on an 8192-key prefix 110 us at 2 : 1, 113 at 5 : 3, 118 at 5 : 2.
+constexpr int AT_COST_PAIR = 4, AT_COST_PAIR_WINDOW = 5, AT_COST_LANE = 2;
 
 // The bits [lo, hi) of a word, as far as they lie in it.
 __device__ __forceinline__ uint32_t range_bits(int lo, int hi) {
@@ -59,7 +62,8 @@ struct TileArgs {
   int32_t workers;   // two per CTA
 };
 
-// a / b for a >= 0, b > 0 and a quotient below 2^22 (then the estimate is off by one at most).
+// a / b for a >= 0, b > 0 and a quotient below 2^22 (then the estimate is off by one at most): numbers of units, heads, rows and
+// sequences, which the workspace bounds well below that.
 __device__ __forceinline__ int quotient(int a, int b) {
   int q = (int)((float)a * __frcp_rn((float)b));
   const int r = a - q * b;
@@ -206,16 +210,16 @@ __device__ __forceinline__ void make_share(const TileArgs& T, Share& S, int* s_s
   const int pre_tiles = A.prefix > lo ? (A.prefix - origin + AT_KEYS - 1) / AT_KEYS : 0;
   const int n_pair = A.kv_heads * T.pairs * pre_tiles, n_single = T.pairs ? 0 : A.kv_heads * pre_tiles;
   const int mult = A.kv_heads * T.rt, n_lane = n_single + total * mult;
-  const int cost = n_pair * AT_COST_PAIR + n_lane * AT_COST_LANE;
+  const int of_pair = A.window > 0 ? AT_COST_PAIR_WINDOW : AT_COST_PAIR, cost = n_pair * of_pair + n_lane * AT_COST_LANE;
   // Pieces of a unit have to be on consecutive workers: no worker between the first and the last may be empty, so that little
   // work goes to fewer CTAs, each with a tile for both lanes.
-  const int used = max(1, min(n, cost / max(AT_COST_PAIR, 2 * AT_COST_LANE)));
-  const int base = quotient(cost, used), rest = cost - base * used;  // CTA c takes the costs from c * base + c * rest / used on
+  const int used = max(1, min(n, cost / max(of_pair, 2 * AT_COST_LANE)));
+  const int base = cost / used, rest = cost - base * used;  // CTA c takes the costs from c * base + c * rest / used on
   auto start = [&](int i) { i = min(i, used); return i * base + quotient(i * rest, used); };
   const int x0 = start(c), x1 = start(c + 1);
-  auto pair_at = [&](int x) { return min(n_pair, (x + AT_COST_PAIR - 1) / AT_COST_PAIR); };
+  auto pair_at = [&](int x) { return min(n_pair, (x + of_pair - 1) / of_pair); };
   auto lane_at = [&](int x) {
-    x -= n_pair * AT_COST_PAIR;
+    x -= n_pair * of_pair;
     return x <= 0 ? 0 : min(n_lane, (x + AT_COST_LANE - 1) / AT_COST_LANE);
   };
   const int g0 = lane_at(x0), g1 = lane_at(x1), mid = g0 + (g1 - g0) / 2;
