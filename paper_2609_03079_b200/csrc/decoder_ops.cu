@@ -33,6 +33,10 @@ namespace {
 // Blocks that ls_attend_rows_kernel is split into when rows are few: eight blocks of four warps per SM.
 constexpr int kRowsBlocks = 148 * 8;
 constexpr int kRowsMaxGroup = 8;
+// Rows of a norm from which on threads take more of a row each (four blocks to an SM): 2000 x 4096 18.3 us with two chunks a thread
+// against 23.0 with one, 64 x 4096 2.8 with one against 3.0; 8192 x 256 4.9 us with a warp per row against 8.9 with a block.
+// Odd widths from half as many on: 300 x 1001 3.2 us with eight elements a thread against 4.7 with one, 64 x 1001 2.3 with one
+// against 2.7.
 constexpr int kNormManyRows = 148 * 4;
 // Up to this many output rows the pieces of each are joined by eight warps (all blocks are resident at once), else by one.
 constexpr long long kJoinFewRows = 148 * 8;

@@ -95,7 +95,9 @@ __device__ __forceinline__ int attend_len(const AttendArgs& A, int b, bool repor
 }
 
 // ---- one block per (token, key head, up to NG of its query heads, split of the keys) --------------------------------------
-// The route for every layout: any page size, any head dimension that is a multiple of 8 up to 256, any element alignment.
+// The route for every layout: any page size, any head dimension that is a multiple of 8 up to 256, any element alignment (what the
+// tile kernel cannot copy as boxes).  Bound by its own instructions, a fused multiply-add per component, row and key: 64 / 8 heads
+// over 100001 keys 1027 us (400 GB/s) where the tile kernel takes 71; a shared prefix is read again for every sequence.
 // A key belongs to LPK lanes (8 components each), a warp reads 32 / LPK keys at a time and its lane groups and the four
 // warps hold running (maximum, sum, output) triples that are joined once at the end.  All of it in fp32.
 constexpr int AR_THREADS = 128;

@@ -9,14 +9,29 @@
 // start and end inside a unit.  A piece (one unit on one worker) leaves its normalised output and its lse in a slot of the
 // workspace; a second kernel joins the pieces of every row in a fixed order.  Nothing about the lengths is needed on the host.
 //
-// A CTA has two lanes of 128 rows, each with its own score and output accumulators in tensor memory (2 x (128 + dim) columns),
-// and works on both in turn: while the tensor cores multiply for one lane, the four warps of the other do its softmax.  In a
-// pair the lanes share every key and value tile; elsewhere each lane has its own line of (unit, key tile).
-//   warps 8, 11  copy keys (and queries) and values to shared memory (tensor maps, a box per page, a ring of tiles each);
-//   warps 9, 10  issue S = Q K^T and O += P V of lanes 0 and 1 (P is read from tensor memory, where it overwrites S);
-//   warps 0-3, 4-7  softmax of lanes 0 and 1, one thread per row.
+// A CTA has two lanes, each with its own scores and outputs in tensor memory (2 x (128 + dim) columns), and works on both in
+// turn: while the tensor cores multiply for one lane, the four warps of the other do its softmax.  In a pair the lanes share
+// every key and value tile; elsewhere each lane has its own line of (unit, key tile).
+//   warps 0-3, 4-7  softmax of lanes 0 and 1;
+//   warps 8, 11     copy keys (and queries) and values to shared memory (tensor maps, a box per page, a ring of tiles each);
+//   warps 9, 10     issue the products of lanes 0 and 1.
+// Wide pieces (17 to 128 rows): S = Q K^T, one softmax thread per row, P over S in tensor memory, O += P V.
+// Narrow pieces (up to 16 rows: one token of one sequence): S^T = K Q^T, one softmax thread per key, P^T through shared memory,
+// O^T += V^T P^T; the few exponentials are spread over all threads, and products that are 16 wide instead of 128 take a quarter.
 // A row's reference maximum follows its true maximum only when that has risen by more than 2^8: weights stay below 2^8, the
-// final division makes the reference irrelevant, and the accumulator in tensor memory is almost never rescaled.
+// final division makes the reference irrelevant, and the accumulator in tensor memory is almost never rescaled.  The weights are
+// rounded to the 16-bit type because the product with the values takes them so (the values have no more bits); their sum is
+// taken before the rounding.
+//
+// What bounds it (B200, measured rates 6462 GB/s and 1683 TFLOP/s): own units by memory as long as all CTAs work on them (one
+// sequence of 100001 keys, 64 / 8 heads: 71 us, 5.7 TB/s, 0.89 of measured), by the latency of a piece's start and end (about six
+// thousand cycles) where pieces are a few tiles long; pairs by the chain softmax -> P V -> Q K^T of a lane (4.2 thousand cycles
+// for two 128 x 128 tiles against 2.05 of products: tensor memory has no room for a second set of scores).  64 sequences on a
+// 65536-key prefix: 202 us, 687 TFLOP/s, 0.41 of measured.  A fifth of the warps' time was once spent waiting for instructions:
+// the six programs are kept short (loops rolled, one copy of each), which was worth 10 to 20 %.
+// Measured against the alternatives: narrow pieces by the wide program 71 -> 85 us (one long sequence) and 110 -> 127 (128
+// sequences); keys and values copied by one warp 82 -> 91 us with pages of 16; own units in the order sequence by sequence
+// instead of head by head 104 -> 116 (40 key heads); ls_attend_rows_kernel instead of all this 71 -> 1027, 110 -> 9773.
 #pragma once
 #include "ls_attend.cuh"
 #include "ls_tmem.cuh"
@@ -912,7 +927,9 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
 }
 
 // ---- joins the pieces of every row in their order: WARPS warps per row take turns at its pieces ------------------------------
-// (one warp where rows are many and have a few pieces each; eight where rows are few and may be cut into a hundred)
+// (one warp where rows are many and have a few pieces each; eight where rows are few and may be cut into a hundred: 64 rows of 40
+// pieces 85 -> 73 us for the whole call, 8192 rows of 5 pieces with eight 110 -> 131)
+// Bound by latency: five dependent reads of L2, the first outputs asked for together with the weights.
 template <int WD, int D, int WARPS>
 __global__ void __launch_bounds__(256) ls_attend_tile_join_kernel(const TileArgs T) {
   const AttendArgs& A = T.a;
