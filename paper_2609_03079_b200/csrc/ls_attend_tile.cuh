@@ -940,7 +940,6 @@ __global__ void __launch_bounds__(256) ls_attend_tile_join_kernel(const TileArgs
   if (row >= rows) return;  // (a block of its own row when WARPS is 8: all of it returns)
   const int t = (int)(row / A.heads), hd = (int)(row - (long long)t * A.heads), h = hd / A.group, g = hd - h * A.group;
   const int b = t / A.q_len, i = t - b * A.q_len;
-  const bool own = own_keys(T, attend_len(A, b, false)).tiles > 0;
   long long pre_unit, pre_row, pre_step;
   if (T.pairs) {
     const int tile = t / T.tq;
@@ -967,6 +966,7 @@ __global__ void __launch_bounds__(256) ls_attend_tile_join_kernel(const TileArgs
     return 0;
   };
   const int with_pre = *T.plan, pre0 = T.pre_first[pre_unit], pre1 = T.pre_last[pre_unit], own0 = T.own_first[own_unit], own1 = T.own_last[own_unit];
+  const bool own = own_keys(T, attend_len(A, b, false)).tiles > 0;
   if (with_pre > 0) {
     n_pre = pieces(pre0, pre1);
     pre_at = (pre_unit + pre0) * pre_step + pre_row;

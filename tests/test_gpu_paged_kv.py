@@ -168,6 +168,69 @@ def test_long_pieces(heads, hk, q_len, seqs, prefix, own, page):
     run_case(heads=heads, hk=hk, q_len=q_len, lens=[prefix + own + 17 * b for b in range(seqs)], prefix=prefix, page=page, seed=heads + page)
 
 
+@pytest.mark.parametrize("seqs", [384, 385, 1000])
+def test_more_sequences_than_threads(seqs):
+    rng = np.random.default_rng(seqs)
+    lens = [0 if x < 10 else int(x) for x in rng.integers(0, 170, seqs)]
+    run_case(heads=2, hk=1, D=64, lens=lens, prefix=33, seed=seqs)
+    run_case(heads=2, hk=2, D=64, lens=lens, window=40, seed=seqs)
+
+
+def test_two_handles_on_two_streams():
+    """Two caches, two streams, many calls in flight: nothing of one call's workspace is another's."""
+    bs = [Batch(lens=[400, 33, 0, 280], prefix=32, seed=s) for s in (1, 2)]
+    kvs = [b.handle() for b in bs]
+    streams = [torch.cuda.Stream() for _ in bs]
+    torch.cuda.synchronize()
+    for _ in range(50):
+        for b, kv, st in zip(bs, kvs, streams):
+            b.attend(kv, stream=st)
+    torch.cuda.synchronize()
+    for b, kv in zip(bs, kvs):
+        assert ls.ls_paged_kv_status(kv) == 0
+        b.check()
+        kv.close()
+
+
+def test_calls_that_depend_on_each_other_back_to_back():
+    """append -> attend -> norm on one stream with no wait between them, many times: each sees what the one before wrote."""
+    B, heads, hk, D, page = 3, 8, 2, 128, 16
+    gen = torch.Generator(device=DEV).manual_seed(0)
+    kp, vp = (torch.zeros(40, page, hk, D, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    table = torch.arange(39, dtype=torch.int32, device=DEV).view(B, 13)
+    kv = ls.ls_paged_kv_create(kp, vp, heads, max_seqs=B, max_q_len=1, rope=rope_table(208, D))
+    n = 150
+    x = torch.randn(n, B, heads * D, generator=gen, device=DEV)
+    w = (torch.randn(heads * D, (heads + 2 * hk) * D, generator=gen, device=DEV) * (heads * D) ** -0.5).bfloat16()
+    seq = torch.arange(B, dtype=torch.int32, device=DEV)
+    pos = torch.arange(n, dtype=torch.int32, device=DEV)[:, None].expand(n, B).contiguous()
+    length = pos + 1
+
+    def pass_(wait):
+        kp.zero_(), vp.zero_()
+        got = []
+        for t in range(n):
+            h = torch.empty(B, heads * D, dtype=torch.bfloat16, device=DEV)
+            ls.ls_block_norm(x[t], None, None, h)
+            if wait: torch.cuda.synchronize()
+            q, k, v = (h @ w).view(B, heads + 2 * hk, D).split([heads, hk, hk], 1)
+            qo, o = torch.empty(B, heads, D, dtype=torch.bfloat16, device=DEV), torch.empty(B, heads, D, dtype=torch.bfloat16, device=DEV)
+            if wait: torch.cuda.synchronize()
+            ls.ls_paged_kv_append(kv, q, k, v, qo, seq, pos[t], table)
+            if wait: torch.cuda.synchronize()
+            ls.ls_paged_kv_attend(kv, qo, o, length[t], table)
+            if wait: torch.cuda.synchronize()
+            xo = torch.empty_like(x[t])
+            ls.ls_block_norm(x[t], o.view(B, -1), xo, None, post_norm=True)
+            got.append(xo)
+        torch.cuda.synchronize()
+        return torch.stack(got)
+
+    assert torch.equal(pass_(False), pass_(True))
+    assert ls.ls_paged_kv_status(kv) == 0
+    kv.close()
+
+
 @pytest.mark.parametrize("q_len", [2, 3, 8, 31, 33, 130])
 @pytest.mark.parametrize("prefix", [0, 150])
 def test_several_tokens(q_len, prefix):
