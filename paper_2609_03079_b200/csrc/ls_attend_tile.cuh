@@ -61,7 +61,7 @@ struct TileShape {
   // weights of a narrow piece: [2 x 64 keys][32 rows] of 128 bytes, in the last rows of the lane's query buffer
   static constexpr int NARROW_SLOTS = D == 128 ? 3 : 2, P_AT = NARROW_SLOTS * 32 * 128, P_HALF = D == 128 ? HALF : 32 * 128;
   static constexpr int CTL = (2 + STAGES) * TILE;  // offset of the control block
-  static constexpr int SMEM = CTL + 3072;
+  static constexpr int SMEM = CTL + 3 * 1024;
 };
 
 struct TileArgs {
@@ -106,6 +106,7 @@ struct Share {
   int own_h[2], own_b[2], own_r[2], own_t[2];  // where a lane's range starts, if among the own units: head, sequence, row tile, tile
   OwnKeys own_k[2];                   // ... and that sequence's keys
   int batch_pieces[2];                // pieces of each lane that are not of own units (they come first)
+  int sparse;                         // at most a tile for each CTA: lane 1 alone works, and workers are numbered by CTA
 };
 
 // A piece: consecutive tiles of one unit on one lane.  The copying warp walks the line and leaves each piece here, with its
@@ -226,9 +227,10 @@ __device__ __forceinline__ void make_share(const TileArgs& T, Share& S, int* s_s
   const int n_pair = A.kv_heads * T.pairs * pre_tiles, n_single = T.pairs ? 0 : A.kv_heads * pre_tiles;
   const int mult = A.kv_heads * T.rt, n_lane = n_single + total * mult;
   const int of_pair = A.window > 0 ? AT_COST_PAIR_WINDOW : AT_COST_PAIR, cost = n_pair * of_pair + n_lane * AT_COST_LANE;
-  // Pieces of a unit have to be on consecutive workers: no worker between the first and the last may be empty, so that little
-  // work goes to fewer CTAs, each with a tile for both lanes.
-  const int used = max(1, min(n, cost / max(of_pair, 2 * AT_COST_LANE)));
+  // Pieces of a unit have to be on consecutive workers: no worker between the first and the last may be empty.  Little work goes
+  // to one lane of as many CTAs as there are tiles, what is a little more to fewer CTAs, each with a tile for both lanes.
+  const bool sparse = n_pair == 0 && n_lane <= n;
+  const int used = max(1, sparse ? n_lane : min(n, cost / max(of_pair, 2 * AT_COST_LANE)));
   const int base = cost / used, rest = cost - base * used;  // CTA c takes the costs from c * base + c * rest / used on
   auto start = [&](int i) { i = min(i, used); return i * base + quotient(i * rest, used); };
   const int x0 = start(c), x1 = start(c + 1);
@@ -239,7 +241,7 @@ __device__ __forceinline__ void make_share(const TileArgs& T, Share& S, int* s_s
   };
   const int g0 = lane_at(x0), g1 = lane_at(x1), mid = g0 + (g1 - g0) / 2;
   if (tid == 0) {
-    S.pre_lo = lo; S.pre_origin = origin; S.pre_tiles = pre_tiles;
+    S.pre_lo = lo; S.pre_origin = origin; S.pre_tiles = pre_tiles; S.sparse = sparse;
     S.pair0 = pair_at(x0); S.pair1 = pair_at(x1);
     const int pp = S.pair1 > S.pair0 ? quotient(S.pair1 - 1, pre_tiles) - quotient(S.pair0, pre_tiles) + 1 : 0;
     for (int l = 0; l < 2; ++l) {
@@ -339,14 +341,19 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_shared();
   }
-  if (warp == 9) tm_alloc(saddr(&C.tmem), 512);
   if (warp == 8 && lane_id < 4) tma_prefetch_map(lane_id == 0 ? &map_k : lane_id == 1 ? &map_v : lane_id == 2 ? &map_q_all : &map_q_own);
   asm volatile("griddepcontrol.wait;" ::: "memory");  // (all before this overlaps the end of the kernel in front)
   make_share(T, S, C.scan, blockIdx.x, gridDim.x);
-  tm_fence_before();
   __syncthreads();
-  tm_fence_after();
-  const uint32_t tmem = C.tmem;
+  // (the copying warps, which have no use for tensor memory, do not wait for it)
+  uint32_t tmem = 0;
+  if (warp != 8 && warp != 11) {
+    if (warp == 9) tm_alloc(saddr(&C.tmem), 512);
+    tm_fence_before();
+    group_sync(3, AT_THREADS - 64);
+    tm_fence_after();
+    tmem = C.tmem;
+  }
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   // Bounded wait of a whole warp: false (for all of it) once any wait of the CTA has given up.
@@ -625,7 +632,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     const uint32_t t_s = tmem + (quad << 21) + l * AT_KEYS, t_o = tmem + (quad << 21) + 256 + l * D;
     Slots Q(S.batch_pieces[l], q_slots, 0);
     const float scale = A.scale_log2;
-    const int worker = blockIdx.x * 2 + l;
+    const int worker = S.sparse ? blockIdx.x : blockIdx.x * 2 + l;
     int n = 0;
     auto arrive_p = [&]() {
       tm_fence_before();
