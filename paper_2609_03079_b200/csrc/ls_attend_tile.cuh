@@ -85,6 +85,12 @@ __device__ __forceinline__ int quotient(int a, int b) {
   return r < 0 ? q - 1 : r >= b ? q + 1 : q;
 }
 
+// The same for any quotient: a second estimate from what the first one leaves.
+__device__ __forceinline__ int quotient31(int a, int b) {
+  const int q = (int)((float)a * __frcp_rn((float)b)), r = a - q * b;  // (off by 2^-22 of itself: r fits)
+  return r >= 0 ? q + quotient(r, b) : q - quotient(b - 1 - r, b);
+}
+
 // The keys of sequence b that are its own: [lo, hi) is what any of its tokens sees, tiles start at `origin`.
 struct OwnKeys { int lo, hi, origin, tiles; };
 __device__ __forceinline__ OwnKeys own_keys(const TileArgs& T, int len) {
@@ -226,15 +232,17 @@ __device__ __forceinline__ void make_share(const TileArgs& T, Share& S, int* s_s
   const int pre_tiles = A.prefix > lo ? (A.prefix - origin + AT_KEYS - 1) / AT_KEYS : 0;
   const int n_pair = A.kv_heads * T.pairs * pre_tiles, n_single = T.pairs ? 0 : A.kv_heads * pre_tiles;
   const int mult = A.kv_heads * T.rt, n_lane = n_single + total * mult;
-  const int of_pair = A.window > 0 ? AT_COST_PAIR_WINDOW : AT_COST_PAIR, cost = n_pair * of_pair + n_lane * AT_COST_LANE;
+  const bool windowed = A.window > 0;
+  const int of_pair = windowed ? AT_COST_PAIR_WINDOW : AT_COST_PAIR, cost = n_pair * of_pair + n_lane * AT_COST_LANE;
+  static_assert(AT_COST_PAIR >= 2 * AT_COST_LANE && AT_COST_PAIR_WINDOW >= AT_COST_PAIR, "a CTA's least share is a pair's tile");
   // Pieces of a unit have to be on consecutive workers: no worker between the first and the last may be empty.  Little work goes
   // to one lane of as many CTAs as there are tiles, what is a little more to fewer CTAs, each with a tile for both lanes.
   const bool sparse = n_pair == 0 && n_lane <= n;
-  const int used = max(1, sparse ? n_lane : min(n, cost / max(of_pair, 2 * AT_COST_LANE)));
-  const int base = cost / used, rest = cost - base * used;  // CTA c takes the costs from c * base + c * rest / used on
+  const int used = max(1, sparse ? n_lane : min(n, windowed ? cost / AT_COST_PAIR_WINDOW : cost / AT_COST_PAIR));
+  const int base = quotient31(cost, used), rest = cost - base * used;  // CTA c takes the costs from c * base + c * rest / used on
   auto start = [&](int i) { i = min(i, used); return i * base + quotient(i * rest, used); };
   const int x0 = start(c), x1 = start(c + 1);
-  auto pair_at = [&](int x) { return min(n_pair, (x + of_pair - 1) / of_pair); };
+  auto pair_at = [&](int x) { return min(n_pair, windowed ? (x + of_pair - 1) / AT_COST_PAIR_WINDOW : (x + of_pair - 1) / AT_COST_PAIR); };
   auto lane_at = [&](int x) {
     x -= n_pair * of_pair;
     return x <= 0 ? 0 : min(n_lane, (x + AT_COST_LANE - 1) / AT_COST_LANE);
@@ -243,7 +251,7 @@ __device__ __forceinline__ void make_share(const TileArgs& T, Share& S, int* s_s
   if (tid == 0) {
     S.pre_lo = lo; S.pre_origin = origin; S.pre_tiles = pre_tiles; S.sparse = sparse;
     S.pair0 = pair_at(x0); S.pair1 = pair_at(x1);
-    const int pp = S.pair1 > S.pair0 ? quotient(S.pair1 - 1, pre_tiles) - quotient(S.pair0, pre_tiles) + 1 : 0;
+    const int pp = pre_tiles > 0 && S.pair1 > S.pair0 ? quotient(S.pair1 - 1, pre_tiles) - quotient(S.pair0, pre_tiles) + 1 : 0;
     for (int l = 0; l < 2; ++l) {
       const int from = l ? mid : g0, to = min(l ? g1 : mid, n_single);
       S.lane0[l] = from; S.lane1[l] = l ? g1 : mid;
