@@ -308,7 +308,7 @@ struct Feed {
 // Control block of a CTA, behind the tiles in shared memory.
 template <int NST>
 struct TileCtl {
-  unsigned long long full[2][NST], empty[NST], qfull[2][4], qempty[2][4], s[2][2], p[2], o[2], turn[2], done[2];
+  unsigned long long full[2][NST], empty[NST], qfull[2][4], qempty[2][4], s[2][2], p[2], p_half[2], o[2], turn[2], done[2];
   Share share;
   int scan[2 * AT_THREADS / 32];
   Piece piece[2][4];
@@ -333,7 +333,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
   const int tid = threadIdx.x, lane_id = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const uint32_t q_base = saddr(dyn), ring = q_base + 2 * TS::TILE;
   const uint32_t b_full = saddr(C.full), b_empty = saddr(C.empty), b_qfull = saddr(C.qfull), b_qempty = saddr(C.qempty), b_s = saddr(C.s),
-                 b_p = saddr(C.p), b_o = saddr(C.o), b_turn = saddr(C.turn), b_done = saddr(C.done);
+                 b_p = saddr(C.p), b_ph = saddr(C.p_half), b_o = saddr(C.o), b_turn = saddr(C.turn), b_done = saddr(C.done);
   if (q_base & 1023) {  // (swizzled tiles need it; the first byte of a block's shared memory has it)
     if (tid == 0) set_status(A.status, ST_INTERNAL);
     return;
@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     if (lane_id < NST) mb_init(b_empty + 8 * lane_id, 2);
     if (lane_id < 8) { mb_init(b_qfull + 8 * lane_id, 1); mb_init(b_qempty + 8 * lane_id, 5); }
     if (lane_id < 4) mb_init(b_s + 8 * lane_id, 1);
-    if (lane_id < 2) { mb_init(b_p + 8 * lane_id, 4); mb_init(b_o + 8 * lane_id, 1); mb_init(b_turn + 8 * lane_id, 1); mb_init(b_done + 8 * lane_id, 1); }
+    if (lane_id < 2) { mb_init(b_p + 8 * lane_id, 4); mb_init(b_ph + 8 * lane_id, 4); mb_init(b_o + 8 * lane_id, 1); mb_init(b_turn + 8 * lane_id, 1); mb_init(b_done + 8 * lane_id, 1); }
     if (lane_id == 0) C.dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     fence_async_shared();
@@ -584,7 +584,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
           fence_async_shared();
           __syncwarp();
         }
-        if (!wait(b_p + 8 * l, (r - 1) & 1)) return false;
+        if (!wait((vnarrow ? b_p : b_ph) + 8 * l, (r - 1) & 1)) return false;
         if (r <= n_pair && (l || r > 0) && !wait(b_turn + 8 * l, (l ? r : r - 1) & 1)) return false;
         tm_fence_after();
         const uint64_t v = uniform64(smem_desc(ring + slot * TS::TILE, TS::HALF));
@@ -595,12 +595,23 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
 #pragma unroll
             for (int k = 0; k < AT_KEYS / 16; ++k)
               tm_mma_ss(t_o, va + k * (2048 >> 4), p_desc + (((k / 4) * TS::P_HALF + (k % 4) * 32) >> 4), ID_OT, !(vfresh && k == 0));
+            tm_commit(b_o + 8 * l);
+            tm_commit(b_empty + 8 * slot);
           } else {
 #pragma unroll
-            for (int k = 0; k < AT_KEYS / 16; ++k) tm_mma_ts(t_o, t_s + k * 8, v + k * (2048 >> 4), ID_O, !(vfresh && k == 0));
+            for (int k = 0; k < AT_KEYS / 32; ++k) tm_mma_ts(t_o, t_s + k * 8, v + k * (2048 >> 4), ID_O, !(vfresh && k == 0));
           }
-          tm_commit(b_o + 8 * l);
-          tm_commit(b_empty + 8 * slot);
+        }
+        if (!vnarrow) {
+          __syncwarp();
+          if (!wait(b_p + 8 * l, (r - 1) & 1)) return false;
+          tm_fence_after();
+          if (elect_one()) {
+#pragma unroll
+            for (int k = AT_KEYS / 32; k < AT_KEYS / 16; ++k) tm_mma_ts(t_o, t_s + k * 8, v + k * (2048 >> 4), ID_O, true);
+            tm_commit(b_o + 8 * l);
+            tm_commit(b_empty + 8 * slot);
+          }
         }
         __syncwarp();
         return true;
@@ -642,10 +653,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     const float scale = A.scale_log2;
     const int worker = S.sparse ? blockIdx.x : blockIdx.x * 2 + l;
     int n = 0;
-    auto arrive_p = [&]() {
+    auto arrive_p = [&](uint32_t bar) {
       tm_fence_before();
       __syncwarp();
-      if (lane_id == 0) mb_arrive(b_p + 8 * l);
+      if (lane_id == 0) mb_arrive(bar + 8 * l);
     };
     // Keys [lo, hi) that row x of a piece sees, relative to the piece's first.
     auto row_keys = [&](const Piece& P, int x, int& lo, int& hi) {
@@ -756,7 +767,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
               asm volatile("st.shared.b16 [%0], %1;" ::"r"(p_base + x * 128 + ((p_chunk ^ (x & 7)) << 4) + p_byte), "h"(w[x - g]) : "memory");
           }
         fence_async_shared();
-        arrive_p();
+        arrive_p(b_p);
       }
       float my_sum = 0.f;
 #pragma unroll
@@ -894,6 +905,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
             tm_st16(t_s + 32 * half + 16, s1);
             if (half == 1) break;
             tm_ld32(t_s + 96, s1);
+            tm_wait_st();  // the weights of the first 64 keys can be multiplied while the others are made
+            arrive_p(b_ph);
             tm_wait_ld();
             tm_pin32(s0);
             tm_pin32(s1);
@@ -901,8 +914,8 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
           const uint64_t acc_all = add2(acc[0], acc[1]);
           sum += lo32(acc_all) + hi32(acc_all);
           tm_wait_st();
-        }
-        arrive_p();
+        } else arrive_p(b_ph);
+        arrive_p(b_p);
       }
       // the piece is done: its output and lse go to the workspace
       wait(b_o + 8 * l, (n - 1) & 1);
