@@ -41,10 +41,10 @@ namespace ls {
 constexpr int AT_THREADS = 384;
 constexpr int AT_KEYS = 128;
 constexpr long long AT_SPIN_CLOCKS = 4000LL * 1000 * 1000;  // about two seconds
-// What a key tile costs, in quarters of a CTA's time for a lane's tile and the next one on the other lane: measured 4.9 thousand
-// cycles for a pair's tile (8 with a window, where rows see parts of it) and 3 for a lane's, and best at 2 : 1 (5 : 2 with a
-// window); 128 sequences on an 8192-key prefix 110 us at 2 : 1, 113 at 5 : 3, 118 at 5 : 2.
-constexpr int AT_COST_PAIR = 4, AT_COST_PAIR_WINDOW = 5, AT_COST_LANE = 2;
+// What a key tile costs a CTA, whose lanes take two at once: measured 2.4 us for a pair's tile (4 with a window, where rows see
+// parts of it) and 1.7 for a lane's, start and end of short pieces included.
+constexpr int AT_COST_PAIR = 3, AT_COST_PAIR_WINDOW = 5, AT_COST_LANE = 2;
+constexpr int AT_SHARE = 4, AT_SHARE_WINDOW = 5;  // a CTA's least share: a pair's tile, and a tile for both lanes
 
 // The bits [lo, hi) of a word, as far as they lie in it.
 __device__ __forceinline__ uint32_t range_bits(int lo, int hi) {
@@ -234,11 +234,11 @@ __device__ __forceinline__ void make_share(const TileArgs& T, Share& S, int* s_s
   const int mult = A.kv_heads * T.rt, n_lane = n_single + total * mult;
   const bool windowed = A.window > 0;
   const int of_pair = windowed ? AT_COST_PAIR_WINDOW : AT_COST_PAIR, cost = n_pair * of_pair + n_lane * AT_COST_LANE;
-  static_assert(AT_COST_PAIR >= 2 * AT_COST_LANE && AT_COST_PAIR_WINDOW >= AT_COST_PAIR, "a CTA's least share is a pair's tile");
+  static_assert(AT_SHARE >= AT_COST_PAIR && AT_SHARE_WINDOW >= AT_COST_PAIR_WINDOW && AT_SHARE >= 2 * AT_COST_LANE, "least share");
   // Pieces of a unit have to be on consecutive workers: no worker between the first and the last may be empty.  Little work goes
   // to one lane of as many CTAs as there are tiles, what is a little more to fewer CTAs, each with a tile for both lanes.
   const bool sparse = n_pair == 0 && n_lane <= n;
-  const int used = max(1, sparse ? n_lane : min(n, windowed ? cost / AT_COST_PAIR_WINDOW : cost / AT_COST_PAIR));
+  const int used = max(1, sparse ? n_lane : min(n, windowed ? cost / AT_SHARE_WINDOW : cost / AT_SHARE));
   const int base = quotient31(cost, used), rest = cost - base * used;  // CTA c takes the costs from c * base + c * rest / used on
   auto start = [&](int i) { i = min(i, used); return i * base + quotient(i * rest, used); };
   const int x0 = start(c), x1 = start(c + 1);
@@ -1025,23 +1025,21 @@ __global__ void __launch_bounds__(256) ls_attend_tile_join_kernel(const TileArgs
     const float wl = e == -INFINITY ? 0.f : ex2(e - top);
     tot += warp_sum(wl);
     // (a piece that saw nothing has no output: its place may hold anything)
-    if (p0 == 0) {
+    const int m = min(32, n - p0);
+    for (int j = part; j < m; j += AHEAD * WARPS) {
+      if (p0 + j != part) {
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+          if (j + k * WARPS < m) load(p0 + j + k * WARPS, o[k]);
+      }
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k) {
-        const int j = part + k * WARPS;
-        const float w = __shfl_sync(0xffffffffu, wl, j & 31);
-        if (j < min(32, n) && w != 0.f) {
+        const float w = __shfl_sync(0xffffffffu, wl, (j + k * WARPS) & 31);
+        if (j + k * WARPS < m && w != 0.f) {
 #pragma unroll
           for (int c = 0; c < E; ++c) acc[c] = fmaf(w, o[k][c], acc[c]);
         }
       }
-    }
-    for (int j = part + (p0 == 0 ? AHEAD * WARPS : 0); j < min(32, n - p0); j += WARPS) {
-      const float w = __shfl_sync(0xffffffffu, wl, j);
-      if (w == 0.f) continue;
-      load(p0 + j, o[0]);
-#pragma unroll
-      for (int c = 0; c < E; ++c) acc[c] = fmaf(w, o[0][c], acc[c]);
     }
   }
   const float inv = tot == 0.f ? 0.f : 1.f / tot;
