@@ -49,22 +49,23 @@ __device__ __forceinline__ long long append_slot(const AppendArgs& A, int sq, in
   return id * A.page_stride + (long long)(ps - pg * A.page) * A.token_stride;
 }
 
-// One block per token; 16-byte loads and stores.  A thread has the same two chunks of eight components in every head that it
-// visits (chunks whose components are each other's partners, or two neighbours where nothing is turned), so that it reads its
+// A block of one token, or (SEVERAL) of as many as fit with `width` threads each; 16-byte loads and stores.  A thread has the
+// same two chunks of eight components in every head that it visits (chunks whose components are each other's partners, or two neighbours where nothing is turned), so that it reads its
 // cosines and sines once per token.  For head and rotation sizes of a multiple of 16 and 16-byte aligned operands.
 // Bound by memory: 16 x 1023 tokens of 64 + 2 x 8 heads of 128, 679 MB, 118 us, 5.75 TB/s, 0.89 of measured (the pair kernel below:
 // 579 us; with the token's place looked up before the first loads instead of behind them: 137).  One token: 2.9 us a call,
 // three dependent reads (place, page, slot) and the launch.
-template <int WD>
-__global__ void __launch_bounds__(256) ls_append_kernel(const AppendArgs A) {
+template <int WD, bool SEVERAL>
+__global__ void __launch_bounds__(256) ls_append_kernel(const AppendArgs A, int width) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const long long t = blockIdx.x;
+  const int mine = SEVERAL ? threadIdx.x / width : 0, tid = SEVERAL ? threadIdx.x - mine * width : threadIdx.x;
+  const long long t = SEVERAL ? (long long)blockIdx.x * (blockDim.x / width) + mine : blockIdx.x;
   const int per = A.dim / 16, nq = A.q ? A.heads : 0, heads = nq + 2 * A.kv_heads;
-  const int i = threadIdx.x % per, step = blockDim.x / per;
+  const int i = tid % per, step = (SEVERAL ? width : (int)blockDim.x) / per;
   const bool turned = 16 * i < A.rope_dim;
   const int c0 = turned && !A.interleaved ? 8 * i : 16 * i, c1 = turned && !A.interleaved ? c0 + A.rope_dim / 2 : c0 + 8;
-  if (threadIdx.x >= step * per) return;
+  if (tid >= step * per || (SEVERAL && (mine >= blockDim.x / width || t >= A.n_tokens))) return;
   auto source = [&](int hd) {
     return (hd < nq ? A.q + t * A.q_stride + (long long)hd * A.dim
             : hd < nq + A.kv_heads ? A.k + t * A.k_stride + (long long)(hd - nq) * A.dim
@@ -77,7 +78,7 @@ __global__ void __launch_bounds__(256) ls_append_kernel(const AppendArgs A) {
     a0 = ld_stream128(p + c0); b0 = ld_stream128(p + c1);
     a1 = ld_stream128(q + c0); b1 = ld_stream128(q + c1);
   };
-  int hd = threadIdx.x / per;
+  int hd = tid / per;
   fetch(hd);
   const int sq = A.seq[t], ps = A.pos[t];
   float c[8], s[8];

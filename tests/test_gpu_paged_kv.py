@@ -475,6 +475,13 @@ def test_append_padding_tokens_are_passed_over():
     append_case(seq=[0, -1, 1, 0, -1], pos=[5, 7, -1, 6, -3])
 
 
+@pytest.mark.parametrize("heads,hk,D", [(1, 1, 64), (8, 1, 64), (8, 1, 128), (3, 3, 16), (71, 1, 128), (2, 2, 256)])
+@pytest.mark.parametrize("T", [1, 5, 77])
+def test_append_several_tokens_to_a_block(heads, hk, D, T):
+    for with_q in (True, False):
+        append_case(heads=heads, hk=hk, D=D, r=D, with_q=with_q, seq=[t % 2 for t in range(T)], pos=[3 + t // 2 for t in range(T)])
+
+
 @pytest.mark.parametrize("T", [1, 2, 130, 600])
 def test_append_many_tokens(T):
     append_case(heads=32, hk=8, D=128, r=128, seq=[0] * T, pos=list(range(11, 11 + T)))
