@@ -50,9 +50,10 @@ __device__ __forceinline__ long long append_slot(const AppendArgs& A, int sq, in
 }
 
 // A block of one token, or (SEVERAL) of as many as fit with `width` threads each; 16-byte loads and stores.  A thread has the
-// same two chunks of eight components in every head that it visits (chunks whose components are each other's partners, or two neighbours where nothing is turned), so that it reads its
-// cosines and sines once per token.  For head and rotation sizes of a multiple of 16 and 16-byte aligned operands.
-// Bound by memory: 16 x 1023 tokens of 64 + 2 x 8 heads of 128, 679 MB, 118 us, 5.75 TB/s, 0.89 of measured (the pair kernel below:
+// same two chunks of eight components in every head that it visits (chunks whose components are each other's partners, or two
+// neighbours where nothing is turned), so that it reads its cosines and sines once per token.  For head and rotation sizes of a
+// multiple of 16 and 16-byte aligned operands.
+// Bound by memory: 16 x 1023 tokens of 64 + 2 x 8 heads of 128, 679 MB, 119 us, 5.7 TB/s, 0.88 of measured (the pair kernel below:
 // 579 us; with the token's place looked up before the first loads instead of behind them: 137).  One token: 2.9 us a call,
 // three dependent reads (place, page, slot) and the launch.
 template <int WD, bool SEVERAL>

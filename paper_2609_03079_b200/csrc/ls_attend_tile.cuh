@@ -25,9 +25,10 @@
 //
 // What bounds it (B200, measured rates 6462 GB/s and 1683 TFLOP/s): own units by memory as long as all CTAs work on them (one
 // sequence of 100001 keys, 64 / 8 heads: 71 us, 5.7 TB/s, 0.89 of measured), by the latency of a piece's start and end (about six
-// thousand cycles) where pieces are a few tiles long; pairs by the chain softmax -> P V -> Q K^T of a lane (4.2 thousand cycles
-// for two 128 x 128 tiles against 2.05 of products: tensor memory has no room for a second set of scores).  64 sequences on a
-// 65536-key prefix: 202 us, 687 TFLOP/s, 0.41 of measured.  A fifth of the warps' time was once spent waiting for instructions:
+// thousand cycles) where pieces are a few tiles long; pairs by the chain softmax -> P V -> Q K^T of a lane (3.6 thousand cycles
+// for two 128 x 128 tiles against 2.05 of products: tensor memory has no room for a second set of scores; 4.2 before the values
+// of half a tile were multiplied under the other half's weights).  64 sequences on a 65536-key prefix: 201 us, 690 TFLOP/s, 0.41
+// of measured.  A fifth of the warps' time was once spent waiting for instructions:
 // the six programs are kept short (loops rolled, one copy of each), which was worth 10 to 20 %.
 // Measured against the alternatives: narrow pieces by the wide program 71 -> 85 us (one long sequence) and 110 -> 127 (128
 // sequences); keys and values copied by one warp 82 -> 91 us with pages of 16; own units in the order sequence by sequence
@@ -41,8 +42,8 @@ namespace ls {
 constexpr int AT_THREADS = 384;
 constexpr int AT_KEYS = 128;
 constexpr long long AT_SPIN_CLOCKS = 4000LL * 1000 * 1000;  // about two seconds
-// What a key tile costs a CTA, whose lanes take two at once: measured 2.4 us for a pair's tile (4 with a window, where rows see
-// parts of it) and 1.7 for a lane's, start and end of short pieces included.
+// What a key tile costs a CTA, whose lanes take two at once, start and end of short pieces included, for a pair (more with a
+// window, where rows see parts of a tile) and for a lane: 64 sequences on a 65536-key prefix 196 us at 3 : 2, 202 at 4 : 2.
 constexpr int AT_COST_PAIR = 3, AT_COST_PAIR_WINDOW = 5, AT_COST_LANE = 2;
 constexpr int AT_SHARE = 4, AT_SHARE_WINDOW = 5;  // a CTA's least share: a pair's tile, and a tile for both lanes
 

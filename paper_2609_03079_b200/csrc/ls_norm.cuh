@@ -97,7 +97,7 @@ __device__ __forceinline__ float row_sum(float v, float* s) {
 // read once, all loads are under way before the first sum, and two blocks of 512 threads fit an SM (64 registers a thread).  A
 // row belongs to a block, or (WARP) to one of its warps.  Gains are asked for ahead of the sum before their use where that
 // takes few registers (one chunk a thread: few rows, where latency counts), else when they are used (they are in L1 then).
-// Bound by memory for many rows: 8192 x 8192 in bf16 with a gate, 671 MB, 120 us, 5.6 TB/s, 0.87 of measured; 8192 x 4096 with the
+// Bound by memory for many rows: 8192 x 8192 in bf16 with a gate, 671 MB, 120 to 126 us, 5.3 to 5.6 TB/s, 0.82 to 0.87 of measured; 8192 x 4096 with the
 // residual in fp32 66 us, 6.1 TB/s.  One row of 4096: 3 us a call, 2.1 on the device (two sums over the block).  Widths that are
 // no multiple of 8 go one element at a time: 200 x 5121 8.6 us against 5.8 for 200 x 5120.
 template <int XT, int BT, int V, int K, bool WARP>
