@@ -313,7 +313,9 @@ struct TileCtl {
   Share share;
   int scan[2 * AT_THREADS / 32];
   Piece piece[2][4];
-  float red[2][4][AT_NARROW]; // narrow pieces: maxima or sums of each warp's keys
+  // narrow pieces: maxima and sums of each warp's keys.  (Places of their own: a warp may be at the end of a piece, with its sums,
+  // while another one still reads the maxima of the last tile; no barrier of the four stands between.)
+  float top[2][4][AT_NARROW], sum[2][4][AT_NARROW];
   int lo[2][AT_NARROW], hi[2][AT_NARROW];  // ... keys of each row, relative to the piece's first
   Feed feed[2][2];            // of the warps that copy keys and values, for each lane
   uint32_t tmem;
@@ -726,10 +728,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
             const float v = warp_max(__uint_as_float(s[x]));
             if (lane_id == x) top = v;
           }
-          if (lane_id < NR) C.red[l][quad][lane_id] = top;
+          if (lane_id < NR) C.top[l][quad][lane_id] = top;
           group_sync(1 + l, 128);
           if (lane_id < rows) {
-            top = fmaxf(fmaxf(C.red[l][0][lane_id], C.red[l][1][lane_id]), fmaxf(C.red[l][2][lane_id], C.red[l][3][lane_id])) * scale;
+            top = fmaxf(fmaxf(C.top[l][0][lane_id], C.top[l][1][lane_id]), fmaxf(C.top[l][2][lane_id], C.top[l][3][lane_id])) * scale;
             rise = top + my_off > 8.f;
           } else rise = false;
           const float f = rise ? ex2(-top - my_off) : 1.f;
@@ -783,14 +785,14 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
             for (int x = 0; x < 4; ++x) v[x] += __shfl_xor_sync(0xffffffffu, v[x], o);
 #pragma unroll
           for (int x = 0; x < 4; ++x)
-            if (lane_id == g + x) C.red[l][quad][g + x] = v[x];
+            if (lane_id == g + x) C.sum[l][quad][g + x] = v[x];
         }
       uint32_t o[NR];
       wait(b_o + 8 * l, (n - 1) & 1);
       tm_fence_after();
       tm_ld16(t_o, o);
       group_sync(1 + l, 128);
-      if (lane_id < rows) my_sum = (C.red[l][0][lane_id] + C.red[l][1][lane_id]) + (C.red[l][2][lane_id] + C.red[l][3][lane_id]);
+      if (lane_id < rows) my_sum = (C.sum[l][0][lane_id] + C.sum[l][1][lane_id]) + (C.sum[l][2][lane_id] + C.sum[l][3][lane_id]);
       const float inv = my_sum == 0.f ? 0.f : 1.f / my_sum;
       float *po, *pl;
       const long long at = place_piece(P, po, pl);
