@@ -92,12 +92,17 @@ __device__ __forceinline__ int quotient31(int a, int b) {
   return r >= 0 ? q + quotient(r, b) : q - quotient(b - 1 - r, b);
 }
 
+// First key that any token of a sequence sees.  (The positions are cut at 0 before the window is taken off: a window may be as large as
+// 32 bits allow, and a sequence shorter than q_len.)
+__device__ __forceinline__ int first_seen(const AttendArgs& A, int len) {
+  return A.window > 0 ? max(max(len - A.q_len + 1, 0) - A.window, 0) : 0;
+}
+
 // The keys of sequence b that are its own: [lo, hi) is what any of its tokens sees, tiles start at `origin`.
 struct OwnKeys { int lo, hi, origin, tiles; };
 __device__ __forceinline__ OwnKeys own_keys(const TileArgs& T, int len) {
   OwnKeys k;
-  const int first = T.a.window > 0 ? max(len - T.a.q_len + 1 - T.a.window, 0) : 0;
-  k.lo = max(first, T.a.prefix);
+  k.lo = max(first_seen(T.a, len), T.a.prefix);
   k.hi = len;
   k.origin = k.lo & -T.box;
   k.tiles = k.hi > k.lo ? (k.hi - k.origin + AT_KEYS - 1) / AT_KEYS : 0;
@@ -215,7 +220,7 @@ __device__ __forceinline__ void make_share(const TileArgs& T, Share& S, int* s_s
   for (int b = b0; b < b1; ++b) {
     const int len = attend_len(A, b, c == 0);
     sum += own_keys(T, len).tiles;
-    if (len > 0) lo = min(lo, A.window > 0 ? max(len - A.q_len + 1 - A.window, 0) : 0);
+    if (len > 0) lo = min(lo, first_seen(A, len));
   }
   int incl = sum;
 #pragma unroll

@@ -33,3 +33,27 @@ def test_maxima_that_rise_in_the_last_tile_of_a_piece(dtype, heads, hk, keys):
         assert torch.equal(out, b.out) and torch.equal(lse, b.lse)
     assert ls.ls_paged_kv_status(kv) == 0
     kv.close()
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 3, 2 ** 30])
+@pytest.mark.parametrize("prefix,q_len", [(0, 4), (0, 9), (150, 4), (150, 9)])
+@pytest.mark.parametrize("D", [128, 96])
+def test_a_window_beyond_every_length_is_none(window, prefix, q_len, D):
+    """Such a window is a way to say 'no window', also for sequences shorter than q_len (whose first tokens see nothing)."""
+    kw = dict(D=D, prefix=prefix, q_len=q_len, lens=[1, 2, 3, 0, prefix + 40, prefix + 1, 300 + prefix], seed=q_len)
+    b = Batch(window=window, **kw)
+    kv = b.handle()
+    b.attend(kv)
+    b.check()
+    plain = Batch(window=0, **kw)
+    kv0 = plain.handle()
+    plain.attend(kv0)
+    plain.check()
+    assert ls.ls_paged_kv_status(kv) == 0 and ls.ls_paged_kv_status(kv0) == 0
+    kv.close(), kv0.close()
+    # only short sequences: nobody pulls the first key that is seen down
+    b = Batch(window=window, D=D, prefix=prefix, q_len=q_len, lens=[1, 2], seed=q_len)
+    kv = b.handle()
+    b.attend(kv)
+    b.check()
+    kv.close()
