@@ -21,7 +21,9 @@
 // A row's reference maximum follows its true maximum only when that has risen by more than 2^8: weights stay below 2^8, the
 // final division makes the reference irrelevant, and the accumulator in tensor memory is almost never rescaled.  The weights are
 // rounded to the 16-bit type because the product with the values takes them so (the values have no more bits); their sum is
-// taken before the rounding.
+// taken before the rounding.  In fp16, whose range is short, they are held 2^7 higher (at most 2^15): what is rounded to nothing, or
+// to the steps of 2^-24 that fp16 ends in, lies 2^-32 and 2^-31 below the reference instead of 2^-25 and 2^-24.  (100000 keys at e^-17.5
+// beside a strong one are a quarter of a percent, which would all be lost.)
 //
 // What bounds it (B200, measured rates 6462 GB/s and 1683 TFLOP/s): own units by memory as long as all CTAs work on them (one
 // sequence of 100001 keys, 64 / 8 heads: 71 us, 5.7 TB/s, 0.89 of measured), by the latency of a piece's start and end (about six
@@ -132,6 +134,10 @@ struct Piece {
 };
 
 constexpr int AT_NARROW = 16;
+
+// Exponents: how far a score may lie above its row's reference, and by how much weights are held higher than 2^(score - reference).
+constexpr float AT_RISE = 8.f;
+template <int WD> constexpr float AT_LIFT = WD == WD_FP16 ? 7.f : 0.f;
 
 // Walks one lane's line piece by piece.
 struct Walk {
@@ -659,6 +665,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
     const uint32_t t_s = tmem + (quad << 21) + l * AT_KEYS, t_o = tmem + (quad << 21) + 256 + l * D;
     Slots Q(S.batch_pieces[l], q_slots, 0);
     const float scale = A.scale_log2;
+    constexpr float LIFT = AT_LIFT<WD>;
     const int worker = S.sparse ? blockIdx.x : blockIdx.x * 2 + l;
     int n = 0;
     auto arrive_p = [&](uint32_t bar) {
@@ -695,7 +702,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
 
     // Narrow pieces: at most 16 rows.  The product is turned round, S^T = K Q^T: a thread has one key and the scores of all
     // rows, so that the few exponentials are spread over all 128 threads.  Weights go to shared memory as P^T's other operand.
-    // The reference of a row is kept as its negative in the exponent, `off`; 3e38 stands for a row that has seen nothing, so that
+    // The reference of a row is kept in what is added to the exponent, `off` = lift - reference; 3e38 stands for a row that has seen nothing, so that
     // its first score exceeds the reference too.  The rows' sums stay apart, by key, until the end of the piece.
     auto narrow_piece = [&](const Piece& P) {
       constexpr int NR = AT_NARROW;
@@ -724,7 +731,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
         }
         bool rise = false;
 #pragma unroll
-        for (int x = 0; x < NR; ++x) rise |= x < rows && fmaf(__uint_as_float(s[x]), scale, off[x]) > 8.f;
+        for (int x = 0; x < NR; ++x) rise |= x < rows && fmaf(__uint_as_float(s[x]), scale, off[x]) > AT_RISE + LIFT;
         if (group_any(1 + l, 128, rise)) {
           // the rows' true maxima: of each warp's keys, then of all (lane x of every warp keeps row x)
           float top = -INFINITY;
@@ -737,10 +744,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
           group_sync(1 + l, 128);
           if (lane_id < rows) {
             top = fmaxf(fmaxf(C.top[l][0][lane_id], C.top[l][1][lane_id]), fmaxf(C.top[l][2][lane_id], C.top[l][3][lane_id])) * scale;
-            rise = top + my_off > 8.f;
+            rise = top + my_off > AT_RISE + LIFT;
           } else rise = false;
-          const float f = rise ? ex2(-top - my_off) : 1.f;
-          if (rise) my_off = -top;
+          const float f = rise ? ex2(LIFT - top - my_off) : 1.f;
+          if (rise) my_off = LIFT - top;
           uint32_t o[NR];
           if (j > 0) {
             tm_ld16(t_o, o);
@@ -883,7 +890,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
           }
           if (masked) tm_wait_st();
           const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-          const bool rise = live && top > m && (m == -INFINITY || (top - m) * scale > 8.f);
+          const bool rise = live && top > m && (m == -INFINITY || (top - m) * scale > AT_RISE);
           if (__any_sync(0xffffffffu, rise)) {
             const float f = rise ? ex2((m - top) * scale) : 1.f;
             if (rise) { m = top; sum *= f; }
@@ -902,7 +909,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
               }
             }
           }
-          const float off = m == -INFINITY ? 0.f : -m * scale;
+          const float off = m == -INFINITY ? 0.f : fmaf(-m, scale, LIFT);
           const uint64_t off2 = both(off);
 #pragma unroll 1
           for (int half = 0; half < 2; ++half) {
@@ -932,7 +939,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
       const long long at = place_piece(P, po, pl) + row;
       if (warp_live) {
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        if (live) pl[at] = sum == 0.f ? -INFINITY : fmaf(m, scale, log2f(sum));
+        if (live) pl[at] = sum == 0.f ? -INFINITY : fmaf(m, scale, log2f(sum) - LIFT);
 #pragma unroll 1
         for (int c = 0; c < D / 32; ++c) {
           uint32_t o[32];

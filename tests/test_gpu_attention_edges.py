@@ -57,3 +57,45 @@ def test_a_window_beyond_every_length_is_none(window, prefix, q_len, D):
     b.attend(kv)
     b.check()
     kv.close()
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("heads,hk,seqs,prefix", [(2, 2, 1, 0), (16, 1, 1, 0), (32, 1, 1, 0), (64, 1, 3, 1500), (20, 1, 3, 1500)])
+@pytest.mark.parametrize("far", [17.5, 20.0])
+def test_many_keys_far_below_a_strong_one(dtype, heads, hk, seqs, prefix, far):
+    """A strong key in every tile, whose value is zero, beside 127 keys e^-far below it: what they weigh together is all of the output.
+    Tolerance: a weight is rounded to 16 bits relative to itself (u), in fp16 by no more than 2^-32 of the row's largest (its smallest
+    step is 2^-24, weights are held 2^7 above what the sum divides by); the output once more."""
+    b = Batch(dtype=dtype, heads=heads, hk=hk, D=64, page=64, lens=[prefix + 1500 + 10 * s for s in range(seqs)], prefix=prefix, seed=7)
+    b.q.zero_()
+    b.q[..., 0] = 16.0  # the score is 2 k[0]
+    gen = torch.Generator(device=DEV).manual_seed(11)
+    pages = [(b.prefix_pages, 0, prefix)] if prefix else []
+    pages += [(b.table[s], prefix, n) for s, n in enumerate(b.lens)]
+    for ids, lo, hi in pages:
+        p = torch.arange(lo, hi, device=DEV)
+        pg, sl = ids[p // b.page].long(), p % b.page
+        strong = p % 128 == 64
+        k = torch.zeros(hi - lo, hk, 64, device=DEV)
+        k[strong, :, 0] = far / 2
+        v = 200 + 800 * torch.rand(hi - lo, hk, 64, generator=gen, device=DEV)
+        v[strong] = 0
+        b.kp[pg, sl], b.vp[pg, sl] = k.to(b.kp.dtype), v.to(b.vp.dtype)
+    kv = b.handle()
+    b.attend(kv)
+    torch.cuda.synchronize()
+    u = 2.0 ** -11 if dtype == "fp16" else 2.0 ** -8
+    for s, n in enumerate(b.lens):
+        p = np.arange(n)
+        ids = np.where(p < prefix, b.prefix_np[np.minimum(p // b.page, max(len(b.prefix_np) - 1, 0))] if prefix else 0, b.table_np[s][p // b.page])
+        k, v = f64(b.kp)[ids, p % b.page], f64(b.vp)[ids, p % b.page]
+        for h in range(heads):
+            kh, vh = k[:, h * hk // heads], v[:, h * hk // heads]
+            w = np.exp(2 * kh[:, 0] - far)
+            ref, absv = (w @ vh) / w.sum(), vh.sum(0) / w.sum()
+            tol = (2 * u + 2.0 ** -18) * ref + (2.0 ** -32 * absv if dtype == "fp16" else 0.0) + 2.0 ** -24
+            got = f64(b.out[s, 0, h])
+            assert (np.abs(got - ref) <= tol).all(), (s, h, got[:3], ref[:3], tol[:3])
+            assert abs(float(b.lse[s, 0, h]) - (far + np.log(w.sum()))) <= 2.0 ** -16
+    assert ls.ls_paged_kv_status(kv) == 0
+    kv.close()
