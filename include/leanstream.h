@@ -396,6 +396,7 @@ int32_t ls_controller_build(int32_t n_layers, int32_t n_states, int32_t n_plans,
  *   Scores and softmax are fp32; weights are rounded to the 16-bit type for the product with the values.
  *   Memory that no token of a sequence sees (slots behind its end or before its window) may hold anything.  A value that is
  *   infinite or NaN at a position that some token of the batch sees may make NaN of a token that does not see it.
+ *   Positions end at 2^31 - 65536: a longer prefix is refused, a longer sequence treated as one beyond its table.
  * Lengths beyond the table, and table entries outside the pool, are skipped (their keys count for nothing or as zeros, never
  * read out of bounds) and recorded: ls_paged_kv_status reads and clears the handle's status word (it synchronises).
  */

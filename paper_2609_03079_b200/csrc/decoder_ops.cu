@@ -391,6 +391,7 @@ int32_t ls_paged_kv_attend(ls_paged_kv* kv, const void* d_q, int64_t q_stride, v
                 D.max_q_len);
   if (n_seqs == 0 || q_len == 0) return LS_OK;
   if (!d_q || !d_out || !d_seq_len || (!d_table && table_width > 0)) return fail(LS_ERR_INVALID, "ls_paged_kv_attend: q, out, seq_len and table are required");
+  if (prefix_len > ls::MAX_POSITIONS) return fail(LS_ERR_INVALID, "ls_paged_kv_attend: prefix_len beyond %d positions", ls::MAX_POSITIONS);
   if (prefix_len > 0 && !d_prefix_pages) return fail(LS_ERR_INVALID, "ls_paged_kv_attend: prefix_len without prefix pages");
   const int64_t qw = (int64_t)D.n_q_heads * D.head_dim;
   if (q_stride < qw || out_stride < qw) return fail(LS_ERR_INVALID, "ls_paged_kv_attend: a token stride is smaller than a token");

@@ -83,10 +83,13 @@ __device__ __forceinline__ void load8(const uint16_t* p, bool vec, float (&f)[8]
   unpack8<WD>(v, f);
 }
 
-// Length of a sequence as far as its table reaches; a longer or negative one is reported.
+// Positions that the kernels count in 32 bits: what they add to one (tiles, batches of page numbers) stays below 2^31.
+constexpr int MAX_POSITIONS = 0x7fff0000;
+
+// Length of a sequence as far as its table and the positions reach; a longer or negative one is reported.
 __device__ __forceinline__ int attend_len(const AttendArgs& A, int b, bool report) {
   const int n = A.seq_len[b];
-  const long long most = max((long long)A.table_width * A.page, 0LL);
+  const long long most = min((long long)A.table_width * A.page, (long long)MAX_POSITIONS);
   if (n < 0 || n > most) {
     if (report) set_status(A.status, ST_BAD_INDEX);
     return n < 0 ? 0 : (int)most;

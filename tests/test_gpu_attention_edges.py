@@ -99,3 +99,29 @@ def test_many_keys_far_below_a_strong_one(dtype, heads, hk, seqs, prefix, far):
             assert abs(float(b.lse[s, 0, h]) - (far + np.log(w.sum()))) <= 2.0 ** -16
     assert ls.ls_paged_kv_status(kv) == 0
     kv.close()
+
+
+@pytest.mark.parametrize("D,heads", [(64, 2), (96, 2), (64, 40)])
+@pytest.mark.parametrize("q_len", [1, 3])
+def test_positions_near_the_end_of_32_bits(D, heads, q_len):
+    """A table that reaches 2^31 positions (all of them slots of one page), lengths at and beyond the last position that is counted: the
+    last keys are seen, longer lengths are reported and cut there."""
+    page, last = 65536, 2 ** 31 - 65536
+    gen = torch.Generator(device=DEV).manual_seed(0)
+    kp, vp = (torch.randn(1, page, 1, D, generator=gen, device=DEV).bfloat16() for _ in range(2))
+    q = torch.randn(1, q_len, heads, D, generator=gen, device=DEV).bfloat16()
+    table = torch.zeros(1, 2 ** 31 // page, dtype=torch.int32, device=DEV)
+    kv = ls.ls_paged_kv_create(kp, vp, heads, max_seqs=1, max_q_len=q_len)
+    for n, status in ((last, 0), (2 ** 31 - 1, ls.LS_ERR_INVALID), (last - 7, 0), (2 ** 31 - 200, ls.LS_ERR_INVALID)):
+        out = torch.full_like(q, float("nan"))
+        ls.ls_paged_kv_attend(kv, q, out, torch.tensor([n], dtype=torch.int32, device=DEV), table, window=150)
+        assert ls.ls_paged_kv_status(kv) == status
+        for i in range(q_len):
+            hi = min(n, last) - q_len + i + 1
+            p = torch.arange(hi - 150, hi, device=DEV) % page
+            k, v = kp[0, p, 0].double(), vp[0, p, 0].double()
+            w = torch.softmax(q[0, i].double() @ k.T * D ** -0.5, -1)
+            assert ((out[0, i].double() - w @ v).abs() <= 2.0 ** -8 * (w @ v.abs() * 1.1 + (w @ v).abs()) + 2.0 ** -24).all()
+    with pytest.raises(ls.LeanStreamError, match="prefix_len"):
+        ls.ls_paged_kv_attend(kv, q, out, torch.tensor([n], dtype=torch.int32, device=DEV), table, table[0], last + 1, window=150)
+    kv.close()
