@@ -399,6 +399,7 @@ int32_t ls_controller_build(int32_t n_layers, int32_t n_states, int32_t n_plans,
  *   Positions end at 2^31 - 65536: a longer prefix is refused, a longer sequence treated as one beyond its table.
  * Lengths beyond the table, and table entries outside the pool, are skipped (their keys count for nothing or as zeros, never
  * read out of bounds) and recorded: ls_paged_kv_status reads and clears the handle's status word (it synchronises).
+ * LS_ERR_TIMEOUT there: a wait inside the attention kernel gave up; all outputs of that call are NaN.
  */
 typedef struct ls_paged_kv ls_paged_kv;
 typedef struct {

@@ -135,7 +135,9 @@ int32_t create_tiles(ls_paged_kv* kv) {
   kv->pre_units = c.pre_units;
   kv->own_units = c.own_units;
   LS_TRY(dalloc(&kv->tile_ws, (kv->pre_slots + kv->own_slots) * (d.head_dim + 1)));
-  LS_TRY(dalloc(&kv->tile_ids, 2 * (kv->pre_units + kv->own_units) + 1));
+  const size_t ids = ls::AT_MAX_CTAS / 4 + 2 * (kv->pre_units + kv->own_units) + 1;
+  LS_TRY(dalloc(&kv->tile_ids, ids));
+  LS_CUDA(cudaMemset(kv->tile_ids, 0, ids * sizeof(int32_t)));
   kv->tiles = true;
   return LS_OK;
 }
@@ -168,7 +170,8 @@ int32_t attend_tiles(ls_paged_kv* kv, const ls::AttendArgs& a, cudaStream_t st) 
   t.tq = c.tq; t.tb = c.tb; t.ts = c.ts; t.rt = c.rt; t.pairs = c.pairs; t.box = kv->box;
   t.pre_o = kv->tile_ws; t.own_o = t.pre_o + kv->pre_slots * D;
   t.pre_lse = t.own_o + kv->own_slots * D; t.own_lse = t.pre_lse + kv->pre_slots;
-  t.pre_first = kv->tile_ids; t.pre_last = t.pre_first + kv->pre_units;
+  t.gave_up = reinterpret_cast<uint8_t*>(kv->tile_ids);
+  t.pre_first = kv->tile_ids + ls::AT_MAX_CTAS / 4; t.pre_last = t.pre_first + kv->pre_units;
   t.own_first = t.pre_last + kv->pre_units; t.own_last = t.own_first + kv->own_units;
   t.plan = t.own_last + kv->own_units;
   t.workers = 2 * kv->sm_count;
@@ -198,7 +201,7 @@ int32_t create_kv(ls_paged_kv* kv) {
     const size_t rows = (size_t)kRowsBlocks * kRowsMaxGroup;
     LS_TRY(dalloc(&kv->part_o, rows * d.head_dim));
     LS_TRY(dalloc(&kv->part_lse, rows));
-    if (tiles_apply(d)) LS_TRY(create_tiles(kv));
+    if (tiles_apply(d) && sms <= ls::AT_MAX_CTAS) LS_TRY(create_tiles(kv));
   }
   return LS_OK;
 }

@@ -43,6 +43,7 @@ namespace ls {
 
 constexpr int AT_THREADS = 384;
 constexpr int AT_KEYS = 128;
+constexpr int AT_MAX_CTAS = 256;
 constexpr long long AT_SPIN_CLOCKS = 4000LL * 1000 * 1000;  // about two seconds
 // What a key tile costs a CTA, whose lanes take two at once, start and end of short pieces included, for a pair (more with a
 // window, where rows see parts of a tile) and for a lane: 64 sequences on a 65536-key prefix 196 us at 3 : 2, 202 at 4 : 2.
@@ -78,6 +79,7 @@ struct TileArgs {
   int32_t *pre_first, *pre_last, *own_first, *own_last;  // per unit: the worker of its first and last piece
   int32_t* plan;     // [1] key tiles of the prefix
   int32_t workers;   // two per CTA
+  uint8_t* gave_up;  // [AT_MAX_CTAS], 8-byte aligned, per CTA: a wait of its gave up in this call
 };
 
 // a / b for a >= 0, b > 0 and a quotient below 2^22 (then the estimate is off by one at most): numbers of units, heads, rows and
@@ -348,11 +350,6 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
   const uint32_t q_base = saddr(dyn), ring = q_base + 2 * TS::TILE;
   const uint32_t b_full = saddr(C.full), b_empty = saddr(C.empty), b_qfull = saddr(C.qfull), b_qempty = saddr(C.qempty), b_s = saddr(C.s),
                  b_p = saddr(C.p), b_ph = saddr(C.p_half), b_o = saddr(C.o), b_turn = saddr(C.turn), b_done = saddr(C.done);
-  if (q_base & 1023) {  // (swizzled tiles need it; the first byte of a block's shared memory has it)
-    if (tid == 0) set_status(A.status, ST_INTERNAL);
-    return;
-  }
-
   if (warp == 0) {
     if (lane_id < 2 * NST) mb_init(b_full + 8 * lane_id, 1);
     if (lane_id < NST) mb_init(b_empty + 8 * lane_id, 2);
@@ -365,6 +362,10 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
   }
   if (warp == 8 && lane_id < 4) tma_prefetch_map(lane_id == 0 ? &map_k : lane_id == 1 ? &map_v : lane_id == 2 ? &map_q_all : &map_q_own);
   asm volatile("griddepcontrol.wait;" ::: "memory");  // (all before this overlaps the end of the kernel in front)
+  if (q_base & 1023) {  // (swizzled tiles need it; the first byte of a block's shared memory has it)
+    if (tid == 0) { set_status(A.status, ST_INTERNAL); T.gave_up[blockIdx.x] = 1; }
+    return;
+  }
   make_share(T, S, C.scan, blockIdx.x, gridDim.x);
   __syncthreads();
   // (the copying warps, which have no use for tensor memory, do not wait for it)
@@ -960,6 +961,7 @@ __global__ void __launch_bounds__(AT_THREADS, 1)
   }
   if (blockIdx.x == 0 && tid == 0) *T.plan = S.pre_tiles;
   __syncthreads();
+  if (tid == 0) T.gave_up[blockIdx.x] = C.dead != 0;
   if (C.dead) {  // copies and products that are still in flight get time to land before the CTA's memory goes
     const long long t0 = clock64();
     while (clock64() - t0 < AT_SPIN_CLOCKS / 1000) {}
@@ -1002,12 +1004,15 @@ __global__ void __launch_bounds__(256) ls_attend_tile_join_kernel(const TileArgs
   if (WARPS > 1) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   int n_pre = 0, n_own = 0;
   long long pre_at = 0, own_at = 0;
-  // (a kernel that gave up on a wait leaves workers unnoted: its rows are reported and come out as zeros)
+  // (notes of a call that gave up are old ones, or none)
   auto pieces = [&](int first, int last) {
     if (first >= 0 && first <= last && last < T.workers) return last - first + 1;
     set_status(A.status, ST_INTERNAL);
     return 0;
   };
+  // A CTA that gave up on a wait (it has set the status) leaves notes and slots as an older call left them: nothing of this call is
+  // to be used, and every row says so with NaN.  (Asked for here, used at the end: nothing waits for it.)
+  const uint2 gave_up = reinterpret_cast<const uint2*>(T.gave_up)[lane];
   const int with_pre = *T.plan, pre0 = T.pre_first[pre_unit], pre1 = T.pre_last[pre_unit], own0 = T.own_first[own_unit], own1 = T.own_last[own_unit];
   const bool own = own_keys(T, attend_len(A, b, false)).tiles > 0;
   if (with_pre > 0) {
@@ -1057,9 +1062,10 @@ __global__ void __launch_bounds__(256) ls_attend_tile_join_kernel(const TileArgs
       }
     }
   }
-  const float inv = tot == 0.f ? 0.f : 1.f / tot;
+  const bool broken = __any_sync(0xffffffffu, (gave_up.x | gave_up.y) != 0);
+  const float inv = broken ? NAN : tot == 0.f ? 0.f : 1.f / tot;
   uint16_t* dst = static_cast<uint16_t*>(A.out) + t * A.out_stride + (long long)hd * D;
-  if (lane == 0 && part == 0 && A.lse) A.lse[row] = tot == 0.f ? -INFINITY : (top + log2f(tot)) * LN2;
+  if (lane == 0 && part == 0 && A.lse) A.lse[row] = broken ? NAN : tot == 0.f ? -INFINITY : (top + log2f(tot)) * LN2;
   if (WARPS > 1) {
 #pragma unroll
     for (int c = 0; c < E; ++c) s_acc[warp][lane * E + c] = acc[c];
