@@ -203,6 +203,8 @@ int32_t create_kv(ls_paged_kv* kv) {
     LS_TRY(dalloc(&kv->part_lse, rows));
     if (tiles_apply(d) && sms <= ls::AT_MAX_CTAS) LS_TRY(create_tiles(kv));
   }
+  // (the clearing above runs on the default stream, which other streams need not wait for)
+  LS_CUDA(cudaStreamSynchronize(nullptr));
   return LS_OK;
 }
 
@@ -330,6 +332,7 @@ int32_t ls_paged_kv_status(ls_paged_kv* kv, int32_t* host_status) {
   int v = 0;
   LS_CUDA(cudaMemcpy(&v, kv->status, sizeof v, cudaMemcpyDeviceToHost));
   LS_CUDA(cudaMemset(kv->status, 0, sizeof v));
+  LS_CUDA(cudaStreamSynchronize(nullptr));  // (a later call on a stream that does not wait for the default one may report something)
   *host_status = v;
   return LS_OK;
 }

@@ -125,3 +125,24 @@ def test_positions_near_the_end_of_32_bits(D, heads, q_len):
     with pytest.raises(ls.LeanStreamError, match="prefix_len"):
         ls.ls_paged_kv_attend(kv, q, out, torch.tensor([n], dtype=torch.int32, device=DEV), table, table[0], last + 1, window=150)
     kv.close()
+
+
+def test_a_handle_is_ready_for_any_stream_when_it_is_made():
+    """A report of a call right behind the handle's creation, or behind a status call, on a stream that does not wait for the default
+    one is not wiped by their clearing (which the default stream may be late with)."""
+    st = torch.cuda.Stream()
+    busy = torch.randn(4096, 4096, device=DEV)
+    b = Batch(D=64, lens=[200, 90])
+    b.table[0, 2] = -1
+    torch.cuda.synchronize()
+    for _ in range(5):
+        with torch.cuda.stream(torch.cuda.default_stream()):
+            for _ in range(20):
+                busy @ busy
+        kv = b.handle()
+        for _ in range(3):
+            b.attend(kv, stream=st)
+            assert ls.ls_paged_kv_status(kv) == ls.LS_ERR_INVALID
+        b.attend(kv, stream=st)
+        assert ls.ls_paged_kv_status(kv) == ls.LS_ERR_INVALID and ls.ls_paged_kv_status(kv) == 0
+        kv.close()
