@@ -43,6 +43,12 @@ constexpr long long kJoinFewRows = 148 * 8;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+// Each pointer (NULL among them) lies at a multiple of its element's `size` bytes: the kernels' accesses would fault otherwise.
+template <class... P>
+bool elements_aligned(size_t size, P... p) {
+  return ((reinterpret_cast<uintptr_t>(p) | ...) & (size - 1)) == 0;
+}
+
 void free_kv(ls_paged_kv* kv) {
   cudaFree(kv->part_o); cudaFree(kv->part_lse); cudaFree(kv->status); cudaFree(kv->tile_ws); cudaFree(kv->tile_ids);
   delete kv;
@@ -352,6 +358,8 @@ int32_t ls_paged_kv_append(ls_paged_kv* kv, const void* d_q, int64_t q_stride, v
   if (k_stride < kw || v_stride < kw || (d_q && (q_stride < qw || q_out_stride < qw)))
     return fail(LS_ERR_INVALID, "ls_paged_kv_append: a token stride is smaller than a token");
   if (n_seqs > 1 && table_stride < table_width) return fail(LS_ERR_INVALID, "ls_paged_kv_append: table_stride is smaller than table_width");
+  if (!elements_aligned(2, d_q, d_q_out, d_k, d_v) || !elements_aligned(4, d_seq, d_pos, d_table))
+    return fail(LS_ERR_INVALID, "ls_paged_kv_append: a misaligned pointer");
   DeviceGuard guard(D.device);
   ls::AppendArgs a{};
   a.q = static_cast<const uint16_t*>(d_q); a.q_out = static_cast<uint16_t*>(d_q_out);
@@ -403,6 +411,8 @@ int32_t ls_paged_kv_attend(ls_paged_kv* kv, const void* d_q, int64_t q_stride, v
   if (q_stride < qw || out_stride < qw) return fail(LS_ERR_INVALID, "ls_paged_kv_attend: a token stride is smaller than a token");
   if (n_seqs > 1 && table_stride < table_width) return fail(LS_ERR_INVALID, "ls_paged_kv_attend: table_stride is smaller than table_width");
   if (!(scale > 0.f) || scale > 1e30f) return fail(LS_ERR_INVALID, "ls_paged_kv_attend: scale must be positive and finite");
+  if (!elements_aligned(2, d_q, d_out) || !elements_aligned(4, d_lse, d_seq_len, d_table, d_prefix_pages))
+    return fail(LS_ERR_INVALID, "ls_paged_kv_attend: a misaligned pointer");
   DeviceGuard guard(D.device);
   ls::AttendArgs a{};
   a.q = d_q; a.out = d_out; a.lse = d_lse; a.k = D.d_k; a.v = D.d_v; a.seq_len = d_seq_len; a.table = d_table; a.prefix_pages = d_prefix_pages;
@@ -440,6 +450,9 @@ int32_t ls_block_norm(const void* d_x, int64_t x_stride, int32_t x_dtype, const 
   if (n > 1 && (x_stride < d || (d_y && y_stride < d) || (d_x_out && x_out_stride < d) || (d_h && h_stride < d) ||
                 (d_gate && gate_stride != 0 && gate_stride < d)))
     return fail(LS_ERR_INVALID, "ls_block_norm: a row stride is smaller than a row");
+  if (!elements_aligned(x_dtype == LS_DTYPE_F32 ? 4 : 2, d_x, d_x_out) ||
+      !elements_aligned(dtype == LS_DTYPE_F32 ? 4 : 2, d_y, d_h, d_gate) || !elements_aligned(4, d_w_post, d_w_pre))
+    return fail(LS_ERR_INVALID, "ls_block_norm: a misaligned pointer");
   int dev = -1;
   LS_CUDA(cudaGetDevice(&dev));
   static const int n_dev = [] { int k = 0; return cudaGetDeviceCount(&k) == cudaSuccess ? k : 0; }();
