@@ -313,10 +313,8 @@ int32_t ls_paged_kv_create(const ls_paged_kv_desc* D, ls_paged_kv** out) {
   if (!D->d_rope) kv->d.rope_dim = kv->d.rope_positions = 0;
   const int32_t rc = create_kv(kv);
   if (rc != LS_OK) {
-    const std::string keep = g_err;
-    free_kv(kv);
+    free_kv(kv);  // (leaves the error's text alone)
     cudaGetLastError();
-    g_err = keep;
     return rc;
   }
   *out = kv;

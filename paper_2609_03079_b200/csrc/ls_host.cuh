@@ -54,14 +54,20 @@ struct KernelTimer {
   KernelTimer(int kind, cudaStream_t s) : st(s), on(g_timing.load(std::memory_order_relaxed) != 0) {
     if (!on) return;
     t.kind = kind;
-    if (cudaEventCreate(&t.a) != cudaSuccess || cudaEventCreate(&t.b) != cudaSuccess) { on = false; return; }
+    if (cudaEventCreate(&t.a) != cudaSuccess) { on = false; return; }
+    if (cudaEventCreate(&t.b) != cudaSuccess) { cudaEventDestroy(t.a); on = false; return; }
     cudaEventRecord(t.a, st);
   }
   ~KernelTimer() {
     if (!on) return;
     cudaEventRecord(t.b, st);
-    std::lock_guard<std::mutex> lk(g_timing_mu);
-    g_timed.push_back(t);
+    try {
+      std::lock_guard<std::mutex> lk(g_timing_mu);
+      g_timed.push_back(t);
+    } catch (...) {  // (no memory for it: the launch goes untimed, nothing is thrown through the C ABI)
+      cudaEventDestroy(t.a);
+      cudaEventDestroy(t.b);
+    }
   }
 };
 
