@@ -9,7 +9,7 @@ fp32, as the FFN half keeps it, and holds one row per sequence.
 from __future__ import annotations
 
 from dataclasses import dataclass
-from typing import List, Optional
+from typing import List, Optional, Tuple
 
 import torch
 
@@ -34,16 +34,25 @@ class PagePool:
         self.held: List[List[int]] = [[] for _ in range(max_seqs)]
 
     def reserve(self, seq: int, positions: int, first: int = 0) -> None:
-        """Gives sequence ``seq`` pages for positions [first, positions) that it does not have yet (``first``: where its own start)."""
-        at = first // self.page_size + len(self.held[seq])
-        new = []
-        while at + len(new) < -(-positions // self.page_size):
-            if not self.free:
-                raise ls.LeanStreamError(ls.LS_ERR_CAPACITY, "no free page")
-            new.append(self.free.pop())
-        if new:
-            self.table[seq, at:at + len(new)] = torch.tensor(new, dtype=torch.int32, device=self.table.device)
-            self.held[seq] += new
+        """Gives sequence ``seq`` pages for positions [first, positions) that it does not have yet (``first``: where its own start).
+        Nothing changes if it cannot have all of them."""
+        self.reserve_all([(seq, positions)], first)
+
+    def reserve_all(self, wanted: List[Tuple[int, int]], first: int = 0) -> None:
+        """``reserve`` for several (sequence, positions): all of them, or none."""
+        start, need = first // self.page_size, []
+        for seq, positions in wanted:
+            at, end = start + len(self.held[seq]), -(-positions // self.page_size)
+            if end > self.table.shape[1]:
+                raise ls.LeanStreamError(ls.LS_ERR_CAPACITY, f"{positions} positions, the table holds {self.table.shape[1]} pages of {self.page_size}")
+            need.append((seq, at, max(0, end - at)))
+        if sum(n for _, _, n in need) > len(self.free):
+            raise ls.LeanStreamError(ls.LS_ERR_CAPACITY, "no free page")
+        for seq, at, n in need:
+            if n:
+                new = [self.free.pop() for _ in range(n)]
+                self.table[seq, at:at + n] = torch.tensor(new, dtype=torch.int32, device=self.table.device)
+                self.held[seq] += new
 
     def release(self, seq: int) -> None:
         self.free += self.held[seq]
@@ -118,10 +127,10 @@ class Decoder:
         self.seq = torch.arange(max_seqs, dtype=torch.int32, device=dev)
 
     def step(self, x: torch.Tensor) -> torch.Tensor:
-        """The next token of every sequence: x [max_seqs, d] fp32 in place through all layers."""
-        for b in range(self.max_seqs):
-            self.pool.reserve(b, self.lens[b] + 1, self.prefix_len)
-            self.lens[b] += 1
+        """The next token of every sequence: x [max_seqs, d] fp32 in place through all layers.  Nothing has happened if there is no room
+        for one of them."""
+        self.pool.reserve_all([(b, self.lens[b] + 1) for b in range(self.max_seqs)], self.prefix_len)
+        self.lens = [n + 1 for n in self.lens]
         seq_len = torch.tensor(self.lens, dtype=torch.int32).to(x.device)
         for layer in self.layers:
             layer.decode(x, self.seq, seq_len - 1, seq_len, self.pool.table[:self.max_seqs], self.prefix_pages, self.prefix_len)
