@@ -123,6 +123,7 @@ class Decoder:
         self.max_seqs = max_seqs
         self.lens = [0] * max_seqs
         self.prefix_len = 0
+        self.prefix_held: List[int] = []  # pages of the prefix, and the same on the device
         self.prefix_pages: Optional[torch.Tensor] = None
         self.seq = torch.arange(max_seqs, dtype=torch.int32, device=dev)
 
@@ -137,17 +138,19 @@ class Decoder:
         return x
 
     def share_prefix(self, seq: int = 0) -> None:
-        """Makes what sequence ``seq`` has decoded so far (a whole number of pages of it) the prefix of all sequences; the others
-        must be empty.  The rest of the sequence is dropped."""
+        """Makes what sequence ``seq`` has decoded so far (a whole number of pages of it, a prefix that it stands on among them) the
+        prefix of all sequences; the others must have nothing of their own.  The rest of the sequence is dropped."""
         ps = self.pool.page_size
         n = self.lens[seq] // ps * ps
-        if any(self.lens[b] for b in range(self.max_seqs) if b != seq):
-            raise ls.LeanStreamError(ls.LS_ERR_STATE, "the other sequences must be empty")
-        pages = self.pool.held[seq][: n // ps]
-        self.pool.free += self.pool.held[seq][n // ps:]
-        self.pool.held[seq] = []
+        if any(self.lens[b] > self.prefix_len for b in range(self.max_seqs) if b != seq):
+            raise ls.LeanStreamError(ls.LS_ERR_STATE, "the other sequences must have nothing of their own")
+        held = self.pool.held[seq]
+        kept = (n - self.prefix_len) // ps
+        self.prefix_held += held[:kept]
+        self.pool.held[seq] = held[kept:]
+        self.pool.release(seq)
         self.prefix_len = n
-        self.prefix_pages = torch.tensor(pages, dtype=torch.int32, device=self.pool.table.device)
+        self.prefix_pages = torch.tensor(self.prefix_held, dtype=torch.int32, device=self.pool.table.device)
         self.lens = [n] * self.max_seqs
 
     def close(self) -> None:

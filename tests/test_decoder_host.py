@@ -49,3 +49,39 @@ def test_a_step_without_room_changes_nothing(pages):
     pool.free += [100, 101, 102][: 6 - pages]
     d.step(x)
     assert d.lens == [3, 3, 3] and all(len(h) == 2 for h in pool.held) and not pool.free
+
+
+@pytest.mark.parametrize("seqs", [1, 3])
+def test_a_prefix_can_be_extended(seqs):
+    """A second share_prefix keeps the first one's pages in front; every page is in one place."""
+    pool = PagePool(40, 4, seqs, 128, "cpu")
+    one, d = Decoder([], pool, 1), Decoder([], pool, seqs)
+    x = torch.zeros(1, 8)
+    for _ in range(10):
+        one.step(x)
+    d.lens[0] = one.lens[0]
+    first = pool.held[0][:2]
+    d.share_prefix(0)
+    assert d.prefix_len == 8 and d.prefix_pages.tolist() == first and d.lens == [8] * seqs and len(pool.free) == 38
+    if seqs > 1:
+        d.step(torch.zeros(seqs, 8))
+        with pytest.raises(ls.LeanStreamError) as e:
+            d.share_prefix(0)
+        assert e.value.code == ls.LS_ERR_STATE
+        for b in range(seqs):
+            pool.release(b)
+        d.lens = [8] * seqs
+        d.share_prefix(1)
+        assert d.prefix_len == 8 and d.prefix_pages.tolist() == first and d.lens == [8] * seqs
+        return
+    for _ in range(7):
+        d.step(x)
+    own = list(pool.held[0])
+    assert d.lens == [15] and len(own) == 2 and pool.table[0, 2:4].tolist() == own
+    d.share_prefix(0)
+    assert d.prefix_len == 12 and d.prefix_pages.tolist() == first + own[:1] and d.lens == [12]
+    assert sorted(pool.free + d.prefix_held) == list(range(40)) and pool.held == [[]]
+    d.step(x)
+    assert d.lens == [13] and pool.table[0, 3].item() == pool.held[0][0]
+    d.share_prefix(0)  # less than a page more: the prefix stays
+    assert d.prefix_len == 12 and d.prefix_pages.tolist() == first + own[:1] and d.lens == [12] and pool.held == [[]]
