@@ -384,7 +384,8 @@ int32_t ls_controller_build(int32_t n_layers, int32_t n_states, int32_t n_plans,
  *   value in the token's slot (position d_pos[t] of sequence d_seq[t]); the turned query goes to d_q_out.  d_q, d_k, d_v and
  *   d_q_out are [n_tokens][heads][head_dim] with token strides (heads side by side), so slices of one projection's output
  *   need no copy; d_q NULL: keys and values only; d_q_out may be d_q.  A token with a negative sequence or position is
- *   padding: nothing is stored for it, its query is copied.  Two tokens of one call with the same slot: either one lands.
+ *   padding: nothing is stored for it.  Queries are turned by the position alone, padding or not; one whose position is negative
+ *   or beyond rope_positions is copied as it is.  Two tokens of one call with the same slot: the slot holds parts of either.
  *
  * ls_paged_kv_attend: causal attention of the last q_len tokens of each of n_seqs sequences; token i of sequence b stands at
  *   position d_seq_len[b] - q_len + i and sees the positions up to its own, the last `window` of them (window = 0: all).

@@ -50,7 +50,8 @@ def attend(q, k_pages, v_pages, seq_len, table, prefix_pages, prefix_len, window
 
 
 def rotate(x, pos, table, interleaved):
-    """x [tokens, heads, dim] turned by rows ``pos`` of table [positions, r] (cosines, then sines); table None: as it is."""
+    """x [tokens, heads, dim] turned by rows ``pos`` of table [positions, r] (cosines, then sines); table None, or a negative position: as it
+    is."""
     y = x.copy()
     if table is None:
         return y

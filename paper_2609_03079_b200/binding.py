@@ -565,7 +565,8 @@ def _raw(stream) -> Optional[int]:
 
 def ls_paged_kv_append(kv: PagedKV, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, q_out: Optional[torch.Tensor],
                        seq: torch.Tensor, pos: torch.Tensor, table: torch.Tensor, stream=None) -> None:
-    """q, k, v, q_out: [tokens, heads, head_dim] (any token stride); seq, pos: int32 [tokens]; table: int32 [sequences, pages]."""
+    """q, k, v, q_out: [tokens, heads, head_dim] (any token stride); seq, pos: int32 [tokens] (negative: padding, stored nowhere; a query is
+    turned by its position all the same, unless that is negative); table: int32 [sequences, pages]."""
     rc = _fast.append(kv.plan, q, k, v, q_out, seq, pos, table, _raw(stream))
     if rc:
         _check(rc)

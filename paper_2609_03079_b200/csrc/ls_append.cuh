@@ -39,7 +39,8 @@ __device__ __forceinline__ uint16_t narrow(float x) {
 }
 
 // Where token t's keys and values go (element offset of head 0 in the pages), or -1: padding (a negative sequence or
-// position) is passed over silently, anything out of range is passed over and reported.
+// position) is passed over silently, anything out of range is passed over and reported.  (What becomes of the token's query does
+// not depend on this: it is turned if its position is in the rotation table.)
 __device__ __forceinline__ long long append_slot(const AppendArgs& A, int sq, int ps) {
   if (sq < 0 || ps < 0) return -1;
   const int pg = ps / A.page;
