@@ -26,11 +26,6 @@ struct NormArgs {
 };
 
 template <int DT>
-__device__ __forceinline__ float ld1(const void* p, long long i) {
-  if (DT == DT_F32) return static_cast<const float*>(p)[i];
-  return widen<DT == DT_F32 ? 0 : DT>(static_cast<const uint16_t*>(p)[i]);
-}
-template <int DT>
 __device__ __forceinline__ void st1(void* p, long long i, float v) {
   if (DT == DT_F32) static_cast<float*>(p)[i] = v;
   else static_cast<uint16_t*>(p)[i] = narrow<DT == DT_F32 ? 0 : DT>(v);
