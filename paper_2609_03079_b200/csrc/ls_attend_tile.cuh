@@ -29,8 +29,8 @@
 // sequence of 100001 keys, 64 / 8 heads: 71 us, 5.7 TB/s, 0.89 of measured), by the latency of a piece's start and end (about six
 // thousand cycles) where pieces are a few tiles long; pairs by the chain softmax -> P V -> Q K^T of a lane (3.6 thousand cycles
 // for two 128 x 128 tiles against 2.05 of products: tensor memory has no room for a second set of scores; 4.2 before the values
-// of half a tile were multiplied under the other half's weights).  64 sequences on a 65536-key prefix: 201 us, 690 TFLOP/s, 0.41
-// of measured.  A fifth of the warps' time was once spent waiting for instructions:
+// of half a tile were multiplied under the other half's weights).  64 sequences on a 65536-key prefix: 191 to 204 us,
+// depending on the card, 680 to 725 TFLOP/s, 0.41 to 0.43 of measured.  A fifth of the warps' time was once spent waiting for instructions:
 // the six programs are kept short (loops rolled, one copy of each), which was worth 10 to 20 %.
 // Measured against the alternatives: narrow pieces by the wide program 71 -> 85 us (one long sequence) and 110 -> 127 (128
 // sequences); keys and values copied by one warp 82 -> 91 us with pages of 16; own units in the order sequence by sequence
@@ -45,8 +45,11 @@ constexpr int AT_THREADS = 384;
 constexpr int AT_KEYS = 128;
 constexpr int AT_MAX_CTAS = 256;
 constexpr long long AT_SPIN_CLOCKS = 4000LL * 1000 * 1000;  // about two seconds
-// What a key tile costs a CTA, whose lanes take two at once, start and end of short pieces included, for a pair (more with a
-// window, where rows see parts of a tile) and for a lane: 64 sequences on a 65536-key prefix 196 us at 3 : 2, 202 at 4 : 2.
+// What a key tile costs a CTA, whose lanes take two at once, start and end of short pieces included, for a pair and for a lane.
+// 3 : 2 against 4 : 2, in turn on one card: 64 sequences on a 65536-key prefix 197.5 us against 204, 128 on 8192 keys 109 against 111.
+// With a window more, because rows then see parts of a tile, whose masks cost a pair twice the time: 16 sequences of 4 drafts whose
+// windows start inside the prefix 48 us with 5 against 62 with 3.  Where the window leaves most of the prefix whole, 5 is too much:
+// 128 sequences on 8192 keys with a window of 4096 88 us against 71, 64 of 4 tokens with 6000 133 against 124.
 constexpr int AT_COST_PAIR = 3, AT_COST_PAIR_WINDOW = 5, AT_COST_LANE = 2;
 constexpr int AT_SHARE = 4, AT_SHARE_WINDOW = 5;  // a CTA's least share: a pair's tile, and a tile for both lanes
 
