@@ -310,6 +310,9 @@ int32_t ls_set_option(int32_t option, int32_t value);
 #define LS_TIMED_ATTEND 5  /* the kernels of one ls_paged_kv_attend */
 #define LS_TIMED_APPEND 6  /* ls_paged_kv_append */
 #define LS_TIMED_NORM 7    /* ls_block_norm */
+#define LS_TIMED_ATTEND4 8 /* ls_paged_kv4_attend */
+#define LS_TIMED_APPEND4 9 /* ls_paged_kv4_append */
+#define LS_TIMED_READ4 10  /* ls_paged_kv4_read */
 int32_t ls_timing_enable(int32_t on);
 int32_t ls_timing_read(int32_t kind, int64_t *launches, double *total_ms);
 
@@ -424,6 +427,61 @@ int32_t ls_paged_kv_attend(ls_paged_kv *kv, const void *d_q, int64_t q_stride, v
                            int64_t table_stride, const int32_t *d_prefix_pages, int32_t prefix_len, int32_t window, float scale,
                            void *stream);
 int32_t ls_paged_kv_status(ls_paged_kv *kv, int32_t *host_status);
+
+/*
+ * The same cache in 4 bits: a quarter of the bytes to keep and to read, for conversations whose keys and values are most of a
+ * step.  A layer's attention block is the one above with these calls in place of ls_paged_kv_append and ls_paged_kv_attend.
+ *
+ * `group` consecutive components of one token's key or value of one head share a scale and a zero of the 16-bit type `dtype`.  With
+ * x the components as a 16-bit cache would hold them (a key is turned in 64 bits, rounded to 32 and then to 16):
+ *   zero = min x,  scale = (max x - min x) / 15 rounded to dtype,  code = min(15, (x - zero) / scale rounded to nearest, ties to even)
+ * and the cache holds scale * code + zero.  A scale of 0 makes all codes 0; components whose range is not finite are held as NaN.
+ * head_dim: 64, 128 or 256; group: 32, 64 or 128, at most head_dim; page_size: a multiple of 16; heads as for ls_paged_kv.
+ * The pages are the CALLER's device memory, borrowed: block (page, head), ls_paged_kv4_block_bytes() long, starts at byte
+ * page * page_stride + head * head_stride of d_pages; the address and both strides are multiples of 16.  A block is a row of tiles of
+ * 16 tokens (16 (head_dim + 8 head_dim / group) bytes), each 16 rows of key codes (head_dim / 2 bytes), 16 rows of value codes, 16 rows
+ * of head_dim / group (scale, zero) pairs of keys, and as many of values.  Within a code row, words of eight codes (four bits each, the
+ * lowest bits first) lie thus, r being the row's number in its tile, n = min(4, head_dim / 32), m = head_dim / 64:
+ *   keys: components 8 w ... 8 w + 7 are word (w % 4) n + (w / 4) % n of a part of 4 n words; with head_dim 256 there are two parts, in
+ *     which part w / 16 is in place w / 16 ^ r % 2;
+ *   values: components 64 j + 4 i ... + 3 (low half) and 64 j + 32 + 4 i ... + 3 (high half), i < 8, are word i m + j; pieces of 8 words are in
+ *     place piece ^ s, s = 0, r / 2 % 2, r % 4 for head_dim 64, 128, 256.
+ *
+ * ls_paged_kv4_append, ls_paged_kv4_attend: as their 16-bit namesakes.  A sequence's prefix pages are listed in its row of d_table like
+ *   any others (sequences may share pages): there is no separate prefix.  A position appended twice in one call holds parts of either.
+ * ls_paged_kv4_attend: scores, softmax statistics and sums are fp32; weights times scales are rounded to fp16 for the product with
+ *   the codes.  A token's result depends on nothing that it does not see.  Meant for a few tokens per sequence; rows of
+ *   q_len * n_q_heads / n_kv_heads beyond 32 (16 for head_dim 256) read the keys again.
+ * ls_paged_kv4_read: keys and values of tokens (position d_pos[t] of sequence d_seq[t]) as the 16-bit type; d_k_out or d_v_out NULL: not
+ *   wanted.  Rows of padding (a negative sequence or position) and of tokens that are out of range are left as they were.
+ * Handles, streams, capture, status and errors as for ls_paged_kv.  Positions end at 2^31 - 65536.
+ */
+typedef struct ls_paged_kv4 ls_paged_kv4;
+typedef struct {
+  uint32_t struct_size;
+  int32_t device;
+  int32_t dtype, n_q_heads, n_kv_heads, head_dim, group, page_size, n_pages;
+  void *d_pages;
+  int64_t page_stride, head_stride; /* bytes */
+  int32_t max_seqs, max_q_len;
+  const float *d_rope;
+  int32_t rope_positions, rope_dim, rope_interleaved;
+} ls_paged_kv4_desc;
+/* Bytes of one block, or LS_ERR_INVALID. */
+int64_t ls_paged_kv4_block_bytes(int32_t page_size, int32_t head_dim, int32_t group);
+int32_t ls_paged_kv4_create(const ls_paged_kv4_desc *desc, ls_paged_kv4 **out);
+int32_t ls_paged_kv4_destroy(ls_paged_kv4 *kv);
+int32_t ls_paged_kv4_append(ls_paged_kv4 *kv, const void *d_q, int64_t q_stride, void *d_q_out, int64_t q_out_stride, const void *d_k,
+                            int64_t k_stride, const void *d_v, int64_t v_stride, int32_t n_tokens, const int32_t *d_seq,
+                            const int32_t *d_pos, const int32_t *d_table, int32_t n_seqs, int32_t table_width, int64_t table_stride,
+                            void *stream);
+int32_t ls_paged_kv4_attend(ls_paged_kv4 *kv, const void *d_q, int64_t q_stride, void *d_out, int64_t out_stride, float *d_lse,
+                            int32_t n_seqs, int32_t q_len, const int32_t *d_seq_len, const int32_t *d_table, int32_t table_width,
+                            int64_t table_stride, int32_t window, float scale, void *stream);
+int32_t ls_paged_kv4_read(ls_paged_kv4 *kv, void *d_k_out, int64_t k_stride, void *d_v_out, int64_t v_stride, int32_t n_tokens,
+                          const int32_t *d_seq, const int32_t *d_pos, const int32_t *d_table, int32_t n_seqs, int32_t table_width,
+                          int64_t table_stride, void *stream);
+int32_t ls_paged_kv4_status(ls_paged_kv4 *kv, int32_t *host_status);
 
 /*
  * The norms before and after a block, fused with its gate, residual scale and residual sum, for n rows of d elements:

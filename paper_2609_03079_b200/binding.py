@@ -27,7 +27,8 @@ EXPORTS = [
     "ls_last_error", "ls_version", "ls_timing_enable", "ls_timing_read", "ls_set_option", "ls_topk_select_static", "ls_stack_create",
     "ls_stack_destroy", "ls_stack_decode", "ls_controller_quantize", "ls_controller_build", "ls_hash_predictor_create",
     "ls_hash_predictor_destroy", "ls_hash_predict", "ls_paged_kv_create", "ls_paged_kv_destroy", "ls_paged_kv_append",
-    "ls_paged_kv_attend", "ls_paged_kv_status", "ls_block_norm",
+    "ls_paged_kv_attend", "ls_paged_kv_status", "ls_block_norm", "ls_paged_kv4_block_bytes", "ls_paged_kv4_create",
+    "ls_paged_kv4_destroy", "ls_paged_kv4_append", "ls_paged_kv4_attend", "ls_paged_kv4_read", "ls_paged_kv4_status",
 ]
 
 
@@ -83,6 +84,13 @@ class ls_paged_kv_desc(C.Structure):
                 ("rope_interleaved", C.c_int32)]
 
 
+class ls_paged_kv4_desc(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("device", C.c_int32), ("dtype", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("group", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32), ("d_pages", C.c_void_p),
+                ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("max_seqs", C.c_int32), ("max_q_len", C.c_int32), ("d_rope", C.c_void_p),
+                ("rope_positions", C.c_int32), ("rope_dim", C.c_int32), ("rope_interleaved", C.c_int32)]
+
+
 _lib = None
 
 
@@ -127,13 +135,21 @@ def lib() -> C.CDLL:
         L.ls_paged_kv_attend.argtypes = [P, P, N, P, N, P, I, I, P, P, I, N, P, I, I, C.c_float, P]
         L.ls_paged_kv_status.argtypes = [P, C.POINTER(I)]
         L.ls_block_norm.argtypes = [P, N, I, P, N, I, P, N, P, N, I, I, I, P, P, N, C.c_float, I, P, C.c_float, P]
+        L.ls_paged_kv4_block_bytes.argtypes = [I, I, I]
+        L.ls_paged_kv4_create.argtypes = [C.POINTER(ls_paged_kv4_desc), C.POINTER(P)]
+        L.ls_paged_kv4_destroy.argtypes = [P]
+        L.ls_paged_kv4_append.argtypes = [P, P, N, P, N, P, N, P, N, I, P, P, P, I, I, N, P]
+        L.ls_paged_kv4_attend.argtypes = [P, P, N, P, N, P, I, I, P, P, I, N, I, C.c_float, P]
+        L.ls_paged_kv4_read.argtypes = [P, P, N, P, N, I, P, P, P, I, I, N, P]
+        L.ls_paged_kv4_status.argtypes = [P, C.POINTER(I)]
         L.ls_timing_enable.argtypes = [C.c_int32]
         L.ls_timing_read.argtypes = [C.c_int32, C.POINTER(C.c_int64), C.POINTER(C.c_double)]
         L.ls_kernel_launches.restype = C.c_int64
         L.ls_last_error.argtypes = [C.c_char_p, C.c_size_t]
         L.ls_last_error.restype = C.c_size_t
+        L.ls_paged_kv4_block_bytes.restype = C.c_int64
         for name in EXPORTS:
-            if name not in ("ls_kernel_launches", "ls_last_error"):
+            if name not in ("ls_kernel_launches", "ls_last_error", "ls_paged_kv4_block_bytes"):
                 getattr(L, name).restype = C.c_int32
         _lib = L
     return _lib
@@ -151,7 +167,8 @@ def _marshal():
         m = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(m)
         L = lib()
-        m.bind(*(C.cast(f, C.c_void_p).value for f in (L.ls_paged_kv_append, L.ls_paged_kv_attend, L.ls_block_norm)))
+        m.bind(*(C.cast(f, C.c_void_p).value for f in (L.ls_paged_kv_append, L.ls_paged_kv_attend, L.ls_block_norm, L.ls_paged_kv4_append,
+                                                          L.ls_paged_kv4_attend, L.ls_paged_kv4_read)))
         _fast = m
     return _fast
 
@@ -345,6 +362,7 @@ def ls_version() -> int:
 
 LS_TIMED_GATEUP, LS_TIMED_DOWN, LS_TIMED_PREDICT, LS_TIMED_FUSED, LS_TIMED_STACK = 0, 1, 2, 3, 4
 LS_TIMED_ATTEND, LS_TIMED_APPEND, LS_TIMED_NORM = 5, 6, 7
+LS_TIMED_ATTEND4, LS_TIMED_APPEND4, LS_TIMED_READ4 = 8, 9, 10
 
 
 def ls_timing_enable(on: bool) -> None:
@@ -578,6 +596,96 @@ def ls_paged_kv_attend(kv: PagedKV, q: torch.Tensor, out: torch.Tensor, seq_len:
     """q, out: [sequences, q_len, heads, head_dim], or [sequences, heads, head_dim] for one token each; seq_len: int32
     [sequences]; table: int32 [sequences, pages]; lse: float, one per row of q.  ``scale`` defaults to head_dim ** -0.5."""
     rc = _fast.attend(kv.plan, q, out, seq_len, table, prefix_pages, prefix_len, window, kv.head_dim ** -0.5 if scale is None else scale, lse, _raw(stream))
+    if rc:
+        _check(rc)
+
+
+class PagedKV4:
+    """Owner of one ``ls_paged_kv4*`` handle (keeps the borrowed pages and rotation table alive)."""
+
+    def __init__(self, handle: int, pages: torch.Tensor, n_q_heads: int, head_dim: int, page_size: int, dtype: torch.dtype, group: int, max_seqs: int,
+                 max_q_len: int, rope: Optional[torch.Tensor]):
+        self.handle, self.plan = handle, None
+        self.pages, self.rope = pages, rope
+        self.n_pages, self.n_kv_heads = pages.shape[:2]
+        self.n_q_heads, self.head_dim, self.page_size, self.group = n_q_heads, head_dim, page_size, group
+        self.max_seqs, self.max_q_len = max_seqs, max_q_len
+        self.dtype, self.device = dtype, pages.device.index
+        self.plan = _marshal().plan4(handle, pages, torch.empty(0, dtype=dtype), n_q_heads, head_dim, page_size)
+
+    def close(self) -> None:
+        if self.handle:
+            lib().ls_paged_kv4_destroy(self.handle)
+            self.handle = self.plan = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def ls_paged_kv4_block_bytes(page_size: int, head_dim: int, group: int = 64) -> int:
+    """Bytes of one page of one key head (keys, values, their scales and zeros)."""
+    n = lib().ls_paged_kv4_block_bytes(page_size, head_dim, group)
+    if n < 0:
+        _check(int(n))
+    return int(n)
+
+
+def ls_paged_kv4_create(pages: torch.Tensor, n_q_heads: int, head_dim: int, page_size: int, dtype: torch.dtype = torch.bfloat16, group: int = 64,
+                        max_seqs: int = 0, max_q_len: int = 0, rope: Optional[torch.Tensor] = None, rope_interleaved: bool = False) -> PagedKV4:
+    """One layer's cache in 4 bits over the caller's pages: uint8 [n_pages, n_kv_heads, ls_paged_kv4_block_bytes(...)], any strides of a
+    multiple of 16 that keep a block contiguous.  ``dtype``: of queries, keys, values, outputs, scales and zeros; ``group``: components
+    that share a scale; ``rope``, ``max_seqs``, ``max_q_len`` as for ``ls_paged_kv_create``."""
+    block = ls_paged_kv4_block_bytes(page_size, head_dim, group)
+    assert pages.dtype == torch.uint8 and pages.is_cuda and pages.dim() == 3 and pages.shape[2] == block and pages.stride(2) == 1
+    assert dtype in (torch.bfloat16, torch.float16)
+    d = ls_paged_kv4_desc()
+    d.struct_size = C.sizeof(ls_paged_kv4_desc)
+    d.device, d.dtype = pages.device.index, _DTYPE[dtype]
+    d.n_q_heads, d.n_kv_heads, d.head_dim, d.group, d.page_size, d.n_pages = n_q_heads, pages.shape[1], head_dim, group, page_size, pages.shape[0]
+    d.d_pages, d.page_stride, d.head_stride = pages.data_ptr(), pages.stride(0), pages.stride(1)
+    d.max_seqs, d.max_q_len = max_seqs, max_q_len if max_seqs else 0
+    if rope is not None:
+        assert rope.dtype == torch.float32 and rope.dim() == 2 and rope.is_contiguous() and rope.device == pages.device
+        d.d_rope, d.rope_positions, d.rope_dim, d.rope_interleaved = rope.data_ptr(), rope.shape[0], rope.shape[1], int(rope_interleaved)
+    out = C.c_void_p()
+    _check(lib().ls_paged_kv4_create(C.byref(d), C.byref(out)))
+    return PagedKV4(out.value, pages, n_q_heads, head_dim, page_size, dtype, group, max_seqs, max_q_len, rope)
+
+
+def ls_paged_kv4_destroy(kv: PagedKV4) -> None:
+    kv.close()
+
+
+def ls_paged_kv4_status(kv: PagedKV4) -> int:
+    v = C.c_int32(0)
+    _check(lib().ls_paged_kv4_status(kv.handle, C.byref(v)))
+    return v.value
+
+
+def ls_paged_kv4_append(kv: PagedKV4, q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, q_out: Optional[torch.Tensor], seq: torch.Tensor,
+                        pos: torch.Tensor, table: torch.Tensor, stream=None) -> None:
+    """Operands as of ``ls_paged_kv_append``; keys and values are stored in 4 bits."""
+    rc = _fast.append4(kv.plan, q, k, v, q_out, seq, pos, table, _raw(stream))
+    if rc:
+        _check(rc)
+
+
+def ls_paged_kv4_attend(kv: PagedKV4, q: torch.Tensor, out: torch.Tensor, seq_len: torch.Tensor, table: torch.Tensor, window: int = 0,
+                        scale: Optional[float] = None, lse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Operands as of ``ls_paged_kv_attend``, without a prefix (sequences may list the same pages)."""
+    rc = _fast.attend4(kv.plan, q, out, seq_len, table, window, kv.head_dim ** -0.5 if scale is None else scale, lse, _raw(stream))
+    if rc:
+        _check(rc)
+
+
+def ls_paged_kv4_read(kv: PagedKV4, k_out: Optional[torch.Tensor], v_out: Optional[torch.Tensor], seq: torch.Tensor, pos: torch.Tensor,
+                      table: torch.Tensor, stream=None) -> None:
+    """What the cache holds of tokens (position pos[t] of sequence seq[t], int32) in 16 bits: k_out, v_out [tokens, kv_heads, head_dim] (any
+    token stride; either may be None).  Rows of negative sequences or positions are left as they were."""
+    rc = _fast.read4(kv.plan, k_out, v_out, seq, pos, table, _raw(stream))
     if rc:
         _check(rc)
 

@@ -3,7 +3,6 @@
 
 #include <algorithm>
 #include <new>
-#include <utility>
 
 #include "ls_append.cuh"
 #include "ls_attend.cuh"
@@ -40,14 +39,6 @@ constexpr int kRowsMaxGroup = 8;
 constexpr int kNormManyRows = 148 * 4;
 // Up to this many output rows the pieces of each are joined by eight warps (all blocks are resident at once), else by one.
 constexpr long long kJoinFewRows = 148 * 8;
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-
-// Each pointer (NULL among them) lies at a multiple of its element's `size` bytes: the kernels' accesses would fault otherwise.
-template <class... P>
-bool elements_aligned(size_t size, P... p) {
-  return ((reinterpret_cast<uintptr_t>(p) | ...) & (size - 1)) == 0;
-}
 
 void free_kv(ls_paged_kv* kv) {
   cudaFree(kv->part_o); cudaFree(kv->part_lse); cudaFree(kv->status); cudaFree(kv->tile_ws); cudaFree(kv->tile_ids);
@@ -145,24 +136,6 @@ int32_t create_tiles(ls_paged_kv* kv) {
   LS_TRY(dalloc(&kv->tile_ids, ids));
   LS_CUDA(cudaMemset(kv->tile_ids, 0, ids * sizeof(int32_t)));
   kv->tiles = true;
-  return LS_OK;
-}
-
-// Launches that may start while the kernel in front of them ends; the kernels wait for it before they touch memory.
-template <class... P, class... Q>
-int32_t launch_early(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, Q&&... args) {
-  cudaLaunchAttribute at{};
-  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at.val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3((unsigned)threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cfg.attrs = &at;
-  cfg.numAttrs = 1;
-  LS_CUDA(cudaLaunchKernelEx(&cfg, kernel, std::forward<Q>(args)...));
-  LS_LAUNCHED();
   return LS_OK;
 }
 

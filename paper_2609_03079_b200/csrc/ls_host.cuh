@@ -10,6 +10,7 @@
 #include <cstdio>
 #include <mutex>
 #include <string>
+#include <utility>
 #include <vector>
 
 namespace ls_host {
@@ -91,6 +92,32 @@ int32_t dalloc(T** p, size_t n) {
   cudaError_t e = cudaMalloc(reinterpret_cast<void**>(p), n * sizeof(T));
   if (e != cudaSuccess) return fail(e == cudaErrorMemoryAllocation ? LS_ERR_NOMEM : LS_ERR_CUDA, "cudaMalloc(%zu bytes): %s",
                                     n * sizeof(T), cudaGetErrorString(e));
+  return LS_OK;
+}
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// Each pointer (NULL among them) lies at a multiple of its element's `size` bytes: the kernels' accesses would fault otherwise.
+template <class... P>
+bool elements_aligned(size_t size, P... p) {
+  return ((reinterpret_cast<uintptr_t>(p) | ...) & (size - 1)) == 0;
+}
+
+// Launches that may start while the kernel in front of them ends; the kernels wait for it before they touch memory.
+template <class... P, class... Q>
+int32_t launch_early(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, Q&&... args) {
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  LS_CUDA(cudaLaunchKernelEx(&cfg, kernel, std::forward<Q>(args)...));
+  LS_LAUNCHED();
   return LS_OK;
 }
 

@@ -13,9 +13,12 @@ namespace {
 decltype(&ls_paged_kv_append) f_append = nullptr;
 decltype(&ls_paged_kv_attend) f_attend = nullptr;
 decltype(&ls_block_norm) f_norm = nullptr;
+decltype(&ls_paged_kv4_append) f_append4 = nullptr;
+decltype(&ls_paged_kv4_attend) f_attend4 = nullptr;
+decltype(&ls_paged_kv4_read) f_read4 = nullptr;
 
 struct Plan {  // what the checks need to know of a paged cache
-  ls_paged_kv* handle;
+  void* handle;  // ls_paged_kv or ls_paged_kv4, by the capsule's name
   int device;
   at::ScalarType dtype;
   int64_t heads, kv_heads, dim, page;
@@ -105,8 +108,9 @@ PyObject* guarded(F f) {
   }
   return nullptr;
 }
-Plan* plan_of(PyObject* o) {
-  Plan* p = static_cast<Plan*>(PyCapsule_GetPointer(o, "ls_paged_kv"));
+constexpr const char *kPlan = "ls_paged_kv", *kPlan4 = "ls_paged_kv4";
+Plan* plan_of(PyObject* o, const char* name) {
+  Plan* p = static_cast<Plan*>(PyCapsule_GetPointer(o, name));
   if (!p) throw Refusal{nullptr};
   return p;
 }
@@ -116,10 +120,13 @@ bool count(Py_ssize_t n, Py_ssize_t want) {
   return false;
 }
 
-// bind(append, attend, norm): addresses of the C functions
+// bind(append, attend, norm, append4, attend4, read4): addresses of the C functions
 PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!count(n, 3)) return nullptr;
+  if (!count(n, 6)) return nullptr;
   return guarded([&] {
+    f_append4 = reinterpret_cast<decltype(f_append4)>((uintptr_t)integer(a[3]));
+    f_attend4 = reinterpret_cast<decltype(f_attend4)>((uintptr_t)integer(a[4]));
+    f_read4 = reinterpret_cast<decltype(f_read4)>((uintptr_t)integer(a[5]));
     f_append = reinterpret_cast<decltype(f_append)>((uintptr_t)integer(a[0]));
     f_attend = reinterpret_cast<decltype(f_attend)>((uintptr_t)integer(a[1]));
     f_norm = reinterpret_cast<decltype(f_norm)>((uintptr_t)integer(a[2]));
@@ -127,13 +134,13 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// plan(handle, k_pages, n_q_heads) -> capsule
-PyObject* py_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!count(n, 3)) return nullptr;
+template <class F>
+PyObject* new_plan(const char* name, F make) {
   try {
-    const at::Tensor& k = tensor(a[1], "k_pages: a tensor");
-    Plan* p = new Plan{reinterpret_cast<ls_paged_kv*>((uintptr_t)integer(a[0])), (int)k.get_device(), k.scalar_type(), integer(a[2]), k.size(2), k.size(3), k.size(1)};
-    return PyCapsule_New(p, "ls_paged_kv", [](PyObject* c) { delete static_cast<Plan*>(PyCapsule_GetPointer(c, "ls_paged_kv")); });
+    Plan* p = new Plan(make());
+    PyObject* c = PyCapsule_New(p, name, [](PyObject* c) { delete static_cast<Plan*>(PyCapsule_GetPointer(c, PyCapsule_GetName(c))); });
+    if (!c) delete p;
+    return c;
   } catch (const Refusal& r) {
     if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, r.what);
   } catch (const std::exception& e) {
@@ -142,11 +149,30 @@ PyObject* py_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return nullptr;
 }
 
-// append(plan, q, k, v, q_out, seq, pos, table, stream)
-PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+// plan(handle, k_pages, n_q_heads) -> capsule
+PyObject* py_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!count(n, 3)) return nullptr;
+  return new_plan(kPlan, [&] {
+    const at::Tensor& k = tensor(a[1], "k_pages: a tensor");
+    return Plan{reinterpret_cast<void*>((uintptr_t)integer(a[0])), (int)k.get_device(), k.scalar_type(), integer(a[2]), k.size(2), k.size(3), k.size(1)};
+  });
+}
+
+// plan4(handle, pages, like, n_q_heads, head_dim, page_size) -> capsule; `like`: a tensor of the cache's 16-bit type
+PyObject* py_plan4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!count(n, 6)) return nullptr;
+  return new_plan(kPlan4, [&] {
+    const at::Tensor &k = tensor(a[1], "pages: a tensor"), &like = tensor(a[2], "like: a tensor");
+    return Plan{reinterpret_cast<void*>((uintptr_t)integer(a[0])), (int)k.get_device(), like.scalar_type(), integer(a[3]), k.size(1), integer(a[4]), integer(a[5])};
+  });
+}
+
+// append(plan, q, k, v, q_out, seq, pos, table, stream), for either cache
+template <class H, class F>
+PyObject* append_to(const char* name, F call, PyObject* const* a, Py_ssize_t n) {
   if (!count(n, 9)) return nullptr;
   return guarded([&] {
-    const Plan& p = *plan_of(a[0]);
+    const Plan& p = *plan_of(a[0], name);
     const at::Tensor &k = tensor(a[2], "k: a tensor"), &v = tensor(a[3], "v: a tensor"), &seq = tensor(a[5], "seq: a tensor"), &pos = tensor(a[6], "pos: a tensor");
     const int64_t T = k.dim() == 3 ? k.size(0) : -1;
     need(T >= 0, "k: [tokens, kv_heads, head_dim]");
@@ -166,24 +192,51 @@ PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
       qo = to.data_ptr();
     }
     const Table t = table_of(p, tensor(a[7], "table: a tensor"));
-    return f_append(p.handle, q, sq, qo, so, k.data_ptr(), sk, v.data_ptr(), sv, as32(T), ids(seq, p.device, "seq: int32 [tokens] on the cache's device"),
+    return call(static_cast<H*>(p.handle), q, sq, qo, so, k.data_ptr(), sk, v.data_ptr(), sv, as32(T), ids(seq, p.device, "seq: int32 [tokens] on the cache's device"),
                     ids(pos, p.device, "pos: int32 [tokens] on the cache's device"), t.at, t.rows, t.width, t.stride, stream_of(a[8], p.device));
   });
 }
+
+PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) { return append_to<ls_paged_kv>(kPlan, f_append, a, n); }
+PyObject* py_append4(PyObject*, PyObject* const* a, Py_ssize_t n) { return append_to<ls_paged_kv4>(kPlan4, f_append4, a, n); }
+
+// The operands that both attentions have.
+struct Rows {
+  const void* q;
+  void* out;
+  int64_t sq, so, B, m;
+  const int32_t* len;
+  Table t;
+  float* lse;
+  Rows(const Plan& p, PyObject* oq, PyObject* oo, PyObject* ol, PyObject* ot, PyObject* olse) {
+    const at::Tensor &q = tensor(oq, "q: a tensor"), &out = tensor(oo, "out: a tensor"), &len = tensor(ol, "seq_len: a tensor");
+    need(q.dim() == 3 || q.dim() == 4, "q: [sequences, heads, head_dim] or [sequences, q_len, heads, head_dim]");
+    need(out.sizes() == q.sizes(), "out: of q's shape");
+    B = q.size(0);
+    m = q.dim() == 4 ? q.size(1) : 1;
+    sq = token_stride(p, q, p.heads, "q: heads and components side by side, evenly spaced tokens, of the cache's type and device");
+    so = token_stride(p, out, p.heads, "out: heads and components side by side, evenly spaced tokens, of the cache's type and device");
+    t = table_of(p, tensor(ot, "table: a tensor"));
+    need(len.numel() == B && t.rows == B, "seq_len and table: one row per sequence");
+    this->len = ids(len, p.device, "seq_len: int32 on the cache's device");
+    lse = nullptr;
+    if (olse != Py_None) {
+      const at::Tensor& tl = tensor(olse, "lse: a tensor");
+      need(tl.scalar_type() == at::kFloat && tl.is_cuda() && tl.get_device() == p.device && tl.is_contiguous() && tl.numel() == B * m * p.heads,
+           "lse: dense float32, one value per row of q");
+      lse = static_cast<float*>(tl.data_ptr());
+    }
+    this->q = q.data_ptr();
+    this->out = out.data_ptr();
+  }
+};
 
 // attend(plan, q, out, seq_len, table, prefix_pages, prefix_len, window, scale, lse, stream)
 PyObject* py_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!count(n, 11)) return nullptr;
   return guarded([&] {
-    const Plan& p = *plan_of(a[0]);
-    const at::Tensor &q = tensor(a[1], "q: a tensor"), &out = tensor(a[2], "out: a tensor"), &len = tensor(a[3], "seq_len: a tensor");
-    need(q.dim() == 3 || q.dim() == 4, "q: [sequences, heads, head_dim] or [sequences, q_len, heads, head_dim]");
-    need(out.sizes() == q.sizes(), "out: of q's shape");
-    const int64_t B = q.size(0), m = q.dim() == 4 ? q.size(1) : 1;
-    const int64_t sq = token_stride(p, q, p.heads, "q: heads and components side by side, evenly spaced tokens, of the cache's type and device"),
-                  so = token_stride(p, out, p.heads, "out: heads and components side by side, evenly spaced tokens, of the cache's type and device");
-    const Table t = table_of(p, tensor(a[4], "table: a tensor"));
-    need(len.numel() == B && t.rows == B, "seq_len and table: one row per sequence");
+    const Plan& p = *plan_of(a[0], kPlan);
+    const Rows r(p, a[1], a[2], a[3], a[4], a[9]);
     const long long prefix = integer(a[6]);
     const int32_t* pages = nullptr;
     if (prefix > 0) {
@@ -191,15 +244,44 @@ PyObject* py_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
       pages = ids(tp, p.device, "prefix_pages: int32 on the cache's device");
       need(tp.numel() * p.page >= prefix, "prefix_pages: too few for prefix_len");
     }
-    float* lse = nullptr;
-    if (a[9] != Py_None) {
-      const at::Tensor& tl = tensor(a[9], "lse: a tensor");
-      need(tl.scalar_type() == at::kFloat && tl.is_cuda() && tl.get_device() == p.device && tl.is_contiguous() && tl.numel() == B * m * p.heads,
-           "lse: dense float32, one value per row of q");
-      lse = static_cast<float*>(tl.data_ptr());
-    }
-    return f_attend(p.handle, q.data_ptr(), sq, out.data_ptr(), so, lse, as32(B), as32(m), ids(len, p.device, "seq_len: int32 on the cache's device"), t.at,
-                    t.width, t.stride, pages, as32(prefix), as32(integer(a[7])), (float)real(a[8]), stream_of(a[10], p.device));
+    return f_attend(static_cast<ls_paged_kv*>(p.handle), r.q, r.sq, r.out, r.so, r.lse, as32(r.B), as32(r.m), r.len, r.t.at, r.t.width, r.t.stride, pages,
+                    as32(prefix), as32(integer(a[7])), (float)real(a[8]), stream_of(a[10], p.device));
+  });
+}
+
+// attend4(plan, q, out, seq_len, table, window, scale, lse, stream)
+PyObject* py_attend4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!count(n, 9)) return nullptr;
+  return guarded([&] {
+    const Plan& p = *plan_of(a[0], kPlan4);
+    const Rows r(p, a[1], a[2], a[3], a[4], a[7]);
+    return f_attend4(static_cast<ls_paged_kv4*>(p.handle), r.q, r.sq, r.out, r.so, r.lse, as32(r.B), as32(r.m), r.len, r.t.at, r.t.width, r.t.stride,
+                     as32(integer(a[5])), (float)real(a[6]), stream_of(a[8], p.device));
+  });
+}
+
+// read4(plan, k_out, v_out, seq, pos, table, stream)
+PyObject* py_read4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (!count(n, 7)) return nullptr;
+  return guarded([&] {
+    const Plan& p = *plan_of(a[0], kPlan4);
+    const at::Tensor &seq = tensor(a[3], "seq: a tensor"), &pos = tensor(a[4], "pos: a tensor");
+    const int64_t T = seq.numel();
+    need(pos.numel() == T, "seq and pos disagree about the number of tokens");
+    auto rows = [&](PyObject* o, const char* what, int64_t& stride) -> void* {
+      stride = 0;
+      if (o == Py_None) return nullptr;
+      const at::Tensor& x = tensor(o, what);
+      need(x.dim() == 3 && x.size(0) == T, what);
+      stride = token_stride(p, x, p.kv_heads, what);
+      return x.data_ptr();
+    };
+    int64_t sk, sv;
+    void *k = rows(a[1], "k_out: [tokens, kv_heads, head_dim] of the cache's type and device", sk),
+         *v = rows(a[2], "v_out: [tokens, kv_heads, head_dim] of the cache's type and device", sv);
+    const Table t = table_of(p, tensor(a[5], "table: a tensor"));
+    return f_read4(static_cast<ls_paged_kv4*>(p.handle), k, sk, v, sv, as32(T), ids(seq, p.device, "seq: int32 [tokens] on the cache's device"),
+                   ids(pos, p.device, "pos: int32 [tokens] on the cache's device"), t.at, t.rows, t.width, t.stride, stream_of(a[6], p.device));
   });
 }
 
@@ -252,7 +334,9 @@ PyObject* py_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define LS_FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL
 PyMethodDef methods[] = {{"bind", LS_FAST(py_bind), nullptr},     {"plan", LS_FAST(py_plan), nullptr}, {"append", LS_FAST(py_append), nullptr},
-                         {"attend", LS_FAST(py_attend), nullptr}, {"norm", LS_FAST(py_norm), nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         {"attend", LS_FAST(py_attend), nullptr}, {"norm", LS_FAST(py_norm), nullptr},
+                         {"plan4", LS_FAST(py_plan4), nullptr},   {"append4", LS_FAST(py_append4), nullptr},
+                         {"attend4", LS_FAST(py_attend4), nullptr}, {"read4", LS_FAST(py_read4), nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "ls_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
