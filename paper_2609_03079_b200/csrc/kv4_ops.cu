@@ -6,7 +6,7 @@
 
 #include "ls_host.cuh"
 #include "ls_kv4.cuh"
-#include "ls_kv4_attend.cuh"
+#include "ls_kv4_shapes.cuh"
 
 using namespace ls_host;
 
@@ -17,41 +17,27 @@ struct ls_paged_kv4 {
   float* part = nullptr;       // workspace of the attention
   int32_t* arrived = nullptr;
   size_t part_floats = 0, units = 0;
+  uint16_t* q = nullptr;       // queries that do not lie at a multiple of 16 bytes are copied here
 };
 
 namespace {
 
-// One shape of the attention kernel.
-struct Shape {
-  void (*kernel)(ls::Attend4Args);
-  int rows, threads, smem;
-  size_t piece;  // floats
-};
-template <int D, int G, int NT>
-Shape shape() {
-  using S = ls::K4Shape<D, G, NT>;
-  return {ls::ls_kv4_attend_kernel<D, G, NT>, S::ROWS, S::THREADS, S::SMEM, S::PIECE / sizeof(float)};
-}
-template <int D, int NT>
-Shape shape_of_group(int group) {
-  if (group == 32) return shape<D, 32, NT>();
-  if constexpr (D >= 128) {
-    if (group == 128) return shape<D, 128, NT>();
-  }
-  return shape<D, 64, NT>();
-}
-// Rows of queries of one key head: 8, 16 or 32 at a time (16 with heads of 256, whose sums fill the registers then).
+using ls_kv4::Shape;
+
+// Rows of queries of one key head: 8 or 16 at a time (8 with heads of 256, whose sums fill the registers).
 Shape shape_for(const ls_paged_kv4_desc& d, long long rows) {
-  const int nt = rows <= 8 ? 1 : rows <= 16 || d.head_dim == 256 ? 2 : 4;
-  switch (d.head_dim) {
-    case 64: return nt == 1 ? shape_of_group<64, 1>(d.group) : nt == 2 ? shape_of_group<64, 2>(d.group) : shape_of_group<64, 4>(d.group);
-    case 128: return nt == 1 ? shape_of_group<128, 1>(d.group) : nt == 2 ? shape_of_group<128, 2>(d.group) : shape_of_group<128, 4>(d.group);
-    default: return nt == 1 ? shape_of_group<256, 1>(d.group) : shape_of_group<256, 2>(d.group);
-  }
+  const int nt = rows <= 8 || d.head_dim == 256 ? 1 : 2;
+  return d.dtype == LS_WDTYPE_BF16 ? ls_kv4::shape_bf16(d.head_dim, d.group, nt) : ls_kv4::shape_fp16(d.head_dim, d.group, nt);
+}
+
+ls::FastDiv fast_div(int d) {
+  uint32_t up = 0;
+  while ((1u << up) < (uint32_t)d) ++up;
+  return {(uint32_t)(((1ULL << (31 + up)) + d - 1) / d), 31 + up};
 }
 
 void free_kv(ls_paged_kv4* kv) {
-  cudaFree(kv->part); cudaFree(kv->arrived); cudaFree(kv->status);
+  cudaFree(kv->part); cudaFree(kv->q); cudaFree(kv->arrived); cudaFree(kv->status);
   delete kv;
 }
 
@@ -62,14 +48,14 @@ int32_t create_kv(ls_paged_kv4* kv) {
   LS_CUDA(cudaMemset(kv->status, 0, sizeof(int)));
   if (d.max_seqs > 0) {
     const long long rows = (long long)d.max_q_len * (d.n_q_heads / d.n_kv_heads);
-    for (long long r : {8LL, 16LL, 32LL}) {
+    for (long long r : {8LL, 16LL}) {
       const Shape s = shape_for(d, r);
-      if (r > 8 && rows <= r / 2) break;  // (no call needs this shape)
       LS_CUDA(cudaFuncSetAttribute(s.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, s.smem));
       kv->part_floats = std::max(kv->part_floats, (size_t)kv->sm_count * (s.threads / 32) * 2 * s.piece);
       kv->units = std::max(kv->units, (size_t)d.max_seqs * d.n_kv_heads * ((size_t)(rows + s.rows - 1) / s.rows));
     }
     LS_TRY(dalloc(&kv->part, kv->part_floats));
+    LS_TRY(dalloc(&kv->q, (size_t)d.max_seqs * d.max_q_len * d.n_q_heads * d.head_dim));
     LS_TRY(dalloc(&kv->arrived, kv->units));
     LS_CUDA(cudaMemset(kv->arrived, 0, kv->units * sizeof(int32_t)));
   }
@@ -228,24 +214,40 @@ int32_t ls_paged_kv4_attend(ls_paged_kv4* kv, const void* d_q, int64_t q_stride,
   if (!(scale > 0.f) || scale > 1e30f) return fail(LS_ERR_INVALID, "ls_paged_kv4_attend: scale must be positive and finite");
   if (!elements_aligned(2, d_q, d_out) || !elements_aligned(4, d_lse, d_seq_len)) return fail(LS_ERR_INVALID, "ls_paged_kv4_attend: a misaligned pointer");
   DeviceGuard guard(D.device);
-  ls::Attend4Args a{};
-  a.p = pages_of(kv, d_table, n_seqs, table_width, table_stride);
-  a.q = static_cast<const uint16_t*>(d_q); a.out = static_cast<uint16_t*>(d_out); a.lse = d_lse; a.seq_len = d_seq_len;
-  a.part = kv->part; a.arrived = kv->arrived;
-  a.q_stride = q_stride; a.out_stride = out_stride;
-  a.q_len = q_len; a.heads = D.n_q_heads; a.group = D.n_q_heads / D.n_kv_heads; a.window = window ? window : 0x7fffffff;
-  const bool one = n_seqs * (long long)q_len == 1;
-  a.q_vec = aligned16(d_q) && (one || q_stride % 8 == 0);
-  a.out_vec = (reinterpret_cast<uintptr_t>(d_out) & 7) == 0 && (one || out_stride % 4 == 0);
-  a.bf16 = D.dtype == LS_WDTYPE_BF16; a.scale_log2 = scale * ls::LOG2E;
-  const long long rows = (long long)q_len * a.group;
+  const long long rows = (long long)q_len * (D.n_q_heads / D.n_kv_heads);
   const Shape s = shape_for(D, rows);
-  a.row_tiles = (int)((rows + s.rows - 1) / s.rows);
-  if ((size_t)n_seqs * D.n_kv_heads * a.row_tiles > kv->units || (size_t)kv->sm_count * (s.threads / 32) * 2 * s.piece > kv->part_floats)
+  const long long row_tiles = (rows + s.rows - 1) / s.rows, per_seq = row_tiles * D.n_kv_heads;
+  if ((size_t)n_seqs * per_seq > kv->units || (size_t)kv->sm_count * (s.threads / 32) * 2 * s.piece > kv->part_floats)
     return fail(LS_ERR_INTERNAL, "ls_paged_kv4_attend: workspace");
+  // A launch counts its tiles in 32 bits: of as many sequences as cannot have too many (all of them but for huge tables).
+  const long long most = per_seq * std::max(1LL, std::min((long long)table_width * D.page_size, (long long)ls::MAX_POSITIONS) / 16);
+  if (most > ls::K4_MAX_BLOCKS) return fail(LS_ERR_INVALID, "ls_paged_kv4_attend: q_len * table_width is too large");
+  const int32_t step = (int32_t)std::min<long long>(n_seqs, ls::K4_MAX_BLOCKS / most);
   const cudaStream_t st = (cudaStream_t)stream;
   KernelTimer timer(LS_TIMED_ATTEND4, st);
-  return launch_early(s.kernel, dim3((unsigned)kv->sm_count), s.threads, s.smem, st, a);
+  if (!aligned16(d_q) || (n_seqs * (long long)q_len > 1 && q_stride % 8)) {
+    LS_TRY(launch_early(ls::ls_kv4_align_kernel<256>, dim3((unsigned)(n_seqs * q_len)), 256, 0, st, static_cast<const uint16_t*>(d_q), q_stride, kv->q, (int)qw));
+    d_q = kv->q;
+    q_stride = qw;
+  }
+  for (int32_t b = 0; b < n_seqs; b += step) {
+    ls::Attend4Args a{};
+    const long long tokens = (long long)b * q_len;
+    a.p = pages_of(kv, d_table ? d_table + b * table_stride : nullptr, std::min(step, n_seqs - b), table_width, table_stride);
+    a.q = static_cast<const uint16_t*>(d_q) + tokens * q_stride; a.out = static_cast<uint16_t*>(d_out) + tokens * out_stride;
+    a.lse = d_lse ? d_lse + tokens * D.n_q_heads : nullptr; a.seq_len = d_seq_len + b;
+    a.part = kv->part; a.arrived = kv->arrived;
+    a.q_stride = q_stride; a.out_stride = out_stride;
+    a.q_len = q_len; a.heads = D.n_q_heads; a.group = D.n_q_heads / D.n_kv_heads; a.window = window ? window : 0x7fffffff;
+    a.row_tiles = (int)row_tiles;
+    a.most = (int)std::min((long long)table_width * D.page_size, (long long)ls::MAX_POSITIONS);
+    a.behind = (int)std::min<long long>(0x7fffffff, (long long)a.window + q_len - 1);
+    a.by_group = fast_div(a.group); a.by_row_tiles = fast_div(a.row_tiles); a.by_page = fast_div(D.page_size / 16);
+    a.out_vec = (reinterpret_cast<uintptr_t>(d_out) & 7) == 0 && (n_seqs * (long long)q_len == 1 || out_stride % 4 == 0);
+    a.scale_log2 = scale * ls::LOG2E; a.four = 4;
+    LS_TRY(launch_early(s.kernel, dim3((unsigned)kv->sm_count), s.threads, s.smem, st, a));
+  }
+  return LS_OK;
 }
 
 int32_t ls_paged_kv4_read(ls_paged_kv4* kv, void* d_k_out, int64_t k_stride, void* d_v_out, int64_t v_stride, int32_t n_tokens,

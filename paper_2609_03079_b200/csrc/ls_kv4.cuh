@@ -249,6 +249,16 @@ __global__ void __launch_bounds__(256) ls_kv4_append_kernel(const Kv4AppendArgs 
   }
 }
 
+// Rows of `n` elements (a multiple of 64) to where they lie side by side, at a multiple of 16 bytes.
+template <int N = 256>
+__global__ void __launch_bounds__(N) ls_kv4_align_kernel(const uint16_t* from, int64_t stride, uint16_t* to, int n) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  from += blockIdx.x * stride;
+  to += (int64_t)blockIdx.x * n;
+  for (int i = threadIdx.x; i < n; i += N) to[i] = from[i];
+}
+
 struct Kv4ReadArgs {
   Kv4Pages p;
   uint16_t* k;  // [n_tokens][kv_heads][dim], either may be NULL
