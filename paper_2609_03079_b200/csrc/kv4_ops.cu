@@ -81,9 +81,18 @@ ls::Kv4Pages pages_of(const ls_paged_kv4* kv, const int32_t* d_table, int32_t n_
   return p;
 }
 
+using AppendKernel = void (*)(ls::Kv4AppendArgs);
+template <int WD, int D>
+AppendKernel append_of_group(int group) {
+  if (group == 32) return ls::ls_kv4_append_kernel<WD, D, 32>;
+  if constexpr (D >= 128) {
+    if (group == 128) return ls::ls_kv4_append_kernel<WD, D, 128>;
+  }
+  return ls::ls_kv4_append_kernel<WD, D, 64>;
+}
 template <int WD>
-auto append_kernel(int dim) {
-  return dim == 64 ? ls::ls_kv4_append_kernel<WD, 64> : dim == 128 ? ls::ls_kv4_append_kernel<WD, 128> : ls::ls_kv4_append_kernel<WD, 256>;
+AppendKernel append_kernel(int dim, int group) {
+  return dim == 64 ? append_of_group<WD, 64>(group) : dim == 128 ? append_of_group<WD, 128>(group) : append_of_group<WD, 256>(group);
 }
 template <int WD>
 auto read_kernel(int dim) {
@@ -188,13 +197,14 @@ int32_t ls_paged_kv4_append(ls_paged_kv4* kv, const void* d_q, int64_t q_stride,
   a.kv_vec = aligned16(d_k) && aligned16(d_v) && (one || (k_stride | v_stride) % 8 == 0);
   a.q_vec = D.rope_dim % 16 == 0 && aligned16(d_q) && aligned16(d_q_out) && aligned16(D.d_rope) && (one || !d_q || (q_stride | q_out_stride) % 8 == 0);
   a.rope_vec = D.rope_dim % 8 == 0 && aligned16(D.d_rope);
-  a.kv_jobs = (int)((kw + 255) / 256);
-  a.jobs = 2 * a.kv_jobs + (d_q ? (int)((qw + 1023) / 1024) : 0);
+  const int64_t kv_job = 128 * ls::K4_SLABS, q_job = 512 * ls::K4_Q_HEADS;
+  a.kv_jobs = (int)((kw + kv_job - 1) / kv_job);
+  a.jobs = 2 * a.kv_jobs + (d_q ? (int)((qw + q_job - 1) / q_job) : 0);
   const unsigned long long blocks = ((unsigned long long)n_tokens * a.jobs + 7) / 8;
   if (blocks > 0x7fffffffULL) return fail(LS_ERR_INVALID, "ls_paged_kv4_append: too many tokens");
   const cudaStream_t st = (cudaStream_t)stream;
   KernelTimer timer(LS_TIMED_APPEND4, st);
-  return launch_early(D.dtype == LS_WDTYPE_BF16 ? append_kernel<ls::WD_BF16>(D.head_dim) : append_kernel<ls::WD_FP16>(D.head_dim), dim3((unsigned)blocks), 256, 0, st, a);
+  return launch_early(D.dtype == LS_WDTYPE_BF16 ? append_kernel<ls::WD_BF16>(D.head_dim, D.group) : append_kernel<ls::WD_FP16>(D.head_dim, D.group), dim3((unsigned)blocks), 256, 0, st, a);
 }
 
 int32_t ls_paged_kv4_attend(ls_paged_kv4* kv, const void* d_q, int64_t q_stride, void* d_out, int64_t out_stride, float* d_lse,
@@ -268,12 +278,17 @@ int32_t ls_paged_kv4_read(ls_paged_kv4* kv, void* d_k_out, int64_t k_stride, voi
   a.k = static_cast<uint16_t*>(d_k_out); a.v = static_cast<uint16_t*>(d_v_out); a.seq = d_seq; a.pos = d_pos;
   a.k_stride = k_stride; a.v_stride = v_stride; a.n_tokens = n_tokens;
   a.vec = aligned16(d_k_out) && aligned16(d_v_out) && (n_tokens == 1 || ((d_k_out ? k_stride : 0) | (d_v_out ? v_stride : 0)) % 8 == 0);
-  const int items = D.n_kv_heads * 2 * (D.head_dim / 16);
-  a.per_block = std::max(1, 512 / items);
+  // Threads of a token: half of its pieces each, or a fraction that leaves fewer of a block's threads idle.
+  const int items = D.n_kv_heads * (D.head_dim / 16);
+  auto busy = [](int width) { return 256 / width * width; };
+  a.width = std::min(256, (items + 1) / 2);
+  for (int part = 3; part <= 6; ++part)
+    if (busy((items + part - 1) / part) > busy(a.width) + 16) a.width = (items + part - 1) / part;
+  const int per_block = 256 / a.width;
   const cudaStream_t st = (cudaStream_t)stream;
   KernelTimer timer(LS_TIMED_READ4, st);
   return launch_early(D.dtype == LS_WDTYPE_BF16 ? read_kernel<ls::WD_BF16>(D.head_dim) : read_kernel<ls::WD_FP16>(D.head_dim),
-                      dim3((unsigned)((n_tokens + (long long)a.per_block - 1) / a.per_block)), 256, 0, st, a);
+                      dim3((unsigned)((n_tokens + (long long)per_block - 1) / per_block)), 256, 0, st, a);
 }
 
 }  // extern "C"

@@ -75,89 +75,157 @@ struct Kv4AppendArgs {
 struct Quad { float x[4]; };
 
 // Four consecutive components.
-template <int WD>
-__device__ __forceinline__ Quad load_quad(const uint16_t* p, bool vec) {
-  uint2 r;
-  if (vec) r = __ldg(reinterpret_cast<const uint2*>(p));
-  else { r.x = p[0] | (uint32_t)p[1] << 16; r.y = p[2] | (uint32_t)p[3] << 16; }
-  return {{widen<WD>((uint16_t)r.x), widen<WD>((uint16_t)(r.x >> 16)), widen<WD>((uint16_t)r.y), widen<WD>((uint16_t)(r.y >> 16))}};
+__device__ __forceinline__ uint2 load_quad(const uint16_t* p, bool vec) {
+  if (vec) return __ldg(reinterpret_cast<const uint2*>(p));
+  return make_uint2(p[0] | (uint32_t)p[1] << 16, p[2] | (uint32_t)p[3] << 16);
 }
-
-// Quantises the lane's quad of a head (components 4 * quad ...) with the other lanes of its group, and stores it.
-template <int WD, int D>
-__device__ __forceinline__ void store_quad(const Kv4AppendArgs& A, const Quad& y, bool value, int quad, int row, uint8_t* tile) {
-  const int lane = threadIdx.x & 31, span = A.p.group / 4;
-  float lo = fminf(fminf(y.x[0], y.x[1]), fminf(y.x[2], y.x[3])), hi = -INFINITY;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) hi = fmaxf(hi, y.x[e] != y.x[e] ? INFINITY : y.x[e]);  // (NaN must not get lost)
-  for (int o = 1; o < span; o <<= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-  }
-  const float range = hi - lo;
-  const bool fine = range < INFINITY;
-  const uint16_t scale16 = fine ? narrow<WD>(__fdiv_rn(range, 15.f)) : 0x7fff, zero16 = fine ? narrow<WD>(lo) : 0x7fff;
-  const float scale = widen<WD>(scale16);
-  uint32_t codes = 0;
-  if (scale > 0.f) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) codes |= (uint32_t)min(15, __float2int_rn(__fdiv_rn(y.x[e] - lo, scale))) << (4 * e);
-  }
-  // a word is two quads: neighbours of a key, 32 components apart of a value
-  const uint32_t other = __shfl_xor_sync(0xffffffffu, codes, value ? 8 : 1);
-  if (!tile) return;
-  const bool low = value ? !(quad & 8) : !(quad & 1);
-  const int word = value ? value_word<D>(quad & 7, quad >> 4, row) : key_word<D>(quad >> 1, row);
-  if (low) *reinterpret_cast<uint32_t*>(tile + ((value ? 16 : 0) + row) * (D / 2) + 4 * word) = codes | other << 16;
-  if (lane % span == 0) {
-    const int groups = D / A.p.group;
-    *reinterpret_cast<uint32_t*>(tile + 16 * D + (((value ? 16 : 0) + row) * groups + quad / span) * 4) = scale16 | (uint32_t)zero16 << 16;
-  }
-}
-
-// The lane's quad of a key, turned by the token's row of the table (in 64 bits: the difference of two products rounds once there, so
-// that the key and with it the codes do not depend on the order of operations), as the 16-bit type holds it.
 template <int WD>
-__device__ __forceinline__ Quad turned_quad(const Kv4AppendArgs& A, const Quad& a, const uint16_t* head, int d0, const float* tab) {
-  const int r = A.rope_dim, r2 = r / 2;
-  if (d0 >= r) return a;
-  Quad b, c, s, y;
-  if (A.rope_vec) {  // half of the turned part is a multiple of four: partners and angles are quads too
-    const int j = A.interleaved ? d0 / 2 : d0 < r2 ? d0 : d0 - r2;
-    if (A.interleaved) {
-      const float2 c2 = __ldg(reinterpret_cast<const float2*>(tab + j)), s2 = __ldg(reinterpret_cast<const float2*>(tab + r2 + j));
-      b = {{a.x[1], a.x[0], a.x[3], a.x[2]}}; c = {{c2.x, c2.x, c2.y, c2.y}}; s = {{s2.x, s2.x, s2.y, s2.y}};
-    } else {
-      const float4 c4 = __ldg(reinterpret_cast<const float4*>(tab + j)), s4 = __ldg(reinterpret_cast<const float4*>(tab + r2 + j));
-      b = load_quad<WD>(head + (d0 < r2 ? d0 + r2 : d0 - r2), A.kv_vec);
-      c = {{c4.x, c4.y, c4.z, c4.w}}; s = {{s4.x, s4.y, s4.z, s4.w}};
-    }
-  } else {
+__device__ __forceinline__ Quad widen_quad(uint2 r) {
+  Quad y;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int d = d0 + e;
-      b.x[e] = c.x[e] = s.x[e] = 0.f;
-      if (d >= r) continue;
-      const int j = A.interleaved ? d / 2 : d < r2 ? d : d - r2;
-      b.x[e] = widen<WD>(head[A.interleaved ? d ^ 1 : d < r2 ? d + r2 : d - r2]);
-      c.x[e] = tab[j]; s.x[e] = tab[r2 + j];
-    }
-  }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int d = d0 + e;
-    if (d >= r) { y.x[e] = a.x[e]; continue; }
-    const bool second = A.interleaved ? d & 1 : d >= r2;
-    const double turn = (double)b.x[e] * (double)s.x[e];
-    const double z = fma((double)a.x[e], (double)c.x[e], second ? turn : -turn);
-    y.x[e] = widen<WD>(narrow<WD>(__double2float_rn(z)));
+  for (int e = 0; e < 2; ++e) {
+    const uint32_t w = e ? r.y : r.x;
+    if (WD == WD_BF16) { y.x[2 * e] = __uint_as_float(w << 16); y.x[2 * e + 1] = __uint_as_float(w & 0xffff0000u); }
+    else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w)); y.x[2 * e] = f.x; y.x[2 * e + 1] = f.y; }
   }
   return y;
 }
+// The larger of each half; NaN if either is.
+template <int WD>
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if (WD == WD_BF16) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 
-// A warp takes 1024 components of a token's queries, or 256 of its keys or of its values (two quads a lane, so that the lanes of a
-// group sit side by side).  Queries are turned in fp32 and rounded once, as in the 16-bit append.
-template <int WD, int D>
+// Where a lane's quad (components 4 quad ...) of a row goes in a tile: the word of which it is a half, and its group's scale and zero.
+template <int D, int G>
+struct QuadPlace {
+  int word, meta;
+  bool first, leads;  // its word is this lane's to store, its group's scale is
+  __device__ __forceinline__ QuadPlace(bool value, int quad, int row) {
+    first = value ? !(quad & 8) : !(quad & 1);
+    leads = quad % (G / 4) == 0;
+    word = ((value ? 16 : 0) + row) * (D / 2) + 4 * (value ? value_word<D>(quad & 7, quad >> 4, row) : key_word<D>(quad >> 1, row));
+    meta = 16 * D + (((value ? 16 : 0) + row) * (D / G) + quad / (G / 4)) * 4;
+  }
+};
+
+// Quantises the lane's quad (as the type holds it) with the other lanes of its group, and stores it in `tile` (NULL: nowhere).
+template <int WD, int D, int G>
+__device__ __forceinline__ void store_quad(uint2 x, bool value, const QuadPlace<D, G>& at, uint8_t* tile) {
+  // (-min, max) of the group, both as maxima of 16-bit halves
+  uint32_t m = 0;
+  {
+    const uint32_t up = max2<WD>(x.x, x.y), down = max2<WD>(x.x ^ 0x80008000u, x.y ^ 0x80008000u);
+    m = max2<WD>(__byte_perm(down, up, 0x5410), __byte_perm(down, up, 0x7632));
+#pragma unroll
+    for (int o = 1; o < G / 4; o <<= 1) m = max2<WD>(m, __shfl_xor_sync(0xffffffffu, m, o));
+  }
+  const float lo = -widen<WD>((uint16_t)m), range = widen<WD>((uint16_t)(m >> 16)) - lo;
+  const bool fine = range < INFINITY;
+  // range / 15, correctly rounded: the quotient by 1 / 15 put right by its remainder
+  const float fifteenth = 0.0666666701436042785645f, about = __fmul_rn(range, fifteenth);
+  const uint16_t scale16 = narrow<WD>(__fmaf_rn(__fmaf_rn(-15.f, about, range), fifteenth, about));
+  const float scale = fine ? widen<WD>(scale16) : 0.f;
+  // (x - zero) / scale to the nearest whole number, ties to even: by a reciprocal, then put right by the remainder, which is exact (a
+  // whole number up to 16 times a 16-bit scale fits fp32, and what is left of x - zero is at most about half a scale).
+  const Quad y = widen_quad<WD>(x);
+  const float inverse = __fdividef(1.f, scale), magic = 12582912.f;
+  float d[4], c[4], over = -1.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    d[e] = __fsub_rn(y.x[e], lo);
+    c[e] = __fmaf_rn(d[e], inverse, magic);  // (whole, in the low bits)
+    over = fmaxf(over, fmaf(2.f, fabsf(fmaf(-__fsub_rn(c[e], magic), scale, d[e])), -scale));
+  }
+  if (!(scale > 1e-30f)) {  // (reciprocals end there; a scale of 0 or NaN: codes of 0)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c[e] = magic + (scale > 0.f ? rintf(__fdiv_rn(d[e], scale)) : 0.f);
+  } else if (over >= 0.f) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float r = fmaf(-__fsub_rn(c[e], magic), scale, d[e]), past = fmaf(2.f, fabsf(r), -scale);
+      if (past > 0.f || (past == 0.f && (__float_as_uint(c[e]) & 1))) c[e] += r > 0.f ? 1.f : -1.f;
+    }
+  }
+  uint32_t codes = 0;
+#pragma unroll
+  for (int e = 3; e >= 0; --e) codes = codes * 16 + __float_as_uint(fminf(c[e], magic + 15.f));
+  codes -= 0x4b400000u * 0x1111u;
+  // a word is two quads: neighbours of a key, 32 components apart of a value
+  const uint32_t other = __shfl_xor_sync(0xffffffffu, codes, value ? 8 : 1);
+  if (!tile) return;
+  if (at.first) *reinterpret_cast<uint32_t*>(tile + at.word) = codes | other << 16;
+  if (at.leads) *reinterpret_cast<uint32_t*>(tile + at.meta) = fine ? scale16 | ((m ^ 0x8000u) & 0xffffu) << 16 : 0x7fff7fffu;
+}
+
+// Cosines and sines of the lane's quad, and where its components' partners are.
+struct Turn { Quad c, s; };
+__device__ __forceinline__ Turn turn_of(const Kv4AppendArgs& A, int d0, const float* tab) {
+  const int r2 = A.rope_dim / 2;
+  Turn t;
+  if (A.rope_vec) {  // half of the turned part is a multiple of four: partners and angles are quads too
+    if (A.interleaved) {
+      const float2 c = __ldg(reinterpret_cast<const float2*>(tab + d0 / 2)), s = __ldg(reinterpret_cast<const float2*>(tab + r2 + d0 / 2));
+      t.c = {{c.x, c.x, c.y, c.y}}; t.s = {{-s.x, s.x, -s.y, s.y}};
+    } else {
+      const int j = d0 < r2 ? d0 : d0 - r2;
+      const float sign = d0 < r2 ? -1.f : 1.f;
+      const float4 c = __ldg(reinterpret_cast<const float4*>(tab + j)), s = __ldg(reinterpret_cast<const float4*>(tab + r2 + j));
+      t.c = {{c.x, c.y, c.z, c.w}}; t.s = {{sign * s.x, sign * s.y, sign * s.z, sign * s.w}};
+    }
+    return t;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int d = d0 + e, j = A.interleaved ? d / 2 : d < r2 ? d : d - r2;
+    t.c.x[e] = 1.f; t.s.x[e] = 0.f;
+    if (d >= A.rope_dim) continue;
+    t.c.x[e] = tab[j];
+    t.s.x[e] = (A.interleaved ? d & 1 : d >= r2) ? tab[r2 + j] : -tab[r2 + j];
+  }
+  return t;
+}
+__device__ __forceinline__ uint2 load_partners(const Kv4AppendArgs& A, const uint16_t* head, int d0, uint2 mine) {
+  const int r2 = A.rope_dim / 2;
+  if (A.rope_vec) {
+    if (A.interleaved) return make_uint2(mine.x >> 16 | mine.x << 16, mine.y >> 16 | mine.y << 16);
+    return load_quad(head + (d0 < r2 ? d0 + r2 : d0 - r2), A.kv_vec);
+  }
+  uint32_t x[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int d = d0 + e;
+    x[e] = d >= A.rope_dim ? 0 : head[A.interleaved ? d ^ 1 : d < r2 ? d + r2 : d - r2];
+  }
+  return make_uint2(x[0] | x[1] << 16, x[2] | x[3] << 16);
+}
+// x c + partner s, as the 16-bit type holds it.  The sum of the two products is taken exactly but for 2^-48 of it (each product as two
+// fp32 numbers, their sum with its error) and rounded to fp32 once, then to the type: keys, and with them codes, are those of 64-bit
+// arithmetic, without its conversions, which kept the conversion units busy.
+template <int WD>
+__device__ __forceinline__ uint2 turned_quad(const Quad& a, const Quad& b, const Turn& t) {
+  float y[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float p = __fmul_rn(a.x[e], t.c.x[e]), q = __fmul_rn(b.x[e], t.s.x[e]);
+    const float low = __fadd_rn(__fmaf_rn(a.x[e], t.c.x[e], -p), __fmaf_rn(b.x[e], t.s.x[e], -q));
+    const float sum = __fadd_rn(p, q), back = __fsub_rn(sum, p);
+    const float lost = __fadd_rn(__fsub_rn(p, __fsub_rn(sum, back)), __fsub_rn(q, back));
+    const float z = __fadd_rn(sum, __fadd_rn(lost, low));
+    y[e] = fabsf(sum) < INFINITY ? z : sum;
+  }
+  return make_uint2(pack2<WD>(y[0], y[1]), pack2<WD>(y[2], y[3]));
+}
+
+constexpr int K4_SLABS = 4;   // quads of a lane: slabs of 128 components that a warp takes of a token's keys or values
+constexpr int K4_Q_HEADS = 4;  // of queries, 32 lanes with 16 components of so many heads each
+
+// A warp takes K4_SLABS slabs of a token's keys or of its values, or 512 K4_Q_HEADS components of its queries; a lane's angles are the
+// same in all of them.  Queries are turned in fp32 and rounded once, as in the 16-bit append.
+template <int WD, int D, int G>
 __global__ void __launch_bounds__(256) ls_kv4_append_kernel(const Kv4AppendArgs A) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -168,53 +236,76 @@ __global__ void __launch_bounds__(256) ls_kv4_append_kernel(const Kv4AppendArgs 
   if (t >= A.n_tokens) return;
   if (job < 2 * A.kv_jobs) {
     const bool value = job >= A.kv_jobs;
-    const int slab0 = 2 * (value ? job - A.kv_jobs : job);
+    const int slab0 = K4_SLABS * (value ? job - A.kv_jobs : job), slabs = (A.p.kv_heads * D + 127) / 128;
     const uint16_t* token = value ? A.v + t * A.v_stride : A.k + t * A.k_stride;
-    int head[2], quad[2];
-    Quad a[2];
+    auto head_of = [&](int i) { return D == 64 ? (slab0 + i) * 2 + lane / 16 : D == 128 ? slab0 + i : (slab0 + i) / 2; };
+    auto quad_of = [&](int i) { return D == 64 ? lane % 16 : D == 128 ? lane : lane + 32 * (i & 1); };
+    uint2 mine[K4_SLABS], other[K4_SLABS];
+    auto source = [&](int i) { return token + (long long)min(head_of(i), A.p.kv_heads - 1) * D; };
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int slab = slab0 + i;  // 128 components
-      head[i] = D == 64 ? slab * 2 + lane / 16 : D == 128 ? slab : slab / 2;
-      quad[i] = D == 64 ? lane % 16 : D == 128 ? lane : lane + 32 * (slab & 1);
-      a[i] = load_quad<WD>(token + (long long)min(head[i], A.p.kv_heads - 1) * D + 4 * quad[i], A.kv_vec);
-    }
+    for (int i = 0; i < K4_SLABS; ++i) mine[i] = load_quad(source(i) + 4 * quad_of(i), A.kv_vec);
     const int sq = A.seq[t], ps = A.pos[t];
-    int row = 0;
-    const long long at = kv4_tile_at(A.p, sq, ps, A.rope_dim > 0 ? A.rope_positions : 0x7fffffff, kv4_tile(D, A.p.group), row);
-    if (at < 0) return;
+    const bool turn = !value && A.rope_dim > 0;
+    if (turn) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (!value && A.rope_dim > 0)
-        a[i] = turned_quad<WD>(A, a[i], token + (long long)min(head[i], A.p.kv_heads - 1) * D, 4 * quad[i], A.rope + (long long)ps * A.rope_dim);
-      store_quad<WD, D>(A, a[i], value, quad[i], row, head[i] < A.p.kv_heads ? A.p.pages + at + head[i] * A.p.head_stride : nullptr);
+      for (int i = 0; i < K4_SLABS; ++i) other[i] = 4 * quad_of(i) < A.rope_dim ? load_partners(A, source(i), 4 * quad_of(i), mine[i]) : make_uint2(0, 0);
+    }
+    int row = 0;
+    const long long at = kv4_tile_at(A.p, sq, ps, A.rope_dim > 0 ? A.rope_positions : 0x7fffffff, kv4_tile(D, G), row);
+    if (at < 0) return;
+    constexpr int kinds = D == 256 ? 2 : 1;
+    Turn angle[kinds];
+#pragma unroll
+    for (int i = 0; i < kinds; ++i)
+      if (turn && 4 * quad_of(i) < A.rope_dim) angle[i] = turn_of(A, 4 * quad_of(i), A.rope + (long long)ps * A.rope_dim);
+    const QuadPlace<D, G> place[2] = {{value, quad_of(0), row}, {value, quad_of(1), row}};
+    uint8_t* tile = A.p.pages + at;
+#pragma unroll
+    for (int i = 0; i < K4_SLABS; ++i) {
+      if (slab0 + i >= slabs) break;
+      uint2 a = mine[i];
+      if (turn && 4 * quad_of(i) < A.rope_dim) {
+        const uint2 b = turned_quad<WD>(widen_quad<WD>(a), widen_quad<WD>(other[i]), angle[i % kinds]);
+        a.x = b.x;
+        if (A.rope_vec || 4 * quad_of(i) + 2 < A.rope_dim) a.y = b.y;  // (a whole number of pairs is turned)
+      }
+      store_quad<WD, D, G>(a, value, place[i % kinds], head_of(i) < A.p.kv_heads ? tile + head_of(i) * A.p.head_stride : nullptr);
     }
     return;
   }
   const int ps = A.pos[t], r2 = A.rope_dim / 2;
   const bool turn = A.rope_dim > 0 && ps >= 0 && ps < A.rope_positions;
   const float* tab = A.rope + (long long)ps * A.rope_dim;
+  const int i = lane % (D / 16), h0 = (job - 2 * A.kv_jobs) * (K4_Q_HEADS * 512 / D) + lane / (D / 16), step = 512 / D;
+  const uint16_t* src = A.q + t * A.q_stride;
+  uint16_t* dst = A.q_out + t * A.q_out_stride;
+  if (A.q_vec) {  // two chunks of eight whose components are each other's partners, or neighbours where nothing is turned
+    const bool turned = turn && 16 * i < A.rope_dim;
+    const int c0 = turned && !A.interleaved ? 8 * i : 16 * i, c1 = turned && !A.interleaved ? c0 + r2 : c0 + 8;
+    uint4 ra[K4_Q_HEADS], rb[K4_Q_HEADS];
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int item = (job - 2 * A.kv_jobs) * 64 + k * 32 + lane, hd = item / (D / 16), i = item % (D / 16);
-    if (hd >= A.heads) return;
-    const uint16_t* src = A.q + t * A.q_stride + (long long)hd * D;
-    uint16_t* dst = A.q_out + t * A.q_out_stride + (long long)hd * D;
-    if (A.q_vec) {  // two chunks of eight whose components are each other's partners, or neighbours where nothing is turned
-      const bool turned = turn && 16 * i < A.rope_dim;
-      const int c0 = turned && !A.interleaved ? 8 * i : 16 * i, c1 = turned && !A.interleaved ? c0 + r2 : c0 + 8;
-      uint4 ra = ld_stream128(src + c0), rb = ld_stream128(src + c1);
+    for (int k = 0; k < K4_Q_HEADS; ++k) {
+      const uint16_t* p = src + (long long)min(h0 + k * step, A.heads - 1) * D;
+      ra[k] = ld_stream128(p + c0);
+      rb[k] = ld_stream128(p + c1);
+    }
+    float c[8], s[8];
+    if (turned) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float4 e = __ldg(reinterpret_cast<const float4*>(tab + 8 * i) + h), f = __ldg(reinterpret_cast<const float4*>(tab + r2 + 8 * i) + h);
+        c[4 * h] = e.x; c[4 * h + 1] = e.y; c[4 * h + 2] = e.z; c[4 * h + 3] = e.w;
+        s[4 * h] = f.x; s[4 * h + 1] = f.y; s[4 * h + 2] = f.z; s[4 * h + 3] = f.w;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < K4_Q_HEADS; ++k) {
+      if (h0 + k * step >= A.heads) break;
+      uint16_t* out = dst + (long long)(h0 + k * step) * D;
       if (turned) {
         float a[8], b[8], x[8], y[8];
-        unpack8<WD>(ra, a);
-        unpack8<WD>(rb, b);
-        float c[8], s[8];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float4 e = __ldg(reinterpret_cast<const float4*>(tab + 8 * i) + h), f = __ldg(reinterpret_cast<const float4*>(tab + r2 + 8 * i) + h);
-          c[4 * h] = e.x; c[4 * h + 1] = e.y; c[4 * h + 2] = e.z; c[4 * h + 3] = e.w;
-          s[4 * h] = f.x; s[4 * h + 1] = f.y; s[4 * h + 2] = f.z; s[4 * h + 3] = f.w;
-        }
+        unpack8<WD>(ra[k], a);
+        unpack8<WD>(rb[k], b);
         if (A.interleaved) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
@@ -227,23 +318,29 @@ __global__ void __launch_bounds__(256) ls_kv4_append_kernel(const Kv4AppendArgs 
 #pragma unroll
           for (int e = 0; e < 8; ++e) { x[e] = a[e] * c[e] - b[e] * s[e]; y[e] = b[e] * c[e] + a[e] * s[e]; }
         }
-        ra = make_uint4(pack2<WD>(x[0], x[1]), pack2<WD>(x[2], x[3]), pack2<WD>(x[4], x[5]), pack2<WD>(x[6], x[7]));
-        rb = make_uint4(pack2<WD>(y[0], y[1]), pack2<WD>(y[2], y[3]), pack2<WD>(y[4], y[5]), pack2<WD>(y[6], y[7]));
+        ra[k] = make_uint4(pack2<WD>(x[0], x[1]), pack2<WD>(x[2], x[3]), pack2<WD>(x[4], x[5]), pack2<WD>(x[6], x[7]));
+        rb[k] = make_uint4(pack2<WD>(y[0], y[1]), pack2<WD>(y[2], y[3]), pack2<WD>(y[4], y[5]), pack2<WD>(y[6], y[7]));
       }
-      *reinterpret_cast<uint4*>(dst + c0) = ra;
-      *reinterpret_cast<uint4*>(dst + c1) = rb;
-      continue;
+      *reinterpret_cast<uint4*>(out + c0) = ra[k];
+      *reinterpret_cast<uint4*>(out + c1) = rb[k];
     }
+    return;
+  }
+  for (int k = 0; k < K4_Q_HEADS; ++k) {
+    const int hd = h0 + k * step;
+    if (hd >= A.heads) return;
+    const uint16_t* from = src + (long long)hd * D;
+    uint16_t* out = dst + (long long)hd * D;
     for (int e = 8 * i; e < 8 * i + 8; ++e) {  // pair by pair: any alignment, any even rope_dim
       const int d0 = A.rope_dim > 0 && !A.interleaved && e < r2 ? e : 2 * e, d1 = A.rope_dim > 0 && !A.interleaved && e < r2 ? e + r2 : 2 * e + 1;
-      const uint16_t a = src[d0], b = src[d1];
+      const uint16_t a = from[d0], b = from[d1];
       if (turn && e < r2) {
         const float x1 = widen<WD>(a), x2 = widen<WD>(b), c = tab[e], s = tab[r2 + e];
-        dst[d0] = narrow<WD>(x1 * c - x2 * s);
-        dst[d1] = narrow<WD>(x2 * c + x1 * s);
+        out[d0] = narrow<WD>(x1 * c - x2 * s);
+        out[d1] = narrow<WD>(x2 * c + x1 * s);
       } else {
-        dst[d0] = a;
-        dst[d1] = b;
+        out[d0] = a;
+        out[d1] = b;
       }
     }
   }
@@ -266,20 +363,31 @@ struct Kv4ReadArgs {
   const int32_t* seq;
   const int32_t* pos;
   int64_t k_stride, v_stride;
-  int32_t n_tokens, per_block, vec;
+  int32_t n_tokens, width, vec;  // width: threads of a token
 };
 
-// Eight codes of a word as scale * code + zero (exact but for the last rounding of the sum), rounded to the type.
+// Pairs of codes as scale * code + zero, rounded once (a fused multiply-add of the type).  The codes come as integers above 1024 (fp16)
+// or 128 (bf16), from which the type's own subtraction takes them exactly.
 template <int WD>
-__device__ __forceinline__ uint4 word_values(uint32_t w, uint32_t meta_lo, uint32_t meta_hi) {
-  float x[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const uint32_t m = e < 4 ? meta_lo : meta_hi;
-    const float code = __uint_as_float((w >> (4 * e) & 15u) | 0x4b000000u) - 8388608.f;
-    x[e] = fmaf(code, widen<WD>((uint16_t)m), widen<WD>((uint16_t)(m >> 16)));
+__device__ __forceinline__ uint32_t pair_values(uint32_t codes, uint32_t scale, uint32_t zero) {
+  uint32_t u, r;
+  if (WD == WD_BF16) {
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(u) : "r"(codes | 0x43004300u), "r"(0x43004300u));
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(u), "r"(scale), "r"(zero));
+  } else {
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(u) : "r"(codes | 0x64006400u), "r"(0x64006400u));
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(u), "r"(scale), "r"(zero));
   }
-  return make_uint4(pack2<WD>(x[0], x[1]), pack2<WD>(x[2], x[3]), pack2<WD>(x[4], x[5]), pack2<WD>(x[6], x[7]));
+  return r;
+}
+// The eight codes of a word, in order.
+template <int WD>
+__device__ __forceinline__ uint4 word_values(uint32_t w, uint32_t meta) {
+  const uint32_t scale = __byte_perm(meta, 0, 0x1010), zero = __byte_perm(meta, 0, 0x3232);
+  uint32_t r[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) r[e] = pair_values<WD>(w >> (4 * e) & 0x000f000fu, scale, zero);
+  return make_uint4(__byte_perm(r[0], r[1], 0x5410), __byte_perm(r[2], r[3], 0x5410), __byte_perm(r[0], r[1], 0x7632), __byte_perm(r[2], r[3], 0x7632));
 }
 
 __device__ __forceinline__ void put8(uint16_t* dst, uint4 v, bool vec) {
@@ -289,36 +397,37 @@ __device__ __forceinline__ void put8(uint16_t* dst, uint4 v, bool vec) {
   for (int e = 0; e < 8; ++e) dst[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
 }
 
-// A thread takes two words of a row at a time: 16 components of a key, or twice 8 of a value, each stored as 16 bytes.
+// `width` threads to a token, each with 16 components of a key and of a value of every head that it visits: two words of each, stored
+// as two times 16 bytes.
 template <int WD, int D>
 __global__ void __launch_bounds__(256) ls_kv4_read_kernel(const Kv4ReadArgs A) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   constexpr int per = D / 16;
-  const int items = A.p.kv_heads * 2 * per, groups = D / A.p.group, n = min(A.per_block, A.n_tokens - (int)blockIdx.x * A.per_block) * items;
-  for (int x = threadIdx.x; x < n; x += 256) {
-    const int tt = x / items, y = x - tt * items;
-    const int j = y % per, value = y / per % 2, h = y / (2 * per);
-    const long long t = (long long)blockIdx.x * A.per_block + tt;
-    uint16_t* out = value ? A.v : A.k;
-    if (!out) continue;
-    int row = 0;
-    const long long at = kv4_tile_at(A.p, A.seq[t], A.pos[t], 0x7fffffff, kv4_tile(D, A.p.group), row);
-    if (at < 0) continue;
-    const uint8_t* tile = A.p.pages + at + h * A.p.head_stride;
-    const uint32_t* codes = reinterpret_cast<const uint32_t*>(tile + (16 * value + row) * (D / 2));
-    const uint32_t* meta = reinterpret_cast<const uint32_t*>(tile + 16 * D) + (16 * value + row) * groups;
-    out += t * (value ? A.v_stride : A.k_stride) + (long long)h * D;
-    if (value) {
-      const int g = 2 * (j % 4), ws = j / 4, lo = 64 * ws + 4 * g;
-      const uint32_t a = codes[value_word<D>(g, ws, row)], b = codes[value_word<D>(g + 1, ws, row)];
-      const uint32_t m0 = meta[lo / A.p.group], m1 = meta[(lo + 32) / A.p.group];
-      put8(out + lo, word_values<WD>((a & 0xffffu) | b << 16, m0, m0), A.vec);
-      put8(out + lo + 32, word_values<WD>(a >> 16 | (b & 0xffff0000u), m1, m1), A.vec);
-    } else {
-      const uint32_t a = codes[key_word<D>(2 * j, row)], b = codes[key_word<D>(2 * j + 1, row)], m = meta[16 * j / A.p.group];
-      put8(out + 16 * j, word_values<WD>(a, m, m), A.vec);
-      put8(out + 16 * j + 8, word_values<WD>(b, m, m), A.vec);
+  const int tt = threadIdx.x / A.width, y0 = threadIdx.x - tt * A.width, items = A.p.kv_heads * per, groups = D / A.p.group;
+  const long long t = (long long)blockIdx.x * (256 / A.width) + tt;
+  if (tt >= 256 / A.width || t >= A.n_tokens) return;
+  int row = 0;
+  const long long at = kv4_tile_at(A.p, A.seq[t], A.pos[t], 0x7fffffff, kv4_tile(D, A.p.group), row);
+  if (at < 0) return;
+  const uint32_t* codes = reinterpret_cast<const uint32_t*>(A.p.pages + at) + row * (D / 8);
+  const uint32_t* meta = reinterpret_cast<const uint32_t*>(A.p.pages + at + 16 * D) + row * groups;
+  uint16_t *k_out = A.k + t * A.k_stride, *v_out = A.v + t * A.v_stride;
+  const int shift = A.p.group == 32 ? 5 : A.p.group == 64 ? 6 : 7;
+#pragma unroll 2
+  for (int y = y0; y < items; y += A.width) {
+    const int h = y / per, j = y % per, g = 2 * (j % 4), ws = j / 4, lo = 64 * ws + 4 * g;
+    const long long to = h * A.p.head_stride / 4;
+    if (A.k) {
+      const uint32_t a = __ldg(codes + to + key_word<D>(2 * j, row)), b = __ldg(codes + to + key_word<D>(2 * j + 1, row)), m = __ldg(meta + to + (16 * j >> shift));
+      put8(k_out + h * D + 16 * j, word_values<WD>(a, m), A.vec);
+      put8(k_out + h * D + 16 * j + 8, word_values<WD>(b, m), A.vec);
+    }
+    if (A.v) {
+      const uint32_t a = __ldg(codes + to + 2 * D + value_word<D>(g, ws, row)), b = __ldg(codes + to + 2 * D + value_word<D>(g + 1, ws, row));
+      const uint32_t m0 = __ldg(meta + to + 16 * groups + (lo >> shift)), m1 = __ldg(meta + to + 16 * groups + ((lo + 32) >> shift));
+      put8(v_out + h * D + lo, word_values<WD>(__byte_perm(a, b, 0x5410), m0), A.vec);
+      put8(v_out + h * D + lo + 32, word_values<WD>(__byte_perm(a, b, 0x7632), m1), A.vec);
     }
   }
 }
