@@ -196,12 +196,12 @@ int32_t ls_paged_kv4_append(ls_paged_kv4* kv, const void* d_q, int64_t q_stride,
   const bool one = n_tokens == 1;
   a.kv_vec = aligned16(d_k) && aligned16(d_v) && (one || (k_stride | v_stride) % 8 == 0);
   a.q_vec = D.rope_dim % 16 == 0 && aligned16(d_q) && aligned16(d_q_out) && aligned16(D.d_rope) && (one || !d_q || (q_stride | q_out_stride) % 8 == 0);
-  a.rope_vec = D.rope_dim % 8 == 0 && aligned16(D.d_rope);
-  const int64_t kv_job = 128 * ls::K4_SLABS, q_job = 512 * ls::K4_Q_HEADS;
+  a.rope_vec = D.rope_dim % 16 == 0 && aligned16(D.d_rope);
+  const int64_t kv_job = 256 * ls::K4_SLABS, q_job = 512 * ls::K4_Q_HEADS;
   a.kv_jobs = (int)((kw + kv_job - 1) / kv_job);
   a.jobs = 2 * a.kv_jobs + (d_q ? (int)((qw + q_job - 1) / q_job) : 0);
   const unsigned long long blocks = ((unsigned long long)n_tokens * a.jobs + 7) / 8;
-  if (blocks > 0x7fffffffULL) return fail(LS_ERR_INVALID, "ls_paged_kv4_append: too many tokens");
+  if (blocks > 0x1fffffffULL) return fail(LS_ERR_INVALID, "ls_paged_kv4_append: too many tokens");
   const cudaStream_t st = (cudaStream_t)stream;
   KernelTimer timer(LS_TIMED_APPEND4, st);
   return launch_early(D.dtype == LS_WDTYPE_BF16 ? append_kernel<ls::WD_BF16>(D.head_dim, D.group) : append_kernel<ls::WD_FP16>(D.head_dim, D.group), dim3((unsigned)blocks), 256, 0, st, a);

@@ -72,23 +72,10 @@ struct Kv4AppendArgs {
   int32_t kv_vec, q_vec, rope_vec;
 };
 
-struct Quad { float x[4]; };
-
-// Four consecutive components.
-__device__ __forceinline__ uint2 load_quad(const uint16_t* p, bool vec) {
-  if (vec) return __ldg(reinterpret_cast<const uint2*>(p));
-  return make_uint2(p[0] | (uint32_t)p[1] << 16, p[2] | (uint32_t)p[3] << 16);
-}
-template <int WD>
-__device__ __forceinline__ Quad widen_quad(uint2 r) {
-  Quad y;
-#pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const uint32_t w = e ? r.y : r.x;
-    if (WD == WD_BF16) { y.x[2 * e] = __uint_as_float(w << 16); y.x[2 * e + 1] = __uint_as_float(w & 0xffff0000u); }
-    else { const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w)); y.x[2 * e] = f.x; y.x[2 * e + 1] = f.y; }
-  }
-  return y;
+// Eight consecutive components.
+__device__ __forceinline__ uint4 load_oct(const uint16_t* p, bool vec) {
+  if (vec) return ld_stream128(p);
+  return make_uint4(p[0] | (uint32_t)p[1] << 16, p[2] | (uint32_t)p[3] << 16, p[4] | (uint32_t)p[5] << 16, p[6] | (uint32_t)p[7] << 16);
 }
 // The larger of each half; NaN if either is.
 template <int WD>
@@ -99,29 +86,31 @@ __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
   return r;
 }
 
-// Where a lane's quad (components 4 quad ...) of a row goes in a tile: the word of which it is a half, and its group's scale and zero.
+// Where a lane's eight components (8 oct ...) of a row go in a tile: the word that it stores, and its group's scale and zero.
 template <int D, int G>
-struct QuadPlace {
+struct OctPlace {
   int word, meta;
-  bool first, leads;  // its word is this lane's to store, its group's scale is
-  __device__ __forceinline__ QuadPlace(bool value, int quad, int row) {
-    first = value ? !(quad & 8) : !(quad & 1);
-    leads = quad % (G / 4) == 0;
-    word = ((value ? 16 : 0) + row) * (D / 2) + 4 * (value ? value_word<D>(quad & 7, quad >> 4, row) : key_word<D>(quad >> 1, row));
-    meta = 16 * D + (((value ? 16 : 0) + row) * (D / G) + quad / (G / 4)) * 4;
+  bool leads, high;  // its group's scale is this lane's to store; (values) its components are the high halves of their words
+  __device__ __forceinline__ OctPlace(bool value, int oct, int row) {
+    leads = oct % (G / 8) == 0;
+    high = oct & 4;
+    word = ((value ? 16 : 0) + row) * (D / 2) + 4 * (value ? value_word<D>(oct % 4 * 2 + high, oct >> 3, row) : key_word<D>(oct, row));
+    meta = 16 * D + (((value ? 16 : 0) + row) * (D / G) + oct / (G / 8)) * 4;
   }
 };
 
-// Quantises the lane's quad (as the type holds it) with the other lanes of its group, and stores it in `tile` (NULL: nowhere).
+// Quantises the lane's eight components (as the type holds them) with the other lanes of their group, and stores them in `tile` (NULL:
+// nowhere).
 template <int WD, int D, int G>
-__device__ __forceinline__ void store_quad(uint2 x, bool value, const QuadPlace<D, G>& at, uint8_t* tile) {
+__device__ __forceinline__ void store_oct(uint4 x, bool value, const OctPlace<D, G>& at, uint8_t* tile) {
   // (-min, max) of the group, both as maxima of 16-bit halves
-  uint32_t m = 0;
+  const uint32_t neg = 0x80008000u;
+  uint32_t m;
   {
-    const uint32_t up = max2<WD>(x.x, x.y), down = max2<WD>(x.x ^ 0x80008000u, x.y ^ 0x80008000u);
+    const uint32_t up = max2<WD>(max2<WD>(x.x, x.y), max2<WD>(x.z, x.w)), down = max2<WD>(max2<WD>(x.x ^ neg, x.y ^ neg), max2<WD>(x.z ^ neg, x.w ^ neg));
     m = max2<WD>(__byte_perm(down, up, 0x5410), __byte_perm(down, up, 0x7632));
 #pragma unroll
-    for (int o = 1; o < G / 4; o <<= 1) m = max2<WD>(m, __shfl_xor_sync(0xffffffffu, m, o));
+    for (int o = 1; o < G / 8; o <<= 1) m = max2<WD>(m, __shfl_xor_sync(0xffffffffu, m, o));
   }
   const float lo = -widen<WD>((uint16_t)m), range = widen<WD>((uint16_t)(m >> 16)) - lo;
   const bool fine = range < INFINITY;
@@ -131,145 +120,153 @@ __device__ __forceinline__ void store_quad(uint2 x, bool value, const QuadPlace<
   const float scale = fine ? widen<WD>(scale16) : 0.f;
   // (x - zero) / scale to the nearest whole number, ties to even: by a reciprocal, then put right by the remainder, which is exact (a
   // whole number up to 16 times a 16-bit scale fits fp32, and what is left of x - zero is at most about half a scale).
-  const Quad y = widen_quad<WD>(x);
+  float y[8];
+  unpack8<WD>(x, y);
   const float inverse = __fdividef(1.f, scale), magic = 12582912.f;
-  float d[4], c[4], over = -1.f;
+  float c[8], over = 0.f;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    d[e] = __fsub_rn(y.x[e], lo);
-    c[e] = __fmaf_rn(d[e], inverse, magic);  // (whole, in the low bits)
-    over = fmaxf(over, fmaf(2.f, fabsf(fmaf(-__fsub_rn(c[e], magic), scale, d[e])), -scale));
+  for (int e = 0; e < 8; ++e) {
+    y[e] = __fsub_rn(y[e], lo);
+    c[e] = __fmaf_rn(y[e], inverse, magic);  // (whole, in the low bits)
+    over = fmaxf(over, fabsf(fmaf(-__fsub_rn(c[e], magic), scale, y[e])));
   }
   if (!(scale > 1e-30f)) {  // (reciprocals end there; a scale of 0 or NaN: codes of 0)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) c[e] = magic + (scale > 0.f ? rintf(__fdiv_rn(d[e], scale)) : 0.f);
-  } else if (over >= 0.f) {
+    for (int e = 0; e < 8; ++e) c[e] = magic + (scale > 0.f ? rintf(__fdiv_rn(y[e], scale)) : 0.f);
+  } else if (2.f * over >= scale) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float r = fmaf(-__fsub_rn(c[e], magic), scale, d[e]), past = fmaf(2.f, fabsf(r), -scale);
+    for (int e = 0; e < 8; ++e) {
+      const float r = fmaf(-__fsub_rn(c[e], magic), scale, y[e]), past = fmaf(2.f, fabsf(r), -scale);
       if (past > 0.f || (past == 0.f && (__float_as_uint(c[e]) & 1))) c[e] += r > 0.f ? 1.f : -1.f;
     }
   }
   uint32_t codes = 0;
 #pragma unroll
-  for (int e = 3; e >= 0; --e) codes = codes * 16 + __float_as_uint(fminf(c[e], magic + 15.f));
-  codes -= 0x4b400000u * 0x1111u;
-  // a word is two quads: neighbours of a key, 32 components apart of a value
-  const uint32_t other = __shfl_xor_sync(0xffffffffu, codes, value ? 8 : 1);
+  for (int e = 7; e >= 0; --e) codes = codes * 16 + __float_as_uint(fminf(c[e], magic + 15.f));
+  codes -= 0x4b400000u * 0x11111111u;
+  if (value) {  // components 32 apart share a word: the lower four of each are one lane's word, the upper four the other's
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, codes, 4);
+    codes = at.high ? __byte_perm(other, codes, 0x7632) : __byte_perm(codes, other, 0x5410);
+  }
   if (!tile) return;
-  if (at.first) *reinterpret_cast<uint32_t*>(tile + at.word) = codes | other << 16;
+  *reinterpret_cast<uint32_t*>(tile + at.word) = codes;
   if (at.leads) *reinterpret_cast<uint32_t*>(tile + at.meta) = fine ? scale16 | ((m ^ 0x8000u) & 0xffffu) << 16 : 0x7fff7fffu;
 }
 
-// Cosines and sines of the lane's quad, and where its components' partners are.
-struct Turn { Quad c, s; };
+// Cosines and signed sines of the lane's components, and their partners.
+struct Turn { float c[8], s[8]; };
 __device__ __forceinline__ Turn turn_of(const Kv4AppendArgs& A, int d0, const float* tab) {
   const int r2 = A.rope_dim / 2;
   Turn t;
-  if (A.rope_vec) {  // half of the turned part is a multiple of four: partners and angles are quads too
+  if (A.rope_vec) {  // half of the turned part is a multiple of eight: partners and angles are eights too
+    const bool far = !A.interleaved && d0 >= r2;
+    const float4* at = reinterpret_cast<const float4*>(tab + (A.interleaved ? d0 / 2 : far ? d0 - r2 : d0));
+    const float4 c = __ldg(at), s = __ldg(at + r2 / 4);
     if (A.interleaved) {
-      const float2 c = __ldg(reinterpret_cast<const float2*>(tab + d0 / 2)), s = __ldg(reinterpret_cast<const float2*>(tab + r2 + d0 / 2));
-      t.c = {{c.x, c.x, c.y, c.y}}; t.s = {{-s.x, s.x, -s.y, s.y}};
+      const float cc[4] = {c.x, c.y, c.z, c.w}, ss[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) { t.c[e] = cc[e / 2]; t.s[e] = e & 1 ? ss[e / 2] : -ss[e / 2]; }
     } else {
-      const int j = d0 < r2 ? d0 : d0 - r2;
-      const float sign = d0 < r2 ? -1.f : 1.f;
-      const float4 c = __ldg(reinterpret_cast<const float4*>(tab + j)), s = __ldg(reinterpret_cast<const float4*>(tab + r2 + j));
-      t.c = {{c.x, c.y, c.z, c.w}}; t.s = {{sign * s.x, sign * s.y, sign * s.z, sign * s.w}};
+      const float4 c1 = __ldg(at + 1), s1 = __ldg(at + 1 + r2 / 4);
+      const float cc[8] = {c.x, c.y, c.z, c.w, c1.x, c1.y, c1.z, c1.w}, ss[8] = {s.x, s.y, s.z, s.w, s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) { t.c[e] = cc[e]; t.s[e] = far ? ss[e] : -ss[e]; }
     }
     return t;
   }
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
+  for (int e = 0; e < 8; ++e) {
     const int d = d0 + e, j = A.interleaved ? d / 2 : d < r2 ? d : d - r2;
-    t.c.x[e] = 1.f; t.s.x[e] = 0.f;
+    t.c[e] = 1.f; t.s[e] = 0.f;
     if (d >= A.rope_dim) continue;
-    t.c.x[e] = tab[j];
-    t.s.x[e] = (A.interleaved ? d & 1 : d >= r2) ? tab[r2 + j] : -tab[r2 + j];
+    t.c[e] = tab[j];
+    t.s[e] = (A.interleaved ? d & 1 : d >= r2) ? tab[r2 + j] : -tab[r2 + j];
   }
   return t;
 }
-__device__ __forceinline__ uint2 load_partners(const Kv4AppendArgs& A, const uint16_t* head, int d0, uint2 mine) {
+__device__ __forceinline__ uint4 load_partners(const Kv4AppendArgs& A, const uint16_t* head, int d0, uint4 mine) {
   const int r2 = A.rope_dim / 2;
-  if (A.rope_vec) {
-    if (A.interleaved) return make_uint2(mine.x >> 16 | mine.x << 16, mine.y >> 16 | mine.y << 16);
-    return load_quad(head + (d0 < r2 ? d0 + r2 : d0 - r2), A.kv_vec);
-  }
-  uint32_t x[4];
+  if (A.interleaved)
+    return make_uint4(__byte_perm(mine.x, 0, 0x1032), __byte_perm(mine.y, 0, 0x1032), __byte_perm(mine.z, 0, 0x1032), __byte_perm(mine.w, 0, 0x1032));
+  if (A.rope_vec) return load_oct(head + (d0 < r2 ? d0 + r2 : d0 - r2), A.kv_vec);
+  uint32_t x[8];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
+  for (int e = 0; e < 8; ++e) {
     const int d = d0 + e;
-    x[e] = d >= A.rope_dim ? 0 : head[A.interleaved ? d ^ 1 : d < r2 ? d + r2 : d - r2];
+    x[e] = d >= A.rope_dim ? 0 : head[d < r2 ? d + r2 : d - r2];
   }
-  return make_uint2(x[0] | x[1] << 16, x[2] | x[3] << 16);
+  return make_uint4(x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16);
 }
 // x c + partner s, as the 16-bit type holds it.  The sum of the two products is taken exactly but for 2^-48 of it (each product as two
 // fp32 numbers, their sum with its error) and rounded to fp32 once, then to the type: keys, and with them codes, are those of 64-bit
 // arithmetic, without its conversions, which kept the conversion units busy.
 template <int WD>
-__device__ __forceinline__ uint2 turned_quad(const Quad& a, const Quad& b, const Turn& t) {
-  float y[4];
+__device__ __forceinline__ uint4 turned_oct(uint4 mine, uint4 partners, const Turn& t) {
+  float a[8], b[8];
+  unpack8<WD>(mine, a);
+  unpack8<WD>(partners, b);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float p = __fmul_rn(a.x[e], t.c.x[e]), q = __fmul_rn(b.x[e], t.s.x[e]);
-    const float low = __fadd_rn(__fmaf_rn(a.x[e], t.c.x[e], -p), __fmaf_rn(b.x[e], t.s.x[e], -q));
+  for (int e = 0; e < 8; ++e) {
+    const float p = __fmul_rn(a[e], t.c[e]), q = __fmul_rn(b[e], t.s[e]);
+    const float low = __fadd_rn(__fmaf_rn(a[e], t.c[e], -p), __fmaf_rn(b[e], t.s[e], -q));
     const float sum = __fadd_rn(p, q), back = __fsub_rn(sum, p);
     const float lost = __fadd_rn(__fsub_rn(p, __fsub_rn(sum, back)), __fsub_rn(q, back));
     const float z = __fadd_rn(sum, __fadd_rn(lost, low));
-    y[e] = fabsf(sum) < INFINITY ? z : sum;
+    a[e] = fabsf(sum) < INFINITY ? z : sum;
   }
-  return make_uint2(pack2<WD>(y[0], y[1]), pack2<WD>(y[2], y[3]));
+  return make_uint4(pack2<WD>(a[0], a[1]), pack2<WD>(a[2], a[3]), pack2<WD>(a[4], a[5]), pack2<WD>(a[6], a[7]));
 }
 
-constexpr int K4_SLABS = 4;   // quads of a lane: slabs of 128 components that a warp takes of a token's keys or values
+constexpr int K4_SLABS = 2;    // slabs of 256 components that a warp takes of a token's keys or values, eight to a lane
 constexpr int K4_Q_HEADS = 4;  // of queries, 32 lanes with 16 components of so many heads each
 
 // A warp takes K4_SLABS slabs of a token's keys or of its values, or 512 K4_Q_HEADS components of its queries; a lane's angles are the
 // same in all of them.  Queries are turned in fp32 and rounded once, as in the 16-bit append.
 template <int WD, int D, int G>
-__global__ void __launch_bounds__(256) ls_kv4_append_kernel(const Kv4AppendArgs A) {
+__global__ void __launch_bounds__(256, 4) ls_kv4_append_kernel(const Kv4AppendArgs A) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int lane = threadIdx.x & 31;
-  const unsigned long long id = (unsigned long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const long long t = (long long)(id / (unsigned)A.jobs);
-  const int job = (int)(id - (unsigned long long)t * (unsigned)A.jobs);
+  const uint32_t id = blockIdx.x * 8 + (threadIdx.x >> 5);
+  const long long t = id / (uint32_t)A.jobs;
+  const int job = (int)(id - (uint32_t)t * (uint32_t)A.jobs);
   if (t >= A.n_tokens) return;
   if (job < 2 * A.kv_jobs) {
     const bool value = job >= A.kv_jobs;
-    const int slab0 = K4_SLABS * (value ? job - A.kv_jobs : job), slabs = (A.p.kv_heads * D + 127) / 128;
-    const uint16_t* token = value ? A.v + t * A.v_stride : A.k + t * A.k_stride;
-    auto head_of = [&](int i) { return D == 64 ? (slab0 + i) * 2 + lane / 16 : D == 128 ? slab0 + i : (slab0 + i) / 2; };
-    auto quad_of = [&](int i) { return D == 64 ? lane % 16 : D == 128 ? lane : lane + 32 * (i & 1); };
-    uint2 mine[K4_SLABS], other[K4_SLABS];
-    auto source = [&](int i) { return token + (long long)min(head_of(i), A.p.kv_heads - 1) * D; };
+    const int oct = lane % (D / 8), step = 256 / D, h0 = K4_SLABS * (value ? job - A.kv_jobs : job) * step + lane / (D / 8);
+    const uint16_t* token = (value ? A.v + t * A.v_stride : A.k + t * A.k_stride) + 8 * oct;
+    const bool turn = !value && 8 * oct < A.rope_dim;
+    uint4 mine[K4_SLABS], other[K4_SLABS];
+    auto source = [&](int i) { return token + (long long)min(h0 + i * step, A.p.kv_heads - 1) * D; };
 #pragma unroll
-    for (int i = 0; i < K4_SLABS; ++i) mine[i] = load_quad(source(i) + 4 * quad_of(i), A.kv_vec);
+    for (int i = 0; i < K4_SLABS; ++i) mine[i] = load_oct(source(i), A.kv_vec);
     const int sq = A.seq[t], ps = A.pos[t];
-    const bool turn = !value && A.rope_dim > 0;
     if (turn) {
 #pragma unroll
-      for (int i = 0; i < K4_SLABS; ++i) other[i] = 4 * quad_of(i) < A.rope_dim ? load_partners(A, source(i), 4 * quad_of(i), mine[i]) : make_uint2(0, 0);
+      for (int i = 0; i < K4_SLABS; ++i) other[i] = load_partners(A, source(i) - 8 * oct, 8 * oct, mine[i]);
     }
     int row = 0;
     const long long at = kv4_tile_at(A.p, sq, ps, A.rope_dim > 0 ? A.rope_positions : 0x7fffffff, kv4_tile(D, G), row);
     if (at < 0) return;
-    constexpr int kinds = D == 256 ? 2 : 1;
-    Turn angle[kinds];
+    if (turn) {
+      const Turn angle = turn_of(A, 8 * oct, A.rope + (long long)ps * A.rope_dim);
 #pragma unroll
-    for (int i = 0; i < kinds; ++i)
-      if (turn && 4 * quad_of(i) < A.rope_dim) angle[i] = turn_of(A, 4 * quad_of(i), A.rope + (long long)ps * A.rope_dim);
-    const QuadPlace<D, G> place[2] = {{value, quad_of(0), row}, {value, quad_of(1), row}};
+      for (int i = 0; i < K4_SLABS; ++i) {
+        const uint4 b = turned_oct<WD>(mine[i], other[i], angle);
+        const int left = A.rope_vec ? 8 : A.rope_dim - 8 * oct;  // (whole pairs are turned; the rest stays as it is)
+        mine[i].x = b.x;
+        if (left > 2) mine[i].y = b.y;
+        if (left > 4) mine[i].z = b.z;
+        if (left > 6) mine[i].w = b.w;
+      }
+    }
+    const OctPlace<D, G> place(value, oct, row);
     uint8_t* tile = A.p.pages + at;
 #pragma unroll
     for (int i = 0; i < K4_SLABS; ++i) {
-      if (slab0 + i >= slabs) break;
-      uint2 a = mine[i];
-      if (turn && 4 * quad_of(i) < A.rope_dim) {
-        const uint2 b = turned_quad<WD>(widen_quad<WD>(a), widen_quad<WD>(other[i]), angle[i % kinds]);
-        a.x = b.x;
-        if (A.rope_vec || 4 * quad_of(i) + 2 < A.rope_dim) a.y = b.y;  // (a whole number of pairs is turned)
-      }
-      store_quad<WD, D, G>(a, value, place[i % kinds], head_of(i) < A.p.kv_heads ? tile + head_of(i) * A.p.head_stride : nullptr);
+      const int h = h0 + i * step;
+      if (h - lane / (D / 8) >= A.p.kv_heads) break;
+      store_oct<WD, D, G>(mine[i], value, place, h < A.p.kv_heads ? tile + h * A.p.head_stride : nullptr);
     }
     return;
   }
