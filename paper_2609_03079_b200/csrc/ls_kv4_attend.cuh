@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
     const int seg = min(u0 + blocks, gaps ? pos + share : end) - pos;
     if (seg <= 0) return;
     const int h = A.by_row_tiles(unit), row0 = (unit - h * A.row_tiles) * S::ROWS, rows = min(S::ROWS, A.q_len * A.group - row0);
-    const int n = (unsigned)(seg + w - 1 - wi) / (unsigned)w;
+    const int n = dead ? 0 : (unsigned)(seg + w - 1 - wi) / (unsigned)w;
     const int block0 = k4_first<KT>(A, len) + pos - u0 + wi;
 
     // queries: the lane's columns of the operand are components 8 (4 j + t) ... of row g
@@ -276,37 +276,49 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
     };
     ask(0, id);
     ask(32, id_next);
-    uint32_t good[KT], skip = 0;  // (skip: KT bits by stage, tiles without a page)
+    uint32_t good[KT], skip = 0;  // (skip: KT bits by stage, tiles without a page; kept once there is one)
+    bool patchy = false, joined = false;
     const uint8_t* src[KT];
     auto settle = [&](int j) {  // turns the asked numbers into addresses for blocks j ... j + 31
+      bool all = true;
 #pragma unroll
       for (int i = 0; i < KT; ++i) {
         const int tile = (block0 + (j + lane) * w) * KT + i;
-        const bool ok = id[i] >= 0 && id[i] < A.p.n_pages;
+        const bool none = i && tile * 16 >= len;  // (behind the sequence's end: what nobody sees may be the tile before)
+        if (none) src[i] = src[0];
+        const bool ok = none || (id[i] >= 0 && id[i] < A.p.n_pages);
         if (!ok && j + lane < n && tile * 16 < len) set_status(A.p.status, ST_BAD_INDEX);
-        good[i] = __ballot_sync(0xffffffffu, ok);
-        src[i] = A.p.pages + (id[i] * A.p.page_stride + h * A.p.head_stride + (long long)(tile - A.by_page(tile) * (A.p.page >> 4)) * S::TILE);
+        all &= ok || j + lane >= n;
+        good[i] = __ballot_sync(0xffffffffu, none ? good[0] >> lane & 1 : ok);
+        if (!none) src[i] = A.p.pages + (id[i] * A.p.page_stride + h * A.p.head_stride + (long long)(tile - A.by_page(tile) * (A.p.page >> 4)) * S::TILE);
       }
+      joined = KT == 2 && all && src[KT - 1] == src[0] + S::TILE;  // (the lane's tiles side by side: one copy)
+      patchy |= !__all_sync(0xffffffffu, all);
+    };
+    auto bulk = [&](int tile, const uint8_t* from, uint32_t bytes, uint32_t to) {
+      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(saddr(ring + tile * S::TILE)),
+                   "l"(from), "r"(bytes), "r"(to), "l"(once) : "memory");
     };
     auto copy = [&](int j, int to) {
-      uint32_t here[KT], bytes = 0;
+      uint32_t here = (1u << KT) - 1;
+      if (patchy) {
+        here = 0;
 #pragma unroll
-      for (int i = 0; i < KT; ++i) {
-        here[i] = good[i] >> (j & 31) & 1;
-        bytes += here[i] ? S::TILE : 0;
-        skip = (skip & ~(1u << (to * KT + i))) | (here[i] ^ 1) << (to * KT + i);
+        for (int i = 0; i < KT; ++i) here |= (good[i] >> (j & 31) & 1) << i;
+        skip = (skip & ~(((1u << KT) - 1) << (to * KT))) | (here ^ ((1u << KT) - 1)) << (to * KT);
       }
       if (lane == (j & 31)) {
-        mb_expect(bar + 8 * to, bytes);
+        mb_expect(bar + 8 * to, __popc(here) * S::TILE);
+        if (joined) bulk(to * KT, src[0], KT * S::TILE, bar + 8 * to);
+        else {
 #pragma unroll
-        for (int i = 0; i < KT; ++i)
-          if (here[i])
-            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(
-                             saddr(ring + (to * KT + i) * S::TILE)), "l"(src[i]), "r"(S::TILE), "r"(bar + 8 * to), "l"(once) : "memory");
+          for (int i = 0; i < KT; ++i)
+            if (here >> i & 1) bulk(to * KT + i, src[i], S::TILE, bar + 8 * to);
+        }
       }
     };
     settle(0);
-    if (!dead) {
+    {
       int to = stage;
 #pragma unroll 1
       for (int j = 0; j < min(n, ST); ++j) {
@@ -370,11 +382,18 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[x][ws][e / 8][e / 4 % 2][e % 4] = 0.f;
     }
-    const int seen_by_all = len - A.q_len + A.by_group(row0), last_row = len - A.q_len + A.by_group(row0 + rows - 1);
-    const int hidden_from_some = max(last_row, -1) - A.window;  // (at least -2^31: a window is at most 2^31 - 1)
+    // Blocks that all rows see all of: from `plain` on, `plains` of them.
+    int plain, plains;
+    {
+      const int first_row = len - A.q_len + A.by_group(row0), last_row = len - A.q_len + A.by_group(row0 + rows - 1);
+      const int upto = max(first_row + 1, 0) / (16 * KT);                                     // (blocks below it end at the first row or before)
+      const int since = (int)((unsigned)max(max(last_row, 0) - A.window + 16 * KT, 0) / (16 * KT));  // (its first key and all behind are seen by the last row)
+      plain = (unsigned)max(since - block0 + w - 1, 0) / (unsigned)w;
+      plains = max((int)((unsigned)max(upto - block0 + w - 1, 0) / (unsigned)w) - plain, 0);
+    }
 
 #pragma unroll 1
-    for (int j = 0; j < n && !dead; ++j) {
+    for (int j = 0; j < n; ++j) {
       bool here = mb_try(bar + 8 * stage, parity);
       if (!__all_sync(0xffffffffu, here)) {
         const long long began = clock64();
@@ -389,11 +408,9 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
           break;
         }
       }
-      const uint32_t gone = skip >> (stage * KT) & ((1u << KT) - 1);
-      if (gone != (1u << KT) - 1) {
+      {
         const uint8_t* tile = ring + stage * KT * S::TILE;
-        const int pos0 = (block0 + j * w) * 16 * KT;
-        const bool edge = pos0 + 16 * KT - 1 > seen_by_all || pos0 <= hidden_from_some || gone;
+        const bool edge = (unsigned)(j - plain) >= (unsigned)plains || patchy;
 
         // scores: rows are tokens tok0 and tok0 + 8 of a tile, columns rows of queries
         float x[KT][NT][4];
@@ -448,6 +465,8 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
           for (int k = 0; k < NG; ++k) { va[z][k] = both_halves<WD>(ma[k]); vb[z][k] = both_halves<WD>(mb[k]); }
         }
         if (edge) {
+          const uint32_t gone = skip >> (stage * KT);
+          const int pos0 = (block0 + j * w) * 16 * KT;
           // Tokens that nobody sees may hold anything, and one that some rows see may hold NaN: neither must meet a weight of zero.
 #pragma unroll
           for (int z = 0; z < KT; ++z) {
@@ -479,19 +498,21 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
         }
         // Weights relative to M, which moves only when the weights times their scales leave what fp16 holds.  (Their sum tells: none of them
         // is negative, and one that is NaN may hide nothing; 2^-60 keeps weights of scales of zero in range.)
-        float p[KT][NT][4], most = 0.f;
+        float p[KT][NT][4], most[2] = {0.f, 0.f};
 #pragma unroll
-        for (int z = 0; z < KT; ++z)
+        for (int z = 0; z < KT; ++z) {
+          float all[2] = {8.67361737988403547e-19f, 8.67361737988403547e-19f};
+#pragma unroll
+          for (int k = 0; k < NG; ++k) { all[0] += va[z][k].x; all[1] += vb[z][k].x; }
 #pragma unroll
           for (int y = 0; y < NT; ++y)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               p[z][y][e] = ex2(fmaf(x[z][y][e], cn[y][e & 1], -M[y][e & 1]));
-              most = fmaf(p[z][y][e], 8.67361737988403547e-19f, most);
-#pragma unroll
-              for (int k = 0; k < NG; ++k) most = fmaf(p[z][y][e], e < 2 ? va[z][k].x : vb[z][k].x, most);
+              most[e / 2] = fmaf(p[z][y][e], all[e / 2], most[e / 2]);
             }
-        if (__any_sync(0xffffffffu, !(most <= 16384.f))) {
+        }
+        if (__any_sync(0xffffffffu, !(most[0] + most[1] <= 16384.f))) {
           float big[KT][2];
 #pragma unroll
           for (int z = 0; z < KT; ++z) {
