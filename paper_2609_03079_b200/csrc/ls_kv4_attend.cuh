@@ -173,29 +173,26 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
   // Shares: whatever ends first, by blocks that a warp has one after another.  Either units follow each other without a gap, so that every
   // team has as much but begins and ends inside a unit; or each unit begins with a new share, one for all of it, or several.  (Shares
   // may be a little larger than they need to be: fp32 will do.)
-  int w = 1, share = 1;
-  bool gaps = false;
-  {
+  int w, share;
+  bool gaps;
+  {  // (a lane for each size of a team)
+    w = lane == 0 ? S::WARPS : max(1, 8 >> lane);
     const float units = (float)(n_seqs * per_seq), all = (float)total, above = 1.f + 1e-6f;
-    float best = 1e30f;
-#pragma unroll 1
-    for (int x = S::WARPS; x >= 1; x = x > 4 ? 4 : x / 2) {
-      const float each = __fdividef(1.f, (float)x), teams = floorf(S::WARPS * each + 0.01f) * gridDim.x;
-      const float even = floorf(__fdividef(all, teams) * above) + 1.f, some = floorf(__fdividef(all, teams - units) * above) + 1.f;
-      auto join = [&](float of) {  // for every time that the team's place is filled, and for every piece that its threads add up
-        const float n = __fdividef((float)longest, of) + 1.f;
-        return K4_JOIN + n * each * ((float)S::PIECE / S::RING + K4_ADD * (float)(S::ROWS * D));
-      };
-      const float cost_even = even * each + K4_UNIT * (1.f + fmaxf(1.f, __fdividef(even * units, all))) + join(even);
-      const float cost_some = units < teams ? some * each + K4_UNIT + join(some) : 1e30f, cost_one = units <= teams ? longest * each + K4_UNIT : 1e30f;
-      const float cost = fminf(cost_even, fminf(cost_some, cost_one));
-      if (cost < best) {
-        best = cost;
-        w = x;
-        gaps = cost != cost_even;
-        share = cost == cost_even ? (int)even : cost == cost_one ? longest : (int)some;
-      }
-    }
+    const float each = __fdividef(1.f, (float)w), teams = (float)(S::WARPS / w * gridDim.x);
+    const float even = floorf(__fdividef(all, teams) * above) + 1.f, some = floorf(__fdividef(all, teams - units) * above) + 1.f;
+    auto join = [&](float of) {  // for every time that the team's place is filled, and for every piece that its threads add up
+      const float n = __fdividef((float)longest, of) + 1.f;
+      return K4_JOIN + n * each * ((float)S::PIECE / S::RING + K4_ADD * (float)(S::ROWS * D));
+    };
+    const float cost_even = even * each + K4_UNIT * (1.f + fmaxf(1.f, __fdividef(even * units, all))) + join(even);
+    const float cost_some = units < teams ? some * each + K4_UNIT + join(some) : 1e30f, cost_one = units <= teams ? longest * each + K4_UNIT : 1e30f;
+    const float cost = fminf(cost_even, fminf(cost_some, cost_one));
+    gaps = cost != cost_even;
+    share = cost == cost_even ? (int)even : cost == cost_one ? longest : (int)some;
+    const int best = __reduce_min_sync(0xffffffffu, (__float_as_uint(cost) & ~31u) | lane) & 31;
+    w = __shfl_sync(0xffffffffu, w, best);
+    share = __shfl_sync(0xffffffffu, share, best);
+    gaps = __shfl_sync(0xffffffffu, gaps, best);
   }
   const int mates = warp / w, wi = warp - mates * w, team = mates * gridDim.x + blockIdx.x;
   int pos = team * share;
