@@ -254,7 +254,7 @@ int32_t ls_paged_kv4_attend(ls_paged_kv4* kv, const void* d_q, int64_t q_stride,
     a.behind = (int)std::min<long long>(0x7fffffff, (long long)a.window + q_len - 1);
     a.by_group = fast_div(a.group); a.by_row_tiles = fast_div(a.row_tiles); a.by_page = fast_div(D.page_size / 16);
     a.out_vec = (reinterpret_cast<uintptr_t>(d_out) & 7) == 0 && (n_seqs * (long long)q_len == 1 || out_stride % 4 == 0);
-    a.scale_log2 = scale * ls::LOG2E; a.four = 4;
+    a.scale_log2 = scale * ls::LOG2E;
     LS_TRY(launch_early(s.kernel, dim3((unsigned)kv->sm_count), s.threads, s.smem, st, a));
   }
   return LS_OK;

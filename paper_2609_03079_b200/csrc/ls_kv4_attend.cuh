@@ -33,7 +33,6 @@ struct Attend4Args {
   int32_t q_len, heads, group, window, row_tiles, out_vec;
   int32_t most, behind;  // positions that a sequence can have; of those, how many from its end on are seen by any of its tokens
   FastDiv by_group, by_row_tiles, by_page;  // (by_page: tiles of a page)
-  uint32_t four;       // 4: a factor that the compiler does not know, so that it shifts with the multiplier, which has nothing else to do
   float scale_log2;
 };
 
@@ -46,20 +45,25 @@ constexpr long long K4_MAX_BLOCKS = 1LL << 30;
 // Shapes of the kernel: D components a head, groups of G, NT times 8 rows of queries at once.
 template <int D, int G, int NT>
 struct K4Shape {
-  static constexpr int WARPS = D * NT <= 128 ? 12 : 8;                  // (168 registers a thread, or 255)
-  static constexpr int KT = D * NT > 128 && D / G >= 4 ? 1 : 2;         // tiles of a block, which a warp takes at once
+  static constexpr int WARPS = D * NT <= 128 ? 12 : 8;           // (168 registers a thread, or 255)
+  static constexpr int KT = D == 256 && G == 32 ? 1 : 2;         // tiles of a block, which a warp takes at once
   static constexpr int THREADS = WARPS * 32;
   static constexpr int ROWS = 8 * NT;
   static constexpr int NG = D / G;
   static constexpr int TILE = kv4_tile(D, G);
   static constexpr int LINE = D + 4;                     // floats of a row's piece
   static constexpr int PIECE = ROWS * LINE * 4;
-  static constexpr int FIT = (232448 - 256 - WARPS * 64) / (WARPS * KT * TILE);
+  // Operands of the queries stay in registers, or, where sums of values fill those, in shared memory (each lane's own).
+  static constexpr bool Q_SHARED = D * NT > 128 && NT > 1;
+  static constexpr int Q_BYTES = Q_SHARED ? NT * (D / 32) * 512 : 0;
+  static constexpr int FIT = (232448 - 256 - WARPS * (64 + Q_BYTES)) / (WARPS * KT * TILE);
   static constexpr int STAGES = FIT < 8 ? FIT : 8;
   // a warp's ring of blocks; once it is empty, at a unit's end, the same place holds the warp's piece
-  // (three of a warp at least, where a unit's are fetched)
-  static constexpr int RING = (STAGES * KT * TILE > 3 * PIECE ? STAGES * KT * TILE : 3 * PIECE);
-  static constexpr int SMEM = WARPS * (RING + 64) + 256;
+  // (three of the smallest team at least, where a unit's are fetched)
+  static constexpr int LEAST = Q_SHARED ? 2 : 1;
+  static constexpr int ENOUGH = (3 * PIECE / LEAST + 127) / 128 * 128;
+  static constexpr int RING = STAGES * KT * TILE > ENOUGH ? STAGES * KT * TILE : ENOUGH;
+  static constexpr int SMEM = WARPS * (RING + Q_BYTES + 64) + 256;
   static_assert(STAGES >= 2 && SMEM <= 232448, "ring");
 };
 
@@ -139,7 +143,8 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
   extern __shared__ __align__(128) uint8_t smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   uint8_t* ring = smem + warp * S::RING;
-  uint8_t* rest = smem + S::WARPS * S::RING;
+  uint8_t* q_shared = smem + S::WARPS * S::RING + warp * S::Q_BYTES + lane * 16;
+  uint8_t* rest = smem + S::WARPS * (S::RING + S::Q_BYTES);
   const uint32_t bar = saddr(rest + warp * 64);
   int* s_last = reinterpret_cast<int*>(rest + S::WARPS * 64);  // [WARPS]
   int* s_dead = s_last + S::WARPS;                             // bits by warp
@@ -148,6 +153,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
   fence_async_shared();
   __syncthreads();
   asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
   // All blocks of a head, and the most that a sequence has.  Every warp adds up for itself, four sequences to a lane at a time.
   const int per_seq = A.p.kv_heads * A.row_tiles, n_seqs = A.p.n_seqs;
@@ -176,7 +182,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
   int w, share;
   bool gaps;
   {  // (a lane for each size of a team)
-    w = lane == 0 ? S::WARPS : max(1, 8 >> lane);
+    w = lane == 0 ? S::WARPS : max(S::LEAST, 8 >> lane);
     const float units = (float)(n_seqs * per_seq), all = (float)total, above = 1.f + 1e-6f;
     const float each = __fdividef(1.f, (float)w), teams = (float)(S::WARPS / w * gridDim.x);
     const float even = floorf(__fdividef(all, teams) * above) + 1.f, some = floorf(__fdividef(all, teams - units) * above) + 1.f;
@@ -228,7 +234,6 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
   const int end = gaps ? pos + 1 : min(total, pos + share);
 
   const int tok0 = (g & 1) ? 7 - (g >> 1) : g >> 1;   // row g of a product of keys; row g + 8 is 8 tokens further
-  const uint32_t four = A.four;
   const uint64_t once = l2_evict_first();  // (pages pass through L2 without driving the kernel's own code out of it)
   int stage = 0;
   uint32_t parity = 0;
@@ -324,7 +329,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
       }
     }
 
-    uint32_t qf[NT][KW][4];
+    uint32_t qf[S::Q_SHARED ? 1 : NT][KW][4];
     float qs[NT][NG][2], cn[NT][2], M[NT][2], l[NT][2], zs[NT][NG][2], cs[NT][NG][4], o[NT][NW][2][2][4];
 #pragma unroll
     for (int x = 0; x < NT; ++x) {
@@ -354,10 +359,10 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
           f[e] = both_halves<WD>(u[e]);
           part[32 * j / G] = fmaf(f[e].x, up, fmaf(f[e].y, up, part[32 * j / G]));
         }
-        qf[x][j][0] = halves(f[0].x * up, f[2].x * up);
-        qf[x][j][1] = halves(f[0].y * up16, f[2].y * up16);
-        qf[x][j][2] = halves(f[1].x * up, f[3].x * up);
-        qf[x][j][3] = halves(f[1].y * up16, f[3].y * up16);
+        const uint4 q = make_uint4(halves(f[0].x * up, f[2].x * up), halves(f[0].y * up16, f[2].y * up16), halves(f[1].x * up, f[3].x * up),
+                                   halves(f[1].y * up16, f[3].y * up16));
+        if constexpr (S::Q_SHARED) *reinterpret_cast<uint4*>(q_shared + (x * KW + j) * 512) = q;
+        else { qf[x][j][0] = q.x; qf[x][j][1] = q.y; qf[x][j][2] = q.z; qf[x][j][3] = q.w; }
       }
       const float c = fminf(fmaxf(A.scale_log2 * 4194304.f * __uint_as_float((uint32_t)(ex - 14 + 127) << 23), 1e-37f), 1e38f);  // (a masked score times it stays -inf)
 #pragma unroll
@@ -411,44 +416,60 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
 
         // scores: rows are tokens tok0 and tok0 + 8 of a tile, columns rows of queries
         float x[KT][NT][4];
-#pragma unroll
-        for (int z = 0; z < KT; ++z) {
-          const uint8_t* mine = tile + z * S::TILE;
-          uint32_t ka[KW], kb[KW], ma[NG], mb[NG];
+        {
+          uint32_t ka[KT][KW], kb[KT][KW], ma[KT][NG], mb[KT][NG];
           constexpr int n4 = D == 64 ? 2 : 4;
 #pragma unroll
-          for (int half = 0; half < KW / n4; ++half) {
-            const int off = ((D == 256 ? half ^ (tok0 & 1) : 0) * 4 + t) * n4 * 4;
-            uint32_t a[n4], c[n4];
-            lds_words<n4>(mine + tok0 * (D / 2) + off, a);
-            lds_words<n4>(mine + (tok0 + 8) * (D / 2) + off, c);
+          for (int z = 0; z < KT; ++z) {
+            const uint8_t* mine = tile + z * S::TILE;
 #pragma unroll
-            for (int i = 0; i < n4; ++i) { ka[half * n4 + i] = a[i]; kb[half * n4 + i] = c[i]; }
+            for (int half = 0; half < KW / n4; ++half) {
+              const int off = ((D == 256 ? half ^ (tok0 & 1) : 0) * 4 + t) * n4 * 4;
+              uint32_t a[n4], c[n4];
+              lds_words<n4>(mine + tok0 * (D / 2) + off, a);
+              lds_words<n4>(mine + (tok0 + 8) * (D / 2) + off, c);
+#pragma unroll
+              for (int i = 0; i < n4; ++i) { ka[z][half * n4 + i] = a[i]; kb[z][half * n4 + i] = c[i]; }
+            }
+            lds_words<NG>(mine + 16 * D + tok0 * 4 * NG, ma[z]);
+            lds_words<NG>(mine + 16 * D + (tok0 + 8) * 4 * NG, mb[z]);
           }
-          lds_words<NG>(mine + 16 * D + tok0 * 4 * NG, ma);
-          lds_words<NG>(mine + 16 * D + (tok0 + 8) * 4 * NG, mb);
 #pragma unroll
           for (int k = 0; k < NG; ++k) {
-            float acc[NT][4];
+            float acc[KT][NT][4];
 #pragma unroll
             for (int i = k * G / 32; i < (k + 1) * G / 32; ++i) {
+              uint32_t q[NT][4];
 #pragma unroll
-              for (int s = 0; s < 2; ++s) {
-                const uint32_t a = s ? ka[i] >> 6 : ka[i] * four, c = s ? kb[i] >> 6 : kb[i] * four;
+              for (int y = 0; y < NT; ++y) {
+                if constexpr (S::Q_SHARED) lds_words<4>(q_shared + (y * KW + i) * 512, q[y]);
+                else {
 #pragma unroll
-                for (int y = 0; y < NT; ++y)
-                  mma_f16(acc[y], a & 0x003c003cu, c & 0x003c003cu, a & 0x03c003c0u, c & 0x03c003c0u, qf[y][i][2 * s], qf[y][i][2 * s + 1], i == k * G / 32 && s == 0);
+                  for (int e = 0; e < 4; ++e) q[y][e] = qf[y][i][e];
+                }
               }
+#pragma unroll
+              for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int z = 0; z < KT; ++z) {
+                  const uint32_t a = s ? ka[z][i] >> 6 : ka[z][i] << 2, c = s ? kb[z][i] >> 6 : kb[z][i] << 2;
+#pragma unroll
+                  for (int y = 0; y < NT; ++y)
+                    mma_f16(acc[z][y], a & 0x003c003cu, c & 0x003c003cu, a & 0x03c003c0u, c & 0x03c003c0u, q[y][2 * s], q[y][2 * s + 1], i == k * G / 32 && s == 0);
+                }
             }
-            const float2 sa = both_halves<WD>(ma[k]), sc = both_halves<WD>(mb[k]);
 #pragma unroll
-            for (int y = 0; y < NT; ++y)
+            for (int z = 0; z < KT; ++z) {
+              const float2 sa = both_halves<WD>(ma[z][k]), sc = both_halves<WD>(mb[z][k]);
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float2 m = e < 2 ? sa : sc;
-                const float zero = k ? fmaf(m.y, qs[y][k][e & 1], x[z][y][e]) : m.y * qs[y][k][e & 1];
-                x[z][y][e] = fmaf(m.x, acc[y][e], zero);
-              }
+              for (int y = 0; y < NT; ++y)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const float2 m = e < 2 ? sa : sc;
+                  const float zero = k ? fmaf(m.y, qs[y][k][e & 1], x[z][y][e]) : m.y * qs[y][k][e & 1];
+                  x[z][y][e] = fmaf(m.x, acc[z][y][e], zero);
+                }
+            }
           }
         }
         // scales and zeros of the values of the same tokens
@@ -578,7 +599,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
 #pragma unroll
               for (int s = 0; s < 2; ++s) {
                 const int k = (64 * ws + 32 * half) / G;
-                const uint32_t d = s ? a >> 6 : a * four, f = s ? c >> 6 : c * four;
+                const uint32_t d = s ? a >> 6 : a << 2, f = s ? c >> 6 : c << 2;
 #pragma unroll
                 for (int y = 0; y < NT; ++y)
                   mma_f16(o[y][ws][half][s], d & 0x003c003cu, d & 0x03c003c0u, f & 0x003c003cu, f & 0x03c003c0u, pf[z][y][k][0], pf[z][y][k][1]);
