@@ -2,12 +2,14 @@
 sequence's own pages, output projection, gated residual sum) and the activation-sparse FFN half (speculate, staged step).
 
     python -m paper_2609_03079_b200.decoder          # a small stack, a prompt shared by the batch, a few decode steps
+    python -m paper_2609_03079_b200.decoder 4        # the same with its keys and values in 4 bits
 
 The projections are ordinary matrix products and stay with PyTorch; everything else is a call of the C ABI.  The residual is
 fp32, as the FFN half keeps it, and holds one row per sequence.
 """
 from __future__ import annotations
 
+import sys
 from dataclasses import dataclass
 from typing import List, Optional, Tuple
 
@@ -73,15 +75,23 @@ class DecoderLayer:
     """One layer: its attention weights, its paged cache and its FFN layer (``ls.Layer``)."""
 
     def __init__(self, att: AttentionWeights, ffn: ls.Layer, heads: int, kv_heads: int, head_dim: int, n_pages: int, page_size: int, max_seqs: int,
-                 rope: Optional[torch.Tensor], k_select: int, n_chunks: int = 8, eps: float = 1e-5, window: int = 0):
+                 rope: Optional[torch.Tensor], k_select: int, n_chunks: int = 8, eps: float = 1e-5, window: int = 0, kv_bits: int = 16, kv_group: int = 64):
+        """``kv_bits`` = 4 keeps keys and values in 4 bits, ``kv_group`` components to a scale (``page_size`` a multiple of 16 then)."""
+        if kv_bits not in (4, 16):
+            raise ValueError("kv_bits: 4 or 16")
         dev, dt = att.w_qkv.device, att.w_qkv.dtype
         self.att, self.ffn = att, ffn
         self.heads, self.kv_heads, self.head_dim = heads, kv_heads, head_dim
         self.eps, self.window, self.k, self.n_chunks = eps, window, k_select, n_chunks
+        self.kv_bits = kv_bits
         # zeros, not because the kernels need them (slots nobody sees may hold anything) but so that a dump is readable
-        self.k_pages = torch.zeros(n_pages, page_size, kv_heads, head_dim, dtype=dt, device=dev)
-        self.v_pages = torch.zeros_like(self.k_pages)
-        self.kv = ls.ls_paged_kv_create(self.k_pages, self.v_pages, heads, max_seqs=max_seqs, max_q_len=1, rope=rope)
+        if kv_bits == 4:
+            self.pages = torch.zeros(n_pages, kv_heads, ls.ls_paged_kv4_block_bytes(page_size, head_dim, kv_group), dtype=torch.uint8, device=dev)
+            self.kv = ls.ls_paged_kv4_create(self.pages, heads, head_dim, page_size, dtype=dt, group=kv_group, max_seqs=max_seqs, max_q_len=1, rope=rope)
+        else:
+            self.k_pages = torch.zeros(n_pages, page_size, kv_heads, head_dim, dtype=dt, device=dev)
+            self.v_pages = torch.zeros_like(self.k_pages)
+            self.kv = ls.ls_paged_kv_create(self.k_pages, self.v_pages, heads, max_seqs=max_seqs, max_q_len=1, rope=rope)
         d = ffn.d_model
         self.h = torch.empty(max_seqs, d, dtype=dt, device=dev)
         self.q = torch.empty(max_seqs, heads, head_dim, dtype=dt, device=dev)
@@ -101,14 +111,31 @@ class DecoderLayer:
         """One token for each of n sequences: x [n, d] fp32 is replaced by the layer's output."""
         n = x.shape[0]
         q, k, v = self.qkv(x)
-        ls.ls_paged_kv_append(self.kv, q, k, v, self.q[:n], seq, pos, table)
-        ls.ls_paged_kv_attend(self.kv, self.q[:n], self.o[:n], seq_len, table, prefix_pages, prefix_len, window=self.window)
+        if self.kv_bits == 4:  # (the prefix stands in the table like any other pages)
+            ls.ls_paged_kv4_append(self.kv, q, k, v, self.q[:n], seq, pos, table)
+            ls.ls_paged_kv4_attend(self.kv, self.q[:n], self.o[:n], seq_len, table, window=self.window)
+        else:
+            ls.ls_paged_kv_append(self.kv, q, k, v, self.q[:n], seq, pos, table)
+            ls.ls_paged_kv_attend(self.kv, self.q[:n], self.o[:n], seq_len, table, prefix_pages, prefix_len, window=self.window)
         y = self.o[:n].view(n, -1) @ self.att.w_out
         a = self.att
         ls.ls_block_norm(x, y, x, None, post_norm=a.gain_post is not None, w_post=a.gain_post, gate=a.gate, scale=a.residual_scale, eps=self.eps)
         ls.ls_predict(self.ffn, x, self.k, self.sel)
         ls.ls_sparse_ffn_step(self.ffn, None, x, x, self.sel, self.n_chunks)
         return x
+
+    def cached(self, seq: torch.Tensor, pos: torch.Tensor, table: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Keys (turned) and values, 16-bit [tokens, kv_heads, head_dim], that the cache holds at positions ``pos`` of sequences ``seq`` (int32)."""
+        if self.kv_bits == 4:
+            k, v = (torch.empty(seq.numel(), self.kv_heads, self.head_dim, dtype=self.kv.dtype, device=table.device) for _ in range(2))
+            ls.ls_paged_kv4_read(self.kv, k, v, seq, pos, table)
+            return k, v
+        page = self.k_pages.shape[1]
+        at = table[seq.long(), torch.div(pos, page, rounding_mode="floor").long()].long()
+        return self.k_pages[at, (pos % page).long()], self.v_pages[at, (pos % page).long()]
+
+    def status(self) -> int:
+        return ls.ls_paged_kv4_status(self.kv) if self.kv_bits == 4 else ls.ls_paged_kv_status(self.kv)
 
     def close(self) -> None:
         self.kv.close()
@@ -151,7 +178,15 @@ class Decoder:
         self.pool.release(seq)
         self.prefix_len = n
         self.prefix_pages = torch.tensor(self.prefix_held, dtype=torch.int32, device=self.pool.table.device)
+        self.pool.table[:self.max_seqs, :len(self.prefix_held)] = self.prefix_pages
         self.lens = [n] * self.max_seqs
+
+    def cached(self, seq: int) -> List[Tuple[torch.Tensor, torch.Tensor]]:
+        """Keys and values of every layer for all positions of a sequence (its prefix among them), in 16 bits: to be looked at, moved to
+        another machine or kept."""
+        n = self.lens[seq]
+        pos = torch.arange(n, dtype=torch.int32, device=self.pool.table.device)
+        return [layer.cached(torch.full_like(pos, seq), pos, self.pool.table) for layer in self.layers]
 
     def close(self) -> None:
         for layer in self.layers:
@@ -173,7 +208,7 @@ def make_attention(spec: wl.StackSpec, layer: int, heads: int, kv_heads: int, he
 
 
 def build(spec: wl.StackSpec, n_layers: int, heads: int, kv_heads: int, head_dim: int, max_seqs: int, max_positions: int, page_size: int = 16, device: int = 0,
-          post: bool = False) -> Decoder:
+          post: bool = False, kv_bits: int = 16, kv_group: int = 64) -> Decoder:
     dev = torch.device("cuda", device)
     n_pages = (max_seqs + 1) * -(-max_positions // page_size)
     pool = PagePool(n_pages, page_size, max_seqs, max_positions, dev)
@@ -182,14 +217,14 @@ def build(spec: wl.StackSpec, n_layers: int, heads: int, kv_heads: int, head_dim
     for i, arrays in enumerate(wl.make_stack(spec, n_layers)):
         ffn = ls.ls_layer_create(arrays, device, max_batch=max_seqs)
         layers.append(DecoderLayer(make_attention(spec, i, heads, kv_heads, head_dim, dev, post), ffn, heads, kv_heads, head_dim, n_pages, page_size, max_seqs, rope,
-                                   spec.k))
+                                   spec.k, kv_bits=kv_bits, kv_group=kv_group))
     return Decoder(layers, pool, max_seqs)
 
 
-def main() -> None:
+def main(kv_bits: int = 16) -> None:
     torch.manual_seed(0)
     spec, batch, prompt, steps = wl.SPECS["tiny4"], 4, 40, 8
-    dec = build(spec, spec.n_layers, heads=4, kv_heads=2, head_dim=64, max_seqs=batch, max_positions=256, post=True)
+    dec = build(spec, spec.n_layers, heads=4, kv_heads=2, head_dim=64, max_seqs=batch, max_positions=256, post=True, kv_bits=kv_bits)
     dev = torch.device("cuda", 0)
     tokens = torch.from_numpy(wl.make_tokens(spec, prompt)).to(dev)
     one = Decoder(dec.layers, dec.pool, 1)  # sequence 0 alone, through the same layers and pool
@@ -203,10 +238,12 @@ def main() -> None:
         x = dec.step(x)
         x = x / x.square().mean(1, keepdim=True).sqrt()
         print(f"step {t}: lengths {dec.lens}, residual rms {x.square().mean().sqrt().item():.3f}, first values {[round(v, 4) for v in x[0, :3].tolist()]}")
-    bad = [ls.ls_paged_kv_status(layer.kv) for layer in dec.layers]
+    k, v = dec.cached(0)[0]
+    print(f"layer 0 keeps {k.shape[0]} positions of sequence 0 in {kv_bits} bits; rms of its keys {k.float().square().mean().sqrt().item():.3f}, of its values {v.float().square().mean().sqrt().item():.3f}")
+    bad = [layer.status() for layer in dec.layers]
     assert not any(bad), bad
     dec.close()
 
 
 if __name__ == "__main__":
-    main()
+    main(int(sys.argv[1]) if len(sys.argv) > 1 else 16)
