@@ -37,12 +37,13 @@ struct Attend4Args {
 };
 
 constexpr long long K4_SPIN_CLOCKS = 4000000000LL;  // about two seconds
-// What a unit's beginning and end, and the joining of its pieces, cost a warp, in blocks.
-constexpr float K4_UNIT = 4.f, K4_JOIN = 2.f, K4_ADD = 1.5e-4f;
+// What a unit's beginning and end, and the joining of its pieces, cost a warp, in tiles.
+constexpr float K4_UNIT_TILES = 8.f, K4_JOIN_TILES = 4.f, K4_ADD_TILES = 3e-4f;
 // Blocks that one call may deal out (they are counted in 32 bits); the host cuts larger batches.
 constexpr long long K4_MAX_BLOCKS = 1LL << 30;
 
-// Shapes of the kernel: D components a head, groups of G, NT times 8 rows of queries at once.
+// Shapes of the kernel: D components a head, groups of G, NT times 8 rows of queries at once.  Up to 8 rows are the columns of the
+// products (S^T = K Q^T, O^T = V^T P^T: the codes are the operand with 16 rows), 16 rows are their rows (S = Q K^T, O = P V).
 template <int D, int G, int NT>
 struct K4Shape {
   static constexpr int WARPS = D * NT <= 128 ? 12 : 8;           // (168 registers a thread, or 255)
@@ -54,7 +55,7 @@ struct K4Shape {
   static constexpr int LINE = D + 4;                     // floats of a row's piece
   static constexpr int PIECE = ROWS * LINE * 4;
   // Operands of the queries stay in registers, or, where sums of values fill those, in shared memory (each lane's own).
-  static constexpr bool Q_SHARED = D * NT > 128 && NT > 1;
+  static constexpr bool Q_SHARED = NT > 1;
   static constexpr int Q_BYTES = Q_SHARED ? NT * (D / 32) * 512 : 0;
   static constexpr int FIT = (232448 - 256 - WARPS * (64 + Q_BYTES)) / (WARPS * KT * TILE);
   static constexpr int STAGES = FIT < 8 ? FIT : 8;
@@ -105,6 +106,10 @@ __device__ __forceinline__ float quad_sum(float x) {  // over the four lanes of 
   x += __shfl_xor_sync(0xffffffffu, x, 1);
   return x + __shfl_xor_sync(0xffffffffu, x, 2);
 }
+__device__ __forceinline__ float quad_max(float x) {
+  x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+  return fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+}
 __device__ __forceinline__ float rows_sum(float x) {  // over the eight lanes of a column
   x += __shfl_xor_sync(0xffffffffu, x, 4);
   x += __shfl_xor_sync(0xffffffffu, x, 8);
@@ -140,6 +145,7 @@ template <int WD, int D, int G, int NT>
 __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_kernel(const __grid_constant__ Attend4Args A) {
   using S = K4Shape<D, G, NT>;
   constexpr int NG = S::NG, NW = D / 64, KW = D / 32, ST = S::STAGES, KT = S::KT;
+  constexpr bool WIDE = NT == 2;
   extern __shared__ __align__(128) uint8_t smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   uint8_t* ring = smem + warp * S::RING;
@@ -183,6 +189,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
   bool gaps;
   {  // (a lane for each size of a team)
     w = lane == 0 ? S::WARPS : max(S::LEAST, 8 >> lane);
+    constexpr float K4_UNIT = K4_UNIT_TILES / KT, K4_JOIN = K4_JOIN_TILES / KT, K4_ADD = K4_ADD_TILES / KT;
     const float units = (float)(n_seqs * per_seq), all = (float)total, above = 1.f + 1e-6f;
     const float each = __fdividef(1.f, (float)w), teams = (float)(S::WARPS / w * gridDim.x);
     const float even = floorf(__fdividef(all, teams) * above) + 1.f, some = floorf(__fdividef(all, teams - units) * above) + 1.f;
@@ -329,8 +336,13 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
       }
     }
 
+    // Everything below is kept for the lane's two rows: 2 t and 2 t + 1, or g and g + 8.
     uint32_t qf[S::Q_SHARED ? 1 : NT][KW][4];
-    float qs[NT][NG][2], cn[NT][2], M[NT][2], l[NT][2], zs[NT][NG][2], cs[NT][NG][4], o[NT][NW][2][2][4];
+    float qs[NG][2], cn[2], M[2] = {-1e30f, -1e30f}, l[2] = {0.f, 0.f}, zs[NG][2], cs[NG][4], o[NW][2][2][NT][4];
+#pragma unroll
+    for (int e = 0; e < 4 * NG; ++e) { cs[e / 4][e % 4] = 0.f; zs[e / 4][e % 2] = 0.f; }
+#pragma unroll
+    for (int e = 0; e < 16 * NT * NW; ++e) o[e / (16 * NT)][e / (8 * NT) % 2][e / (4 * NT) % 2][e / 4 % NT][e % 4] = 0.f;
 #pragma unroll
     for (int x = 0; x < NT; ++x) {
       float top = 0.f, part[NG];
@@ -365,24 +377,14 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
         else { qf[x][j][0] = q.x; qf[x][j][1] = q.y; qf[x][j][2] = q.z; qf[x][j][3] = q.w; }
       }
       const float c = fminf(fmaxf(A.scale_log2 * 4194304.f * __uint_as_float((uint32_t)(ex - 14 + 127) << 23), 1e-37f), 1e38f);  // (a masked score times it stays -inf)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        cn[x][e] = __shfl_sync(0xffffffffu, c, 8 * t + 4 * e);
-        M[x][e] = -1e30f;
-        l[x][e] = 0.f;
-      }
+      if (WIDE) cn[x] = c;
+      else { cn[0] = __shfl_sync(0xffffffffu, c, 8 * t); cn[1] = __shfl_sync(0xffffffffu, c, 8 * t + 4); }
 #pragma unroll
       for (int k = 0; k < NG; ++k) {
-        const float p = quad_sum(part[k]) * 2.384185791015625e-7f;  // 2^-22
-#pragma unroll
-        for (int e = 0; e < 2; ++e) { qs[x][k][e] = __shfl_sync(0xffffffffu, p, 8 * t + 4 * e); zs[x][k][e] = 0.f; }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) cs[x][k][e] = 0.f;
+        const float f = quad_sum(part[k]) * 2.384185791015625e-7f;  // 2^-22
+        if (WIDE) qs[k][x] = f;
+        else { qs[k][0] = __shfl_sync(0xffffffffu, f, 8 * t); qs[k][1] = __shfl_sync(0xffffffffu, f, 8 * t + 4); }
       }
-#pragma unroll
-      for (int ws = 0; ws < NW; ++ws)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[x][ws][e / 8][e / 4 % 2][e % 4] = 0.f;
     }
     // Blocks that all rows see all of: from `plain` on, `plains` of them.
     int plain, plains;
@@ -414,10 +416,14 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
         const uint8_t* tile = ring + stage * KT * S::TILE;
         const bool edge = (unsigned)(j - plain) >= (unsigned)plains || patchy;
 
-        // scores: rows are tokens tok0 and tok0 + 8 of a tile, columns rows of queries
-        float x[KT][NT][4];
+        // Scores.  NK keys of a tile are the lane's: tok0 and tok0 + 8, or t, 7 - t, 8 + t, 15 - t; score e is of row_of(e), key_of(e).
+        constexpr int NK = 2 * NT, NX = 2 * NK;
+        auto row_of = [](int e) { return WIDE ? e / 2 % 2 : e % 2; };
+        auto key_of = [](int e) { return WIDE ? e / 4 * 2 + e % 2 : e / 2; };
+        auto token_of = [&](int k) { return WIDE ? (k & 2) * 4 + (k & 1 ? 7 - t : t) : tok0 + 8 * k; };
+        float x[KT][NX];
         {
-          uint32_t ka[KT][KW], kb[KT][KW], ma[KT][NG], mb[KT][NG];
+          uint32_t ka[KT][KW], kb[KT][KW], meta[KT][NK][NG];
           constexpr int n4 = D == 64 ? 2 : 4;
 #pragma unroll
           for (int z = 0; z < KT; ++z) {
@@ -431,8 +437,8 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
 #pragma unroll
               for (int i = 0; i < n4; ++i) { ka[z][half * n4 + i] = a[i]; kb[z][half * n4 + i] = c[i]; }
             }
-            lds_words<NG>(mine + 16 * D + tok0 * 4 * NG, ma[z]);
-            lds_words<NG>(mine + 16 * D + (tok0 + 8) * 4 * NG, mb[z]);
+#pragma unroll
+            for (int k = 0; k < NK; ++k) lds_words<NG>(mine + 16 * D + token_of(k) * 4 * NG, meta[z][k]);
           }
 #pragma unroll
           for (int k = 0; k < NG; ++k) {
@@ -453,135 +459,151 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
 #pragma unroll
                 for (int z = 0; z < KT; ++z) {
                   const uint32_t a = s ? ka[z][i] >> 6 : ka[z][i] << 2, c = s ? kb[z][i] >> 6 : kb[z][i] << 2;
-#pragma unroll
-                  for (int y = 0; y < NT; ++y)
-                    mma_f16(acc[z][y], a & 0x003c003cu, c & 0x003c003cu, a & 0x03c003c0u, c & 0x03c003c0u, q[y][2 * s], q[y][2 * s + 1], i == k * G / 32 && s == 0);
+                  const uint32_t a0 = a & 0x003c003cu, a1 = a & 0x03c003c0u, c0 = c & 0x003c003cu, c1 = c & 0x03c003c0u;
+                  const bool first = i == k * G / 32 && s == 0;
+                  if constexpr (WIDE) {
+                    mma_f16(acc[z][0], q[0][2 * s], q[1][2 * s], q[0][2 * s + 1], q[1][2 * s + 1], a0, a1, first);
+                    mma_f16(acc[z][1], q[0][2 * s], q[1][2 * s], q[0][2 * s + 1], q[1][2 * s + 1], c0, c1, first);
+                  } else mma_f16(acc[z][0], a0, c0, a1, c1, q[0][2 * s], q[0][2 * s + 1], first);
                 }
             }
 #pragma unroll
             for (int z = 0; z < KT; ++z) {
-              const float2 sa = both_halves<WD>(ma[z][k]), sc = both_halves<WD>(mb[z][k]);
+              float2 m[NK];
 #pragma unroll
-              for (int y = 0; y < NT; ++y)
+              for (int i = 0; i < NK; ++i) m[i] = both_halves<WD>(meta[z][i][k]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  const float2 m = e < 2 ? sa : sc;
-                  const float zero = k ? fmaf(m.y, qs[y][k][e & 1], x[z][y][e]) : m.y * qs[y][k][e & 1];
-                  x[z][y][e] = fmaf(m.x, acc[z][y][e], zero);
-                }
+              for (int e = 0; e < NX; ++e) {
+                const float2 sz = m[key_of(e)];
+                const float zero = k ? fmaf(sz.y, qs[k][row_of(e)], x[z][e]) : sz.y * qs[k][row_of(e)];
+                x[z][e] = fmaf(sz.x, acc[z][e / 4][e % 4], zero);
+              }
             }
           }
         }
         // scales and zeros of the values of the same tokens
-        float2 va[KT][NG], vb[KT][NG];
+        float2 va[KT][NK][NG];
 #pragma unroll
-        for (int z = 0; z < KT; ++z) {
-          uint32_t ma[NG], mb[NG];
-          lds_words<NG>(tile + z * S::TILE + 16 * D + 64 * NG + tok0 * 4 * NG, ma);
-          lds_words<NG>(tile + z * S::TILE + 16 * D + 64 * NG + (tok0 + 8) * 4 * NG, mb);
+        for (int z = 0; z < KT; ++z)
 #pragma unroll
-          for (int k = 0; k < NG; ++k) { va[z][k] = both_halves<WD>(ma[k]); vb[z][k] = both_halves<WD>(mb[k]); }
-        }
+          for (int i = 0; i < NK; ++i) {
+            uint32_t meta[NG];
+            lds_words<NG>(tile + z * S::TILE + 16 * D + 64 * NG + token_of(i) * 4 * NG, meta);
+#pragma unroll
+            for (int k = 0; k < NG; ++k) va[z][i][k] = both_halves<WD>(meta[k]);
+          }
         if (edge) {
           const uint32_t gone = skip >> (stage * KT);
           const int pos0 = (block0 + j * w) * 16 * KT;
           // Tokens that nobody sees may hold anything, and one that some rows see may hold NaN: neither must meet a weight of zero.
+          int hi[2], lo[2];
 #pragma unroll
-          for (int z = 0; z < KT; ++z) {
-            const int p0 = pos0 + 16 * z + tok0, p1 = p0 + 8;
-            const bool there = !(gone >> z & 1);
-            bool any0 = false, any1 = false;
-            const float nan = __int_as_float(0x7fffffff);
-#pragma unroll
-            for (int y = 0; y < NT; ++y)
-#pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const int r = 8 * y + 2 * t + e, hi = there && r < rows ? len - A.q_len + A.by_group(row0 + r) : -1, lo = max(hi, -1) - A.window;
-                const bool on0 = p0 <= hi && p0 > lo, on1 = p1 <= hi && p1 > lo;
-                if (!on0) x[z][y][e] = -INFINITY;
-                if (!on1) x[z][y][e + 2] = -INFINITY;
-                any0 |= on0; any1 |= on1;
-#pragma unroll
-                for (int k = 0; k < NG; ++k)
-                  if ((on0 && !(fabsf(va[z][k].x) + fabsf(va[z][k].y) < INFINITY)) || (on1 && !(fabsf(vb[z][k].x) + fabsf(vb[z][k].y) < INFINITY))) zs[y][k][e] = nan;
-              }
-            any0 |= __shfl_xor_sync(0xffffffffu, any0, 1); any1 |= __shfl_xor_sync(0xffffffffu, any1, 1);
-            any0 |= __shfl_xor_sync(0xffffffffu, any0, 2); any1 |= __shfl_xor_sync(0xffffffffu, any1, 2);
-#pragma unroll
-            for (int k = 0; k < NG; ++k) {
-              if (!any0 || !(fabsf(va[z][k].x) + fabsf(va[z][k].y) < INFINITY)) va[z][k] = make_float2(0.f, 0.f);
-              if (!any1 || !(fabsf(vb[z][k].x) + fabsf(vb[z][k].y) < INFINITY)) vb[z][k] = make_float2(0.f, 0.f);
-            }
+          for (int e = 0; e < 2; ++e) {
+            const int r = WIDE ? 8 * e + g : 2 * t + e;
+            hi[e] = r < rows ? len - A.q_len + A.by_group(row0 + r) : -1;
+            lo[e] = max(hi[e], -1) - A.window;
           }
+#pragma unroll
+          for (int z = 0; z < KT; ++z)
+#pragma unroll
+            for (int i = 0; i < NK; ++i) {
+              const int at = pos0 + 16 * z + token_of(i);
+              bool on[2], fine[NG];
+#pragma unroll
+              for (int e = 0; e < 2; ++e) on[e] = !(gone >> z & 1) && at <= hi[e] && at > lo[e];
+#pragma unroll
+              for (int e = 0; e < NX; ++e)
+                if (key_of(e) == i && !on[row_of(e)]) x[z][e] = -INFINITY;
+              // (the lanes that share the key: those of the same t, or of the same g)
+              const bool any = __ballot_sync(0xffffffffu, on[0] || on[1]) & (WIDE ? 0x11111111u << t : 15u << (lane & 28));
+#pragma unroll
+              for (int k = 0; k < NG; ++k) {
+                fine[k] = fabsf(va[z][i][k].x) + fabsf(va[z][i][k].y) < INFINITY;
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                  if (on[e] && !fine[k]) zs[k][e] = __int_as_float(0x7fffffff);
+                if (!any || !fine[k]) va[z][i][k] = make_float2(0.f, 0.f);
+              }
+            }
         }
         // Weights relative to M, which moves only when the weights times their scales leave what fp16 holds.  (Their sum tells: none of them
         // is negative, and one that is NaN may hide nothing; 2^-60 keeps weights of scales of zero in range.)
-        float p[KT][NT][4], most[2] = {0.f, 0.f};
+        float p[KT][NX], most[2] = {0.f, 0.f};
 #pragma unroll
         for (int z = 0; z < KT; ++z) {
-          float all[2] = {8.67361737988403547e-19f, 8.67361737988403547e-19f};
+          float all[NK];
 #pragma unroll
-          for (int k = 0; k < NG; ++k) { all[0] += va[z][k].x; all[1] += vb[z][k].x; }
+          for (int i = 0; i < NK; ++i) {
+            all[i] = 8.67361737988403547e-19f;
 #pragma unroll
-          for (int y = 0; y < NT; ++y)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              p[z][y][e] = ex2(fmaf(x[z][y][e], cn[y][e & 1], -M[y][e & 1]));
-              most[e / 2] = fmaf(p[z][y][e], all[e / 2], most[e / 2]);
-            }
-        }
-        if (__any_sync(0xffffffffu, !(most[0] + most[1] <= 16384.f))) {
-          float big[KT][2];
-#pragma unroll
-          for (int z = 0; z < KT; ++z) {
-            big[z][0] = big[z][1] = 8.67361737988403547e-19f;
-#pragma unroll
-            for (int k = 0; k < NG; ++k) { big[z][0] = fmaxf(big[z][0], va[z][k].x); big[z][1] = fmaxf(big[z][1], vb[z][k].x); }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) big[z][e] = __log2f(big[z][e]) - 4.f;
+            for (int k = 0; k < NG; ++k) all[i] += va[z][i][k].x;
           }
 #pragma unroll
-          for (int y = 0; y < NT; ++y)
+          for (int e = 0; e < NX; ++e) {
+            p[z][e] = ex2(fmaf(x[z][e], cn[row_of(e)], -M[row_of(e)]));
+            most[e % 2] = fmaf(p[z][e], all[key_of(e)], most[e % 2]);
+          }
+        }
+        if (__any_sync(0xffffffffu, !(most[0] + most[1] <= 16384.f))) {
+          float m[2] = {-INFINITY, -INFINITY}, f[2];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              float m = -INFINITY;
+          for (int z = 0; z < KT; ++z) {
+            float big[NK];
 #pragma unroll
-              for (int z = 0; z < KT; ++z) m = max3(m, fmaf(x[z][y][e], cn[y][e], big[z][0]), fmaf(x[z][y][e + 2], cn[y][e], big[z][1]));
-              const float to = fmaxf(M[y][e], rows_max(m)), f = ex2(M[y][e] - to);
-              M[y][e] = to;
-              l[y][e] *= f;
+            for (int i = 0; i < NK; ++i) {
+              big[i] = 8.67361737988403547e-19f;
 #pragma unroll
-              for (int k = 0; k < NG; ++k) { zs[y][k][e] *= f; cs[y][k][e] *= f; }
-#pragma unroll
-              for (int i = 0; i < 4 * NW; ++i) { o[y][i / 4][i / 2 % 2][i % 2][e] *= f; o[y][i / 4][i / 2 % 2][i % 2][e + 2] *= f; }
-#pragma unroll
-              for (int z = 0; z < KT; ++z) {
-                p[z][y][e] = ex2(fmaf(x[z][y][e], cn[y][e], -to));
-                p[z][y][e + 2] = ex2(fmaf(x[z][y][e + 2], cn[y][e], -to));
-              }
+              for (int k = 0; k < NG; ++k) big[i] = fmaxf(big[i], va[z][i][k].x);
+              big[i] = __log2f(big[i]) - 4.f;
             }
+#pragma unroll
+            for (int e = 0; e < NX; ++e) m[row_of(e)] = fmaxf(m[row_of(e)], fmaf(x[z][e], cn[row_of(e)], big[key_of(e)]));
+          }
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float to = fmaxf(M[e], WIDE ? quad_max(m[e]) : rows_max(m[e]));
+            f[e] = ex2(M[e] - to);
+            M[e] = to;
+            l[e] *= f[e];
+#pragma unroll
+            for (int k = 0; k < NG; ++k) zs[k][e] *= f[e];
+          }
+#pragma unroll
+          for (int k = 0; k < NG; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) cs[k][e] *= f[WIDE ? e / 2 : e % 2];
+#pragma unroll
+          for (int e = 0; e < 16 * NT * NW; ++e) o[e / (16 * NT)][e / (8 * NT) % 2][e / (4 * NT) % 2][e / 4 % NT][e % 4] *= f[WIDE ? e / 2 % 2 : e % 2];
+#pragma unroll
+          for (int z = 0; z < KT; ++z)
+#pragma unroll
+            for (int e = 0; e < NX; ++e) p[z][e] = ex2(fmaf(x[z][e], cn[row_of(e)], -M[row_of(e)]));
         }
         // Weights times scales, rounded to fp16 for the product with the codes.  The codes count from the middle of their range, 8: the
         // rounding then weighs s |u - 8|, about a value's own size.  8 sum(p s) is taken off with the rounded weights (a product with
         // ones), and added back, unrounded, with the zeros.
-        uint32_t pf[KT][NT][NG][2];
+        uint32_t pf[KT][NG][NK];
 #pragma unroll
-        for (int z = 0; z < KT; ++z)
+        for (int z = 0; z < KT; ++z) {
 #pragma unroll
-          for (int y = 0; y < NT; ++y) {
+          for (int e = 0; e < NX; ++e) l[row_of(e)] += p[z][e];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) l[y][e] += p[z][y][e] + p[z][y][e + 2];
+          for (int k = 0; k < NG; ++k) {
 #pragma unroll
-            for (int k = 0; k < NG; ++k) {
-              const float z0 = fmaf(va[z][k].x, 8.f, va[z][k].y), z1 = fmaf(vb[z][k].x, 8.f, vb[z][k].y);
-#pragma unroll
-              for (int e = 0; e < 2; ++e) zs[y][k][e] = fmaf(p[z][y][e], z0, fmaf(p[z][y][e + 2], z1, zs[y][k][e]));
-              pf[z][y][k][0] = transpose8(halves(p[z][y][0] * va[z][k].x, p[z][y][1] * va[z][k].x));
-              pf[z][y][k][1] = transpose8(halves(p[z][y][2] * vb[z][k].x, p[z][y][3] * vb[z][k].x));
-              mma_f16(cs[y][k], 0x3c003c00u, 0u, 0x3c003c00u, 0u, pf[z][y][k][0], pf[z][y][k][1]);
+            for (int e = 0; e < NX; ++e) {
+              const float2 sz = va[z][key_of(e)][k];
+              zs[k][row_of(e)] = fmaf(p[z][e], fmaf(sz.x, 8.f, sz.y), zs[k][row_of(e)]);
             }
+#pragma unroll
+            for (int e = 0; e < NX; e += 2) {
+              const uint32_t two = halves(p[z][e] * va[z][key_of(e)][k].x, p[z][e + 1] * va[z][key_of(e + 1)][k].x);
+              pf[z][k][e / 2] = WIDE ? two : transpose8(two);
+            }
+            if constexpr (WIDE) mma_f16(cs[k], pf[z][k][0], pf[z][k][1], pf[z][k][2], pf[z][k][3], 0x3c003c00u, 0x3c003c00u);
+            else mma_f16(cs[k], 0x3c003c00u, 0u, 0x3c003c00u, 0u, pf[z][k][0], pf[z][k][1]);
           }
-        // values: rows are components, summed over the tokens t, 7 - t, 8 + t, 15 - t of the lane
+        }
+        // Values, summed over the tokens t, 7 - t, 8 + t, 15 - t of the lane.  Its words hold components of g.
 #pragma unroll
         for (int z = 0; z < KT; ++z) {
           const uint8_t* base = tile + z * S::TILE + 16 * (D / 2);
@@ -600,9 +622,11 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
               for (int s = 0; s < 2; ++s) {
                 const int k = (64 * ws + 32 * half) / G;
                 const uint32_t d = s ? a >> 6 : a << 2, f = s ? c >> 6 : c << 2;
-#pragma unroll
-                for (int y = 0; y < NT; ++y)
-                  mma_f16(o[y][ws][half][s], d & 0x003c003cu, d & 0x03c003c0u, f & 0x003c003cu, f & 0x03c003c0u, pf[z][y][k][0], pf[z][y][k][1]);
+                const uint32_t d0 = d & 0x003c003cu, d1 = d & 0x03c003c0u, f0 = f & 0x003c003cu, f1 = f & 0x03c003c0u;
+                if constexpr (WIDE) {
+                  mma_f16(o[ws][half][s][0], pf[z][k][0], pf[z][k][1], pf[z][k][2], pf[z][k][3], d0, f0);
+                  mma_f16(o[ws][half][s][1], pf[z][k][0], pf[z][k][1], pf[z][k][2], pf[z][k][3], d1, f1);
+                } else mma_f16(o[ws][half][s][0], d0, d1, f0, f1, pf[z][k][0], pf[z][k][1]);
               }
             }
         }
@@ -624,25 +648,24 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
     {
       float* piece = reinterpret_cast<float*>(ring);
 #pragma unroll
-      for (int y = 0; y < NT; ++y)
+      for (int e = 0; e < 2; ++e) {
+        const float sum_l = WIDE ? quad_sum(l[e]) : rows_sum(l[e]);
+        float zero[NG];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float sum_l = rows_sum(l[y][e]);
-          float z[NG];
+        for (int k = 0; k < NG; ++k) zero[k] = fmaf(-8.f, cs[k][WIDE ? 2 * e : e], WIDE ? quad_sum(zs[k][e]) : rows_sum(zs[k][e]));
+        float* line = piece + (WIDE ? 8 * e + g : 2 * t + e) * S::LINE;
+        // four components side by side: of g, or, twice, of 2 t and 2 t + 1
 #pragma unroll
-          for (int k = 0; k < NG; ++k) z[k] = fmaf(-8.f, cs[y][k][e], rows_sum(zs[y][k][e]));
-          float* line = piece + (8 * y + 2 * t + e) * S::LINE;
-#pragma unroll
-          for (int ws = 0; ws < NW; ++ws)
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              const float zz = z[(64 * ws + 32 * half) / G];
-              const auto& a = o[y][ws][half];
-              *reinterpret_cast<float4*>(line + 64 * ws + 32 * half + 4 * g) =
-                  make_float4(fmaf(a[0][e], 4194304.f, zz), fmaf(a[0][e + 2], 262144.f, zz), fmaf(a[1][e], 4194304.f, zz), fmaf(a[1][e + 2], 262144.f, zz));
-            }
-          if (g == 0) *reinterpret_cast<float2*>(line + D) = make_float2(M[y][e], sum_l);
+        for (int i = 0; i < 2 * NW * NT; ++i) {
+          const int at = i / NT, c = WIDE ? 2 * e + i % 2 : e;
+          const float zz = zero[32 * at / G];
+          const auto& a = o[at / 2][at % 2];
+          const float first = a[0][0][c], second = WIDE ? a[0][NT - 1][c] : a[0][0][c + 2], third = a[1][0][c], last = WIDE ? a[1][NT - 1][c] : a[1][0][c + 2];
+          *reinterpret_cast<float4*>(line + 32 * at + 4 * (WIDE ? 2 * t + i % 2 : g)) =
+              make_float4(fmaf(first, 4194304.f, zz), fmaf(second, 262144.f, zz), fmaf(third, 4194304.f, zz), fmaf(last, 262144.f, zz));
         }
+        if (WIDE ? t == 0 : g == 0) *reinterpret_cast<float2*>(line + D) = make_float2(M[e], sum_l);
+      }
     }
     team_sync();
     // The team's pieces are added up, to the output or to the workspace; there, the team that comes last fetches the unit's pieces, as many as
