@@ -230,7 +230,8 @@ int32_t ls_paged_kv4_attend(ls_paged_kv4* kv, const void* d_q, int64_t q_stride,
   if ((size_t)n_seqs * per_seq > kv->units || (size_t)kv->sm_count * (s.threads / 32) * 2 * s.piece > kv->part_floats)
     return fail(LS_ERR_INTERNAL, "ls_paged_kv4_attend: workspace");
   // A launch counts its tiles in 32 bits: of as many sequences as cannot have too many (all of them but for huge tables).
-  const long long most = per_seq * std::max(1LL, std::min((long long)table_width * D.page_size, (long long)ls::MAX_POSITIONS) / 16);
+  // (64: more than what a unit's beginning counts for)
+  const long long most = per_seq * (64 + std::min((long long)table_width * D.page_size, (long long)ls::MAX_POSITIONS) / 16);
   if (most > ls::K4_MAX_BLOCKS) return fail(LS_ERR_INVALID, "ls_paged_kv4_attend: q_len * table_width is too large");
   const int32_t step = (int32_t)std::min<long long>(n_seqs, ls::K4_MAX_BLOCKS / most);
   const cudaStream_t st = (cudaStream_t)stream;

@@ -128,13 +128,12 @@ __device__ __forceinline__ void k4_add(float& m, float& l, float4& v, float m1, 
   v = make_float4(fmaf(g, v1.x, v.x * f), fmaf(g, v1.y, v.y * f), fmaf(g, v1.z, v.z * f), fmaf(g, v1.w, v.w * f));
 }
 
-// What has to be read of a sequence of n positions: its first block (16 KT keys) and its number of blocks (an empty sequence has one, which
-// shows nothing).
+// What has to be read of a sequence of n positions: its first block (16 KT keys) and its number of blocks.
 __device__ __forceinline__ int k4_len(const Attend4Args& A, int n) { return min(max(n, 0), A.most); }
 template <int KT>
 __device__ __forceinline__ int k4_first(const Attend4Args& A, int n) { return max(0, n - A.behind) / (16 * KT); }
 template <int KT>
-__device__ __forceinline__ int k4_blocks(const Attend4Args& A, int n) { return max(1, (n + 16 * KT - 1) / (16 * KT) - k4_first<KT>(A, n)); }
+__device__ __forceinline__ int k4_blocks(const Attend4Args& A, int n) { return (n + 16 * KT - 1) / (16 * KT) - k4_first<KT>(A, n); }
 
 // A unit is one sequence's blocks (16 KT keys each) for one key head and one row tile of its queries.  All units' blocks stand in one line,
 // cut into equal shares; a share belongs to a team (a whole CTA, or 4, 2 or 1 of its warps), which deal out its blocks among themselves.  A warp copies its
@@ -163,7 +162,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
 
   // All blocks of a head, and the most that a sequence has.  Every warp adds up for itself, four sequences to a lane at a time.
   const int per_seq = A.p.kv_heads * A.row_tiles, n_seqs = A.p.n_seqs;
-  int total = 0, longest = 1;
+  int total = 0, longest = 1, busy = 0;
   bool bad = false;
 #pragma unroll 1
   for (int b0 = lane; b0 < n_seqs; b0 += 128) {
@@ -173,7 +172,8 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int len = k4_len(A, n[i]), blocks = b0 + 32 * i < n_seqs ? k4_blocks<KT>(A, len) : 0;
-      bad |= blocks && len != n[i];
+      bad |= b0 + 32 * i < n_seqs && len != n[i];
+      busy += blocks > 0;
       total += blocks;
       longest = max(longest, blocks);
     }
@@ -181,23 +181,43 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
   if (bad && blockIdx.x == 0 && warp == 0) set_status(A.p.status, ST_BAD_INDEX);
   total = __reduce_add_sync(0xffffffffu, total) * per_seq;
   longest = __reduce_max_sync(0xffffffffu, longest);
+  busy = __reduce_add_sync(0xffffffffu, busy);
+  // sequences without a key
+  if (busy < n_seqs) {
+#pragma unroll 1
+    for (int b = blockIdx.x; b < n_seqs; b += gridDim.x) {
+      if (k4_len(A, A.seq_len[b])) continue;
+#pragma unroll 1
+      for (long long tk = (long long)b * A.q_len; tk < (long long)(b + 1) * A.q_len; ++tk) {
+#pragma unroll 1
+        for (int x = threadIdx.x; x < A.heads * (D / 4); x += S::THREADS) {
+          uint16_t* dst = A.out + tk * A.out_stride + 4 * x;
+          if (A.out_vec) *reinterpret_cast<uint2*>(dst) = make_uint2(0, 0);
+          else dst[0] = dst[1] = dst[2] = dst[3] = 0;
+        }
+#pragma unroll 1
+        for (int x = threadIdx.x; A.lse && x < A.heads; x += S::THREADS) A.lse[tk * A.heads + x] = -INFINITY;
+      }
+    }
+  }
 
   // Shares: whatever ends first, by blocks that a warp has one after another.  Either units follow each other without a gap, so that every
-  // team has as much but begins and ends inside a unit; or each unit begins with a new share, one for all of it, or several.  (Shares
-  // may be a little larger than they need to be: fp32 will do.)
-  int w, share;
+  // team has as much but begins and ends inside a unit; what a unit's beginning and end cost a team (K4_UNIT blocks of each warp) stands
+  // in the line in front of it.  Or each unit begins with a new share, one for all of it, or several.  (Shares may be a little larger than
+  // they need to be: fp32 will do.)
+  int w, share, extra;
   bool gaps;
   {  // (a lane for each size of a team)
     w = lane == 0 ? S::WARPS : max(S::LEAST, 8 >> lane);
     constexpr float K4_UNIT = K4_UNIT_TILES / KT, K4_JOIN = K4_JOIN_TILES / KT, K4_ADD = K4_ADD_TILES / KT;
-    const float units = (float)(n_seqs * per_seq), all = (float)total, above = 1.f + 1e-6f;
+    const float units = (float)(busy * per_seq), all = (float)total, above = 1.f + 1e-6f;
     const float each = __fdividef(1.f, (float)w), teams = (float)(S::WARPS / w * gridDim.x);
-    const float even = floorf(__fdividef(all, teams) * above) + 1.f, some = floorf(__fdividef(all, teams - units) * above) + 1.f;
+    const float ahead = ceilf(K4_UNIT * (float)w), even = floorf(__fdividef(all + units * ahead, teams) * above) + 1.f, some = floorf(__fdividef(all, teams - units) * above) + 1.f;
     auto join = [&](float of) {  // for every time that the team's place is filled, and for every piece that its threads add up
       const float n = __fdividef((float)longest, of) + 1.f;
       return K4_JOIN + n * each * ((float)S::PIECE / S::RING + K4_ADD * (float)(S::ROWS * D));
     };
-    const float cost_even = even * each + K4_UNIT * (1.f + fmaxf(1.f, __fdividef(even * units, all))) + join(even);
+    const float cost_even = even * each + K4_UNIT + join(even);
     const float cost_some = units < teams ? some * each + K4_UNIT + join(some) : 1e30f, cost_one = units <= teams ? longest * each + K4_UNIT : 1e30f;
     const float cost = fminf(cost_even, fminf(cost_some, cost_one));
     gaps = cost != cost_even;
@@ -206,6 +226,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
     w = __shfl_sync(0xffffffffu, w, best);
     share = __shfl_sync(0xffffffffu, share, best);
     gaps = __shfl_sync(0xffffffffu, gaps, best);
+    extra = gaps ? 0 : (int)__shfl_sync(0xffffffffu, ahead, best);
   }
   const int mates = warp / w, wi = warp - mates * w, team = mates * gridDim.x + blockIdx.x;
   int pos = team * share;
@@ -213,9 +234,9 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
     if (w == 1) __syncwarp();
     else group_sync(1 + mates, 32 * w);
   };
-  // A unit's length in the line (where there are gaps, at least its blocks; a share too many is one that has nothing).
+  // A unit's length in the line (where there are gaps, at least its blocks; a share too many is one that has nothing).  Nothing of nothing.
   const float per_share = __fdividef(1.f + 1e-6f, (float)share);
-  auto length = [&](int blocks) { return gaps ? ((int)((float)(blocks - 1) * per_share) + 1) * share : blocks; };
+  auto length = [&](int blocks) { return blocks == 0 ? 0 : gaps ? ((int)((float)(blocks - 1) * per_share) + 1) * share : blocks + extra; };
 
   // The sequence in which the share begins, and where its units begin in the line.
   int b = 0, first = 0;
@@ -238,7 +259,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
     }
     first += __shfl_sync(0xffffffffu, sum, 31);
   }
-  const int end = gaps ? pos + 1 : min(total, pos + share);
+  const int end = pos + share;  // (or where the line ends)
 
   const int tok0 = (g & 1) ? 7 - (g >> 1) : g >> 1;   // row g of a product of keys; row g + 8 is 8 tokens further
   const uint64_t once = l2_evict_first();  // (pages pass through L2 without driving the kernel's own code out of it)
@@ -250,15 +271,18 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
     int len = k4_len(A, A.seq_len[b]), blocks = k4_blocks<KT>(A, len);
     while (pos >= first + length(blocks) * per_seq) {
       first += length(blocks) * per_seq;
-      len = k4_len(A, A.seq_len[++b]);
+      if (++b >= n_seqs) return;
+      len = k4_len(A, A.seq_len[b]);
       blocks = k4_blocks<KT>(A, len);
     }
-    const int line = length(blocks), unit = (unsigned)(pos - first) / (unsigned)line, u0 = first + unit * line;
-    const int seg = min(u0 + blocks, gaps ? pos + share : end) - pos;
-    if (seg <= 0) return;
+    // blocks from ... upto of a unit that begins in u0 of the line, with `extra` in front of its blocks
+    const int line = length(blocks), unit = (unsigned)(pos - first) / (unsigned)line, u0 = first + unit * line, from_block = max(pos - u0 - extra, 0);
+    const int seg = min(end - u0 - extra, blocks) - from_block;
+    pos = min(u0 + line, end);
+    if (seg <= 0) continue;
     const int h = A.by_row_tiles(unit), row0 = (unit - h * A.row_tiles) * S::ROWS, rows = min(S::ROWS, A.q_len * A.group - row0);
     const int n = dead ? 0 : (unsigned)(seg + w - 1 - wi) / (unsigned)w;
-    const int block0 = k4_first<KT>(A, len) + pos - u0 + wi;
+    const int block0 = k4_first<KT>(A, len) + from_block + wi;
 
     // queries: the lane's columns of the operand are components 8 (4 j + t) ... of row g
     uint4 raw[NT][KW];
@@ -670,7 +694,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
     team_sync();
     // The team's pieces are added up, to the output or to the workspace; there, the team that comes last fetches the unit's pieces, as many as
     // its place holds at a time, and adds them up by the same code (which the SM has at hand by now; code of its own is cold).
-    const int i0 = u0 / share, i1 = (u0 + blocks - 1) / share;  // the unit's teams
+    const int i0 = (u0 + extra) / share, i1 = (u0 + extra + blocks - 1) / share;  // the unit's teams
     const int items = rows * (D / 4), threads = 32 * w, me = wi * 32 + lane, room = w * S::RING / S::PIECE;
     float* place = reinterpret_cast<float*>(smem + (warp - wi) * S::RING);
     const float* from = place;                                                                // what is added up: `count` pieces,
@@ -751,7 +775,6 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
     }
     team_sync();
     fence_async_shared();  // (the next copies land where the piece was)
-    pos += seg;
   }
 }
 
