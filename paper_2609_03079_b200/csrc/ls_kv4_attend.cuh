@@ -234,9 +234,14 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
     if (w == 1) __syncwarp();
     else group_sync(1 + mates, 32 * w);
   };
-  // A unit's length in the line (where there are gaps, at least its blocks; a share too many is one that has nothing).  Nothing of nothing.
+  // A unit's length in the line: nothing of nothing; where there are gaps, its blocks rounded up to whole shares (by a reciprocal that is never
+  // too small and too large by less than one share, which is put right).
   const float per_share = __fdividef(1.f + 1e-6f, (float)share);
-  auto length = [&](int blocks) { return blocks == 0 ? 0 : gaps ? ((int)((float)(blocks - 1) * per_share) + 1) * share : blocks + extra; };
+  auto length = [&](int blocks) {
+    if (!gaps) return blocks == 0 ? 0 : blocks + extra;
+    const int full = (int)((float)(blocks - 1) * per_share);
+    return blocks == 0 ? 0 : (full * share <= blocks - 1 ? full + 1 : full) * share;
+  };
 
   // The sequence in which the share begins, and where its units begin in the line.
   int b = 0, first = 0;

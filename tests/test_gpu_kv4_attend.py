@@ -308,3 +308,90 @@ def test_calls_back_to_back():
         assert ls.ls_paged_kv4_status(final) == 0
         b.check()
     final.close()
+
+
+@pytest.mark.parametrize("q_len", [1, 4])
+def test_idle_slots(q_len):
+    """Most slots of a batch idle, a few long: the idle ones take no part, wherever they stand; rows that lie off 16 bytes too."""
+    lens = [0] * 120
+    for i, n in ((0, 700), (1, 1), (63, 1500), (64, 2), (118, 33)):
+        lens[i] = n
+    run_case(lens=lens, q_len=q_len, seed=q_len)
+    run_case(lens=lens[1:], q_len=q_len, D=64, dtype="fp16", q_view="misaligned", window=50)
+    run_case(lens=[3] * 150 + [5000], q_len=q_len, heads=4, hk=1)
+
+
+def test_a_table_without_columns_and_no_lse():
+    b = Batch(lens=[20, 5])
+    kv = b.handle()
+    b.attend(kv)
+    out = torch.full_like(b.out, float("nan"))
+    ls.ls_paged_kv4_attend(kv, b.q, out, b.seq_len, b.table, lse=None)
+    assert ls.ls_paged_kv4_status(kv) == 0 and torch.equal(out, b.out)
+    ls.ls_paged_kv4_attend(kv, b.q, out, b.seq_len, b.table[:, :0].contiguous(), lse=b.lse)
+    assert ls.ls_paged_kv4_status(kv) == -1  # (lengths beyond a table of nothing)
+    assert (out == 0).all() and torch.isneginf(b.lse).all()
+    ls.ls_paged_kv4_attend(kv, b.q, out, torch.zeros_like(b.seq_len), b.table[:, :0].contiguous())
+    assert ls.ls_paged_kv4_status(kv) == 0
+    kv.close()
+
+
+def test_tables_of_all_positions():
+    """Tables of 2^31 positions: a launch's line of blocks cannot hold all sequences, or, refused, not even one."""
+    b = Batch(lens=[2050, 0, 37, 1024, 1], heads=8, hk=4, page=1024)
+    kv = b.handle()
+    wide = torch.full((5, 2 ** 21), 2 ** 30, dtype=torch.int32, device=DEV)
+    wide[:, : b.table.shape[1]] = b.table
+    b.table = wide
+    b.attend(kv)
+    assert ls.ls_paged_kv4_status(kv) == 0
+    b.check()
+    kv.close()
+    many = Batch(lens=[40], heads=16, hk=16, page=1024)
+    kv = many.handle()
+    with pytest.raises(ls.LeanStreamError, match="too large"):
+        ls.ls_paged_kv4_attend(kv, many.q, many.out, many.seq_len, wide[:1])
+    many.attend(kv)
+    many.check()
+    kv.close()
+
+
+def test_shares_of_sequences_of_many_millions():
+    """One page listed R times by as many sequences as there are processors, each a share of its own: the page's own result, and a log of
+    the sum that is larger by log R.  A warp adds up R 512 / 12 pairs of tiles; a pair adds up to 4 2^-24 of rounding to the sum of weights and
+    2 2^-23 to the sums of values."""
+    page, R = 16384, 2930
+    b = Batch(lens=[page], heads=1, hk=1, D=64, page=page)
+    kv = b.handle()
+    b.attend(kv)
+    b.check()
+    kv.close()
+    S = torch.cuda.get_device_properties(0).multi_processor_count
+    kv = b.handle(max_seqs=S)
+    table = b.table[:, :1].expand(S, R).contiguous()
+    out, lse = torch.full((S, 1, 1, 64), float("nan"), dtype=b.q.dtype, device=DEV), torch.full((S, 1, 1), float("nan"), device=DEV)
+    ls.ls_paged_kv4_attend(kv, b.q.expand(S, -1, -1, -1).contiguous(), out, torch.full((S,), R * page, dtype=torch.int32, device=DEV), table, lse=lse)
+    assert ls.ls_paged_kv4_status(kv) == 0
+    room = R * 512 / 12 * 2.0 ** -22
+    _, _, e, _ = orc.attend(f64(b.q), b.pages.cpu().numpy(), page, b.group, b.dtype, b.lens, b.table_np, 0, b.scale)
+    assert (np.abs(f64(out) - f64(b.out)) <= 2 * room * e["parts"] + 2.0 ** -8 * np.abs(f64(out)) + 2.0 ** -8 * np.abs(f64(b.out))).all()
+    assert (np.abs(f64(lse) - f64(b.lse) - np.log(R)) <= 2 * room).all()
+    kv.close()
+
+
+def test_two_handles_at_once():
+    """Two caches' calls on two streams, many times: neither sees the other's workspace."""
+    one, two = Batch(lens=[900, 30, 0, 2000], heads=16, hk=2, seed=3), Batch(lens=[900, 30, 0, 2000], heads=16, hk=2, seed=4)
+    k1, k2 = one.handle(), two.handle()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(50):
+        with torch.cuda.stream(s1):
+            one.attend(k1)
+        with torch.cuda.stream(s2):
+            two.attend(k2)
+    assert ls.ls_paged_kv4_status(k1) == 0 and ls.ls_paged_kv4_status(k2) == 0
+    one.check()
+    two.check()
+    k1.close()
+    k2.close()
