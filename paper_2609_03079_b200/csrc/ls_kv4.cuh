@@ -217,11 +217,17 @@ __device__ __forceinline__ uint4 turned_oct(uint4 mine, uint4 partners, const Tu
   return make_uint4(pack2<WD>(a[0], a[1]), pack2<WD>(a[2], a[3]), pack2<WD>(a[4], a[5]), pack2<WD>(a[6], a[7]));
 }
 
-constexpr int K4_SLABS = 2;    // slabs of 256 components that a warp takes of a token's keys or values, eight to a lane
-constexpr int K4_Q_HEADS = 4;  // of queries, 32 lanes with 16 components of so many heads each
+// Slabs of 256 components that a warp takes of a token's keys or values, eight to a lane, and heads of queries that each lane takes 16
+// components of.  More of them share a lane's angles and keep more loads on their way; fewer leave more warps.  In us, 16 chunks of 1023 tokens, 64 / 8
+// heads of 128 (floor 98): slabs 1, 2, 4: 130, 117, 134; heads 1, 2, 4: 162, 129, 117.  One token: 2.6, 3.0, 4.6; 2.9, 3.0, 3.0.
+constexpr int K4_SLABS = 2;
+constexpr int K4_Q_HEADS = 4;
 
 // A warp takes K4_SLABS slabs of a token's keys or of its values, or 512 K4_Q_HEADS components of its queries; a lane's angles are the
 // same in all of them.  Queries are turned in fp32 and rounded once, as in the 16-bit append.
+// Bound by memory: 117 us for the chunks above, 0.84 of the rate of a copy; with as many key heads as query heads (4 chunks of 1023, 40 / 40 heads)
+// by the arithmetic of the keys' codes, 80 us for a floor of 30.  Four CTAs to an SM (3: 129 us, 5: 192, which spills).  Operands that do not lie
+// at multiples of 16 bytes are read element by element: 439 us.
 template <int WD, int D, int G>
 __global__ void __launch_bounds__(256, 4) ls_kv4_append_kernel(const Kv4AppendArgs A) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -343,7 +349,8 @@ __global__ void __launch_bounds__(256, 4) ls_kv4_append_kernel(const Kv4AppendAr
   }
 }
 
-// Rows of `n` elements (a multiple of 64) to where they lie side by side, at a multiple of 16 bytes.
+// Rows of `n` elements (a multiple of 64) to where they lie side by side, at a multiple of 16 bytes: queries that the attention could
+// not load 16 bytes at a time.
 template <int N = 256>
 __global__ void __launch_bounds__(N) ls_kv4_align_kernel(const uint16_t* from, int64_t stride, uint16_t* to, int n) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -395,7 +402,8 @@ __device__ __forceinline__ void put8(uint16_t* dst, uint4 v, bool vec) {
 }
 
 // `width` threads to a token, each with 16 components of a key and of a value of every head that it visits: two words of each, stored
-// as two times 16 bytes.
+// as two times 16 bytes.  Bound by memory, four fifths of it writes: 134 us for 16 sequences of fp16 with a floor of 109; rows that do not
+// lie at multiples of 16 bytes are written element by element (1261 us).
 template <int WD, int D>
 __global__ void __launch_bounds__(256) ls_kv4_read_kernel(const Kv4ReadArgs A) {
   asm volatile("griddepcontrol.wait;" ::: "memory");

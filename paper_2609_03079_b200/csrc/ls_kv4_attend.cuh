@@ -7,7 +7,19 @@
 // shifts and logical instructions and no conversion.  The sums of a product are aligned to 2^-14, not to what the subnormal numbers come
 // to, so a code at bit 0 loses what lies below 2^-14 of a unit (lse was off by 4e-6): they stand at bits 2 and 6 (2^-16; the 2^-4 between the
 // two goes into the query, and into the sums of values when they are done).
-// Queries are scaled to a power of two per row and are exact in fp16, whatever the cache's type.
+// Queries are scaled to a power of two per row and are exact in fp16, whatever the cache's type.  A row's tensor-core work is a small part
+// of its instructions: scales, zeros and weights of 16 keys cost about 240 instructions of a warp (a scale for 128 components, up to 8
+// rows), 276 (for 64) or 404 (for 64, 16 rows).
+//
+// Bounds and figures (B200, passes among others):
+//   128 sequences of up to 9216 keys, 64 / 8 heads of 128, one scale a head: 157 us, 0.80 of the rate at which memory is copied; a call of
+//     one sequence of 100001 keys 32 us, whose steady state runs at 0.93 of it: about 13 us of a call are its beginning (lengths, shares,
+//     table, first tile, all of it cold code) and its end (the team's sums, then the joining of a unit's pieces);
+//   33 sequences of up to 2000 keys, 40 / 40 heads (one row in eight is used), a scale for 32: 75 us, 0.56, bound by the latency of the
+//     instructions above at three warps to a scheduler;
+//   16 rows (draft tokens): 16 sequences of a window of 4096 33 us, 0.27, the same at two warps to a scheduler.
+// What did not help: a software pipeline of scores and values (170 us for 174, others slower), halves of words picked by byte
+// permutations instead of shifts (the same within 1 %), scores of 32 rows at once (163 us for two passes' 100).
 #pragma once
 #include "ls_attend.cuh"
 #include "ls_kv4.cuh"
@@ -37,7 +49,8 @@ struct Attend4Args {
 };
 
 constexpr long long K4_SPIN_CLOCKS = 4000000000LL;  // about two seconds
-// What a unit's beginning and end, and the joining of its pieces, cost a warp, in tiles.
+// What a unit's beginning and end, and the joining of its pieces, cost a warp, in tiles.  (A unit at 4, 6, 8, 10: one sequence of 100001 keys 35.2, 32.6,
+// 32.3, 32.6 us; 33 of up to 2000 72.5, 73.8, 75.2, 75.3; three of 20001 21.7, 20.9, 19.5, 19.6; 200 tiny ones and a long one 36.6, 36.5, 37.3, 45.8.)
 constexpr float K4_UNIT_TILES = 8.f, K4_JOIN_TILES = 4.f, K4_ADD_TILES = 3e-4f;
 // Blocks that one call may deal out (they are counted in 32 bits); the host cuts larger batches.
 constexpr long long K4_MAX_BLOCKS = 1LL << 30;
@@ -46,8 +59,11 @@ constexpr long long K4_MAX_BLOCKS = 1LL << 30;
 // products (S^T = K Q^T, O^T = V^T P^T: the codes are the operand with 16 rows), 16 rows are their rows (S = Q K^T, O = P V).
 template <int D, int G, int NT>
 struct K4Shape {
-  static constexpr int WARPS = D * NT <= 128 ? 12 : 8;           // (168 registers a thread, or 255)
-  static constexpr int KT = D == 256 && G == 32 ? 1 : 2;         // tiles of a block, which a warp takes at once
+  // 12 warps of 168 registers, or 8 of 255 where sums fill more.  Two tiles at once give a warp independent work (in us, warps x tiles; 8 rows of
+  // heads of 128: 12 x 2, 8 x 2, 16 x 2, 16 x 1: 128 long sequences 177, 198, 170, 200; one long 36, 46, 40, 60; 200 of 300 keys 24, 36,
+  // 27, 27.  16 rows, window of 4096: 8 x 2, 8 x 1, 12 x 1, 10 x 2: 35, 39, 50, 61).
+  static constexpr int WARPS = D * NT <= 128 ? 12 : 8;
+  static constexpr int KT = D == 256 && G == 32 ? 1 : 2;         // (two would spill 660 bytes a thread, one 180)
   static constexpr int THREADS = WARPS * 32;
   static constexpr int ROWS = 8 * NT;
   static constexpr int NG = D / G;
@@ -205,6 +221,10 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
   // team has as much but begins and ends inside a unit; what a unit's beginning and end cost a team (K4_UNIT blocks of each warp) stands
   // in the line in front of it.  Or each unit begins with a new share, one for all of it, or several.  (Shares may be a little larger than
   // they need to be: fp32 will do.)
+  // What each way is for, in us (the rule; always the first; never one share to a unit; always whole CTAs; always the smallest teams): one short
+  // sequence 6.7, 8.9, 9.0, 6.5, 17; one of 100001 keys 33, 37, 33, 33, 361; 33 of up to 2000 75, 75, 75, 152, 76; a window of 4096 35, 87, 87,
+  // 34, 40; 128 long ones 163, 162, 163, 198, 159; 200 of 300 23, 29, 29, 88, 23; three of 20001 20, 24, 20, 20, 108.  And without the units' own
+  // cost in the line, idle and tiny units fall to one team: 64 idle of 80 191 us instead of 34.
   int w, share, extra;
   bool gaps;
   {  // (a lane for each size of a team)
