@@ -12,14 +12,16 @@
 // rows), 276 (for 64) or 404 (for 64, 16 rows).
 //
 // Bounds and figures (B200, passes among others):
-//   128 sequences of up to 9216 keys, 64 / 8 heads of 128, one scale a head: 157 us, 0.80 of the rate at which memory is copied; a call of
+//   128 sequences of up to 9216 keys, 64 / 8 heads of 128, one scale a head: 157 us, 0.80 of the rate at which memory is copied
+//     (171 to 178 us where seconds of such calls meet the card's power limit); a call of
 //     one sequence of 100001 keys 32 us, whose steady state runs at 0.93 of it: about 13 us of a call are its beginning (lengths, shares,
 //     table, first tile, all of it cold code) and its end (the team's sums, then the joining of a unit's pieces);
 //   33 sequences of up to 2000 keys, 40 / 40 heads (one row in eight is used), a scale for 32: 75 us, 0.56, bound by the latency of the
 //     instructions above at three warps to a scheduler;
 //   16 rows (draft tokens): 16 sequences of a window of 4096 33 us, 0.27, the same at two warps to a scheduler.
-// What did not help: a software pipeline of scores and values (170 us for 174, others slower), halves of words picked by byte
-// permutations instead of shifts (the same within 1 %), scores of 32 rows at once (163 us for two passes' 100).
+// What did not help: a software pipeline of scores and values (170 us for 174, others slower), codes brought to their bits by byte
+// permutations (the same within 1 %) or by the high half of a product (5 to 15 % slower) instead of right shifts, scores of 32 rows at
+// once (163 us for two passes' 100).
 #pragma once
 #include "ls_attend.cuh"
 #include "ls_kv4.cuh"
