@@ -24,9 +24,10 @@ namespace {
 
 using ls_kv4::Shape;
 
-// Rows of queries of one key head: 8 or 16 at a time (8 with heads of 256, whose sums fill the registers).
+// Rows of queries of one key head: 8 or 16 at a time (8 with heads of 256, whose sums fill the registers), or so few that 8 columns
+// hold each row for each group.
 Shape shape_for(const ls_paged_kv4_desc& d, long long rows) {
-  const int nt = rows <= 8 || d.head_dim == 256 ? 1 : 2;
+  const int groups = d.head_dim / d.group, nt = groups > 1 && rows * groups <= 8 ? 0 : rows <= 8 || d.head_dim == 256 ? 1 : 2;
   return d.dtype == LS_WDTYPE_BF16 ? ls_kv4::shape_bf16(d.head_dim, d.group, nt) : ls_kv4::shape_fp16(d.head_dim, d.group, nt);
 }
 
@@ -48,7 +49,7 @@ int32_t create_kv(ls_paged_kv4* kv) {
   LS_CUDA(cudaMemset(kv->status, 0, sizeof(int)));
   if (d.max_seqs > 0) {
     const long long rows = (long long)d.max_q_len * (d.n_q_heads / d.n_kv_heads);
-    for (long long r : {8LL, 16LL}) {
+    for (long long r : {1LL, 8LL, 16LL}) {
       const Shape s = shape_for(d, r);
       LS_CUDA(cudaFuncSetAttribute(s.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, s.smem));
       kv->part_floats = std::max(kv->part_floats, (size_t)kv->sm_count * (s.threads / 32) * 2 * s.piece);

@@ -16,8 +16,8 @@
 //     (171 to 178 us where seconds of such calls meet the card's power limit); a call of
 //     one sequence of 100001 keys 32 us, whose steady state runs at 0.93 of it: about 13 us of a call are its beginning (lengths, shares,
 //     table, first tile, all of it cold code) and its end (the team's sums, then the joining of a unit's pieces);
-//   33 sequences of up to 2000 keys, 40 / 40 heads (one row in eight is used), a scale for 32: 75 us, 0.56, bound by the latency of the
-//     instructions above at three warps to a scheduler;
+//   33 sequences of up to 2000 keys, 40 / 40 heads, a scale for 32: 58 us, 0.73 (75 us with a column for a row, of which seven in eight
+//     are idle, and a sum for each group);
 //   16 rows (draft tokens): 16 sequences of a window of 4096 33 us, 0.27, the same at two warps to a scheduler.
 // What did not help: a software pipeline of scores and values (170 us for 174, others slower), codes brought to their bits by byte
 // permutations (the same within 1 %) or by the high half of a product (5 to 15 % slower) instead of right shifts, scores of 32 rows at
@@ -59,16 +59,21 @@ constexpr long long K4_MAX_BLOCKS = 1LL << 30;
 
 // Shapes of the kernel: D components a head, groups of G, NT times 8 rows of queries at once.  Up to 8 rows are the columns of the
 // products (S^T = K Q^T, O^T = V^T P^T: the codes are the operand with 16 rows), 16 rows are their rows (S = Q K^T, O = P V).
+// NT = 0: so few rows that the 8 columns hold each of them once for every group, with the components of that group alone.  One sum then
+// holds what a scale and a zero have to be applied to, two columns to a lane, instead of one sum for each group.  (In us, with and
+// without: 33 sequences of up to 2000 keys, one row, four groups: 57.7, 75.5; 8 of 8001, one row, two groups: 44.8, 47.1; 200 of 300 keys, four
+// rows, two groups: 21.5, 23.3; 200 of 17 and one of 40000: 39.4, 37.2.)
 template <int D, int G, int NT>
 struct K4Shape {
   // 12 warps of 168 registers, or 8 of 255 where sums fill more.  Two tiles at once give a warp independent work (in us, warps x tiles; 8 rows of
   // heads of 128: 12 x 2, 8 x 2, 16 x 2, 16 x 1: 128 long sequences 177, 198, 170, 200; one long 36, 46, 40, 60; 200 of 300 keys 24, 36,
   // 27, 27.  16 rows, window of 4096: 8 x 2, 8 x 1, 12 x 1, 10 x 2: 35, 39, 50, 61).
-  static constexpr int WARPS = D * NT <= 128 ? 12 : 8;
+  static constexpr int N8 = NT == 2 ? 2 : 1;
+  static constexpr int WARPS = D * N8 <= 128 ? 12 : 8;
   static constexpr int KT = D == 256 && G == 32 ? 1 : 2;         // (two would spill 660 bytes a thread, one 180)
   static constexpr int THREADS = WARPS * 32;
-  static constexpr int ROWS = 8 * NT;
   static constexpr int NG = D / G;
+  static constexpr int ROWS = NT == 0 ? 8 / NG : 8 * NT;
   static constexpr int TILE = kv4_tile(D, G);
   static constexpr int LINE = D + 4;                     // floats of a row's piece
   static constexpr int PIECE = ROWS * LINE * 4;
@@ -162,7 +167,9 @@ template <int WD, int D, int G, int NT>
 __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_kernel(const __grid_constant__ Attend4Args A) {
   using S = K4Shape<D, G, NT>;
   constexpr int NG = S::NG, NW = D / 64, KW = D / 32, ST = S::STAGES, KT = S::KT;
-  constexpr bool WIDE = NT == 2;
+  constexpr int N8 = S::N8;
+  constexpr bool WIDE = NT == 2, COLS = NT == 0;
+  constexpr int NS = COLS ? 1 : NG, NV = COLS ? 2 : NG, NR = COLS ? 1 : 2;  // sums of scores, scales of a token that are the lane's, rows of the lane
   extern __shared__ __align__(128) uint8_t smem[];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
   uint8_t* ring = smem + warp * S::RING;
@@ -224,7 +231,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
   // in the line in front of it.  Or each unit begins with a new share, one for all of it, or several.  (Shares may be a little larger than
   // they need to be: fp32 will do.)
   // What each way is for, in us (the rule; always the first; never one share to a unit; always whole CTAs; always the smallest teams): one short
-  // sequence 6.7, 8.9, 9.0, 6.5, 17; one of 100001 keys 33, 37, 33, 33, 361; 33 of up to 2000 75, 75, 75, 152, 76; a window of 4096 35, 87, 87,
+  // sequence 6.7, 8.9, 9.0, 6.5, 17; one of 100001 keys 33, 37, 33, 33, 361; 33 of up to 2000 (a column for a row) 75, 75, 75, 152, 76; a window of 4096 35, 87, 87,
   // 34, 40; 128 long ones 163, 162, 163, 198, 159; 200 of 300 23, 29, 29, 88, 23; three of 20001 20, 24, 20, 20, 108.  And without the units' own
   // cost in the line, idle and tiny units fall to one team: 64 idle of 80 191 us instead of 34.
   int w, share, extra;
@@ -312,10 +319,10 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
     const int block0 = k4_first<KT>(A, len) + from_block + wi;
 
     // queries: the lane's columns of the operand are components 8 (4 j + t) ... of row g
-    uint4 raw[NT][KW];
+    uint4 raw[N8][KW];
 #pragma unroll
-    for (int x = 0; x < NT; ++x) {
-      const int r = row0 + 8 * x + g, i = A.by_group(r);
+    for (int x = 0; x < N8; ++x) {
+      const int r = row0 + (COLS ? g / NG : 8 * x + g), i = A.by_group(r);
       const uint16_t* src_q = A.q + ((long long)b * A.q_len + i) * A.q_stride + (long long)(h * A.group + r - i * A.group) * D + 8 * t;
 #pragma unroll
       for (int j = 0; j < KW; ++j) {
@@ -387,16 +394,16 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
       }
     }
 
-    // Everything below is kept for the lane's two rows: 2 t and 2 t + 1, or g and g + 8.
-    uint32_t qf[S::Q_SHARED ? 1 : NT][KW][4];
-    float qs[NG][2], cn[2], M[2] = {-1e30f, -1e30f}, l[2] = {0.f, 0.f}, zs[NG][2], cs[NG][4], o[NW][2][2][NT][4];
+    // Everything below is kept for the lane's two rows: 2 t and 2 t + 1, or g and g + 8 (or the columns 2 t and 2 t + 1 of one row).
+    uint32_t qf[S::Q_SHARED ? 1 : N8][KW][4];
+    float qs[NS][2], cn[2], M[2] = {-1e30f, -1e30f}, l[2] = {0.f, 0.f}, zs[NS][2], cs[NS][4], o[NW][2][2][N8][4];
 #pragma unroll
-    for (int e = 0; e < 4 * NG; ++e) { cs[e / 4][e % 4] = 0.f; zs[e / 4][e % 2] = 0.f; }
+    for (int e = 0; e < 4 * NS; ++e) { cs[e / 4][e % 4] = 0.f; zs[e / 4][e % 2] = 0.f; }
 #pragma unroll
-    for (int e = 0; e < 16 * NT * NW; ++e) o[e / (16 * NT)][e / (8 * NT) % 2][e / (4 * NT) % 2][e / 4 % NT][e % 4] = 0.f;
+    for (int e = 0; e < 16 * N8 * NW; ++e) o[e / (16 * N8)][e / (8 * N8) % 2][e / (4 * N8) % 2][e / 4 % N8][e % 4] = 0.f;
 #pragma unroll
-    for (int x = 0; x < NT; ++x) {
-      float top = 0.f, part[NG];
+    for (int x = 0; x < N8; ++x) {
+      float top = 0.f, part[NS];
 #pragma unroll
       for (int j = 0; j < KW; ++j) {
         const uint32_t u[4] = {raw[x][j].x, raw[x][j].y, raw[x][j].z, raw[x][j].w};
@@ -412,15 +419,18 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
       const int ex = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 113);
       const float up = __uint_as_float((uint32_t)(14 - ex + 127) << 23), up16 = up * 0.0625f;
 #pragma unroll
-      for (int k = 0; k < NG; ++k) part[k] = 0.f;
+      for (int k = 0; k < NS; ++k) part[k] = 0.f;
 #pragma unroll
       for (int j = 0; j < KW; ++j) {
         const uint32_t u[4] = {raw[x][j].x, raw[x][j].y, raw[x][j].z, raw[x][j].w};
+        const int k = COLS ? 0 : 32 * j / G;
+        const bool here = !COLS || 32 * j / G == g % NG;  // (a column without the components holds zeros)
         float2 f[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           f[e] = both_halves<WD>(u[e]);
-          part[32 * j / G] = fmaf(f[e].x, up, fmaf(f[e].y, up, part[32 * j / G]));
+          if (!here) f[e] = make_float2(0.f, 0.f);
+          part[k] = fmaf(f[e].x, up, fmaf(f[e].y, up, part[k]));
         }
         const uint4 q = make_uint4(halves(f[0].x * up, f[2].x * up), halves(f[0].y * up16, f[2].y * up16), halves(f[1].x * up, f[3].x * up),
                                    halves(f[1].y * up16, f[3].y * up16));
@@ -431,7 +441,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
       if (WIDE) cn[x] = c;
       else { cn[0] = __shfl_sync(0xffffffffu, c, 8 * t); cn[1] = __shfl_sync(0xffffffffu, c, 8 * t + 4); }
 #pragma unroll
-      for (int k = 0; k < NG; ++k) {
+      for (int k = 0; k < NS; ++k) {
         const float f = quad_sum(part[k]) * 2.384185791015625e-7f;  // 2^-22
         if (WIDE) qs[k][x] = f;
         else { qs[k][0] = __shfl_sync(0xffffffffu, f, 8 * t); qs[k][1] = __shfl_sync(0xffffffffu, f, 8 * t + 4); }
@@ -468,13 +478,14 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
         const bool edge = (unsigned)(j - plain) >= (unsigned)plains || patchy;
 
         // Scores.  NK keys of a tile are the lane's: tok0 and tok0 + 8, or t, 7 - t, 8 + t, 15 - t; score e is of row_of(e), key_of(e).
-        constexpr int NK = 2 * NT, NX = 2 * NK;
-        auto row_of = [](int e) { return WIDE ? e / 2 % 2 : e % 2; };
-        auto key_of = [](int e) { return WIDE ? e / 4 * 2 + e % 2 : e / 2; };
+        constexpr int NK = 2 * N8, NX = NR * NK;
+        auto row_of = [](int e) { return COLS ? 0 : WIDE ? e / 2 % 2 : e % 2; };
+        auto key_of = [](int e) { return COLS ? e : WIDE ? e / 4 * 2 + e % 2 : e / 2; };
         auto token_of = [&](int k) { return WIDE ? (k & 2) * 4 + (k & 1 ? 7 - t : t) : tok0 + 8 * k; };
+        const int my_group = COLS ? 2 * t % NG * 4 : 0;
         float x[KT][NX];
         {
-          uint32_t ka[KT][KW], kb[KT][KW], meta[KT][NK][NG];
+          uint32_t ka[KT][KW], kb[KT][KW], meta[KT][NK][NV];
           constexpr int n4 = D == 64 ? 2 : 4;
 #pragma unroll
           for (int z = 0; z < KT; ++z) {
@@ -489,16 +500,17 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
               for (int i = 0; i < n4; ++i) { ka[z][half * n4 + i] = a[i]; kb[z][half * n4 + i] = c[i]; }
             }
 #pragma unroll
-            for (int k = 0; k < NK; ++k) lds_words<NG>(mine + 16 * D + token_of(k) * 4 * NG, meta[z][k]);
+            for (int k = 0; k < NK; ++k) lds_words<NV>(mine + 16 * D + token_of(k) * 4 * NG + my_group, meta[z][k]);
           }
 #pragma unroll
-          for (int k = 0; k < NG; ++k) {
-            float acc[KT][NT][4];
+          for (int k = 0; k < NS; ++k) {
+            constexpr int part = KW / NS;  // (words of a code row for one sum)
+            float acc[KT][N8][4];
 #pragma unroll
-            for (int i = k * G / 32; i < (k + 1) * G / 32; ++i) {
-              uint32_t q[NT][4];
+            for (int i = k * part; i < (k + 1) * part; ++i) {
+              uint32_t q[N8][4];
 #pragma unroll
-              for (int y = 0; y < NT; ++y) {
+              for (int y = 0; y < N8; ++y) {
                 if constexpr (S::Q_SHARED) lds_words<4>(q_shared + (y * KW + i) * 512, q[y]);
                 else {
 #pragma unroll
@@ -511,7 +523,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
                 for (int z = 0; z < KT; ++z) {
                   const uint32_t a = s ? ka[z][i] >> 6 : ka[z][i] << 2, c = s ? kb[z][i] >> 6 : kb[z][i] << 2;
                   const uint32_t a0 = a & 0x003c003cu, a1 = a & 0x03c003c0u, c0 = c & 0x003c003cu, c1 = c & 0x03c003c0u;
-                  const bool first = i == k * G / 32 && s == 0;
+                  const bool first = i == k * part && s == 0;
                   if constexpr (WIDE) {
                     mma_f16(acc[z][0], q[0][2 * s], q[1][2 * s], q[0][2 * s + 1], q[1][2 * s + 1], a0, a1, first);
                     mma_f16(acc[z][1], q[0][2 * s], q[1][2 * s], q[0][2 * s + 1], q[1][2 * s + 1], c0, c1, first);
@@ -520,28 +532,39 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
             }
 #pragma unroll
             for (int z = 0; z < KT; ++z) {
-              float2 m[NK];
+              if constexpr (COLS) {
 #pragma unroll
-              for (int i = 0; i < NK; ++i) m[i] = both_halves<WD>(meta[z][i][k]);
+                for (int i = 0; i < NK; ++i) {
+                  const float2 m0 = both_halves<WD>(meta[z][i][0]), m1 = both_halves<WD>(meta[z][i][1]);
+                  float v = fmaf(m0.x, acc[z][0][2 * i], m0.y * qs[0][0]) + fmaf(m1.x, acc[z][0][2 * i + 1], m1.y * qs[0][1]);
+                  if (NG >= 4) v += __shfl_xor_sync(0xffffffffu, v, 1);
+                  if (NG >= 8) v += __shfl_xor_sync(0xffffffffu, v, 2);
+                  x[z][i] = v;
+                }
+              } else {
+                float2 m[NK];
 #pragma unroll
-              for (int e = 0; e < NX; ++e) {
-                const float2 sz = m[key_of(e)];
-                const float zero = k ? fmaf(sz.y, qs[k][row_of(e)], x[z][e]) : sz.y * qs[k][row_of(e)];
-                x[z][e] = fmaf(sz.x, acc[z][e / 4][e % 4], zero);
+                for (int i = 0; i < NK; ++i) m[i] = both_halves<WD>(meta[z][i][k]);
+#pragma unroll
+                for (int e = 0; e < NX; ++e) {
+                  const float2 sz = m[key_of(e)];
+                  const float zero = k ? fmaf(sz.y, qs[k][row_of(e)], x[z][e]) : sz.y * qs[k][row_of(e)];
+                  x[z][e] = fmaf(sz.x, acc[z][e / 4][e % 4], zero);
+                }
               }
             }
           }
         }
         // scales and zeros of the values of the same tokens
-        float2 va[KT][NK][NG];
+        float2 va[KT][NK][NV];
 #pragma unroll
         for (int z = 0; z < KT; ++z)
 #pragma unroll
           for (int i = 0; i < NK; ++i) {
-            uint32_t meta[NG];
-            lds_words<NG>(tile + z * S::TILE + 16 * D + 64 * NG + token_of(i) * 4 * NG, meta);
+            uint32_t meta[NV];
+            lds_words<NV>(tile + z * S::TILE + 16 * D + 64 * NG + token_of(i) * 4 * NG + my_group, meta);
 #pragma unroll
-            for (int k = 0; k < NG; ++k) va[z][i][k] = both_halves<WD>(meta[k]);
+            for (int k = 0; k < NV; ++k) va[z][i][k] = both_halves<WD>(meta[k]);
           }
         if (edge) {
           const uint32_t gone = skip >> (stage * KT);
@@ -549,8 +572,8 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
           // Tokens that nobody sees may hold anything, and one that some rows see may hold NaN: neither must meet a weight of zero.
           int hi[2], lo[2];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int r = WIDE ? 8 * e + g : 2 * t + e;
+          for (int e = 0; e < NR; ++e) {
+            const int r = COLS ? 2 * t / NG : WIDE ? 8 * e + g : 2 * t + e;
             hi[e] = r < rows ? len - A.q_len + A.by_group(row0 + r) : -1;
             lo[e] = max(hi[e], -1) - A.window;
           }
@@ -559,20 +582,20 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
 #pragma unroll
             for (int i = 0; i < NK; ++i) {
               const int at = pos0 + 16 * z + token_of(i);
-              bool on[2], fine[NG];
+              bool on[2] = {false, false}, fine[NV];
 #pragma unroll
-              for (int e = 0; e < 2; ++e) on[e] = !(gone >> z & 1) && at <= hi[e] && at > lo[e];
+              for (int e = 0; e < NR; ++e) on[e] = !(gone >> z & 1) && at <= hi[e] && at > lo[e];
 #pragma unroll
               for (int e = 0; e < NX; ++e)
                 if (key_of(e) == i && !on[row_of(e)]) x[z][e] = -INFINITY;
               // (the lanes that share the key: those of the same t, or of the same g)
               const bool any = __ballot_sync(0xffffffffu, on[0] || on[1]) & (WIDE ? 0x11111111u << t : 15u << (lane & 28));
 #pragma unroll
-              for (int k = 0; k < NG; ++k) {
+              for (int k = 0; k < NV; ++k) {
                 fine[k] = fabsf(va[z][i][k].x) + fabsf(va[z][i][k].y) < INFINITY;
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
-                  if (on[e] && !fine[k]) zs[k][e] = __int_as_float(0x7fffffff);
+                for (int e = 0; e < NR; ++e)
+                  if (on[e] && !fine[k]) zs[COLS ? 0 : k][COLS ? k : e] = __int_as_float(0x7fffffff);
                 if (!any || !fine[k]) va[z][i][k] = make_float2(0.f, 0.f);
               }
             }
@@ -587,7 +610,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
           for (int i = 0; i < NK; ++i) {
             all[i] = 8.67361737988403547e-19f;
 #pragma unroll
-            for (int k = 0; k < NG; ++k) all[i] += va[z][i][k].x;
+            for (int k = 0; k < NV; ++k) all[i] += va[z][i][k].x;
           }
 #pragma unroll
           for (int e = 0; e < NX; ++e) {
@@ -604,27 +627,31 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
             for (int i = 0; i < NK; ++i) {
               big[i] = 8.67361737988403547e-19f;
 #pragma unroll
-              for (int k = 0; k < NG; ++k) big[i] = fmaxf(big[i], va[z][i][k].x);
+              for (int k = 0; k < NV; ++k) big[i] = fmaxf(big[i], va[z][i][k].x);
               big[i] = __log2f(big[i]) - 4.f;
             }
 #pragma unroll
             for (int e = 0; e < NX; ++e) m[row_of(e)] = fmaxf(m[row_of(e)], fmaf(x[z][e], cn[row_of(e)], big[key_of(e)]));
           }
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float to = fmaxf(M[e], WIDE ? quad_max(m[e]) : rows_max(m[e]));
+          for (int e = 0; e < NR; ++e) {
+            float to = fmaxf(M[e], WIDE ? quad_max(m[e]) : rows_max(m[e]));
+            if (COLS && NG >= 4) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, 1));
+            if (COLS && NG >= 8) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, 2));
             f[e] = ex2(M[e] - to);
             M[e] = to;
             l[e] *= f[e];
-#pragma unroll
-            for (int k = 0; k < NG; ++k) zs[k][e] *= f[e];
           }
+          if (COLS) f[1] = f[0];
 #pragma unroll
-          for (int k = 0; k < NG; ++k)
+          for (int k = 0; k < NS; ++k) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) zs[k][e] *= f[e];
 #pragma unroll
             for (int e = 0; e < 4; ++e) cs[k][e] *= f[WIDE ? e / 2 : e % 2];
+          }
 #pragma unroll
-          for (int e = 0; e < 16 * NT * NW; ++e) o[e / (16 * NT)][e / (8 * NT) % 2][e / (4 * NT) % 2][e / 4 % NT][e % 4] *= f[WIDE ? e / 2 % 2 : e % 2];
+          for (int e = 0; e < 16 * N8 * NW; ++e) o[e / (16 * N8)][e / (8 * N8) % 2][e / (4 * N8) % 2][e / 4 % N8][e % 4] *= f[WIDE ? e / 2 % 2 : e % 2];
 #pragma unroll
           for (int z = 0; z < KT; ++z)
 #pragma unroll
@@ -633,22 +660,32 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
         // Weights times scales, rounded to fp16 for the product with the codes.  The codes count from the middle of their range, 8: the
         // rounding then weighs s |u - 8|, about a value's own size.  8 sum(p s) is taken off with the rounded weights (a product with
         // ones), and added back, unrounded, with the zeros.
-        uint32_t pf[KT][NG][NK];
+        uint32_t pf[KT][NS][NK];
 #pragma unroll
         for (int z = 0; z < KT; ++z) {
 #pragma unroll
           for (int e = 0; e < NX; ++e) l[row_of(e)] += p[z][e];
 #pragma unroll
-          for (int k = 0; k < NG; ++k) {
+          for (int k = 0; k < NS; ++k) {
+            if constexpr (COLS) {
 #pragma unroll
-            for (int e = 0; e < NX; ++e) {
-              const float2 sz = va[z][key_of(e)][k];
-              zs[k][row_of(e)] = fmaf(p[z][e], fmaf(sz.x, 8.f, sz.y), zs[k][row_of(e)]);
-            }
+              for (int i = 0; i < NK; ++i) {
+                const float2 a = va[z][i][0], c = va[z][i][1];
+                zs[0][0] = fmaf(p[z][i], fmaf(a.x, 8.f, a.y), zs[0][0]);
+                zs[0][1] = fmaf(p[z][i], fmaf(c.x, 8.f, c.y), zs[0][1]);
+                pf[z][0][i] = transpose8(halves(p[z][i] * a.x, p[z][i] * c.x));
+              }
+            } else {
 #pragma unroll
-            for (int e = 0; e < NX; e += 2) {
-              const uint32_t two = halves(p[z][e] * va[z][key_of(e)][k].x, p[z][e + 1] * va[z][key_of(e + 1)][k].x);
-              pf[z][k][e / 2] = WIDE ? two : transpose8(two);
+              for (int e = 0; e < NX; ++e) {
+                const float2 sz = va[z][key_of(e)][k];
+                zs[k][row_of(e)] = fmaf(p[z][e], fmaf(sz.x, 8.f, sz.y), zs[k][row_of(e)]);
+              }
+#pragma unroll
+              for (int e = 0; e < NX; e += 2) {
+                const uint32_t two = halves(p[z][e] * va[z][key_of(e)][k].x, p[z][e + 1] * va[z][key_of(e + 1)][k].x);
+                pf[z][k][e / 2] = WIDE ? two : transpose8(two);
+              }
             }
             if constexpr (WIDE) mma_f16(cs[k], pf[z][k][0], pf[z][k][1], pf[z][k][2], pf[z][k][3], 0x3c003c00u, 0x3c003c00u);
             else mma_f16(cs[k], 0x3c003c00u, 0u, 0x3c003c00u, 0u, pf[z][k][0], pf[z][k][1]);
@@ -671,7 +708,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
               const uint32_t a = __byte_perm(v[0][ws], v[1][ws], half ? 0x7632 : 0x5410), c = __byte_perm(v[2][ws], v[3][ws], half ? 0x7632 : 0x5410);
 #pragma unroll
               for (int s = 0; s < 2; ++s) {
-                const int k = (64 * ws + 32 * half) / G;
+                const int k = COLS ? 0 : (64 * ws + 32 * half) / G;
                 const uint32_t d = s ? a >> 6 : a << 2, f = s ? c >> 6 : c << 2;
                 const uint32_t d0 = d & 0x003c003cu, d1 = d & 0x03c003c0u, f0 = f & 0x003c003cu, f1 = f & 0x03c003c0u;
                 if constexpr (WIDE) {
@@ -700,22 +737,23 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
       float* piece = reinterpret_cast<float*>(ring);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float sum_l = WIDE ? quad_sum(l[e]) : rows_sum(l[e]);
-        float zero[NG];
+        const float sum_l = WIDE ? quad_sum(l[e]) : rows_sum(l[COLS ? 0 : e]);
+        float zero[NS];
 #pragma unroll
-        for (int k = 0; k < NG; ++k) zero[k] = fmaf(-8.f, cs[k][WIDE ? 2 * e : e], WIDE ? quad_sum(zs[k][e]) : rows_sum(zs[k][e]));
-        float* line = piece + (WIDE ? 8 * e + g : 2 * t + e) * S::LINE;
-        // four components side by side: of g, or, twice, of 2 t and 2 t + 1
+        for (int k = 0; k < NS; ++k) zero[k] = fmaf(-8.f, cs[k][WIDE ? 2 * e : e], WIDE ? quad_sum(zs[k][e]) : rows_sum(zs[k][e]));
+        float* line = piece + (COLS ? (2 * t + e) / NG : WIDE ? 8 * e + g : 2 * t + e) * S::LINE;
+        // four components side by side: of g, or, twice, of 2 t and 2 t + 1 (of a column that stands for one group, that group's)
 #pragma unroll
-        for (int i = 0; i < 2 * NW * NT; ++i) {
-          const int at = i / NT, c = WIDE ? 2 * e + i % 2 : e;
-          const float zz = zero[32 * at / G];
+        for (int i = 0; i < 2 * NW * N8; ++i) {
+          const int at = i / N8, c = WIDE ? 2 * e + i % 2 : e;
+          if (COLS && (2 * t + e) % NG != 32 * at / G) continue;
+          const float zz = zero[COLS ? 0 : 32 * at / G];
           const auto& a = o[at / 2][at % 2];
-          const float first = a[0][0][c], second = WIDE ? a[0][NT - 1][c] : a[0][0][c + 2], third = a[1][0][c], last = WIDE ? a[1][NT - 1][c] : a[1][0][c + 2];
+          const float first = a[0][0][c], second = WIDE ? a[0][N8 - 1][c] : a[0][0][c + 2], third = a[1][0][c], last = WIDE ? a[1][N8 - 1][c] : a[1][0][c + 2];
           *reinterpret_cast<float4*>(line + 32 * at + 4 * (WIDE ? 2 * t + i % 2 : g)) =
               make_float4(fmaf(first, 4194304.f, zz), fmaf(second, 262144.f, zz), fmaf(third, 4194304.f, zz), fmaf(last, 262144.f, zz));
         }
-        if (WIDE ? t == 0 : g == 0) *reinterpret_cast<float2*>(line + D) = make_float2(M[e], sum_l);
+        if (WIDE ? t == 0 : g == 0 && (!COLS || (2 * t + e) % NG == 0)) *reinterpret_cast<float2*>(line + D) = make_float2(M[COLS ? 0 : e], sum_l);
       }
     }
     team_sync();

@@ -184,6 +184,7 @@ class Decoder:
     def cached(self, seq: int) -> List[Tuple[torch.Tensor, torch.Tensor]]:
         """Keys and values of every layer for all positions of a sequence (its prefix among them), in 16 bits: to be looked at, moved to
         another machine or kept."""
+        seq = range(self.max_seqs)[seq]
         n = self.lens[seq]
         pos = torch.arange(n, dtype=torch.int32, device=self.pool.table.device)
         return [layer.cached(torch.full_like(pos, seq), pos, self.pool.table) for layer in self.layers]

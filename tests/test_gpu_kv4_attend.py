@@ -395,3 +395,34 @@ def test_two_handles_at_once():
     two.check()
     k1.close()
     k2.close()
+
+
+@pytest.mark.parametrize("D,group", [(64, 32), (128, 32), (128, 64), (256, 32), (256, 64), (256, 128)])
+@pytest.mark.parametrize("per,q_len", [(1, 1), (1, 2), (2, 1), (1, 3), (3, 1), (2, 2), (4, 1), (1, 4), (5, 1)])
+def test_few_rows(D, group, per, q_len):
+    """Rows of which several copies, one for each group, fit 8 columns, and just more than that."""
+    run_case(D=D, group=group, heads=3 * per, hk=3, q_len=q_len, lens=[70, 0, 1, 333, 2], seed=D + per)
+    run_case(D=D, group=group, heads=3 * per, hk=3, q_len=q_len, lens=[50, 129, 2000], dtype="fp16", page=48, window=40, vstd=2.0, std=5.0, seed=group + per)
+
+
+@pytest.mark.parametrize("D,group", [(128, 32), (128, 64), (256, 32)])
+def test_few_rows_and_tokens_that_are_not_finite(D, group):
+    """As above for two draft tokens of one head: NaN stays with the group, and with the token, that sees it."""
+    b = Batch(lens=[50, 20], q_len=2, heads=2, hk=2, D=D, group=group)
+    kv = b.handle()
+    b.attend(kv)
+    torch.cuda.synchronize()
+    clean = b.out.clone()
+    pos = torch.tensor([48, 49], dtype=torch.int32, device=DEV)
+    k, v = (torch.randn(2, 2, D, device=DEV).bfloat16() for _ in range(2))
+    v[0, 0, group + 3] = float("nan")
+    k[1, 1, 0] = float("inf")
+    ls.ls_paged_kv4_append(kv, None, k, v, None, torch.zeros_like(pos), pos, b.table)
+    b.attend(kv)
+    torch.cuda.synchronize()
+    assert torch.equal(b.out[1], clean[1])
+    hit = torch.zeros(2, 2, D, dtype=torch.bool, device=DEV)
+    hit[:, 0, group:2 * group] = True
+    hit[1, 1] = True
+    assert torch.equal(torch.isnan(b.out[0]), hit)
+    kv.close()
