@@ -51,8 +51,8 @@ struct Attend4Args {
 };
 
 constexpr long long K4_SPIN_CLOCKS = 4000000000LL;  // about two seconds
-// What a unit's beginning and end, and the joining of its pieces, cost a warp, in tiles.  (A unit at 4, 6, 8, 10: one sequence of 100001 keys 35.2, 32.6,
-// 32.3, 32.6 us; 33 of up to 2000 72.5, 73.8, 75.2, 75.3; three of 20001 21.7, 20.9, 19.5, 19.6; 200 tiny ones and a long one 36.6, 36.5, 37.3, 45.8.)
+// What a unit's beginning and end, and the joining of its pieces, cost a warp, in tiles.  (A unit at 4, 6, 8 and 10 or 11: one sequence of 100001 keys 35.2, 32.6,
+// 32.3, 32.6 us; 33 of up to 2000 57.0, 57.3, 57.7, 58.4; three of 20001 20.7, 20.2, 18.7, 18.4; 200 tiny ones and a long one 34, 40, 39, 40.)
 constexpr float K4_UNIT_TILES = 8.f, K4_JOIN_TILES = 4.f, K4_ADD_TILES = 3e-4f;
 // Blocks that one call may deal out (they are counted in 32 bits); the host cuts larger batches.
 constexpr long long K4_MAX_BLOCKS = 1LL << 30;
