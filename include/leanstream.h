@@ -452,8 +452,8 @@ int32_t ls_paged_kv_status(ls_paged_kv *kv, int32_t *host_status);
  * ls_paged_kv4_attend: scores, softmax statistics and sums are fp32; weights times scales are rounded to fp16 for the product with
  *   the codes.  A token's result depends on nothing that it does not see.  Meant for a few tokens per sequence; rows of
  *   q_len * n_q_heads / n_kv_heads beyond 16 (8 for head_dim 256) read the keys again.  Refused: a table of so many positions that one
- *   sequence would need more than 2^30 tiles, n_kv_heads * ceil(rows / 16 (8)) * (64 + table_width * page_size / 16).  A query with a
- *   component of 2^115 or more counts as one that is not finite.
+ *   sequence would need more than 2^30 tiles, n_kv_heads * ceil(rows / 16 (8)) * (64 + table_width * page_size / 16).  A query whose
+ *   largest component times `scale` is 2^119 or more counts as one that is not finite.
  * ls_paged_kv4_read: keys and values of tokens (position d_pos[t] of sequence d_seq[t]) rounded to the 16-bit type; d_k_out or d_v_out NULL:
  *   not wanted.  Rows of padding (a negative sequence or position) and of tokens that are out of range are left as they were.
  * Handles, streams, capture, status and errors as for ls_paged_kv; after LS_ERR_TIMEOUT the rows that miss something are NaN.  Positions

@@ -396,7 +396,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
 
     // Everything below is kept for the lane's two rows: 2 t and 2 t + 1, or g and g + 8 (or the columns 2 t and 2 t + 1 of one row).
     uint32_t qf[S::Q_SHARED ? 1 : N8][KW][4];
-    float qs[NS][2], cn[2], M[2] = {-1e30f, -1e30f}, l[2] = {0.f, 0.f}, zs[NS][2], cs[NS][4], o[NW][2][2][N8][4];
+    float qs[NS][2], cn[2], M[2] = {-3e38f, -3e38f}, l[2] = {0.f, 0.f}, zs[NS][2], cs[NS][4], o[NW][2][2][N8][4];
 #pragma unroll
     for (int e = 0; e < 4 * NS; ++e) { cs[e / 4][e % 4] = 0.f; zs[e / 4][e % 2] = 0.f; }
 #pragma unroll
@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       // the largest component of a row lies in [2^14, 2^15)
-      const int ex = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 113);
+      const int ex = min(max((int)(__float_as_uint(top) >> 23) - 127, -100), 127);
       const float up = __uint_as_float((uint32_t)(14 - ex + 127) << 23), up16 = up * 0.0625f;
 #pragma unroll
       for (int k = 0; k < NS; ++k) part[k] = 0.f;
@@ -437,7 +437,8 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
         if constexpr (S::Q_SHARED) *reinterpret_cast<uint4*>(q_shared + (x * KW + j) * 512) = q;
         else { qf[x][j][0] = q.x; qf[x][j][1] = q.y; qf[x][j][2] = q.z; qf[x][j][3] = q.w; }
       }
-      const float c = fminf(fmaxf(A.scale_log2 * 4194304.f * __uint_as_float((uint32_t)(ex - 14 + 127) << 23), 1e-37f), 1e38f);  // (a masked score times it stays -inf)
+      const float c = fmaxf(A.scale_log2 * 4194304.f * __uint_as_float((uint32_t)(ex - 14 + 127) << 23), 1e-37f);  // (a masked score times it stays -inf)
+      if (!(c < INFINITY)) part[0] = __int_as_float(0x7fffffff);
       if (WIDE) cn[x] = c;
       else { cn[0] = __shfl_sync(0xffffffffu, c, 8 * t); cn[1] = __shfl_sync(0xffffffffu, c, 8 * t + 4); }
 #pragma unroll
@@ -619,25 +620,26 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
           }
         }
         if (__any_sync(0xffffffffu, !(most[0] + most[1] <= 16384.f))) {
-          float m[2] = {-INFINITY, -INFINITY}, f[2];
+          // (Scores so large that their last place counts are rounded before M is, and no weight is above what M allows: a row's largest
+          // score then has a weight that is neither 0 nor infinite.)
+          float m[2] = {-INFINITY, -INFINITY}, f[2], big[KT][NK];
 #pragma unroll
           for (int z = 0; z < KT; ++z) {
-            float big[NK];
 #pragma unroll
             for (int i = 0; i < NK; ++i) {
-              big[i] = 8.67361737988403547e-19f;
+              big[z][i] = 8.67361737988403547e-19f;
 #pragma unroll
-              for (int k = 0; k < NV; ++k) big[i] = fmaxf(big[i], va[z][i][k].x);
-              big[i] = __log2f(big[i]) - 4.f;
+              for (int k = 0; k < NV; ++k) big[z][i] = fmaxf(big[z][i], va[z][i][k].x);
+              if (COLS && NG >= 4) big[z][i] = fmaxf(big[z][i], __shfl_xor_sync(0xffffffffu, big[z][i], 1));  // (one weight for all groups)
+              if (COLS && NG >= 8) big[z][i] = fmaxf(big[z][i], __shfl_xor_sync(0xffffffffu, big[z][i], 2));
+              big[z][i] = __log2f(big[z][i]) - 4.f;
             }
 #pragma unroll
-            for (int e = 0; e < NX; ++e) m[row_of(e)] = fmaxf(m[row_of(e)], fmaf(x[z][e], cn[row_of(e)], big[key_of(e)]));
+            for (int e = 0; e < NX; ++e) m[row_of(e)] = fmaxf(m[row_of(e)], __fmul_rn(x[z][e], cn[row_of(e)]) + big[z][key_of(e)]);
           }
 #pragma unroll
           for (int e = 0; e < NR; ++e) {
-            float to = fmaxf(M[e], WIDE ? quad_max(m[e]) : rows_max(m[e]));
-            if (COLS && NG >= 4) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, 1));
-            if (COLS && NG >= 8) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, 2));
+            const float to = fmaxf(M[e], WIDE ? quad_max(m[e]) : rows_max(m[e]));
             f[e] = ex2(M[e] - to);
             M[e] = to;
             l[e] *= f[e];
@@ -655,7 +657,10 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
 #pragma unroll
           for (int z = 0; z < KT; ++z)
 #pragma unroll
-            for (int e = 0; e < NX; ++e) p[z][e] = ex2(fmaf(x[z][e], cn[row_of(e)], -M[row_of(e)]));
+            for (int e = 0; e < NX; ++e) {
+              const float y = __fsub_rn(__fmul_rn(x[z][e], cn[row_of(e)]), M[row_of(e)]), room = -big[z][key_of(e)];
+              p[z][e] = ex2(y > room ? room : y);  // (NaN stays)
+            }
         }
         // Weights times scales, rounded to fp16 for the product with the codes.  The codes count from the middle of their range, 8: the
         // rounding then weighs s |u - 8|, about a value's own size.  8 sum(p s) is taken off with the rounded weights (a product with

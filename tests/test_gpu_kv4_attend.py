@@ -426,3 +426,49 @@ def test_few_rows_and_tokens_that_are_not_finite(D, group):
     hit[1, 1] = True
     assert torch.equal(torch.isnan(b.out[0]), hit)
     kv.close()
+
+
+@pytest.mark.parametrize("heads,q_len", [(4, 1), (16, 1), (16, 2)])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), 2.0 ** 125])
+def test_a_query_that_is_not_finite_keeps_to_its_row(heads, q_len, what):
+    """Few rows, 8 rows and 16 rows to a key head; one component of one row (2^119 times the scale and above count as not finite)."""
+    b = Batch(lens=[50, 400], heads=heads, hk=2, q_len=q_len)
+    kv = b.handle()
+    b.attend(kv)
+    torch.cuda.synchronize()
+    clean, good, lse = b.q.clone(), b.out.clone(), b.lse.clone()
+    b.q[1, 0, 1, 77] = what
+    b.attend(kv)
+    assert ls.ls_paged_kv4_status(kv) == 0
+    assert torch.isnan(b.out[1, 0, 1]).all() and torch.isnan(b.lse[1, 0, 1])
+    b.q, b.out[1, 0, 1], b.lse[1, 0, 1] = clean, good[1, 0, 1], lse[1, 0, 1]
+    b.check()
+    kv.close()
+
+
+@pytest.mark.parametrize("heads,q_len", [(4, 1), (16, 1), (16, 2)])
+@pytest.mark.parametrize("std", [2.0 ** -120, 2.0 ** -60, 2.0 ** 26, 2.0 ** 60, 2.0 ** 105, 2.0 ** 114])
+def test_queries_of_any_size(heads, q_len, std):
+    """The last place of a large score is far more than a weight's room: one key is left, and its value."""
+    run_case(lens=[50, 400], heads=heads, hk=2, q_len=q_len, std=std)
+    run_case(lens=[50, 400], heads=heads, hk=2, q_len=q_len, std=std, group=32)
+
+
+@pytest.mark.parametrize("heads,group", [(2, 32), (4, 64), (16, 64), (32, 128)])
+def test_scores_far_below_zero(heads, group):
+    """All of them: the largest is still found, and the outputs are sums of values with weights of one."""
+    b = Batch(lens=[50, 400], heads=heads, hk=2, group=group)
+    kv = b.handle()
+    n = 400
+    k = torch.full((n, 2, 128), 1e6, device=DEV, dtype=torch.bfloat16)
+    v = torch.ones(n, 2, 128, device=DEV, dtype=torch.bfloat16)
+    pos = torch.arange(n, dtype=torch.int32, device=DEV)
+    ls.ls_paged_kv4_append(kv, None, k, v, None, torch.full_like(pos, 1), pos, b.table)
+    for size in (1.0, 1e6, 1e26):  # scores about -1e9, -1e15, -1e35
+        b.q.fill_(-size)
+        b.attend(kv)
+        assert ls.ls_paged_kv4_status(kv) == 0
+        score = -128 * float(b.q[1, 0, 0, 0].abs().item()) * float(k[0, 0, 0].item()) * b.scale
+        assert (b.out[1] - 1).abs().max() <= 2.0 ** -8, size
+        assert (b.lse[1].double() / score - 1).abs().max() <= 2.0 ** -20, size
+    kv.close()
