@@ -556,7 +556,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
             }
           }
         }
-        // scales and zeros of the values of the same tokens
+        // scales and zeros of the values of the same tokens, as scales and middles
         float2 va[KT][NK][NV];
 #pragma unroll
         for (int z = 0; z < KT; ++z)
@@ -565,7 +565,10 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
             uint32_t meta[NV];
             lds_words<NV>(tile + z * S::TILE + 16 * D + 64 * NG + token_of(i) * 4 * NG + my_group, meta);
 #pragma unroll
-            for (int k = 0; k < NV; ++k) va[z][i][k] = both_halves<WD>(meta[k]);
+            for (int k = 0; k < NV; ++k) {
+              va[z][i][k] = both_halves<WD>(meta[k]);
+              va[z][i][k].y = fmaf(va[z][i][k].x, 8.f, va[z][i][k].y);  // (the middle of what the codes stand for)
+            }
           }
         if (edge) {
           const uint32_t gone = skip >> (stage * KT);
@@ -601,8 +604,10 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
               }
             }
         }
-        // Weights relative to M, which moves only when the weights times their scales leave what fp16 holds.  (Their sum tells: none of them
-        // is negative, and one that is NaN may hide nothing; 2^-60 keeps weights of scales of zero in range.)
+        // Weights relative to M, which moves only when the weights times their scales leave what fp16 holds, or times their middles 2^104 (bf16
+        // alone can: sums of 2^24 of them stay in fp32's range).  (Their sum tells: none of them is negative, and one that is NaN may hide
+        // nothing; 2^-60 keeps weights of scales of zero in range.)
+        auto size_of = [](float2 v) { return WD == WD_BF16 ? fmaf(fabsf(v.y), 0x1p-90f, v.x) : v.x; };
         float p[KT][NX], most[2] = {0.f, 0.f};
 #pragma unroll
         for (int z = 0; z < KT; ++z) {
@@ -611,7 +616,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
           for (int i = 0; i < NK; ++i) {
             all[i] = 8.67361737988403547e-19f;
 #pragma unroll
-            for (int k = 0; k < NV; ++k) all[i] += va[z][i][k].x;
+            for (int k = 0; k < NV; ++k) all[i] += size_of(va[z][i][k]);
           }
 #pragma unroll
           for (int e = 0; e < NX; ++e) {
@@ -629,7 +634,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
             for (int i = 0; i < NK; ++i) {
               big[z][i] = 8.67361737988403547e-19f;
 #pragma unroll
-              for (int k = 0; k < NV; ++k) big[z][i] = fmaxf(big[z][i], va[z][i][k].x);
+              for (int k = 0; k < NV; ++k) big[z][i] = fmaxf(big[z][i], size_of(va[z][i][k]));
               if (COLS && NG >= 4) big[z][i] = fmaxf(big[z][i], __shfl_xor_sync(0xffffffffu, big[z][i], 1));  // (one weight for all groups)
               if (COLS && NG >= 8) big[z][i] = fmaxf(big[z][i], __shfl_xor_sync(0xffffffffu, big[z][i], 2));
               big[z][i] = __log2f(big[z][i]) - 4.f;
@@ -676,16 +681,13 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
 #pragma unroll
               for (int i = 0; i < NK; ++i) {
                 const float2 a = va[z][i][0], c = va[z][i][1];
-                zs[0][0] = fmaf(p[z][i], fmaf(a.x, 8.f, a.y), zs[0][0]);
-                zs[0][1] = fmaf(p[z][i], fmaf(c.x, 8.f, c.y), zs[0][1]);
+                zs[0][0] = fmaf(p[z][i], a.y, zs[0][0]);
+                zs[0][1] = fmaf(p[z][i], c.y, zs[0][1]);
                 pf[z][0][i] = transpose8(halves(p[z][i] * a.x, p[z][i] * c.x));
               }
             } else {
 #pragma unroll
-              for (int e = 0; e < NX; ++e) {
-                const float2 sz = va[z][key_of(e)][k];
-                zs[k][row_of(e)] = fmaf(p[z][e], fmaf(sz.x, 8.f, sz.y), zs[k][row_of(e)]);
-              }
+              for (int e = 0; e < NX; ++e) zs[k][row_of(e)] = fmaf(p[z][e], va[z][key_of(e)][k].y, zs[k][row_of(e)]);
 #pragma unroll
               for (int e = 0; e < NX; e += 2) {
                 const uint32_t two = halves(p[z][e] * va[z][key_of(e)][k].x, p[z][e + 1] * va[z][key_of(e + 1)][k].x);

@@ -1,0 +1,57 @@
+"""ls_paged_kv4_attend on values that are hard to sum: constant and huge values.  Bounds are those of test_gpu_kv4_attend, for each component by
+itself, down to the smallest values of the type."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv4_oracle as orc
+from paper_2609_03079_b200 import binding as ls
+from test_gpu_kv4_attend import DEV, U, Batch, f64
+
+pytestmark = pytest.mark.gpu
+# heads, key heads, tokens: two rows to a key head (a column for each group of them, where there are several), eight, sixteen
+ROWS = [(4, 2, 1), (8, 1, 1), (16, 2, 2)]
+
+
+def store(b, make):
+    """Replaces the values of a batch: make(n) -> [n, hk, D] for each sequence (keys are drawn anew)."""
+    kv = ls.ls_paged_kv4_create(b.pages, b.heads, b.D, b.page, dtype=orc.DT[b.dtype], group=b.group)
+    gen = torch.Generator(device=DEV).manual_seed(77)
+    for i, n in enumerate(b.lens):
+        if n:
+            k = torch.randn(n, b.hk, b.D, generator=gen, device=DEV)
+            pos = torch.arange(n, dtype=torch.int32, device=DEV)
+            ls.ls_paged_kv4_append(kv, None, k.to(orc.DT[b.dtype]), make(n).to(orc.DT[b.dtype]), None, torch.full_like(pos, i), pos, b.table)
+    assert ls.ls_paged_kv4_status(kv) == 0
+    kv.close()
+
+
+def run(b):
+    kv = b.handle()
+    b.attend(kv)
+    assert ls.ls_paged_kv4_status(kv) == 0
+    kv.close()
+
+
+def check_each_component(b):
+    """As Batch.check, with nothing absolute in the bound but half of the type's smallest step."""
+    ref, _, e, absqk = orc.attend(f64(b.q), b.pages.cpu().numpy(), b.page, b.group, b.dtype, b.lens, b.table_np, b.window, b.scale)
+    got, n = f64(b.out), max(b.lens)
+    ds = absqk * b.scale * 2.0 ** -21
+    tol = ((2 * ds + 2.0 ** -18)[..., None] * e["absout"] + 2.0 ** -11 * e["rounded"] + 2.0 ** -26 * n * e["top"] + 2.0 ** -20 * e["parts"]
+           + U[b.dtype] * np.abs(ref) * (1 + 2.0 ** -6) + (2.0 ** -25 if b.dtype == "fp16" else 2.0 ** -134))
+    assert np.isfinite(got).all(), "not finite"
+    over = np.abs(got - ref) / tol
+    assert over.max() <= 1, f"off by {over.max():.3g} times the bound at {np.unravel_index(over.argmax(), over.shape)}"
+
+
+@pytest.mark.parametrize("heads,hk,q_len", ROWS)
+@pytest.mark.parametrize("D,group", [(64, 64), (128, 32), (128, 64), (128, 128), (256, 128)])
+@pytest.mark.parametrize("dtype,size", [("bf16", 1.0), ("bf16", 1e17), ("bf16", 1e38), ("bf16", 1e-20), ("fp16", 60000.0)])
+def test_constant_values(dtype, size, D, group, heads, hk, q_len):
+    """Values that are the same within each group (all scales are 0), of one size or of random signs."""
+    for signs in (False, True):
+        b = Batch(dtype=dtype, heads=heads, hk=hk, q_len=q_len, D=D, group=group, lens=[400, 17])
+        store(b, lambda n: size * (torch.randint(0, 2, (n, hk, D // group), device=DEV) * 2.0 - 1 if signs else torch.ones(n, hk, D // group, device=DEV)).repeat_interleave(group, -1))
+        run(b)
+        check_each_component(b)
