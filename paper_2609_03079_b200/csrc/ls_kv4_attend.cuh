@@ -56,6 +56,7 @@ constexpr long long K4_SPIN_CLOCKS = 4000000000LL;  // about two seconds
 constexpr float K4_UNIT_TILES = 8.f, K4_JOIN_TILES = 4.f, K4_ADD_TILES = 3e-4f;
 // Blocks that one call may deal out (they are counted in 32 bits); the host cuts larger batches.
 constexpr long long K4_MAX_BLOCKS = 1LL << 30;
+constexpr float K4_FACTOR = 0x1p60f;  // the largest factor of scales
 
 // Shapes of the kernel: D components a head, groups of G, NT times 8 rows of queries at once.  Up to 8 rows are the columns of the
 // products (S^T = K Q^T, O^T = V^T P^T: the codes are the operand with 16 rows), 16 rows are their rows (S = Q K^T, O = P V).
@@ -396,7 +397,10 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
 
     // Everything below is kept for the lane's two rows: 2 t and 2 t + 1, or g and g + 8 (or the columns 2 t and 2 t + 1 of one row).
     uint32_t qf[S::Q_SHARED ? 1 : N8][KW][4];
-    float qs[NS][2], cn[2], M[2] = {-3e38f, -3e38f}, l[2] = {0.f, 0.f}, zs[NS][2], cs[NS][4], o[NW][2][2][N8][4];
+    // (E: factors of scales, of the groups, or of the lane's columns)
+    float qs[NS][2], cn[2], M[2] = {-3e38f, -3e38f}, l[2] = {0.f, 0.f}, E[NV], zs[NS][2], cs[NS][4], o[NW][2][2][N8][4];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) E[k] = NG > 1 ? K4_FACTOR : 1.f;
 #pragma unroll
     for (int e = 0; e < 4 * NS; ++e) { cs[e / 4][e % 4] = 0.f; zs[e / 4][e % 2] = 0.f; }
 #pragma unroll
@@ -604,10 +608,17 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
               }
             }
         }
+        // Scales of a head's groups may differ by any power: each counts times a factor E, a power of two that brings the largest of a group so far
+        // near 1 (none where a head has one group), which is taken off in the end.
         // Weights relative to M, which moves only when the weights times their scales leave what fp16 holds, or times their middles 2^104 (bf16
         // alone can: sums of 2^24 of them stay in fp32's range).  (Their sum tells: none of them is negative, and one that is NaN may hide
         // nothing; 2^-60 keeps weights of scales of zero in range.)
-        auto size_of = [](float2 v) { return WD == WD_BF16 ? fmaf(fabsf(v.y), 0x1p-90f, v.x) : v.x; };
+        auto scaled = [&](int z, int i, int k) { return NG > 1 ? va[z][i][k].x * E[k] : va[z][i][k].x; };
+        auto size_of = [&](int z, int i, int k, float and_) {
+          const float2 v = va[z][i][k];
+          if (WD == WD_BF16) and_ = fmaf(fabsf(v.y), 0x1p-90f, and_);
+          return NG > 1 ? fmaf(v.x, E[k], and_) : v.x + and_;
+        };
         float p[KT][NX], most[2] = {0.f, 0.f};
 #pragma unroll
         for (int z = 0; z < KT; ++z) {
@@ -616,7 +627,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
           for (int i = 0; i < NK; ++i) {
             all[i] = 8.67361737988403547e-19f;
 #pragma unroll
-            for (int k = 0; k < NV; ++k) all[i] += size_of(va[z][i][k]);
+            for (int k = 0; k < NV; ++k) all[i] = size_of(z, i, k, all[i]);
           }
 #pragma unroll
           for (int e = 0; e < NX; ++e) {
@@ -627,14 +638,31 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
         if (__any_sync(0xffffffffu, !(most[0] + most[1] <= 16384.f))) {
           // (Scores so large that their last place counts are rounded before M is, and no weight is above what M allows: a row's largest
           // score then has a weight that is neither 0 nor infinite.)
-          float m[2] = {-INFINITY, -INFINITY}, f[2], big[KT][NK];
+          float m[2] = {-INFINITY, -INFINITY}, f[2], big[KT][NK], h[NV];
+#pragma unroll
+          for (int k = 0; k < NV; ++k) {
+            h[k] = 1.f;
+            if constexpr (NG > 1) {
+              float s = 0.f;
+#pragma unroll
+              for (int z = 0; z < KT; ++z)
+#pragma unroll
+                for (int i = 0; i < NK; ++i) s = fmaxf(s, va[z][i][k].x);
+              s = WIDE ? quad_max(s) : rows_max(s);
+              if (s * E[k] > 64.f) {
+                const float to = __uint_as_float((254u - (__float_as_uint(s) >> 23)) << 23);
+                h[k] = __fdividef(to, E[k]);
+                E[k] = to;
+              }
+            }
+          }
 #pragma unroll
           for (int z = 0; z < KT; ++z) {
 #pragma unroll
             for (int i = 0; i < NK; ++i) {
               big[z][i] = 8.67361737988403547e-19f;
 #pragma unroll
-              for (int k = 0; k < NV; ++k) big[z][i] = fmaxf(big[z][i], size_of(va[z][i][k]));
+              for (int k = 0; k < NV; ++k) big[z][i] = fmaxf(big[z][i], size_of(z, i, k, 0.f));
               if (COLS && NG >= 4) big[z][i] = fmaxf(big[z][i], __shfl_xor_sync(0xffffffffu, big[z][i], 1));  // (one weight for all groups)
               if (COLS && NG >= 8) big[z][i] = fmaxf(big[z][i], __shfl_xor_sync(0xffffffffu, big[z][i], 2));
               big[z][i] = __log2f(big[z][i]) - 4.f;
@@ -655,10 +683,11 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
 #pragma unroll
             for (int e = 0; e < 2; ++e) zs[k][e] *= f[e];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) cs[k][e] *= f[WIDE ? e / 2 : e % 2];
+            for (int e = 0; e < 4; ++e) cs[k][e] *= f[WIDE ? e / 2 : e % 2] * h[COLS ? e % 2 : k];
           }
 #pragma unroll
-          for (int e = 0; e < 16 * N8 * NW; ++e) o[e / (16 * N8)][e / (8 * N8) % 2][e / (4 * N8) % 2][e / 4 % N8][e % 4] *= f[WIDE ? e / 2 % 2 : e % 2];
+          for (int e = 0; e < 16 * N8 * NW; ++e)
+            o[e / (16 * N8)][e / (8 * N8) % 2][e / (4 * N8) % 2][e / 4 % N8][e % 4] *= f[WIDE ? e / 2 % 2 : e % 2] * h[COLS ? e % 2 : 32 * (e / (8 * N8)) / G];
 #pragma unroll
           for (int z = 0; z < KT; ++z)
 #pragma unroll
@@ -683,14 +712,14 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
                 const float2 a = va[z][i][0], c = va[z][i][1];
                 zs[0][0] = fmaf(p[z][i], a.y, zs[0][0]);
                 zs[0][1] = fmaf(p[z][i], c.y, zs[0][1]);
-                pf[z][0][i] = transpose8(halves(p[z][i] * a.x, p[z][i] * c.x));
+                pf[z][0][i] = transpose8(halves(p[z][i] * scaled(z, i, 0), p[z][i] * scaled(z, i, 1)));
               }
             } else {
 #pragma unroll
               for (int e = 0; e < NX; ++e) zs[k][row_of(e)] = fmaf(p[z][e], va[z][key_of(e)][k].y, zs[k][row_of(e)]);
 #pragma unroll
               for (int e = 0; e < NX; e += 2) {
-                const uint32_t two = halves(p[z][e] * va[z][key_of(e)][k].x, p[z][e + 1] * va[z][key_of(e + 1)][k].x);
+                const uint32_t two = halves(p[z][e] * scaled(z, key_of(e), k), p[z][e + 1] * scaled(z, key_of(e + 1), k));
                 pf[z][k][e / 2] = WIDE ? two : transpose8(two);
               }
             }
@@ -745,20 +774,23 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const float sum_l = WIDE ? quad_sum(l[e]) : rows_sum(l[COLS ? 0 : e]);
-        float zero[NS];
+        float zero[NS], one[NS];
 #pragma unroll
-        for (int k = 0; k < NS; ++k) zero[k] = fmaf(-8.f, cs[k][WIDE ? 2 * e : e], WIDE ? quad_sum(zs[k][e]) : rows_sum(zs[k][e]));
+        for (int k = 0; k < NS; ++k) {
+          one[k] = __fdividef(1.f, E[COLS ? e : k]);
+          zero[k] = fmaf(-8.f * one[k], cs[k][WIDE ? 2 * e : e], WIDE ? quad_sum(zs[k][e]) : rows_sum(zs[k][e]));
+        }
         float* line = piece + (COLS ? (2 * t + e) / NG : WIDE ? 8 * e + g : 2 * t + e) * S::LINE;
         // four components side by side: of g, or, twice, of 2 t and 2 t + 1 (of a column that stands for one group, that group's)
 #pragma unroll
         for (int i = 0; i < 2 * NW * N8; ++i) {
           const int at = i / N8, c = WIDE ? 2 * e + i % 2 : e;
           if (COLS && (2 * t + e) % NG != 32 * at / G) continue;
-          const float zz = zero[COLS ? 0 : 32 * at / G];
+          const float zz = zero[COLS ? 0 : 32 * at / G], low = 4194304.f * one[COLS ? 0 : 32 * at / G], high = 262144.f * one[COLS ? 0 : 32 * at / G];
           const auto& a = o[at / 2][at % 2];
           const float first = a[0][0][c], second = WIDE ? a[0][N8 - 1][c] : a[0][0][c + 2], third = a[1][0][c], last = WIDE ? a[1][N8 - 1][c] : a[1][0][c + 2];
           *reinterpret_cast<float4*>(line + 32 * at + 4 * (WIDE ? 2 * t + i % 2 : g)) =
-              make_float4(fmaf(first, 4194304.f, zz), fmaf(second, 262144.f, zz), fmaf(third, 4194304.f, zz), fmaf(last, 262144.f, zz));
+              make_float4(fmaf(first, low, zz), fmaf(second, high, zz), fmaf(third, low, zz), fmaf(last, high, zz));
         }
         if (WIDE ? t == 0 : g == 0 && (!COLS || (2 * t + e) % NG == 0)) *reinterpret_cast<float2*>(line + D) = make_float2(M[COLS ? 0 : e], sum_l);
       }

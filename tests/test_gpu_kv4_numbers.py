@@ -1,5 +1,7 @@
-"""ls_paged_kv4_attend on values that are hard to sum: constant and huge values.  Bounds are those of test_gpu_kv4_attend, for each component by
-itself, down to the smallest values of the type."""
+"""ls_paged_kv4_attend on values that are hard to sum: groups of very different sizes, constant and huge values.
+Bounds are those of test_gpu_kv4_attend, for each component by itself, but for products of weights and scales under fp16's normal numbers: a group's
+scales count times a power of two that brings the largest of them, s, between 1 and 64, and the largest product of a row (of any group) stands at 2^4 or above
+when it is met, so that a key adds up to 2^-25 x 8 / 2^4 x 64 of w s: 2^-20 n s in all, with the largest weight at most 1."""
 import numpy as np
 import pytest
 import torch
@@ -34,11 +36,17 @@ def run(b):
 
 
 def check_each_component(b):
-    """As Batch.check, with nothing absolute in the bound but half of the type's smallest step."""
+    """As Batch.check, with nothing absolute in the bound but half of the type's smallest step, and what the head says of small products."""
     ref, _, e, absqk = orc.attend(f64(b.q), b.pages.cpu().numpy(), b.page, b.group, b.dtype, b.lens, b.table_np, b.window, b.scale)
     got, n = f64(b.out), max(b.lens)
+    scales = orc.held(b.pages.cpu().numpy(), b.page, b.D, b.group, b.dtype)[1][1]
+    top = np.zeros(ref.shape)
+    for i, length in enumerate(b.lens):
+        pos = np.arange(length)
+        s = scales[b.table_np[i][pos // b.page], pos % b.page].max(0)
+        top[i] = np.repeat(s, b.heads // b.hk, 0)
     ds = absqk * b.scale * 2.0 ** -21
-    tol = ((2 * ds + 2.0 ** -18)[..., None] * e["absout"] + 2.0 ** -11 * e["rounded"] + 2.0 ** -26 * n * e["top"] + 2.0 ** -20 * e["parts"]
+    tol = ((2 * ds + 2.0 ** -18)[..., None] * e["absout"] + 2.0 ** -11 * e["rounded"] + 2.0 ** -20 * n * top + 2.0 ** -20 * e["parts"]
            + U[b.dtype] * np.abs(ref) * (1 + 2.0 ** -6) + (2.0 ** -25 if b.dtype == "fp16" else 2.0 ** -134))
     assert np.isfinite(got).all(), "not finite"
     over = np.abs(got - ref) / tol
@@ -53,5 +61,26 @@ def test_constant_values(dtype, size, D, group, heads, hk, q_len):
     for signs in (False, True):
         b = Batch(dtype=dtype, heads=heads, hk=hk, q_len=q_len, D=D, group=group, lens=[400, 17])
         store(b, lambda n: size * (torch.randint(0, 2, (n, hk, D // group), device=DEV) * 2.0 - 1 if signs else torch.ones(n, hk, D // group, device=DEV)).repeat_interleave(group, -1))
+        run(b)
+        check_each_component(b)
+
+
+@pytest.mark.parametrize("heads,hk,q_len", ROWS)
+@pytest.mark.parametrize("D,group", [(64, 32), (128, 32), (128, 64), (256, 32), (256, 64), (256, 128)])
+@pytest.mark.parametrize("dtype,octaves", [("bf16", 20), ("bf16", 28), ("bf16", 60), ("fp16", 20)])
+def test_groups_of_very_different_sizes(dtype, octaves, D, group, heads, hk, q_len):
+    """Values whose groups differ by 2^octaves: by group, the same for all tokens, and drawn for each token and group."""
+    groups = D // group
+    top = 10 if dtype == "fp16" else octaves // 2
+    by_group = 2.0 ** (top - octaves * torch.arange(groups, device=DEV) / (groups - 1)).repeat_interleave(group)
+    for each in (False, True):
+        b = Batch(dtype=dtype, heads=heads, hk=hk, q_len=q_len, D=D, group=group, lens=[700, 45], std=3.0, seed=octaves)
+        gen = torch.Generator(device=DEV).manual_seed(5)
+
+        def make(n):
+            v = torch.randn(n, hk, D, generator=gen, device=DEV)
+            return v * (2.0 ** (top - octaves * torch.rand(n, hk, groups, generator=gen, device=DEV))).repeat_interleave(group, -1) if each else v * by_group
+
+        store(b, make)
         run(b)
         check_each_component(b)
