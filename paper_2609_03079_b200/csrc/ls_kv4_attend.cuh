@@ -57,6 +57,10 @@ constexpr float K4_UNIT_TILES = 8.f, K4_JOIN_TILES = 4.f, K4_ADD_TILES = 3e-4f;
 // Blocks that one call may deal out (they are counted in 32 bits); the host cuts larger batches.
 constexpr long long K4_MAX_BLOCKS = 1LL << 30;
 constexpr float K4_FACTOR = 0x1p60f;  // the largest factor of scales
+// The products' sums are truncated each time: what they hold is brought to the middle of the codes every K4_MIDDLE blocks, and a warp's sums end after
+// K4_RUN blocks, to be added up by rounded operations.  (Without either a warp that summed 2^19 keys was off by 4 % of a mean of values.  Every 8, 32, 64
+// blocks, in us: 128 long 159.6, 158.2, 159.0; 33 conversations 60.1, 59.9, 59.8, and 58.1 without.)
+constexpr int K4_MIDDLE = 32, K4_RUN = 512;
 
 // Shapes of the kernel: D components a head, groups of G, NT times 8 rows of queries at once.  Up to 8 rows are the columns of the
 // products (S^T = K Q^T, O^T = V^T P^T: the codes are the operand with 16 rows), 16 rows are their rows (S = Q K^T, O = P V).
@@ -161,7 +165,7 @@ __device__ __forceinline__ int k4_blocks(const Attend4Args& A, int n) { return (
 
 // A unit is one sequence's blocks (16 KT keys each) for one key head and one row tile of its queries.  All units' blocks stand in one line,
 // cut into equal shares; a share belongs to a team (a whole CTA, or 4, 2 or 1 of its warps), which deal out its blocks among themselves.  A warp copies its
-// blocks by itself (bulk copies into a ring of its own) and works alone until a unit's end; then the team adds up, and a unit that
+// blocks by itself (bulk copies into a ring of its own) and works alone until a unit's end (or that of a run of K4_RUN blocks); then the team adds up, and a unit that
 // reaches over several teams is joined, in order, by whichever of them comes last.
 // A call's first pass over any code waits for it to come from L2, which is most of a small call: loops that need not be unrolled are not.
 template <int WD, int D, int G, int NT>
@@ -312,9 +316,9 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
     }
     // blocks from ... upto of a unit that begins in u0 of the line, with `extra` in front of its blocks
     const int line = length(blocks), unit = (unsigned)(pos - first) / (unsigned)line, u0 = first + unit * line, from_block = max(pos - u0 - extra, 0);
-    const int seg = min(end - u0 - extra, blocks) - from_block;
-    pos = min(u0 + line, end);
-    if (seg <= 0) continue;
+    const int left = min(end - u0 - extra, blocks) - from_block, seg = min(left, K4_RUN * w);  // (of the share, of this run)
+    pos = seg < left ? u0 + extra + from_block + seg : min(u0 + line, end);
+    if (left <= 0) continue;
     const int h = A.by_row_tiles(unit), row0 = (unit - h * A.row_tiles) * S::ROWS, rows = min(S::ROWS, A.q_len * A.group - row0);
     const int n = dead ? 0 : (unsigned)(seg + w - 1 - wi) / (unsigned)w;
     const int block0 = k4_first<KT>(A, len) + from_block + wi;
@@ -755,6 +759,17 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
             }
         }
       }
+      if (j % K4_MIDDLE == K4_MIDDLE - 1) {
+#pragma unroll
+        for (int e = 0; e < 16 * N8 * NW; ++e) {
+          const int at = e / (8 * N8), s = e / (4 * N8) % 2, c = e % 4;
+          const bool high = WIDE ? e / 4 % 2 : c >= 2;  // (codes at bit 6)
+          float& sum = o[at / 2][at % 2][s][e / 4 % N8][c];
+          sum = fmaf(high ? -0x1p-15f : -0x1p-19f, cs[COLS ? 0 : 32 * at / G][WIDE ? c : c % 2], sum);
+        }
+#pragma unroll
+        for (int e = 0; e < 4 * NS; ++e) cs[e / 4][e % 4] = 0.f;
+      }
       __syncwarp();
       if (j + ST < n) {
         if (((j + ST) & 31) == 0) {
@@ -800,10 +815,16 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
     // its place holds at a time, and adds them up by the same code (which the SM has at hand by now; code of its own is cold).
     const int i0 = (u0 + extra) / share, i1 = (u0 + extra + blocks - 1) / share;  // the unit's teams
     const int items = rows * (D / 4), threads = 32 * w, me = wi * 32 + lane, room = w * S::RING / S::PIECE;
+    // Of several runs, all but the last leave their sums in the workspace, where the next finds them; M and the sum of weights stand in two places by turns
+    // (other threads may still read the last ones), the last time in the first.
+    const int runs = left == seg ? 0 : (unsigned)(left - seg + K4_RUN * w - 1) / (unsigned)(K4_RUN * w), ml_to = D + 2 * (runs & 1), ml_last = D + 2 * (~runs & 1);
+    bool more = from_block > max(team * share - u0 - extra, 0);
+    const bool whole = from_block + left == blocks && max(team * share - u0 - extra, 0) == 0;
     float* place = reinterpret_cast<float*>(smem + (warp - wi) * S::RING);
     const float* from = place;                                                                // what is added up: `count` pieces,
-    float* to = A.part + (long long)(2 * team + (team == i0)) * (S::PIECE / 4);  // and where it goes
-    int count = w, stride = S::RING / 4, next = seg == blocks ? i1 + 1 : -1;                   // (next: the team whose piece is fetched next)
+    float* kept = A.part + (long long)(2 * team + (team == i0)) * (S::PIECE / 4);
+    float* to = kept;                                                                         // and where it goes
+    int count = w, stride = S::RING / 4, next = whole && runs == 0 ? i1 + 1 : -1;  // (next: the team whose piece is fetched next)
 #pragma unroll 1
     for (;;) {
       const bool done = next > i1;
@@ -812,6 +833,12 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
         const int r = x / (D / 4), c = x % (D / 4) * 4;
         float m = -INFINITY, sum_l = 0.f;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (more) {
+          const float2 ml = __ldcg(reinterpret_cast<const float2*>(kept + r * S::LINE + ml_last));
+          m = ml.x;
+          sum_l = ml.y;
+          v = __ldcg(reinterpret_cast<const float4*>(kept + r * S::LINE + c));
+        }
         const float* line = from + r * S::LINE;
 #pragma unroll 2
         for (int i = 0; i < count; ++i, line += stride) {
@@ -822,7 +849,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
         if (*s_dead & ((1 << w) - 1) << (warp - wi)) sum_l = __int_as_float(0x7fffffff);
         if (!done) {
           *reinterpret_cast<float4*>(to + r * S::LINE + c) = v;
-          if (c == 0) *reinterpret_cast<float2*>(to + r * S::LINE + D) = make_float2(m, sum_l);
+          if (c == 0) *reinterpret_cast<float2*>(to + r * S::LINE + (to == kept ? ml_to : D)) = make_float2(m, sum_l);
           continue;
         }
         const int i = A.by_group(row0 + r), hd = h * A.group + (row0 + r - i * A.group);
@@ -834,7 +861,8 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
         else { dst[0] = (uint16_t)word.x; dst[1] = (uint16_t)(word.x >> 16); dst[2] = (uint16_t)word.y; dst[3] = (uint16_t)(word.y >> 16); }
         if (c == 0 && A.lse) A.lse[tk * A.heads + hd] = sum_l == 0.f ? -INFINITY : (m + __log2f(sum_l)) * LN2;
       }
-      if (done) break;
+      if (done || runs) break;
+      more = false;
       team_sync();
       int have = 1;
       if (next < 0) {

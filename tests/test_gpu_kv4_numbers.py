@@ -1,4 +1,4 @@
-"""ls_paged_kv4_attend on values that are hard to sum: groups of very different sizes, constant and huge values.
+"""ls_paged_kv4_attend on values that are hard to sum: groups of very different sizes, constant and huge values, sums over very many keys.
 Bounds are those of test_gpu_kv4_attend, for each component by itself, but for products of weights and scales under fp16's normal numbers: a group's
 scales count times a power of two that brings the largest of them, s, between 1 and 64, and the largest product of a row (of any group) stands at 2^4 or above
 when it is met, so that a key adds up to 2^-25 x 8 / 2^4 x 64 of w s: 2^-20 n s in all, with the largest weight at most 1."""
@@ -84,3 +84,53 @@ def test_groups_of_very_different_sizes(dtype, octaves, D, group, heads, hk, q_l
         store(b, make)
         run(b)
         check_each_component(b)
+
+
+def even_page(hk, D, group, keys, seed=0):
+    """fp16 values whose scales, zeros and codes are exact in few bits: scale k / 256 (64 <= k < 128), zero a multiple of 1 / 8 in [-4, -2]."""
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    shape = (keys, hk, D // group, 1)
+    s, z = torch.randint(64, 128, shape, generator=gen, device=DEV) / 256.0, torch.randint(-32, -15, shape, generator=gen, device=DEV) / 8.0
+    u = torch.randint(0, 16, (keys, hk, D // group, group), generator=gen, device=DEV)
+    u[..., 3], u[..., 17] = 0, 15
+    return (s * u + z).flatten(-2)
+
+
+def check_flat(b, R, seqs):
+    """One page of ``b`` listed R times by each of ``seqs`` sequences, queries of zero: the page's mean.  All weights are equal.  A warp sums
+    runs of up to 2^14 keys.  Of a run's mean are rounded: weights times scales, 2^-11 of `rounded`; sums of their products with codes, up to 1024 times by at most
+    2^-23 of at most the run's sum over codes from the middle and that of 1024 keys over codes from 0 (a sixteenth of a run, whose codes are up to 15 and not 4 in the
+    mean): 2^-12 of it; a lane's sums of weights, and of weights times the middles 8 s + z (2 at most), up to 4096 times by 2^-24 of what is there so
+    far, on average half: 2^-13.  Then come the runs' and pieces' joins, 2^-23 each, and the last rounding.  A few tokens to a sequence: all but the last
+    see some keys less, which count for q_len / keys."""
+    b.q.zero_()
+    ref, lse, e, _ = orc.attend(f64(b.q), b.pages.cpu().numpy(), b.page, b.group, b.dtype, b.lens, b.table_np, 0, b.scale)
+    table = b.table[:, :1].expand(seqs, R).contiguous()
+    q, lens = b.q.expand(seqs, -1, -1, -1).contiguous(), torch.full((seqs,), R * b.page, dtype=torch.int32, device=DEV)
+    out, got_lse = torch.full_like(q, float("nan")), torch.full(q.shape[:3], float("nan"), device=DEV)
+    kv = b.handle(max_seqs=seqs)
+    ls.ls_paged_kv4_attend(kv, q, out, lens, table, lse=got_lse)
+    assert ls.ls_paged_kv4_status(kv) == 0
+    kv.close()
+    joins = R * b.page / 2 ** 14 + 12
+    want, mean = ref[:, -1:], np.abs(ref[:, -1:])
+    tol = U[b.dtype] * mean + (2.0 ** -11 + 2.0 ** -12 + b.q_len / (R * b.page)) * e["rounded"][:, -1:] + 2.0 ** -13 * (2 + mean) + joins * 2.0 ** -23 * (2 + mean) + 2.0 ** -25
+    over = np.abs(f64(out) - want) / tol
+    assert over.max() <= 1, f"off by {over.max():.3g} times the bound (of {tol.max():.2e}); outputs are of size {mean.mean():.2e}"
+    assert np.abs(f64(got_lse) - np.log(R * b.page)).max() <= 2.0 ** -13 + joins * 2.0 ** -23 + 2.0 ** -20
+
+
+@pytest.mark.parametrize("heads,D,group", [(2, 128, 64), (8, 128, 128), (8, 128, 64), (8, 64, 32), (8, 256, 32), (16, 128, 64), (16, 64, 64)])
+def test_a_warp_that_sums_half_a_million_keys(heads, D, group):
+    """As many sequences as there are warps, so that each has one to itself."""
+    b = Batch(dtype="fp16", heads=heads, hk=1, D=D, group=group, page=1024, lens=[1024])
+    store(b, lambda n: even_page(1, D, group, n))
+    check_flat(b, 512, 12 * torch.cuda.get_device_properties(0).multi_processor_count)
+
+
+@pytest.mark.parametrize("heads", [1, 8, 16])
+def test_means_of_sequences_of_many_millions(heads):
+    """As many sequences as processors, 48 million keys each."""
+    b = Batch(dtype="fp16", heads=heads, hk=1, D=64, group=64, page=16384, lens=[16384])
+    store(b, lambda n: even_page(1, 64, 64, n))
+    check_flat(b, 2930, torch.cuda.get_device_properties(0).multi_processor_count)
