@@ -434,7 +434,8 @@ int32_t ls_paged_kv_status(ls_paged_kv *kv, int32_t *host_status);
  *
  * `group` consecutive components of one token's key or value of one head share a scale and a zero of the 16-bit type `dtype`.  With
  * x the components as a 16-bit cache would hold them (a key is turned in 64 bits, rounded to 32 and then to 16):
- *   zero = min x,  scale = (max x - min x) / 15 rounded to dtype,  code = min(15, (x - zero) / scale rounded to nearest, ties to even)
+ *   zero = min x,  scale = (max x - min x) / 15, each step rounded to 32 bits, rounded to dtype,
+ *   code = min(15, (x - zero) / scale), the difference rounded to 32 bits, its exact quotient to the nearest whole number, ties to even
  * and the cache holds scale * code + zero.  A scale of 0 makes all codes 0; components whose range is not finite are held as NaN.
  * head_dim: 64, 128 or 256; group: 32, 64 or 128, at most head_dim; page_size: a multiple of 16; heads as for ls_paged_kv.
  * The pages are the CALLER's device memory, borrowed: block (page, head), ls_paged_kv4_block_bytes() long, starts at byte

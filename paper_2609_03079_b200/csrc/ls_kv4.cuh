@@ -2,9 +2,10 @@
 //
 // `group` (32, 64 or 128) consecutive components of one token's key or value of one head share a scale and a zero of the cache's
 // 16-bit type.  With x the components as a 16-bit cache would hold them (a key is turned in 64 bits, then rounded to 32 and to 16):
-//   zero = min x;  scale = (max x - min x) / 15 in fp32, rounded to the type;  code = min(15, round((x - zero) / scale)), ties to even
+//   zero = min x;  scale = (max x - min x) / 15, each step in fp32, rounded to the type;  code = min(15, round((x - zero) / scale)), the
+// difference in fp32, the exact quotient of that, ties to even
 // and scale * code + zero is what is held.  scale 0: all codes are 0.  A range that is not finite: scale and zero are NaN.
-// Every step is one exactly rounded operation, so that codes do not depend on who computes them.
+// Every step is rounded as said and no other, so that codes do not depend on who computes them.
 //
 // A block (one page of one key head) is a row of tiles of 16 tokens, each contiguous so that one bulk copy brings it:
 //   16 rows of key codes (dim / 2 bytes), 16 of value codes, 16 x (groups x (scale, zero)) of keys, the same of values.
@@ -114,12 +115,16 @@ __device__ __forceinline__ void store_oct(uint4 x, bool value, const OctPlace<D,
   }
   const float lo = -widen<WD>((uint16_t)m), range = widen<WD>((uint16_t)(m >> 16)) - lo;
   const bool fine = range < INFINITY;
-  // range / 15, correctly rounded: the quotient by 1 / 15 put right by its remainder
+  // range / 15, correctly rounded: the product with 1 / 15 put right by its remainder (P. W. Markstein, IBM J. Res. Dev. 34, 1990), the same as the
+  // quotient for all 2^23 fractions
   const float fifteenth = 0.0666666701436042785645f, about = __fmul_rn(range, fifteenth);
   const uint16_t scale16 = narrow<WD>(__fmaf_rn(__fmaf_rn(-15.f, about, range), fifteenth, about));
   const float scale = fine ? widen<WD>(scale16) : 0.f;
   // (x - zero) / scale to the nearest whole number, ties to even: by a reciprocal, then put right by the remainder, which is exact (a
   // whole number up to 16 times a 16-bit scale fits fp32, and what is left of x - zero is at most about half a scale).
+  // A division's quotient, where reciprocals end, needs none: a number that is not halfway between two codes times the scale is a last place off it at
+  // least, and so is its quotient.  (Deciding ties by what x - zero lost when it was rounded, where exponents are far apart: 128 us for 16
+  // chunks of 1023 tokens, 117 without.)
   float y[8];
   unpack8<WD>(x, y);
   const float inverse = __fdividef(1.f, scale), magic = 12582912.f;
