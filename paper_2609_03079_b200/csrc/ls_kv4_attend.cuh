@@ -7,7 +7,8 @@
 // shifts and logical instructions and no conversion.  The sums of a product are aligned to 2^-14, not to what the subnormal numbers come
 // to, so a code at bit 0 loses what lies below 2^-14 of a unit (lse was off by 4e-6): they stand at bits 2 and 6 (2^-16; the 2^-4 between the
 // two goes into the query, and into the sums of values when they are done).
-// Queries are scaled to a power of two per row and are exact in fp16, whatever the cache's type.  A row's tensor-core work is a small part
+// Queries are scaled to a power of two per row and are exact in fp16, whatever the cache's type (but for bf16 components about 2^27 and more below
+// the row's largest, which lose bits).  A row's tensor-core work is a small part
 // of its instructions: scales, zeros and weights of 16 keys cost about 240 instructions of a warp (a scale for 128 components, up to 8
 // rows), 276 (for 64) or 404 (for 64, 16 rows).
 //

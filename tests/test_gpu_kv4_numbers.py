@@ -134,3 +134,20 @@ def test_means_of_sequences_of_many_millions(heads):
     b = Batch(dtype="fp16", heads=heads, hk=1, D=64, group=64, page=16384, lens=[16384])
     store(b, lambda n: even_page(1, 64, 64, n))
     check_flat(b, 2930, torch.cuda.get_device_properties(0).multi_processor_count)
+
+
+@pytest.mark.parametrize("D,group,heads,hk,q_len", [(128, 64, 4, 2, 1), (128, 128, 8, 1, 1), (128, 32, 8, 1, 1), (128, 64, 16, 2, 2), (256, 64, 8, 1, 1)])
+@pytest.mark.parametrize("size", [0.0, 1e3, 1e30])
+def test_other_rows_of_a_tile(size, D, group, heads, hk, q_len):
+    """Queries of one row of a key head as they were, all others of quite another size: each row within its own bound."""
+    b = Batch(D=D, group=group, heads=heads, hk=hk, q_len=q_len, lens=[900, 333], vstd=1.0)
+    per = heads // hk
+    for row in {0, per - 1}:
+        q = b.q.clone()
+        b.q[:, :, [r for r in range(heads) if r % per != row]] *= size
+        run(b)
+        b.lse.fill_(float("nan"))
+        b.attend(kv := b.handle())
+        b.check()
+        kv.close()
+        b.q = q
