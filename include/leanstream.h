@@ -452,8 +452,8 @@ int32_t ls_paged_kv_status(ls_paged_kv *kv, int32_t *host_status);
  *   any others (sequences may share pages): there is no separate prefix.  A position appended twice in one call holds parts of either.
  * ls_paged_kv4_attend: scores, softmax statistics and sums are fp32; weights times scales are rounded to fp16 for the product with
  *   the codes, each group of a head with a power of two of its own: a product loses bits that is below 2^-18 of the row's largest, when
- *   a group's scales are taken relative to the largest of them (among the keys that any query of the key head sees); so do all groups of a
- *   head one of which holds bf16 values of 2^108 and more.  Otherwise what a token does not see does not reach its result; the order of
+ *   a group's scales are taken relative to the largest of them (among the keys that any query of the key head sees); so do heads
+ *   with bf16 values of 2^108 and more.  Otherwise what a token does not see does not reach its result; the order of
  *   sums does: last bits may change with the lengths of the batch, which decide where sums are cut, and with the other queries of a
  *   key head, which share the moments at which references move.  Meant for a few tokens per sequence; rows of
  *   q_len * n_q_heads / n_kv_heads beyond 16 (8 for head_dim 256) read the keys again.  Refused: a table of so many positions that one

@@ -57,7 +57,7 @@ constexpr long long K4_SPIN_CLOCKS = 4000000000LL;  // about two seconds
 constexpr float K4_UNIT_TILES = 8.f, K4_JOIN_TILES = 4.f, K4_ADD_TILES = 3e-4f;
 // Blocks that one call may deal out (they are counted in 32 bits); the host cuts larger batches.
 constexpr long long K4_MAX_BLOCKS = 1LL << 30;
-constexpr float K4_FACTOR = 0x1p60f;  // the largest factor of scales
+constexpr float K4_FACTOR = 0x1p60f, K4_LEAST_FACTOR = 0x1p-100f;  // bounds of the factors of scales (their reciprocals, times 2^22, fit fp32)
 // The products' sums are truncated each time: what they hold is brought to the middle of the codes every K4_MIDDLE blocks, and a warp's sums end after
 // K4_RUN blocks, to be added up by rounded operations.  (Without either a warp that summed 2^19 keys was off by 4 % of a mean of values.  Every 8, 32, 64
 // blocks, in us: 128 long 159.6, 158.2, 159.0; 33 conversations 60.1, 59.9, 59.8, and 58.1 without.)
@@ -617,7 +617,8 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
         // near 1 (none where a head has one group), which is taken off in the end.
         // Weights relative to M, which moves only when the weights times their scales leave what fp16 holds, or times their middles 2^104 (bf16
         // alone can: sums of 2^24 of them stay in fp32's range).  (Their sum tells: none of them is negative, and one that is NaN may hide
-        // nothing; 2^-60 keeps weights of scales of zero in range.)
+        // nothing; `least` keeps weights of scales of zero in range.)
+        constexpr float least = WD == WD_BF16 ? 0x1p-90f : 0x1p-60f;
         auto scaled = [&](int z, int i, int k) { return NG > 1 ? va[z][i][k].x * E[k] : va[z][i][k].x; };
         auto size_of = [&](int z, int i, int k, float and_) {
           const float2 v = va[z][i][k];
@@ -630,7 +631,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
           float all[NK];
 #pragma unroll
           for (int i = 0; i < NK; ++i) {
-            all[i] = 8.67361737988403547e-19f;
+            all[i] = least;
 #pragma unroll
             for (int k = 0; k < NV; ++k) all[i] = size_of(z, i, k, all[i]);
           }
@@ -655,7 +656,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
                 for (int i = 0; i < NK; ++i) s = fmaxf(s, va[z][i][k].x);
               s = WIDE ? quad_max(s) : rows_max(s);
               if (s * E[k] > 64.f) {
-                const float to = __uint_as_float((254u - (__float_as_uint(s) >> 23)) << 23);
+                const float to = fmaxf(__uint_as_float((254u - (__float_as_uint(s) >> 23)) << 23), K4_LEAST_FACTOR);
                 h[k] = __fdividef(to, E[k]);
                 E[k] = to;
               }
@@ -665,7 +666,7 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
           for (int z = 0; z < KT; ++z) {
 #pragma unroll
             for (int i = 0; i < NK; ++i) {
-              big[z][i] = 8.67361737988403547e-19f;
+              big[z][i] = least;
 #pragma unroll
               for (int k = 0; k < NV; ++k) big[z][i] = fmaxf(big[z][i], size_of(z, i, k, 0.f));
               if (COLS && NG >= 4) big[z][i] = fmaxf(big[z][i], __shfl_xor_sync(0xffffffffu, big[z][i], 1));  // (one weight for all groups)

@@ -86,6 +86,20 @@ def test_groups_of_very_different_sizes(dtype, octaves, D, group, heads, hk, q_l
         check_each_component(b)
 
 
+@pytest.mark.parametrize("heads,hk,q_len", ROWS)
+@pytest.mark.parametrize("D,group", [(64, 32), (128, 32), (128, 64), (128, 128), (256, 64)])
+@pytest.mark.parametrize("dtype,size", [("bf16", 2.0 ** -100), ("bf16", 2.0 ** -60), ("bf16", 2.0 ** 80), ("bf16", 2.0 ** 106), ("bf16", 2.0 ** 125), ("fp16", 2.0 ** 13)])
+def test_values_of_any_size(dtype, size, D, group, heads, hk, q_len):
+    """All groups alike, from tiny numbers to the type's largest (heads of one group: up to 2^108, as the header says)."""
+    if D == group and size > 2.0 ** 108:
+        size = 2.0 ** 107
+    b = Batch(dtype=dtype, heads=heads, hk=hk, q_len=q_len, D=D, group=group, lens=[400, 45], std=3.0)
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    store(b, lambda n: size * torch.randn(n, hk, D, generator=gen, device=DEV).clamp(-3.5, 3.5))
+    run(b)
+    check_each_component(b)
+
+
 def even_page(hk, D, group, keys, seed=0):
     """fp16 values whose scales, zeros and codes are exact in few bits: scale k / 256 (64 <= k < 128), zero a multiple of 1 / 8 in [-4, -2]."""
     gen = torch.Generator(device=DEV).manual_seed(seed)
