@@ -49,8 +49,8 @@ int32_t create_kv(ls_paged_kv4* kv) {
   LS_CUDA(cudaMemset(kv->status, 0, sizeof(int)));
   if (d.max_seqs > 0) {
     const long long rows = (long long)d.max_q_len * (d.n_q_heads / d.n_kv_heads);
-    for (long long r : {1LL, 8LL, 16LL}) {
-      const Shape s = shape_for(d, r);
+    for (long long r : {1LL, 8LL, 16LL}) {  // (one of each shape that so many rows can have)
+      const Shape s = shape_for(d, std::min(r, rows));
       LS_CUDA(cudaFuncSetAttribute(s.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, s.smem));
       kv->part_floats = std::max(kv->part_floats, (size_t)kv->sm_count * (s.threads / 32) * 2 * s.piece);
       kv->units = std::max(kv->units, (size_t)d.max_seqs * d.n_kv_heads * ((size_t)(rows + s.rows - 1) / s.rows));
