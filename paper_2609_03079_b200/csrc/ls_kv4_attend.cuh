@@ -9,19 +9,18 @@
 // two goes into the query, and into the sums of values when they are done).
 // Queries are scaled to a power of two per row and are exact in fp16, whatever the cache's type (but for bf16 components about 2^27 and more below
 // the row's largest, which lose bits).  A row's tensor-core work is a small part
-// of its instructions: scales, zeros and weights of 16 keys cost about 240 instructions of a warp (a scale for 128 components, up to 8
-// rows), 276 (for 64) or 404 (for 64, 16 rows).
+// of its instructions: 16 keys cost about 251 instructions of a warp (a scale for 128 components, up to 8 rows), 296 (for 64) or 437 (for 64, 16 rows).
 //
 // Bounds and figures (B200, passes among others):
-//   128 sequences of up to 9216 keys, 64 / 8 heads of 128, one scale a head: 157 us, 0.80 of the rate at which memory is copied
-//     (171 to 178 us where seconds of such calls meet the card's power limit); a call of
-//     one sequence of 100001 keys 32 us, whose steady state runs at 0.93 of it: about 13 us of a call are its beginning (lengths, shares,
-//     table, first tile, all of it cold code) and its end (the team's sums, then the joining of a unit's pieces);
-//   33 sequences of up to 2000 keys, 40 / 40 heads, a scale for 32: 58 us, 0.73 (75 us with a column for a row, of which seven in eight
-//     are idle, and a sum for each group);
-//   16 rows (draft tokens): 16 sequences of a window of 4096 33 us, 0.27, the same at two warps to a scheduler.
-// What did not help: a software pipeline of scores and values (170 us for 174, others slower), codes brought to their bits by byte
-// permutations (the same within 1 %) or by the high half of a product (5 to 15 % slower) instead of right shifts, scores of 32 rows at
+//   128 sequences of up to 9216 keys, 64 / 8 heads of 128, one scale a head: 169 to 180 us where seconds of such calls meet the card's power
+//     limit, 0.70 to 0.74 of the rate at which memory is copied, and 158 in bursts, 0.79; 16 of 400001 keys 765 us, 0.89;
+//   one sequence of 100001 keys 33 us; two million keys 438, 0.81 (0.84 from one to the other): about 12 us of a call are its beginning
+//     (lengths, shares, table, first tile, all of it cold code) and its end (the team's sums, then the joining of a unit's pieces);
+//   33 sequences of up to 2000 keys, 40 / 40 heads, a scale for 32: 60 us, 0.70, 64 at the power limit (80 us with a column for a row, of which seven
+//     in eight are idle, and a sum for each group);
+//   16 rows (draft tokens): 16 sequences of a window of 4096 35 us, 0.26, two warps to a scheduler.
+// What did not help (all measured on earlier forms): a software pipeline of scores and values (170 us for 174, others slower), codes brought to
+// their bits by byte permutations (the same within 1 %) or by the high half of a product (5 to 15 % slower) instead of right shifts, scores of 32 rows at
 // once (163 us for two passes' 100).
 #pragma once
 #include "ls_attend.cuh"
@@ -52,28 +51,30 @@ struct Attend4Args {
 };
 
 constexpr long long K4_SPIN_CLOCKS = 4000000000LL;  // about two seconds
-// What a unit's beginning and end, and the joining of its pieces, cost a warp, in tiles.  (A unit at 4, 6, 8 and 10 or 11: one sequence of 100001 keys 35.2, 32.6,
-// 32.3, 32.6 us; 33 of up to 2000 57.0, 57.3, 57.7, 58.4; three of 20001 20.7, 20.2, 18.7, 18.4; 200 tiny ones and a long one 34, 40, 39, 40.)
+// What a unit's beginning and end, and the joining of its pieces, cost a warp, in tiles.  (A unit at 4, 6, 8 and 11: one sequence of 100001 keys 35.9, 33.4,
+// 33.1, 32.9 us; 33 of up to 2000 59.1, 59.4, 59.8, 61.3; three of 20001 21.1, 20.1, 18.9, 18.7; 200 of 300 22.1, 22.2, 22.2, 22.1; a window of 4096, 16 rows, 36.0, 36.3,
+// 34.6, 35.1; 128 long ones 156, 155, 158, 158; 200 tiny ones and a long one 36, 41, 40, 41.)
 constexpr float K4_UNIT_TILES = 8.f, K4_JOIN_TILES = 4.f, K4_ADD_TILES = 3e-4f;
 // Blocks that one call may deal out (they are counted in 32 bits); the host cuts larger batches.
 constexpr long long K4_MAX_BLOCKS = 1LL << 30;
 constexpr float K4_FACTOR = 0x1p60f, K4_LEAST_FACTOR = 0x1p-100f;  // bounds of the factors of scales (their reciprocals, times 2^22, fit fp32)
 // The products' sums are truncated each time: what they hold is brought to the middle of the codes every K4_MIDDLE blocks, and a warp's sums end after
 // K4_RUN blocks, to be added up by rounded operations.  (Without either a warp that summed 2^19 keys was off by 4 % of a mean of values.  Every 8, 32, 64
-// blocks, in us: 128 long 159.6, 158.2, 159.0; 33 conversations 60.1, 59.9, 59.8, and 58.1 without.)
+// blocks, in us: 128 long 159.6, 158.2, 159.0; 33 conversations 60.1, 59.9, 59.8, and 58.1 without.  Runs of 512 blocks or none: 16 sequences of 400001 keys 765
+// and 762 us.  Runs of 64 or 128 instead of both: 801, 787; 128 long 164.8, 159.5; 33 conversations 59.2, 59.2.)
 constexpr int K4_MIDDLE = 32, K4_RUN = 512;
 
 // Shapes of the kernel: D components a head, groups of G, NT times 8 rows of queries at once.  Up to 8 rows are the columns of the
 // products (S^T = K Q^T, O^T = V^T P^T: the codes are the operand with 16 rows), 16 rows are their rows (S = Q K^T, O = P V).
 // NT = 0: so few rows that the 8 columns hold each of them once for every group, with the components of that group alone.  One sum then
 // holds what a scale and a zero have to be applied to, two columns to a lane, instead of one sum for each group.  (In us, with and
-// without: 33 sequences of up to 2000 keys, one row, four groups: 57.7, 75.5; 8 of 8001, one row, two groups: 44.8, 47.1; 200 of 300 keys, four
-// rows, two groups: 21.5, 23.3; 200 of 17 and one of 40000: 39.4, 37.2.)
+// without: 33 sequences of up to 2000 keys, one row, four groups: 59.8, 80.3; 8 of 8001, one row, two groups: 45.1, 47.8; 200 of 300 keys, four
+// rows, two groups: 22.2, 23.9; 200 of 17 and one of 40000: 40.3, 38.7.)
 template <int D, int G, int NT>
 struct K4Shape {
-  // 12 warps of 168 registers, or 8 of 255 where sums fill more.  Two tiles at once give a warp independent work (in us, warps x tiles; 8 rows of
-  // heads of 128: 12 x 2, 8 x 2, 16 x 2, 16 x 1: 128 long sequences 177, 198, 170, 200; one long 36, 46, 40, 60; 200 of 300 keys 24, 36,
-  // 27, 27.  16 rows, window of 4096: 8 x 2, 8 x 1, 12 x 1, 10 x 2: 35, 39, 50, 61).
+  // 12 warps of 168 registers, or 8 of 255 where sums fill more.  Two tiles at once give a warp independent work (in us, warps x tiles; up to
+  // 8 rows of heads of 128: 12 x 2, 8 x 2, 16 x 2, 16 x 1: 128 long sequences 158, 184, 156, 200; one of 100001 33, 35, 39, 38; 33 of up to 2000 60, 66, 57, 67;
+  // 200 of 300 keys 22, 28, 24, 26; 16 of 20001, a scale for 32: 71, 70, 95, 91.  16 rows, window of 4096: 8 x 2, 8 x 1, 12 x 1, 10 x 2: 35, 37, 51, 60).
   static constexpr int N8 = NT == 2 ? 2 : 1;
   static constexpr int WARPS = D * N8 <= 128 ? 12 : 8;
   static constexpr int KT = D == 256 && G == 32 ? 1 : 2;         // (two would spill 660 bytes a thread, one 180)
@@ -237,9 +238,9 @@ __global__ void __launch_bounds__(K4Shape<D, G, NT>::THREADS, 1) ls_kv4_attend_k
   // in the line in front of it.  Or each unit begins with a new share, one for all of it, or several.  (Shares may be a little larger than
   // they need to be: fp32 will do.)
   // What each way is for, in us (the rule; always the first; never one share to a unit; always whole CTAs; always the smallest teams): one short
-  // sequence 6.7, 8.9, 9.0, 6.5, 17; one of 100001 keys 33, 37, 33, 33, 361; 33 of up to 2000 (a column for a row) 75, 75, 75, 152, 76; a window of 4096 35, 87, 87,
-  // 34, 40; 128 long ones 163, 162, 163, 198, 159; 200 of 300 23, 29, 29, 88, 23; three of 20001 20, 24, 20, 20, 108.  And without the units' own
-  // cost in the line, idle and tiny units fall to one team: 64 idle of 80 191 us instead of 34.
+  // sequence 7.0, 9.0, 9.1, 7.0, 15; one of 100001 keys 33, 33, 33, 33, 376; 33 of up to 2000 60, 60, 60, 99, 60; a window of 4096 35, 34, 35, 35, 41; 128 long ones 158,
+  // 158, 161, 177, 158; 200 of 300 22, 26, 26, 60, 22; three of 20001 19, 19, 19, 19, 75.  And without the units' own cost in the line, units' beginnings
+  // pile up on some teams: 33 of up to 2000 145 us, 200 tiny ones and a long one 338 instead of 40.
   int w, share, extra;
   bool gaps;
   {  // (a lane for each size of a team)
