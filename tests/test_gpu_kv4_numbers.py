@@ -165,3 +165,59 @@ def test_other_rows_of_a_tile(size, D, group, heads, hk, q_len):
         b.check()
         kv.close()
         b.q = q
+
+
+@pytest.mark.parametrize("heads,D,group", [(2, 128, 32), (8, 64, 64), (16, 64, 32)])
+@pytest.mark.parametrize("seqs", [1, 20, 333])
+def test_means_of_shares_that_begin_and_end_inside_sequences(seqs, heads, D, group):
+    """Long sequences cut among the teams anywhere: runs of a share, its pieces, their joins."""
+    b = Batch(dtype="fp16", heads=heads, hk=1, D=D, group=group, page=4096, lens=[4096])
+    store(b, lambda n: even_page(1, D, group, n))
+    check_flat(b, 4000 if seqs < 100 else 777, seqs)
+
+
+@pytest.mark.parametrize("heads,q_len,window", [(2, 1, 0), (8, 1, 37000), (8, 2, 36000), (4, 2, 0)])
+def test_runs_of_sequences_with_windows_and_missing_pages(heads, q_len, window):
+    """Each warp has a sequence of 40000 keys or a little less (three runs) to itself (with up to eight rows; sixteen are cut anywhere), all over the same
+    pages, one of which, in the second run, is missing."""
+    lens = [40000 - 13 * i for i in range(4)]
+    one = Batch(heads=heads, hk=1, page=64, lens=lens[:1], q_len=q_len, window=window, D=64, std=3.0)
+    S = 12 * torch.cuda.get_device_properties(0).multi_processor_count
+    q, table = one.q.expand(S, -1, -1, -1).contiguous(), one.table.expand(S, -1).contiguous()
+    seq_len = torch.tensor(lens, dtype=torch.int32, device=DEV).repeat(-(-S // 4))[:S]
+    kv = one.handle(max_seqs=S)
+    out, lse = torch.full_like(q, float("nan")), torch.full(q.shape[:3], float("nan"), device=DEV)
+
+    def call():
+        ls.ls_paged_kv4_attend(kv, q, out, seq_len, table, window=window, lse=lse)
+
+    call()
+    assert ls.ls_paged_kv4_status(kv) == 0
+    first, first_lse = out.clone(), lse.clone()
+    for i, n in enumerate(lens):
+        if heads * q_len <= 8:
+            assert torch.equal(out[i::4], out[i:i + 1].expand_as(out[i::4])) and torch.equal(lse[i::4], lse[i:i + 1].expand_as(lse[i::4]))
+        for at in (i, i + 4 * (S // 8), i + 4 * ((S - i - 1) // 4)):
+            one.lens, one.out, one.lse = [n], out[at:at + 1], lse[at:at + 1]
+            one.check()
+    call()
+    assert torch.equal(out, first) and torch.equal(lse, first_lse)
+    # without a page of the second run: as if its keys were not there, the others' weights the larger
+    table[:, 300] = -1
+    call()
+    assert ls.ls_paged_kv4_status(kv) == -1
+    K, V = (orc.values(x)[:, :, 0] for x in orc.held(one.pages.cpu().numpy(), 64, 64, 64, "bf16"))
+    for i, n in enumerate(lens):
+        for m in range(q_len):
+            hi = n - q_len + m + 1
+            pos = np.arange(max(0, hi - window) if window else 0, hi)
+            pos = pos[pos // 64 != 300]
+            at = one.table_np[0][pos // 64], pos % 64
+            s = f64(one.q)[0, m] @ K[at].T * one.scale
+            top = s.max(1, keepdims=True)
+            w = np.exp(s - top)
+            ref = w @ V[at] / w.sum(1, keepdims=True)
+            assert np.abs(f64(lse[i, m]) - (top[:, 0] + np.log(w.sum(1)))).max() <= 2.0 ** -14  # scores of up to 40, to 2^-20 of them
+            # as the bounds of the file's head, values of unit variance, scales of up to 1/2
+            assert np.abs(f64(out[i, m]) - ref).max() <= 2.0 ** -8 * np.abs(ref).max() + 2.0 ** -11 * 4
+    kv.close()
